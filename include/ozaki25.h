@@ -336,6 +336,55 @@ ozaki25_status ozaki25_dgemm_noalloc(int64_t m, int64_t n, int64_t k, const doub
                                      ozaki25_moduli_set set, ozaki25_quantiser quant, int subtract,
                                      void* stream);
 
+/* ---- Products of 16-bit operands ------------------------------------------
+ * Products whose shape a language model gives them, on the 16-bit matrix
+ * cores: bfloat16 or IEEE half operands, FP32 sums, one rounding of the result
+ * (to nearest even).  Row-major matrices with pitches in elements; device
+ * pointers aligned to their element; any pitch of at least the row length up
+ * to OZAKI25_MAX_LD.  Rows that start on 16 bytes and sizes that are multiples
+ * of 8 take the faster loads.  Nothing is allocated, and every call may be
+ * captured into a graph.  Sums run in an order fixed by the sizes and group
+ * ends: the same inputs give the same bits. */
+typedef enum { OZAKI25_BF16 = 0, OZAKI25_F16 = 1, OZAKI25_F32 = 2 } ozaki25_dtype;
+
+#define OZAKI25_MAX_ROWS 1073741824  /* 2^30: rows of an activation */
+#define OZAKI25_MAX_WIDTH 4194304    /* 2^22: columns of an operand */
+#define OZAKI25_MAX_LD 4294967296    /* 2^32: row pitch, elements */
+#define OZAKI25_MAX_GROUPS 65536
+
+/* Grouped product: the rows of X are sorted by group (the tokens of a mixture
+ * of experts), group g holding rows [ends[g-1], ends[g]) with ends[-1] = 0, and
+ *   Y[r, :] = X[r, :] W_g^T          for every row r of group g.
+ *  X: rows x k (ldx);  W: groups matrices n x k (ldw), group_stride elements
+ *  apart (0: one shared by all);  ends: int32 [groups];  Y: rows x n (ldy).
+ *  ends is read on the device: the host needs no group's size.  Each end is
+ *  taken as at least the one before it and at most `rows`; rows past the last
+ *  end are written as zeros.  Groups may be empty.
+ *  type: OZAKI25_BF16 or OZAKI25_F16, of X, W and Y.
+ * Y must not overlap the inputs.  rows == 0 or n == 0: no-op; k == 0: zeros.
+ * Errors: INVALID_VALUE, UNSUPPORTED (sizes beyond the limits above, or more
+ * output tiles than a launch holds), HIP. */
+ozaki25_status ozaki25_grouped_matmul(int64_t rows, int64_t n, int64_t k, int64_t groups, const void* X,
+                                      int64_t ldx, const void* W, int64_t ldw, int64_t group_stride,
+                                      const int32_t* ends, void* Y, int64_t ldy, ozaki25_dtype type,
+                                      void* stream);
+
+/* Its input's gradient: dX[r, :] = dY[r, :] W_g.  dY: rows x n (lddy); W and
+ * ends as above; dX: rows x k (lddx), zeros in rows past the last end. */
+ozaki25_status ozaki25_grouped_matmul_dx(int64_t rows, int64_t n, int64_t k, int64_t groups, const void* dY,
+                                         int64_t lddy, const void* W, int64_t ldw, int64_t group_stride,
+                                         const int32_t* ends, void* dX, int64_t lddx, ozaki25_dtype type,
+                                         void* stream);
+
+/* Its weights' gradient: dW_g = sum of dY[r, :]^T X[r, :] over the rows r of
+ * group g, zeros for an empty group; rows past the last end belong to none.
+ *  dW: groups matrices n x k (lddw), group_stride >= (n - 1) lddw + k elements
+ *  apart, of out_type: `type` or OZAKI25_F32. */
+ozaki25_status ozaki25_grouped_matmul_dw(int64_t rows, int64_t n, int64_t k, int64_t groups, const void* dY,
+                                         int64_t lddy, const void* X, int64_t ldx, const int32_t* ends, void* dW,
+                                         int64_t lddw, int64_t group_stride, ozaki25_dtype type,
+                                         ozaki25_dtype out_type, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -24,6 +24,7 @@ __all__ = [
     "ozaki25_dgemm_planes_workspace_size", "ozaki25_dgemm_planes", "ozaki25_dgemm_noalloc",
     "ozaki25_accurate_exponents_workspace_size", "ozaki25_accurate_exponents",
     "ozaki25_dgemm_accurate_workspace_size", "ozaki25_dgemm_accurate",
+    "ozaki25_grouped_matmul", "ozaki25_grouped_matmul_dx", "ozaki25_grouped_matmul_dw",
 ]
 
 _PKG = os.path.dirname(os.path.abspath(__file__))
@@ -43,6 +44,11 @@ MAX_N = 8388608
 EXP_NONFINITE = -(2 ** 31)
 NUM_STAGE_EVENTS = 5
 NOALLOC_SCRATCH_BYTES = 128 << 20
+BF16, F16, F32 = range(3)   # ozaki25_dtype
+MAX_ROWS = 1 << 30          # limits of the 16-bit products
+MAX_WIDTH = 1 << 22
+MAX_LD = 1 << 32
+MAX_GROUPS = 65536
 
 SUCCESS, ERR_INVALID_VALUE, ERR_UNSUPPORTED, ERR_WORKSPACE, ERR_HIP = range(5)
 
@@ -91,6 +97,9 @@ def lib():
             "ozaki25_dgemm_accurate_workspace_size": ([i64, i64, i64, i32], sz),
             "ozaki25_dgemm_accurate": ([i64, i64, i64, P, i64, P, i64, P, i64, i32, i32, i32, P, sz, P, P],
                                        i32),
+            "ozaki25_grouped_matmul": ([i64, i64, i64, i64, P, i64, P, i64, i64, P, P, i64, i32, P], i32),
+            "ozaki25_grouped_matmul_dx": ([i64, i64, i64, i64, P, i64, P, i64, i64, P, P, i64, i32, P], i32),
+            "ozaki25_grouped_matmul_dw": ([i64, i64, i64, i64, P, i64, P, i64, P, P, i64, i64, i32, i32, P], i32),
         }
         for name, (args, res) in sig.items():
             f = getattr(L, name)
@@ -479,3 +488,120 @@ def ozaki25_dgemm_noalloc(A, B, C=None, subtract: bool = False, set: int = S12, 
     _check(lib().ozaki25_dgemm_noalloc(m, n, k, _ptr(A), lda, _ptr(B), ldb, _ptr(C), ldc, set, quantiser,
                                        1 if subtract else 0, _stream(stream)), "ozaki25_dgemm_noalloc")
     return C
+
+
+# ----------------------------------------------------------------- 16-bit products
+def _half_types():
+    torch = _torch or _tensors()
+    return {torch.bfloat16: BF16, torch.float16: F16}
+
+
+def _pitched(t, name, dims, types, shape=None):
+    """A `dims`-dimensional tensor of one of `types`, elements of a row
+    contiguous; returns (t, row pitch, matrix pitch)."""
+    torch = _torch or _tensors()
+    if not (isinstance(t, torch.Tensor) and t.dtype in types and t.dim() == dims):
+        raise ValueError(f"{name} must be a {dims}-D tensor of dtype {' or '.join(str(d) for d in types)}")
+    if shape is not None and tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {tuple(shape)}")
+    rows, cols = t.shape[-2:]
+    s0, s1 = t.stride()[-2:]
+    if s1 != 1 and cols > 1:
+        raise ValueError(f"{name} must be row-major (unit column stride)")
+    if rows > 1 and s0 < cols:
+        raise ValueError(f"{name} rows overlap (row stride below the row length)")
+    ld = max(s0 if rows > 1 else cols, 1)
+    if dims == 2:
+        return t, ld, 0
+    return t, ld, t.stride(0) if t.shape[0] > 1 else rows * ld
+
+
+def _ends(ends, groups):
+    torch = _torch or _tensors()
+    if not (isinstance(ends, torch.Tensor) and ends.dtype == torch.int32 and ends.dim() == 1 and ends.is_contiguous()):
+        raise ValueError("ends must be a contiguous 1-D int32 tensor")
+    if ends.numel() != groups:
+        raise ValueError(f"ends holds {ends.numel()} groups, expected {groups}")
+    return ends
+
+
+def _new(shape, dtype, device, stream):
+    """An output of the call, allocated on the stream that writes it."""
+    torch = _torch or _tensors()
+    if stream is None or device.type != "cuda":
+        return torch.empty(shape, dtype=dtype, device=device)
+    s = stream if hasattr(stream, "cuda_stream") else torch.cuda.ExternalStream(int(stream), device=device)
+    with torch.cuda.stream(s):
+        return torch.empty(shape, dtype=dtype, device=device)
+
+
+def ozaki25_grouped_matmul(X, W, ends, Y=None, stream=None):
+    """Y[r] = X[r] W[g]^T for the rows r of group g.  X: rows x k, sorted by
+    group; W: groups x n x k; ends: int32 [groups], one past each group's last
+    row (read on the device).  bfloat16 or float16; rows past the last end are
+    zeros.  Returns Y, rows x n."""
+    types = _half_types()
+    X, ldx, _ = _pitched(X, "X", 2, types)
+    rows, k = X.shape
+    W, ldw, stride = _pitched(W, "W", 3, (X.dtype,))
+    groups, n = W.shape[0], W.shape[1]
+    if W.shape[2] != k:
+        raise ValueError(f"W has {W.shape[2]} columns, X has {k}")
+    _ends(ends, groups)
+    if Y is None:
+        Y = _new((rows, n), X.dtype, X.device, stream)
+    Y, ldy, _ = _pitched(Y, "Y", 2, (X.dtype,), (rows, n))
+    _on_gpu([("X", X), ("W", W), ("ends", ends), ("Y", Y)])
+    _check(lib().ozaki25_grouped_matmul(rows, n, k, groups, _ptr(X), ldx, _ptr(W), ldw, stride, _ptr(ends), _ptr(Y),
+                                        ldy, types[X.dtype], _stream(stream)), "ozaki25_grouped_matmul")
+    return Y
+
+
+def ozaki25_grouped_matmul_dx(dY, W, ends, dX=None, stream=None):
+    """dX[r] = dY[r] W[g], the gradient of ozaki25_grouped_matmul's input.
+    Returns dX, rows x k."""
+    types = _half_types()
+    dY, lddy, _ = _pitched(dY, "dY", 2, types)
+    rows, n = dY.shape
+    W, ldw, stride = _pitched(W, "W", 3, (dY.dtype,))
+    groups, k = W.shape[0], W.shape[2]
+    if W.shape[1] != n:
+        raise ValueError(f"W has {W.shape[1]} rows, dY has {n} columns")
+    _ends(ends, groups)
+    if dX is None:
+        dX = _new((rows, k), dY.dtype, dY.device, stream)
+    dX, lddx, _ = _pitched(dX, "dX", 2, (dY.dtype,), (rows, k))
+    _on_gpu([("dY", dY), ("W", W), ("ends", ends), ("dX", dX)])
+    _check(lib().ozaki25_grouped_matmul_dx(rows, n, k, groups, _ptr(dY), lddy, _ptr(W), ldw, stride, _ptr(ends),
+                                           _ptr(dX), lddx, types[dY.dtype], _stream(stream)),
+           "ozaki25_grouped_matmul_dx")
+    return dX
+
+
+def ozaki25_grouped_matmul_dw(dY, X, ends, dW=None, out_dtype=None, stream=None):
+    """dW[g] = sum of dY[r]^T X[r] over the rows r of group g, the gradient of
+    ozaki25_grouped_matmul's weights; zeros for an empty group.  out_dtype:
+    the inputs' (the default) or float32.  Returns dW, groups x n x k."""
+    torch = _torch or _tensors()
+    types = _half_types()
+    dY, lddy, _ = _pitched(dY, "dY", 2, types)
+    rows, n = dY.shape
+    X, ldx, _ = _pitched(X, "X", 2, (dY.dtype,))
+    k = X.shape[1]
+    if X.shape[0] != rows:
+        raise ValueError(f"X has {X.shape[0]} rows, dY has {rows}")
+    if not isinstance(ends, torch.Tensor):
+        raise ValueError("ends must be a contiguous 1-D int32 tensor")
+    groups = ends.numel()
+    _ends(ends, groups)
+    if dW is None:
+        dW = _new((groups, n, k), out_dtype or dY.dtype, dY.device, stream)
+    elif out_dtype is not None and dW.dtype != out_dtype:
+        raise ValueError(f"dW has dtype {dW.dtype}, out_dtype is {out_dtype}")
+    dW, lddw, stride = _pitched(dW, "dW", 3, (dY.dtype, torch.float32), (groups, n, k))
+    _on_gpu([("dY", dY), ("X", X), ("ends", ends), ("dW", dW)])
+    out = F32 if dW.dtype == torch.float32 else types[dY.dtype]
+    _check(lib().ozaki25_grouped_matmul_dw(rows, n, k, groups, _ptr(dY), lddy, _ptr(X), ldx, _ptr(ends), _ptr(dW),
+                                           lddw, stride, types[dY.dtype], out, _stream(stream)),
+           "ozaki25_grouped_matmul_dw")
+    return dW

@@ -1,0 +1,133 @@
+// Products of ragged groups of rows with a stack of weights: the forward
+// product, the gradient of its input and that of the weights.
+//
+//   Y[r, :]  = X[r, :] W_g^T          for the rows r of group g
+//   dX[r, :] = dY[r, :] W_g
+//   dW_g     = sum of dY[r, :]^T X[r, :] over the rows r of g
+//
+// The group ends are device memory: the host launches the most row tiles that
+// any ends could need (rows / BM + groups + 1) and every block finds its group
+// from the ends with two wavefront scans per 64 groups; blocks past the last
+// tile leave at once.
+#include "half_products.hpp"
+
+namespace oz {
+namespace half {
+namespace {
+
+// Place -> (row tile, column tile): row tiles in sets of kSet, column by column
+// inside a set, so that the blocks an XCD runs at a time share panels.
+constexpr uint32_t kSet = 4;
+__device__ __forceinline__ void place_to_tile(uint32_t place, uint32_t tiles_m, uint32_t tiles_n, uint32_t& tm,
+                                              uint32_t& tn) {
+  const uint32_t per = kSet * tiles_n;
+  const uint32_t s = place / per, in = place - s * per;
+  const uint32_t first = s * kSet;
+  const uint32_t size = tiles_m - first < kSet ? tiles_m - first : kSet;
+  tn = in / size;
+  tm = first + in - tn * size;
+}
+
+// Blocks are dealt round-robin over the 8 XCDs; each XCD takes one contiguous
+// range of the places.  False: no place is left for this block.
+__device__ __forceinline__ bool block_place(uint32_t b, uint32_t total, uint32_t& place) {
+  const uint32_t x = b & 7, i = b >> 3, per = total >> 3, rem = total & 7;
+  if (i >= per + (x < rem ? 1 : 0)) return false;
+  place = x * per + (x < rem ? x : rem) + i;
+  return true;
+}
+
+// Y (rows x cols) = X (rows x depth) times the group's weights: kAlong for
+// weights cols x depth, kAcross for depth x cols.
+template <class T, int OUT>
+__global__ __launch_bounds__(T::THREADS, 1) void grouped_rows_kernel(GroupedRows g) {
+  __shared__ __attribute__((aligned(1024))) char lds[T::LDS];
+  const uint32_t tiles_n = ((uint32_t)g.cols + T::BN - 1) / T::BN;
+  const uint32_t tiles_m = count_row_tiles<T::BM>(g.ends, g.groups, g.rows);
+  uint32_t place, tm, tn;
+  if (!block_place(blockIdx.x, tiles_m * tiles_n, place)) return;
+  place_to_tile(place, tiles_m, tiles_n, tm, tn);
+  RowTile t;
+  if (!find_row_tile<T::BM>(g.ends, g.groups, g.rows, (int)tm, t)) return;
+  const int c0 = (int)tn * T::BN;
+  const int cols = g.cols - c0 < T::BN ? g.cols - c0 : T::BN;
+  const bool none = t.group == g.groups;  // rows of no group: zeros
+  const char* w = (const char*)g.w + (none ? 0 : t.group * g.group_stride * 2);
+  const Operand a{(const char*)g.x + t.row * g.ldx * 2, g.ldx, t.rows};
+  const Operand b{w + (T::LB == kAlong ? c0 * g.ldw : (int64_t)c0) * 2, g.ldw, cols};
+  v16f acc[T::MB][T::NB] = {};
+  product<T>(a, b, none ? 0 : g.depth, lds, acc);
+  store<T, OUT>(acc, (typename Out<OUT>::type*)g.y + t.row * g.ldy + c0, g.ldy, t.rows, cols);
+}
+
+// dW_g (n x k) = dY_g^T X_g; a group without rows gets zeros.
+template <class T, int OUT>
+__global__ __launch_bounds__(T::THREADS, 1) void grouped_weights_kernel(GroupedWeights g) {
+  __shared__ __attribute__((aligned(1024))) char lds[T::LDS];
+  const uint32_t tiles_m = ((uint32_t)g.n + T::BM - 1) / T::BM, tiles_n = ((uint32_t)g.k + T::BN - 1) / T::BN;
+  uint32_t place, tm, tn;
+  if (!block_place(blockIdx.x, tiles_m * tiles_n * (uint32_t)g.groups, place)) return;
+  const uint32_t group = place / (tiles_m * tiles_n);
+  place_to_tile(place - group * tiles_m * tiles_n, tiles_m, tiles_n, tm, tn);
+  const int lane = threadIdx.x & 63;
+  int last = 0, first = 0, end = 0;
+  for (int g0 = 0; g0 <= (int)group; g0 += 64) group_rows(g.ends, g.groups, g.rows, g0, lane, last, first, end);
+  first = __builtin_amdgcn_readlane(first, group & 63);
+  end = __builtin_amdgcn_readlane(end, group & 63);
+  const int r0 = (int)tm * T::BM, c0 = (int)tn * T::BN;
+  const int rows = g.n - r0 < T::BM ? g.n - r0 : T::BM, cols = g.k - c0 < T::BN ? g.k - c0 : T::BN;
+  const Operand a{(const char*)g.dy + (first * g.lddy + r0) * 2, g.lddy, rows};
+  const Operand b{(const char*)g.x + (first * g.ldx + c0) * 2, g.ldx, cols};
+  v16f acc[T::MB][T::NB] = {};
+  product<T>(a, b, end - first, lds, acc);
+  store<T, OUT>(acc, (typename Out<OUT>::type*)g.dw + (int64_t)group * g.group_stride + r0 * g.lddw + c0, g.lddw, rows,
+                cols);
+}
+
+template <class T, int OUT>
+hipError_t run_rows(const GroupedRows& g, hipStream_t s) {
+  const int64_t tiles = ((int64_t)g.rows / T::BM + g.groups + 1) * ((g.cols + T::BN - 1) / T::BN);
+  if (tiles * T::THREADS >= ((int64_t)1 << 32)) return hipErrorInvalidConfiguration;
+  grouped_rows_kernel<T, OUT><<<dim3((uint32_t)tiles), dim3(T::THREADS), 0, s>>>(g);
+  return hipGetLastError();
+}
+
+template <class T, int OUT>
+hipError_t run_weights(const GroupedWeights& g, hipStream_t s) {
+  const int64_t tiles = (int64_t)g.groups * ((g.n + T::BM - 1) / T::BM) * ((g.k + T::BN - 1) / T::BN);
+  if (tiles * T::THREADS >= ((int64_t)1 << 32)) return hipErrorInvalidConfiguration;
+  grouped_weights_kernel<T, OUT><<<dim3((uint32_t)tiles), dim3(T::THREADS), 0, s>>>(g);
+  return hipGetLastError();
+}
+
+template <int TYPE, int LB>
+hipError_t rows_of_type(const GroupedRows& g, bool dma, hipStream_t s) {
+  if (dma) return run_rows<Tile<TYPE, kAlong, LB, 4, 4, 2, 2, true>, TYPE>(g, s);
+  return run_rows<Tile<TYPE, kAlong, LB, 2, 2, 2, 2, false>, TYPE>(g, s);
+}
+
+template <int TYPE, int OUT>
+hipError_t weights_of_type(const GroupedWeights& g, bool dma, hipStream_t s) {
+  if (dma) return run_weights<Tile<TYPE, kAcross, kAcross, 4, 4, 2, 2, true>, OUT>(g, s);
+  return run_weights<Tile<TYPE, kAcross, kAcross, 2, 2, 2, 2, false>, OUT>(g, s);
+}
+
+}  // namespace
+
+hipError_t launch_grouped_rows(const GroupedRows& g, int type, bool transposed, hipStream_t s) {
+  const bool dma = dma_operand(g.x, g.ldx, g.depth) && dma_operand(g.w, g.ldw, transposed ? g.cols : g.depth) &&
+                   g.group_stride % 8 == 0 && g.cols % 8 == 0 && g.depth % 8 == 0;
+  if (type == kBF16)
+    return transposed ? rows_of_type<kBF16, kAcross>(g, dma, s) : rows_of_type<kBF16, kAlong>(g, dma, s);
+  return transposed ? rows_of_type<kF16, kAcross>(g, dma, s) : rows_of_type<kF16, kAlong>(g, dma, s);
+}
+
+hipError_t launch_grouped_weights(const GroupedWeights& g, int type, int out, hipStream_t s) {
+  const bool dma = dma_operand(g.dy, g.lddy, g.n) && dma_operand(g.x, g.ldx, g.k);
+  if (type == kBF16)
+    return out == kF32 ? weights_of_type<kBF16, kF32>(g, dma, s) : weights_of_type<kBF16, kBF16>(g, dma, s);
+  return out == kF32 ? weights_of_type<kF16, kF32>(g, dma, s) : weights_of_type<kF16, kF16>(g, dma, s);
+}
+
+}  // namespace half
+}  // namespace oz
