@@ -39,7 +39,7 @@ __device__ __forceinline__ bool block_place(uint32_t b, uint32_t total, uint32_t
 
 // Y (rows x cols) = X (rows x depth) times the group's weights: kAlong for
 // weights cols x depth, kAcross for depth x cols.
-template <class T, int OUT>
+template <class T>
 __global__ __launch_bounds__(T::THREADS, 1) void grouped_rows_kernel(GroupedRows g) {
   __shared__ __attribute__((aligned(1024))) char lds[T::LDS];
   const uint32_t tiles_n = ((uint32_t)g.cols + T::BN - 1) / T::BN;
@@ -57,18 +57,20 @@ __global__ __launch_bounds__(T::THREADS, 1) void grouped_rows_kernel(GroupedRows
   const Operand b{w + (T::LB == kAlong ? c0 * g.ldw : (int64_t)c0) * 2, g.ldw, cols};
   v16f acc[T::MB][T::NB] = {};
   product<T>(a, b, none ? 0 : g.depth, lds, acc);
-  store<T, OUT>(acc, (typename Out<OUT>::type*)g.y + t.row * g.ldy + c0, g.ldy, t.rows, cols);
+  store<T>(acc, lds, (char*)g.y + (t.row * g.ldy + c0) * 2, g.ldy, t.rows, cols, g.vec);
 }
 
 // dW_g (n x k) = dY_g^T X_g; a group without rows gets zeros.
-template <class T, int OUT>
+template <class T>
 __global__ __launch_bounds__(T::THREADS, 1) void grouped_weights_kernel(GroupedWeights g) {
   __shared__ __attribute__((aligned(1024))) char lds[T::LDS];
   const uint32_t tiles_m = ((uint32_t)g.n + T::BM - 1) / T::BM, tiles_n = ((uint32_t)g.k + T::BN - 1) / T::BN;
+  // every group's tiles are spread over the XCDs by themselves: groups differ in depth
+  const uint32_t per = (tiles_m * tiles_n + 7) & ~7u;
+  const uint32_t group = blockIdx.x / per;
   uint32_t place, tm, tn;
-  if (!block_place(blockIdx.x, tiles_m * tiles_n * (uint32_t)g.groups, place)) return;
-  const uint32_t group = place / (tiles_m * tiles_n);
-  place_to_tile(place - group * tiles_m * tiles_n, tiles_m, tiles_n, tm, tn);
+  if (!block_place(blockIdx.x - group * per, tiles_m * tiles_n, place)) return;
+  place_to_tile(place, tiles_m, tiles_n, tm, tn);
   const int lane = threadIdx.x & 63;
   int last = 0, first = 0, end = 0;
   for (int g0 = 0; g0 <= (int)group; g0 += 64) group_rows(g.ends, g.groups, g.rows, g0, lane, last, first, end);
@@ -80,41 +82,43 @@ __global__ __launch_bounds__(T::THREADS, 1) void grouped_weights_kernel(GroupedW
   const Operand b{(const char*)g.x + (first * g.ldx + c0) * 2, g.ldx, cols};
   v16f acc[T::MB][T::NB] = {};
   product<T>(a, b, end - first, lds, acc);
-  store<T, OUT>(acc, (typename Out<OUT>::type*)g.dw + (int64_t)group * g.group_stride + r0 * g.lddw + c0, g.lddw, rows,
-                cols);
+  constexpr int E = sizeof(typename Out<T::OUT>::type);
+  store<T>(acc, lds, (char*)g.dw + (group * g.group_stride + r0 * g.lddw + c0) * E, g.lddw, rows, cols, g.vec);
 }
 
-template <class T, int OUT>
+template <class T>
 hipError_t run_rows(const GroupedRows& g, hipStream_t s) {
   const int64_t tiles = ((int64_t)g.rows / T::BM + g.groups + 1) * ((g.cols + T::BN - 1) / T::BN);
   if (tiles * T::THREADS >= ((int64_t)1 << 32)) return hipErrorInvalidConfiguration;
-  grouped_rows_kernel<T, OUT><<<dim3((uint32_t)tiles), dim3(T::THREADS), 0, s>>>(g);
+  grouped_rows_kernel<T><<<dim3((uint32_t)tiles), dim3(T::THREADS), 0, s>>>(g);
   return hipGetLastError();
 }
 
-template <class T, int OUT>
+template <class T>
 hipError_t run_weights(const GroupedWeights& g, hipStream_t s) {
-  const int64_t tiles = (int64_t)g.groups * ((g.n + T::BM - 1) / T::BM) * ((g.k + T::BN - 1) / T::BN);
+  const int64_t each = (int64_t)((g.n + T::BM - 1) / T::BM) * ((g.k + T::BN - 1) / T::BN);
+  const int64_t tiles = g.groups * ((each + 7) & ~(int64_t)7);
   if (tiles * T::THREADS >= ((int64_t)1 << 32)) return hipErrorInvalidConfiguration;
-  grouped_weights_kernel<T, OUT><<<dim3((uint32_t)tiles), dim3(T::THREADS), 0, s>>>(g);
+  grouped_weights_kernel<T><<<dim3((uint32_t)tiles), dim3(T::THREADS), 0, s>>>(g);
   return hipGetLastError();
 }
 
 template <int TYPE, int LB>
 hipError_t rows_of_type(const GroupedRows& g, bool dma, hipStream_t s) {
-  if (dma) return run_rows<Tile<TYPE, kAlong, LB, 4, 4, 2, 2, true>, TYPE>(g, s);
-  return run_rows<Tile<TYPE, kAlong, LB, 2, 2, 2, 2, false>, TYPE>(g, s);
+  if (dma) return run_rows<Tile<TYPE, kAlong, LB, 2, 4, 4, 2, true, TYPE>>(g, s);
+  return run_rows<Tile<TYPE, kAlong, LB, 2, 2, 2, 2, false, TYPE>>(g, s);
 }
 
 template <int TYPE, int OUT>
 hipError_t weights_of_type(const GroupedWeights& g, bool dma, hipStream_t s) {
-  if (dma) return run_weights<Tile<TYPE, kAcross, kAcross, 4, 4, 2, 2, true>, OUT>(g, s);
-  return run_weights<Tile<TYPE, kAcross, kAcross, 2, 2, 2, 2, false>, OUT>(g, s);
+  if (dma) return run_weights<Tile<TYPE, kAcross, kAcross, 2, 4, 4, 2, true, OUT>>(g, s);
+  return run_weights<Tile<TYPE, kAcross, kAcross, 2, 2, 2, 2, false, OUT>>(g, s);
 }
 
 }  // namespace
 
-hipError_t launch_grouped_rows(const GroupedRows& g, int type, bool transposed, hipStream_t s) {
+hipError_t launch_grouped_rows(GroupedRows g, int type, bool transposed, hipStream_t s) {
+  g.vec = (uintptr_t)g.y % 16 == 0 && g.ldy % 8 == 0 && g.cols % 8 == 0;
   const bool dma = dma_operand(g.x, g.ldx, g.depth) && dma_operand(g.w, g.ldw, transposed ? g.cols : g.depth) &&
                    g.group_stride % 8 == 0 && g.cols % 8 == 0 && g.depth % 8 == 0;
   if (type == kBF16)
@@ -122,7 +126,8 @@ hipError_t launch_grouped_rows(const GroupedRows& g, int type, bool transposed, 
   return transposed ? rows_of_type<kF16, kAcross>(g, dma, s) : rows_of_type<kF16, kAlong>(g, dma, s);
 }
 
-hipError_t launch_grouped_weights(const GroupedWeights& g, int type, int out, hipStream_t s) {
+hipError_t launch_grouped_weights(GroupedWeights g, int type, int out, hipStream_t s) {
+  g.vec = (uintptr_t)g.dw % 16 == 0 && g.lddw % 8 == 0 && g.group_stride % 8 == 0 && g.k % 8 == 0;
   const bool dma = dma_operand(g.dy, g.lddy, g.n) && dma_operand(g.x, g.ldx, g.k);
   if (type == kBF16)
     return out == kF32 ? weights_of_type<kBF16, kF32>(g, dma, s) : weights_of_type<kBF16, kBF16>(g, dma, s);

@@ -16,6 +16,7 @@ struct GroupedRows {
   void* y;  // rows x cols
   int64_t ldy;
   int rows, cols, depth, groups;
+  bool vec;  // 16-byte stores of y (set by the launch)
 };
 
 struct GroupedWeights {
@@ -27,6 +28,7 @@ struct GroupedWeights {
   void* dw;  // a stack of n x k
   int64_t lddw, group_stride;
   int rows, n, k, groups;
+  bool vec;  // 16-byte stores of a 16-bit dw (set by the launch)
 };
 
 // Whether a matrix of `cols` columns can go to LDS by DMA: 16-byte rows, and a
@@ -35,8 +37,8 @@ inline bool dma_operand(const void* p, int64_t ld, int64_t cols) {
   return (uintptr_t)p % 16 == 0 && ld % 8 == 0 && cols % 8 == 0 && ld < ((int64_t)1 << 21);
 }
 
-hipError_t launch_grouped_rows(const GroupedRows& g, int type, bool transposed, hipStream_t s);
-hipError_t launch_grouped_weights(const GroupedWeights& g, int type, int out, hipStream_t s);
+hipError_t launch_grouped_rows(GroupedRows g, int type, bool transposed, hipStream_t s);
+hipError_t launch_grouped_weights(GroupedWeights g, int type, int out, hipStream_t s);
 
 }  // namespace half
 }  // namespace oz

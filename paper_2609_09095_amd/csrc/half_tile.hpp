@@ -31,6 +31,7 @@
 #include <hip/hip_runtime.h>
 
 #include <cstdint>
+#include <type_traits>
 
 namespace oz {
 namespace half {
@@ -42,6 +43,7 @@ typedef __bf16 v8b __attribute__((ext_vector_type(8)));
 typedef _Float16 v8h __attribute__((ext_vector_type(8)));
 typedef float v16f __attribute__((ext_vector_type(16)));
 using lds_ptr = __attribute__((address_space(3))) void*;
+using lds_bytes = const __attribute__((address_space(3))) char*;
 
 constexpr int kBF16 = 0, kF16 = 1, kF32 = 2;  // element types (ozaki25_dtype)
 constexpr int kAlong = 0, kAcross = 1;        // operand layouts
@@ -90,16 +92,24 @@ struct Operand {
   int vecs;    // vectors that exist, at most the tile's
 };
 
+template <class T>
+struct DmaLoads;
+template <class T>
+struct MaskedLoads;
+
 // A tile's shape: WR x WC wavefronts, each MB x NB blocks of 32 x 32 outputs.
-template <int TYPE_, int LA_, int LB_, int WR_, int WC_, int MB_, int NB_, bool DMA_>
+// OUT: the output type.  A 16-bit output's blocks are multiplied transposed
+// (WIDE), which gives a lane four consecutive columns of one row.
+template <int TYPE_, int LA_, int LB_, int WR_, int WC_, int MB_, int NB_, bool DMA_, int OUT_>
 struct Tile {
-  static constexpr int TYPE = TYPE_, LA = LA_, LB = LB_, WR = WR_, WC = WC_, MB = MB_, NB = NB_;
-  static constexpr bool DMA = DMA_;
+  static constexpr int TYPE = TYPE_, LA = LA_, LB = LB_, WR = WR_, WC = WC_, MB = MB_, NB = NB_, OUT = OUT_;
+  static constexpr bool DMA = DMA_, WIDE = OUT_ != kF32;
   static constexpr int BM = WR * MB * 32, BN = WC * NB * 32;
   static constexpr int WAVES = WR * WC, THREADS = WAVES * 64;
   static constexpr int A_BYTES = BM * kDepth * 2, B_BYTES = BN * kDepth * 2;
   static constexpr int STAGE = A_BYTES + B_BYTES, LDS = 2 * STAGE;
   static constexpr int ADMA = A_BYTES / 1024 / WAVES, BDMA = B_BYTES / 1024 / WAVES;
+  using Loads = std::conditional_t<DMA, DmaLoads<Tile>, MaskedLoads<Tile>>;
   static_assert(ADMA * WAVES * 1024 == A_BYTES && BDMA * WAVES * 1024 == B_BYTES, "whole slabs per wavefront");
 };
 
@@ -117,9 +127,19 @@ __device__ __forceinline__ void chunk_at(int o, int& r, int& c) {
   }
 }
 
-// ---- DMA loader -----------------------------------------------------------
+// vmcnt(n) alone
+template <int N>
+__device__ __forceinline__ void wait_loads() {
+  static_assert(N < 64);
+  __builtin_amdgcn_s_waitcnt((N & 15) | ((N >> 4) << 14) | (7 << 4) | (15 << 8));
+}
+
+// ---- loaders ----------------------------------------------------------------
+// Both fill the two stage buffers in prologue() and then, per stage,
+//   early()                  while the stage is multiplied
+//   begin(), late(j), end()  once its buffer is free: load j of the stage after next
 template <int L, int V, int N>
-struct Dma {
+struct DmaSide {
   int voff[N];  // byte offset of each of the wavefront's N slabs' chunks
   int dep[N];   // first depth of that chunk (kAlong)
   const char* p;
@@ -155,9 +175,48 @@ struct Dma {
   }
 };
 
-// ---- masked loader --------------------------------------------------------
+template <class T>
+struct DmaLoads {
+  DmaSide<T::LA, T::BM, T::ADMA> a;
+  DmaSide<T::LB, T::BN, T::BDMA> b;
+  __amdgpu_buffer_rsrc_t ra, rb;
+  int left;
+  __device__ __forceinline__ void init(const Operand& oa, const Operand& ob, int depth, int wave, int lane) {
+    a.init(oa, depth, wave, lane);
+    b.init(ob, depth, wave, lane);
+    left = depth;
+  }
+  __device__ __forceinline__ void begin() {
+    ra = a.rsrc(left);
+    rb = b.rsrc(left);
+  }
+  __device__ __forceinline__ void late(int j, char* buf, int wave, int) {
+    if (j < T::ADMA)
+      a.load(j, ra, buf, wave, left);
+    else
+      b.load(j - T::ADMA, rb, buf + T::A_BYTES, wave, left);
+  }
+  __device__ __forceinline__ void end() {
+    left -= kDepth;
+    a.advance();
+    b.advance();
+  }
+  __device__ __forceinline__ void early(int, int) {}
+  __device__ __forceinline__ void prologue(char* lds, int wave, int lane) {
+#pragma unroll
+    for (int s = 0; s < 2; ++s) {
+      begin();
+#pragma unroll
+      for (int j = 0; j < T::ADMA + T::BDMA; ++j) late(j, lds + s * T::STAGE, wave, lane);
+      end();
+    }
+    wait_loads<T::ADMA + T::BDMA>();
+    __syncthreads();
+  }
+};
+
 template <int L, int V, int N>
-struct Masked {
+struct MaskedSide {
   v4i reg[N];
   const char* p;
   int64_t ld;
@@ -189,69 +248,136 @@ struct Masked {
       }
       reg[i] = v;
     }
+    p += L == kAlong ? kDepth * 2 : ld * kDepth * 2;
   }
-  __device__ __forceinline__ void put(char* lds, int wave, int lane) const {
-#pragma unroll
-    for (int i = 0; i < N; ++i) *(v4i*)(lds + (wave * N + i) * 1024 + lane * 16) = reg[i];
+  __device__ __forceinline__ void put(int i, char* lds, int wave, int lane) const {
+    *(v4i*)(lds + (wave * N + i) * 1024 + lane * 16) = reg[i];
   }
-  __device__ __forceinline__ void advance() { p += L == kAlong ? kDepth * 2 : ld * kDepth * 2; }
 };
 
-// Fragment of the 32 vectors from v0 for depths 16 ks .. + 15 of a stage.
-template <int L, int V>
-__device__ __forceinline__ v4i frag(const char* lds, int v0, int ks, int lane) {
-  if constexpr (L == kAlong) {
-    const int v = v0 + (lane & 31);
-    return *(const v4i*)(lds + v * 128 + (((2 * ks + (lane >> 5)) ^ swz_along(v)) << 4));
-  } else {
-    using tr = __attribute__((address_space(3))) v4s*;
-    const int d = 16 * ks + 8 * (lane >> 5) + ((lane >> 2) & 3);
-    const int piece = ((v0 >> 4) + ((lane >> 4) & 1)) ^ swz_across(d);
-    const char* q = lds + d * (V * 2) + piece * 32 + (lane & 3) * 8;
-    const v4s lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((tr)q);
-    const v4s hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((tr)(q + 4 * V * 2));
-    return __builtin_bit_cast(v4i, v8s{lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]});
+template <class T>
+struct MaskedLoads {
+  MaskedSide<T::LA, T::BM, T::ADMA> a;
+  MaskedSide<T::LB, T::BN, T::BDMA> b;
+  int left;
+  __device__ __forceinline__ void init(const Operand& oa, const Operand& ob, int depth, int, int) {
+    a.init(oa);
+    b.init(ob);
+    left = depth;
   }
-}
+  __device__ __forceinline__ void early(int wave, int lane) {
+    a.load(wave, lane, left);
+    b.load(wave, lane, left);
+    left -= kDepth;
+  }
+  __device__ __forceinline__ void begin() {}
+  __device__ __forceinline__ void late(int j, char* buf, int wave, int lane) {
+    if (j < T::ADMA)
+      a.put(j, buf, wave, lane);
+    else
+      b.put(j - T::ADMA, buf + T::A_BYTES, wave, lane);
+  }
+  __device__ __forceinline__ void end() {}
+  __device__ __forceinline__ void prologue(char* lds, int wave, int lane) {
+#pragma unroll
+    for (int s = 0; s < 2; ++s) {
+      early(wave, lane);
+#pragma unroll
+      for (int j = 0; j < T::ADMA + T::BDMA; ++j) late(j, lds + s * T::STAGE, wave, lane);
+    }
+    __syncthreads();
+  }
+};
 
-// One stage's products; `issue(j)` starts the j-th of ND loads of the next
-// stage among the first MFMAs.
-template <class T, int ND, class F>
-__device__ __forceinline__ void stage_mma(const char* la, const char* lb, int wr, int wc, int lane,
-                                          v16f (&acc)[T::MB][T::NB], F issue) {
-  v4i af[4][T::MB], bf[4][T::NB];
+// Fragments of a wavefront's N blocks of 32 vectors from block w0 on.
+template <int L, int V, int N>
+struct Fragments {
+  // kAlong: by K step (16 depths); kAcross: by block.  LDS byte offsets.
+  int base[L == kAlong ? 4 : N];
+  __device__ __forceinline__ void init(int w0, int lane) {
+    if constexpr (L == kAlong) {
+      const int v = w0 * 32 + (lane & 31);
+      const int c = (lane >> 5) ^ swz_along(v);
 #pragma unroll
-  for (int ks = 0; ks < 4; ++ks) {
+      for (int ks = 0; ks < 4; ++ks) base[ks] = v * 128 + ((c << 4) ^ (ks << 5));
+    } else {
+      const int d = 8 * (lane >> 5) + ((lane >> 2) & 3);
 #pragma unroll
-    for (int x = 0; x < T::MB; ++x) af[ks][x] = frag<T::LA, T::BM>(la, (wr * T::MB + x) * 32, ks, lane);
-#pragma unroll
-    for (int x = 0; x < T::NB; ++x) bf[ks][x] = frag<T::LB, T::BN>(lb, (wc * T::NB + x) * 32, ks, lane);
-  }
-#pragma unroll
-  for (int ks = 0; ks < 4; ++ks)
-#pragma unroll
-    for (int a = 0; a < T::MB; ++a)
-#pragma unroll
-      for (int b = 0; b < T::NB; ++b) {
-        const int j = (ks * T::MB + a) * T::NB + b;
-        if (j < ND) issue(j);
-        acc[a][b] = mfma<T::TYPE>(af[ks][a], bf[ks][b], acc[a][b]);
+      for (int x = 0; x < N; ++x) {
+        const int piece = (2 * (w0 + x) + ((lane >> 4) & 1)) ^ swz_across(d);
+        base[x] = d * (V * 2) + piece * 32 + (lane & 3) * 8;
       }
-  // reads of K step ks + 1 among the MFMAs of step ks, the loads among step 0's
-  constexpr int PER = (T::LA == kAcross ? 2 : 1) * T::MB + (T::LB == kAcross ? 2 : 1) * T::NB;  // reads per step
-  constexpr int M = T::MB * T::NB;                                                           // MFMAs per step
-  __builtin_amdgcn_sched_group_barrier(0x100, PER, 0);
+    }
+  }
+  // block x, K step ks of the stage at lds
+  __device__ __forceinline__ v4i read(lds_bytes lds, int ks, int x) const {
+    if constexpr (L == kAlong) {
+      return *(const __attribute__((address_space(3))) v4i*)(lds + base[ks] + x * 4096);
+    } else {
+      using tr = __attribute__((address_space(3))) v4s*;
+      const auto q = lds + base[x] + ks * (32 * V);
+      const v4s lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((tr)q);
+      const v4s hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((tr)(q + 8 * V));
+      return __builtin_bit_cast(v4i, v8s{lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]});
+    }
+  }
+};
+
+// One stage's products; on entry the fragments of its first K step are in
+// af[0], bf[0].  cur, next: this stage's and the next one's buffer; freed: cur,
+// as the target of the loads.  The three are declared not to alias, or the
+// compiler would wait for all loads in flight before every transposing read:
+// what keeps them apart is the barrier.
+template <class T, class Loader, class FA, class FB>
+__device__ __forceinline__ void stage_products(Loader& ld, const FA& fa, const FB& fb, lds_bytes __restrict__ cur,
+                                               lds_bytes __restrict__ next, char* __restrict__ freed, int wave,
+                                               int lane, v4i (&af)[2][T::MB], v4i (&bf)[2][T::NB],
+                                               v16f (&acc)[T::MB][T::NB]) {
+  constexpr int ND = T::ADMA + T::BDMA, M = T::MB * T::NB, KS = kDepth / 16, R = T::MB + T::NB;
+  ld.early(wave, lane);
 #pragma unroll
-  for (int ks = 0; ks < 4; ++ks)
+  for (int ks = 0; ks < KS; ++ks) {
+    const bool last = ks + 1 == KS;
+    if (last) {
+      __builtin_amdgcn_s_waitcnt(0);
+      __syncthreads();
+      ld.begin();
+    }
+    __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
     for (int i = 0; i < M; ++i) {
-      if (ks < 3) __builtin_amdgcn_sched_group_barrier(0x100, (PER + M - 1) / M, 0);
-      if (ks * M + i < ND) __builtin_amdgcn_sched_group_barrier(0x020, 1, 0);
-      __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+      // this product's share of the next step's fragments
+#pragma unroll
+      for (int f = i * R / M; f < (i + 1) * R / M; ++f) {
+        if (f < T::MB)
+          af[(ks + 1) & 1][f] = fa.read(last ? next : cur, (ks + 1) % KS, f);
+        else
+          bf[(ks + 1) & 1][f - T::MB] = fb.read((last ? next : cur) + T::A_BYTES, (ks + 1) % KS, f - T::MB);
+      }
+      if (last) {
+#pragma unroll
+        for (int j = i * ND / M; j < (i + 1) * ND / M; ++j) ld.late(j, freed, wave, lane);
+      }
+      const int x = i / T::NB, y = i % T::NB;
+      acc[x][y] = T::WIDE ? mfma<T::TYPE>(bf[ks & 1][y], af[ks & 1][x], acc[x][y])
+                          : mfma<T::TYPE>(af[ks & 1][x], bf[ks & 1][y], acc[x][y]);
+      __builtin_amdgcn_sched_barrier(0);
     }
+  }
+  ld.end();
 }
 
 // acc += A B over `depth`; lds: T::LDS bytes, 1024-aligned.
+//
+// Two stages in LDS.  The last K step's products of a stage run behind the
+// barrier that hands over to the next stage: their fragments are in registers
+// by then, so the matrix cores work while the next stage's first fragments
+// are read, and the buffer just freed takes the loads of the stage after
+// next, which then have a whole stage's products to arrive.  The order of
+// reads, loads and products is the written one (sched_barrier).
+//
+// Wavefronts whose rows all lie past the tile's edge load and wait like the
+// others, but multiply nothing (the matrix cores and the clock are theirs).
 template <class T>
 __device__ __forceinline__ void product(const Operand& a, const Operand& b, int depth, char* lds,
                                         v16f (&acc)[T::MB][T::NB]) {
@@ -260,104 +386,123 @@ __device__ __forceinline__ void product(const Operand& a, const Operand& b, int 
   const int wr = wave / T::WC, wc = wave % T::WC;
   const int nst = (depth + kDepth - 1) / kDepth;
   if (nst == 0) return;
-  char* const buf0 = lds;
-  char* const buf1 = lds + T::STAGE;
-  if constexpr (T::DMA) {
-    Dma<T::LA, T::BM, T::ADMA> da;
-    Dma<T::LB, T::BN, T::BDMA> db;
-    da.init(a, depth, wave, lane);
-    db.init(b, depth, wave, lane);
-    int left = depth;
-    auto start = [&](char* buf) {
-      const auto ra = da.rsrc(left), rb = db.rsrc(left);
-#pragma unroll
-      for (int i = 0; i < T::ADMA; ++i) da.load(i, ra, buf, wave, left);
-#pragma unroll
-      for (int i = 0; i < T::BDMA; ++i) db.load(i, rb, buf + T::A_BYTES, wave, left);
-    };
-    auto next = [&]() {
-      left -= kDepth;
-      da.advance();
-      db.advance();
-    };
-    auto stage = [&](char* cur, char* nxt) __attribute__((always_inline)) {
+  constexpr int ND = T::ADMA + T::BDMA;
+  using Loader = typename T::Loads;
+  Loader ld;
+  ld.init(a, b, depth, wave, lane);
+  ld.prologue(lds, wave, lane);
+  const bool active = wr * T::MB * 32 < a.vecs;
+  if (!active) {
+    int cur = 0;
+    for (int s = 0; s < nst; ++s) {
+      ld.early(wave, lane);
       __builtin_amdgcn_s_waitcnt(0);
       __syncthreads();
-      next();
-      const auto ra = da.rsrc(left), rb = db.rsrc(left);
-      stage_mma<T, T::ADMA + T::BDMA>(cur, cur + T::A_BYTES, wr, wc, lane, acc, [&](int j) {
-        if (j < T::ADMA)
-          da.load(j, ra, nxt, wave, left);
-        else
-          db.load(j - T::ADMA, rb, nxt + T::A_BYTES, wave, left);
-      });
-    };
-    start(buf0);
-    for (int s = 0; s < nst; s += 2) {
-      stage(buf0, buf1);
-      if (s + 1 >= nst) break;
-      stage(buf1, buf0);
+      ld.begin();
+#pragma unroll
+      for (int j = 0; j < ND; ++j) ld.late(j, lds + cur, wave, lane);
+      ld.end();
+      cur ^= T::STAGE;
     }
-    __builtin_amdgcn_s_waitcnt(0);  // the look-ahead past the end (zeros) lands before LDS is used again
-    __syncthreads();
   } else {
-    Masked<T::LA, T::BM, T::ADMA> ma;
-    Masked<T::LB, T::BN, T::BDMA> mb;
-    ma.init(a);
-    mb.init(b);
-    int left = depth;
-    ma.load(wave, lane, left);
-    mb.load(wave, lane, left);
-    ma.put(buf0, wave, lane);
-    mb.put(buf0 + T::A_BYTES, wave, lane);
-    char* cur = buf0;
-    char* nxt = buf1;
+    Fragments<T::LA, T::BM, T::MB> fa;
+    Fragments<T::LB, T::BN, T::NB> fb;
+    fa.init(wr * T::MB, lane);
+    fb.init(wc * T::NB, lane);
+    const auto l3 = (lds_bytes)lds;
+    v4i af[2][T::MB], bf[2][T::NB];
+#pragma unroll
+    for (int x = 0; x < T::MB; ++x) af[0][x] = fa.read(l3, 0, x);
+#pragma unroll
+    for (int x = 0; x < T::NB; ++x) bf[0][x] = fb.read(l3 + T::A_BYTES, 0, x);
+    int cur = 0;
     for (int s = 0; s < nst; ++s) {
-      __syncthreads();
-      left -= kDepth;
-      ma.advance();
-      mb.advance();
-      if (s + 1 < nst) {
-        ma.load(wave, lane, left);
-        mb.load(wave, lane, left);
-      }
-      stage_mma<T, 0>(cur, cur + T::A_BYTES, wr, wc, lane, acc, [](int) {});
-      if (s + 1 < nst) {
-        ma.put(nxt, wave, lane);
-        mb.put(nxt + T::A_BYTES, wave, lane);
-      }
-      char* t = cur;
-      cur = nxt;
-      nxt = t;
+      stage_products<T>(ld, fa, fb, l3 + cur, l3 + (cur ^ T::STAGE), lds + cur, wave, lane, af, bf, acc);
+      cur ^= T::STAGE;
     }
-    __syncthreads();
   }
+  __builtin_amdgcn_s_waitcnt(0);  // the look-ahead past the end (zeros) lands before LDS is used again
+  __syncthreads();
 }
 
-// Calls f(row, column, value) for every output of the wavefront's blocks: lane
-// l of a 32 x 32 block holds column l % 32, rows 8 (i / 4) + 4 (l / 32) + i % 4.
-template <class T, class F>
-__device__ __forceinline__ void each_output(const v16f (&acc)[T::MB][T::NB], F f) {
+// The tile's rows < rows and columns < cols to a row-major matrix, rounded
+// once to its type.  16-bit outputs go through LDS (the wavefront's own part,
+// free after the last stage) so that 16 bytes per lane and whole 64-byte runs
+// reach memory; `vec` says that rows start on 16 bytes and cols is a multiple
+// of 8, else single elements are stored from LDS.  32-bit outputs are stored
+// straight from registers, 32 consecutive columns per half wavefront.
+template <class T>
+__device__ __forceinline__ void store(const v16f (&acc)[T::MB][T::NB], char* lds, void* out, int64_t ld, int rows,
+                                      int cols, bool vec) {
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int r0 = wave / T::WC * T::MB * 32 + 4 * (lane >> 5), c0 = wave % T::WC * T::NB * 32 + (lane & 31);
+  const int r0 = wave / T::WC * T::MB * 32, c0 = wave % T::WC * T::NB * 32;
+  if constexpr (T::WIDE) {
+    using O = typename Out<T::OUT>::type;
+    typedef O o2 __attribute__((ext_vector_type(2)));
+    constexpr int PITCH = T::NB * 64, CH = T::NB * 4;  // bytes and 16-byte chunks per row
+    static_assert(T::MB * 32 * PITCH * T::WAVES <= T::LDS, "outputs fit the stages' LDS");
+    char* const mine = lds + wave * (T::MB * 32 * PITCH);
+    const int row = lane & 31, half = lane >> 5;
 #pragma unroll
-  for (int a = 0; a < T::MB; ++a)
+    for (int a = 0; a < T::MB; ++a)
 #pragma unroll
-    for (int i = 0; i < 16; ++i)
+      for (int b = 0; b < T::NB; ++b)
 #pragma unroll
-      for (int b = 0; b < T::NB; ++b) f(r0 + a * 32 + 8 * (i >> 2) + (i & 3), c0 + b * 32, acc[a][b][i]);
-}
-
-// The tile's rows < rows and columns < cols to a row-major matrix, one
-// rounding to its type.
-template <class T, int OUT>
-__device__ __forceinline__ void store(const v16f (&acc)[T::MB][T::NB], void* out, int64_t ld, int rows, int cols) {
-  using O = typename Out<OUT>::type;
-  O* const o = (O*)out;
-  each_output<T>(acc, [&](int r, int c, float v) {
-    if (r < rows && c < cols) o[(int64_t)r * ld + c] = (O)v;
-  });
+        for (int q = 0; q < 4; ++q) {
+          const v16f& c = acc[a][b];
+          const o2 lo = {(O)c[4 * q], (O)c[4 * q + 1]}, hi = {(O)c[4 * q + 2], (O)c[4 * q + 3]};
+          char* p = mine + (a * 32 + row) * PITCH + (((b * 4 + q) ^ (row & (CH - 1))) << 4) + half * 8;
+          *(uint2*)p = uint2{__builtin_bit_cast(uint32_t, lo), __builtin_bit_cast(uint32_t, hi)};
+        }
+    // the wavefront reads what its own lanes wrote
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+    constexpr int RPI = 64 / CH;  // rows per instruction
+    const int lr = lane / CH, ch = lane % CH;
+    const int cleft = cols - c0 - ch * 8;
+    O* const o = (O*)out + (int64_t)(r0 + lr) * ld + c0 + ch * 8;
+    constexpr int ROUNDS = T::MB * 32 / RPI;
+    v4i v[ROUNDS];
+#pragma unroll
+    for (int i = 0; i < ROUNDS; ++i) {
+      const int r = i * RPI + lr;
+      v[i] = *(const v4i*)(mine + r * PITCH + ((ch ^ (r & (CH - 1))) << 4));
+    }
+    const int rleft = cleft > 0 ? rows - r0 - lr : 0;
+    if (vec) {
+#pragma unroll
+      for (int i = 0; i < ROUNDS; ++i)
+        if (i * RPI < rleft) *(v4i*)(o + (int64_t)(i * RPI) * ld) = v[i];
+    } else {
+#pragma unroll
+      for (int i = 0; i < ROUNDS; ++i)
+        if (i * RPI < rleft) {
+          short* const q = (short*)(o + (int64_t)(i * RPI) * ld);
+          const v8s e = __builtin_bit_cast(v8s, v[i]);
+#pragma unroll
+          for (int j = 0; j < 8; ++j)
+            if (j < cleft) q[j] = e[j];
+        }
+    }
+  } else {
+    // lane l of a block: column l % 32, rows 8 (i / 4) + 4 (l / 32) + i % 4
+    const int row = r0 + 4 * (lane >> 5), col = c0 + (lane & 31);
+    float* const o = (float*)out + (int64_t)row * ld + col;
+#pragma unroll
+    for (int a = 0; a < T::MB; ++a)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        const int r = a * 32 + 8 * (i >> 2) + (i & 3);
+        float* const p = o + (int64_t)r * ld;
+        if (row + r < rows) {
+#pragma unroll
+          for (int b = 0; b < T::NB; ++b)
+            if (col + b * 32 < cols) p[b * 32] = acc[a][b][i];
+        }
+      }
+  }
 }
 
 // ---- groups of rows ---------------------------------------------------------
