@@ -385,6 +385,60 @@ ozaki25_status ozaki25_grouped_matmul_dw(int64_t rows, int64_t n, int64_t k, int
                                          int64_t lddw, int64_t group_stride, ozaki25_dtype type,
                                          ozaki25_dtype out_type, void* stream);
 
+#define OZAKI25_MAX_RANK 256
+
+/* A shared projection with low-rank adapters of many requests at once:
+ *   Y[t, :] = X[t, :] W^T + scales[a] (X[t, :] A_a^T) B_a^T,  a = ids[t],
+ * and the projection alone in rows whose id lies outside [0, adapters).
+ *  X: rows x k (ldx);  W: n x k (ldw);  ids: int32 [rows], read on the device,
+ *  in any order;  A: adapters matrices rank x k (lda), a_stride elements apart;
+ *  B: adapters matrices n x rank (ldb), b_stride apart;  scales: float32
+ *  [adapters], or NULL for 1;  Y: rows x n (ldy).  Adapters of lower rank are
+ *  padded with zeros.
+ *  type: OZAKI25_BF16 or OZAKI25_F16, of X, W, A, B and Y.  Both sums run in
+ *    FP32; scales[a] X A_a^T enters the second product as two numbers of the
+ *    type (the rounded value and the rest; beyond the type's range, in half
+ *    65504, it is an infinity).
+ *  workspace: NULL to allocate stream-ordered, else at least
+ *    ozaki25_adapter_matmul_workspace_size() bytes, 256-byte aligned.
+ * Y must not overlap the inputs.  rows == 0 or n == 0: no-op; k == 0: zeros.
+ * Errors: INVALID_VALUE, UNSUPPORTED (sizes; rank beyond OZAKI25_MAX_RANK),
+ * WORKSPACE, HIP. */
+size_t ozaki25_adapter_matmul_workspace_size(int64_t rows, int64_t n, int64_t k, int64_t adapters, int64_t rank);
+ozaki25_status ozaki25_adapter_matmul(int64_t rows, int64_t n, int64_t k, int64_t adapters, int64_t rank,
+                                      const void* X, int64_t ldx, const void* W, int64_t ldw,
+                                      const int32_t* ids, const void* A, int64_t lda, int64_t a_stride,
+                                      const void* B, int64_t ldb, int64_t b_stride, const float* scales,
+                                      void* Y, int64_t ldy, ozaki25_dtype type, void* workspace,
+                                      size_t workspace_bytes, void* stream);
+
+#define OZAKI25_MAX_SIDE 32768 /* rows or columns of a matrix to orthogonalise */
+#define OZAKI25_MAX_STEPS 64
+
+/* Orthogonalisation of a stack of matrices by Newton-Schulz products (the
+ * update of an optimiser that keeps a momentum G per weight matrix):
+ *   X_0 = G / (|G|_F + eps);   `steps` times:  S = X X^T,
+ *   X <- a X + (b S + c S^2) X
+ * (S = X^T X and X <- a X + X (b S + c S^2) where m > n), which maps every
+ * singular value s of X_0 through a s + b s^3 + c s^5.
+ *  G: count matrices m x n (ldg), g_stride elements apart, bfloat16, half or
+ *    float32;  X: the same (ldx, x_stride >= (m - 1) ldx + n), bfloat16.
+ *  a, b, c: e.g. 3.4445, -4.7750, 2.0315 with 5 steps, which brings singular
+ *    values to about [0.7, 1.2].
+ * X is carried from step to step in FP32; the products' operands are rounded
+ * to half (11 bits) and summed in FP32; the norm is a 64-bit sum.  A matrix of
+ * zeros gives zeros; one with a NaN or infinity gives NaN.
+ *  workspace: NULL to allocate stream-ordered, else at least
+ *    ozaki25_orthogonalise_workspace_size() bytes, 256-byte aligned (about 8
+ *    bytes per element and 4 per element of the shorter side squared).
+ * X must not overlap G.  count, m or n == 0: no-op.  Errors: INVALID_VALUE,
+ * UNSUPPORTED (a side beyond OZAKI25_MAX_SIDE), WORKSPACE, HIP. */
+size_t ozaki25_orthogonalise_workspace_size(int64_t count, int64_t m, int64_t n);
+ozaki25_status ozaki25_orthogonalise(int64_t count, int64_t m, int64_t n, const void* G, int64_t ldg,
+                                     int64_t g_stride, ozaki25_dtype type, void* X, int64_t ldx,
+                                     int64_t x_stride, int steps, float a, float b, float c, float eps,
+                                     void* workspace, size_t workspace_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

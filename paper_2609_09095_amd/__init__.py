@@ -25,6 +25,8 @@ __all__ = [
     "ozaki25_accurate_exponents_workspace_size", "ozaki25_accurate_exponents",
     "ozaki25_dgemm_accurate_workspace_size", "ozaki25_dgemm_accurate",
     "ozaki25_grouped_matmul", "ozaki25_grouped_matmul_dx", "ozaki25_grouped_matmul_dw",
+    "ozaki25_adapter_matmul_workspace_size", "ozaki25_adapter_matmul",
+    "ozaki25_orthogonalise_workspace_size", "ozaki25_orthogonalise",
 ]
 
 _PKG = os.path.dirname(os.path.abspath(__file__))
@@ -49,6 +51,9 @@ MAX_ROWS = 1 << 30          # limits of the 16-bit products
 MAX_WIDTH = 1 << 22
 MAX_LD = 1 << 32
 MAX_GROUPS = 65536
+MAX_RANK = 256
+MAX_SIDE = 32768
+MAX_STEPS = 64
 
 SUCCESS, ERR_INVALID_VALUE, ERR_UNSUPPORTED, ERR_WORKSPACE, ERR_HIP = range(5)
 
@@ -74,6 +79,7 @@ def lib():
             raise ImportError(f"{_LIB_PATH} is not built: run `python -m paper_2609_09095_amd.build`")
         L = ctypes.CDLL(_LIB_PATH)
         P, i64, i32, sz = ctypes.c_void_p, ctypes.c_int64, ctypes.c_int, ctypes.c_size_t
+        f32 = ctypes.c_float
         sig = {
             "ozaki25_status_string": ([i32], ctypes.c_char_p),
             "ozaki25_num_moduli": ([i32], i32),
@@ -99,6 +105,12 @@ def lib():
                                        i32),
             "ozaki25_grouped_matmul": ([i64, i64, i64, i64, P, i64, P, i64, i64, P, P, i64, i32, P], i32),
             "ozaki25_grouped_matmul_dx": ([i64, i64, i64, i64, P, i64, P, i64, i64, P, P, i64, i32, P], i32),
+            "ozaki25_adapter_matmul_workspace_size": ([i64, i64, i64, i64, i64], sz),
+            "ozaki25_adapter_matmul": ([i64, i64, i64, i64, i64, P, i64, P, i64, P, P, i64, i64, P, i64, i64, P, P, i64,
+                                        i32, P, sz, P], i32),
+            "ozaki25_orthogonalise_workspace_size": ([i64, i64, i64], sz),
+            "ozaki25_orthogonalise": ([i64, i64, i64, P, i64, i64, i32, P, i64, i64, i32, f32, f32, f32, f32, P, sz, P],
+                                      i32),
             "ozaki25_grouped_matmul_dw": ([i64, i64, i64, i64, P, i64, P, i64, P, P, i64, i64, i32, i32, P], i32),
         }
         for name, (args, res) in sig.items():
@@ -605,3 +617,70 @@ def ozaki25_grouped_matmul_dw(dY, X, ends, dW=None, out_dtype=None, stream=None)
                                            lddw, stride, types[dY.dtype], out, _stream(stream)),
            "ozaki25_grouped_matmul_dw")
     return dW
+
+
+def ozaki25_adapter_matmul_workspace_size(rows: int, n: int, k: int, adapters: int, rank: int) -> int:
+    return lib().ozaki25_adapter_matmul_workspace_size(rows, n, k, adapters, rank)
+
+
+def ozaki25_adapter_matmul(X, W, ids, A, B, scales=None, Y=None, workspace=None, stream=None):
+    """Y[t] = X[t] W^T + scales[a] (X[t] A[a]^T) B[a]^T with a = ids[t]; rows
+    whose id is outside [0, adapters) get the projection alone.  X: rows x k,
+    W: n x k, ids: int32 [rows], A: adapters x rank x k, B: adapters x n x rank,
+    bfloat16 or float16; scales: float32 [adapters].  Returns Y, rows x n."""
+    torch = _torch or _tensors()
+    types = _half_types()
+    X, ldx, _ = _pitched(X, "X", 2, types)
+    rows, k = X.shape
+    W, ldw, _ = _pitched(W, "W", 2, (X.dtype,))
+    n = W.shape[0]
+    if W.shape[1] != k:
+        raise ValueError(f"W has {W.shape[1]} columns, X has {k}")
+    A, lda, a_stride = _pitched(A, "A", 3, (X.dtype,))
+    adapters, rank = A.shape[0], A.shape[1]
+    if A.shape[2] != k:
+        raise ValueError(f"A has {A.shape[2]} columns, X has {k}")
+    B, ldb, b_stride = _pitched(B, "B", 3, (X.dtype,), (adapters, n, rank))
+    if not (isinstance(ids, torch.Tensor) and ids.dtype == torch.int32 and ids.is_contiguous() and ids.shape == (rows,)):
+        raise ValueError(f"ids must be a contiguous int32 tensor of {rows} elements")
+    if scales is not None and not (isinstance(scales, torch.Tensor) and scales.dtype == torch.float32
+                                   and scales.is_contiguous() and scales.shape == (adapters,)):
+        raise ValueError(f"scales must be a contiguous float32 tensor of {adapters} elements")
+    if Y is None:
+        Y = _new((rows, n), X.dtype, X.device, stream)
+    Y, ldy, _ = _pitched(Y, "Y", 2, (X.dtype,), (rows, n))
+    ws_ptr, ws_bytes = _workspace(workspace)
+    _on_gpu([("X", X), ("W", W), ("ids", ids), ("A", A), ("B", B), ("scales", scales), ("Y", Y),
+             ("workspace", workspace)])
+    _check(lib().ozaki25_adapter_matmul(rows, n, k, adapters, rank, _ptr(X), ldx, _ptr(W), ldw, _ptr(ids), _ptr(A), lda,
+                                        a_stride, _ptr(B), ldb, b_stride, _ptr(scales), _ptr(Y), ldy, types[X.dtype],
+                                        ws_ptr, ws_bytes, _stream(stream)), "ozaki25_adapter_matmul")
+    return Y
+
+
+def ozaki25_orthogonalise_workspace_size(count: int, m: int, n: int) -> int:
+    return lib().ozaki25_orthogonalise_workspace_size(count, m, n)
+
+
+def ozaki25_orthogonalise(G, X=None, steps: int = 5, coefficients=(3.4445, -4.7750, 2.0315), eps: float = 1e-7,
+                          workspace=None, stream=None):
+    """The matrices of G (count x m x n, or one m x n; bfloat16, float16 or
+    float32) orthogonalised by `steps` Newton-Schulz products.  Returns X,
+    bfloat16, of G's shape."""
+    torch = _torch or _tensors()
+    if not isinstance(G, torch.Tensor) or G.dim() not in (2, 3):
+        raise ValueError("G must be a 2-D or 3-D tensor")
+    types = {**_half_types(), torch.float32: F32}
+    G, ldg, g_stride = _pitched(G, "G", G.dim(), tuple(types))
+    count = G.shape[0] if G.dim() == 3 else 1
+    m, n = G.shape[-2:]
+    a, b, c = coefficients
+    if X is None:
+        X = _new(G.shape, torch.bfloat16, G.device, stream)
+    X, ldx, x_stride = _pitched(X, "X", G.dim(), (torch.bfloat16,), G.shape)
+    ws_ptr, ws_bytes = _workspace(workspace)
+    _on_gpu([("G", G), ("X", X), ("workspace", workspace)])
+    _check(lib().ozaki25_orthogonalise(count, m, n, _ptr(G), ldg, g_stride, types[G.dtype], _ptr(X), ldx, x_stride,
+                                       steps, a, b, c, eps, ws_ptr, ws_bytes, _stream(stream)),
+           "ozaki25_orthogonalise")
+    return X

@@ -15,28 +15,6 @@ namespace oz {
 namespace half {
 namespace {
 
-// Place -> (row tile, column tile): row tiles in sets of kSet, column by column
-// inside a set, so that the blocks an XCD runs at a time share panels.
-constexpr uint32_t kSet = 4;
-__device__ __forceinline__ void place_to_tile(uint32_t place, uint32_t tiles_m, uint32_t tiles_n, uint32_t& tm,
-                                              uint32_t& tn) {
-  const uint32_t per = kSet * tiles_n;
-  const uint32_t s = place / per, in = place - s * per;
-  const uint32_t first = s * kSet;
-  const uint32_t size = tiles_m - first < kSet ? tiles_m - first : kSet;
-  tn = in / size;
-  tm = first + in - tn * size;
-}
-
-// Blocks are dealt round-robin over the 8 XCDs; each XCD takes one contiguous
-// range of the places.  False: no place is left for this block.
-__device__ __forceinline__ bool block_place(uint32_t b, uint32_t total, uint32_t& place) {
-  const uint32_t x = b & 7, i = b >> 3, per = total >> 3, rem = total & 7;
-  if (i >= per + (x < rem ? 1 : 0)) return false;
-  place = x * per + (x < rem ? x : rem) + i;
-  return true;
-}
-
 // Y (rows x cols) = X (rows x depth) times the group's weights: kAlong for
 // weights cols x depth, kAcross for depth x cols.
 template <class T>

@@ -31,6 +31,59 @@ struct GroupedWeights {
   bool vec;  // 16-byte stores of a 16-bit dw (set by the launch)
 };
 
+struct Adapter {
+  const void* x;  // rows x k
+  int64_t ldx;
+  const void* w;  // n x k
+  int64_t ldw;
+  const int32_t* ids;  // rows
+  const void* a;       // a stack of rank x k
+  int64_t lda, a_stride;
+  const void* b;  // a stack of n x rank
+  int64_t ldb, b_stride;
+  const float* scales;  // adapters, or null: 1
+  void* y;              // rows x n
+  int64_t ldy;
+  int rows, n, k, adapters, rank;
+  float* h;      // workspace: splits x rows x rank_pad
+  int rank_pad;  // rank rounded up to 16
+  int splits;    // parts of the depth of X A^T
+  bool vec;      // 16-byte stores of y (set by the launch)
+};
+
+// Parts into which the depth of X A^T is split, so that a card's worth of
+// blocks has something to read.
+inline int adapter_splits(int64_t rows, int64_t k) {
+  const int64_t tiles = rows <= 256 ? (rows + 15) / 16 * 4 : (rows + 63) / 64;
+  int64_t s = (512 + tiles - 1) / tiles;
+  const int64_t most = (k + 511) / 512;  // at least 512 depths each
+  s = s < most ? s : most;
+  return (int)(s < 1 ? 1 : s > 8 ? 8 : s);
+}
+
+struct Orthogonalise {
+  const void* g;  // count matrices m x n
+  int64_t ldg, g_stride;
+  void* x;  // the same, bfloat16
+  int64_t ldx, x_stride;
+  int count, m, n;
+  int mp, np;  // m, n padded to multiples of 8
+  float a, b, c, eps;
+  // workspace
+  double* squares;  // count x orthogonalise_parts
+  float* x32;       // count x mp x np
+  void* x16[2];     // the same
+  void* s16;        // count x s x s, s the shorter padded side
+  void* p16;        // the same
+  bool vec;         // 16-byte stores of x (set by the launch)
+};
+
+// Blocks (and partial sums) per matrix of the norm.
+inline int orthogonalise_parts(int64_t m, int64_t n) {
+  const int64_t p = (m * n + 16383) / 16384;
+  return (int)(p < 1 ? 1 : p > 128 ? 128 : p);
+}
+
 // Whether a matrix of `cols` columns can go to LDS by DMA: 16-byte rows, and a
 // tile's offsets below 2^31.
 inline bool dma_operand(const void* p, int64_t ld, int64_t cols) {
@@ -39,6 +92,8 @@ inline bool dma_operand(const void* p, int64_t ld, int64_t cols) {
 
 hipError_t launch_grouped_rows(GroupedRows g, int type, bool transposed, hipStream_t s);
 hipError_t launch_grouped_weights(GroupedWeights g, int type, int out, hipStream_t s);
+hipError_t launch_adapter(Adapter p, int type, hipStream_t s);
+hipError_t launch_orthogonalise(Orthogonalise o, int type, int steps, hipStream_t s);
 
 }  // namespace half
 }  // namespace oz

@@ -425,70 +425,89 @@ __device__ __forceinline__ void product(const Operand& a, const Operand& b, int 
   __syncthreads();
 }
 
-// The tile's rows < rows and columns < cols to a row-major matrix, rounded
-// once to its type.  16-bit outputs go through LDS (the wavefront's own part,
-// free after the last stage) so that 16 bytes per lane and whole 64-byte runs
-// reach memory; `vec` says that rows start on 16 bytes and cols is a multiple
-// of 8, else single elements are stored from LDS.  32-bit outputs are stored
-// straight from registers, 32 consecutive columns per half wavefront.
-template <class T>
-__device__ __forceinline__ void store(const v16f (&acc)[T::MB][T::NB], char* lds, void* out, int64_t ld, int rows,
-                                      int cols, bool vec) {
+// Four consecutive outputs of a row, rounded to 16 bits.
+template <int OUT>
+__device__ __forceinline__ uint2 pack4(float x, float y, float z, float w) {
+  using O = typename Out<OUT>::type;
+  typedef O o2 __attribute__((ext_vector_type(2)));
+  const o2 lo = {(O)x, (O)y}, hi = {(O)z, (O)w};
+  return uint2{__builtin_bit_cast(uint32_t, lo), __builtin_bit_cast(uint32_t, hi)};
+}
+
+// What a wavefront wrote to its own part of LDS is there for all its lanes.
+__device__ __forceinline__ void wave_lds_ready() {
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
+
+// The wavefront's blocks (WIDE tiles) through its part of LDS, which is free
+// after the last stage, to a row-major 16-bit matrix: 16 bytes per lane, whole
+// runs of 64 bytes.  rows, cols: what exists of the tile.  `vec`: rows start
+// on 16 bytes and cols is a multiple of 8; else single elements are stored.
+// value(r, c, v): the four outputs from row r, column c on, given the sums.
+template <class T, class F>
+__device__ __forceinline__ void store_wide(const v16f (&acc)[T::MB][T::NB], char* lds, void* out, int64_t ld, int rows,
+                                           int cols, bool vec, F value) {
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int r0 = wave / T::WC * T::MB * 32, c0 = wave % T::WC * T::NB * 32;
-  if constexpr (T::WIDE) {
-    using O = typename Out<T::OUT>::type;
-    typedef O o2 __attribute__((ext_vector_type(2)));
-    constexpr int PITCH = T::NB * 64, CH = T::NB * 4;  // bytes and 16-byte chunks per row
-    static_assert(T::MB * 32 * PITCH * T::WAVES <= T::LDS, "outputs fit the stages' LDS");
-    char* const mine = lds + wave * (T::MB * 32 * PITCH);
-    const int row = lane & 31, half = lane >> 5;
+  constexpr int PITCH = T::NB * 64, CH = T::NB * 4;  // bytes and 16-byte chunks per row
+  static_assert(T::MB * 32 * PITCH * T::WAVES <= T::LDS, "outputs fit the stages' LDS");
+  char* const mine = lds + wave * (T::MB * 32 * PITCH);
+  const int row = lane & 31, half = lane >> 5;
 #pragma unroll
-    for (int a = 0; a < T::MB; ++a)
+  for (int a = 0; a < T::MB; ++a)
 #pragma unroll
-      for (int b = 0; b < T::NB; ++b)
+    for (int b = 0; b < T::NB; ++b)
 #pragma unroll
-        for (int q = 0; q < 4; ++q) {
-          const v16f& c = acc[a][b];
-          const o2 lo = {(O)c[4 * q], (O)c[4 * q + 1]}, hi = {(O)c[4 * q + 2], (O)c[4 * q + 3]};
-          char* p = mine + (a * 32 + row) * PITCH + (((b * 4 + q) ^ (row & (CH - 1))) << 4) + half * 8;
-          *(uint2*)p = uint2{__builtin_bit_cast(uint32_t, lo), __builtin_bit_cast(uint32_t, hi)};
-        }
-    // the wavefront reads what its own lanes wrote
-    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-    __builtin_amdgcn_wave_barrier();
-    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
-    constexpr int RPI = 64 / CH;  // rows per instruction
-    const int lr = lane / CH, ch = lane % CH;
-    const int cleft = cols - c0 - ch * 8;
-    O* const o = (O*)out + (int64_t)(r0 + lr) * ld + c0 + ch * 8;
-    constexpr int ROUNDS = T::MB * 32 / RPI;
-    v4i v[ROUNDS];
+      for (int q = 0; q < 4; ++q) {
+        float v[4] = {acc[a][b][4 * q], acc[a][b][4 * q + 1], acc[a][b][4 * q + 2], acc[a][b][4 * q + 3]};
+        value(r0 + a * 32 + row, c0 + b * 32 + 8 * q + 4 * half, v);
+        char* p = mine + (a * 32 + row) * PITCH + (((b * 4 + q) ^ (row & (CH - 1))) << 4) + half * 8;
+        *(uint2*)p = pack4<T::OUT>(v[0], v[1], v[2], v[3]);
+      }
+  wave_lds_ready();
+  constexpr int RPI = 64 / CH, ROUNDS = T::MB * 32 / RPI;  // rows per instruction
+  const int lr = lane / CH, ch = lane % CH;
+  const int cleft = cols - c0 - ch * 8;
+  short* const o = (short*)out + (int64_t)(r0 + lr) * ld + c0 + ch * 8;
+  v4i v[ROUNDS];
 #pragma unroll
-    for (int i = 0; i < ROUNDS; ++i) {
-      const int r = i * RPI + lr;
-      v[i] = *(const v4i*)(mine + r * PITCH + ((ch ^ (r & (CH - 1))) << 4));
-    }
-    const int rleft = cleft > 0 ? rows - r0 - lr : 0;
-    if (vec) {
+  for (int i = 0; i < ROUNDS; ++i) {
+    const int r = i * RPI + lr;
+    v[i] = *(const v4i*)(mine + r * PITCH + ((ch ^ (r & (CH - 1))) << 4));
+  }
+  const int rleft = cleft > 0 ? rows - r0 - lr : 0;
+  if (vec) {
 #pragma unroll
-      for (int i = 0; i < ROUNDS; ++i)
-        if (i * RPI < rleft) *(v4i*)(o + (int64_t)(i * RPI) * ld) = v[i];
-    } else {
-#pragma unroll
-      for (int i = 0; i < ROUNDS; ++i)
-        if (i * RPI < rleft) {
-          short* const q = (short*)(o + (int64_t)(i * RPI) * ld);
-          const v8s e = __builtin_bit_cast(v8s, v[i]);
-#pragma unroll
-          for (int j = 0; j < 8; ++j)
-            if (j < cleft) q[j] = e[j];
-        }
-    }
+    for (int i = 0; i < ROUNDS; ++i)
+      if (i * RPI < rleft) *(v4i*)(o + (int64_t)(i * RPI) * ld) = v[i];
   } else {
+#pragma unroll
+    for (int i = 0; i < ROUNDS; ++i)
+      if (i * RPI < rleft) {
+        short* const q = o + (int64_t)(i * RPI) * ld;
+        const v8s e = __builtin_bit_cast(v8s, v[i]);
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+          if (j < cleft) q[j] = e[j];
+      }
+  }
+}
+
+// The tile to a row-major matrix of type T::OUT, rounded once.  32-bit outputs
+// are stored straight from registers, 32 consecutive columns per half wavefront.
+template <class T>
+__device__ __forceinline__ void store(const v16f (&acc)[T::MB][T::NB], char* lds, void* out, int64_t ld, int rows,
+                                      int cols, bool vec) {
+  if constexpr (T::WIDE) {
+    store_wide<T>(acc, lds, out, ld, rows, cols, vec, [](int, int, float*) {});
+  } else {
+    const int lane = threadIdx.x & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     // lane l of a block: column l % 32, rows 8 (i / 4) + 4 (l / 32) + i % 4
-    const int row = r0 + 4 * (lane >> 5), col = c0 + (lane & 31);
+    const int row = wave / T::WC * T::MB * 32 + 4 * (lane >> 5), col = wave % T::WC * T::NB * 32 + (lane & 31);
     float* const o = (float*)out + (int64_t)row * ld + col;
 #pragma unroll
     for (int a = 0; a < T::MB; ++a)
@@ -503,6 +522,29 @@ __device__ __forceinline__ void store(const v16f (&acc)[T::MB][T::NB], char* lds
         }
       }
   }
+}
+
+// ---- order of the tiles ------------------------------------------------------
+// Place -> (row tile, column tile): row tiles in sets of kSet, column by column
+// inside a set, so that the blocks an XCD runs at a time share panels.
+constexpr uint32_t kSet = 4;
+__device__ __forceinline__ void place_to_tile(uint32_t place, uint32_t tiles_m, uint32_t tiles_n, uint32_t& tm,
+                                              uint32_t& tn) {
+  const uint32_t per = kSet * tiles_n;
+  const uint32_t s = place / per, in = place - s * per;
+  const uint32_t first = s * kSet;
+  const uint32_t size = tiles_m - first < kSet ? tiles_m - first : kSet;
+  tn = in / size;
+  tm = first + in - tn * size;
+}
+
+// Blocks are dealt round-robin over the 8 XCDs; each XCD takes one contiguous
+// range of the places.  False: no place is left for this block.
+__device__ __forceinline__ bool block_place(uint32_t b, uint32_t total, uint32_t& place) {
+  const uint32_t x = b & 7, i = b >> 3, per = total >> 3, rem = total & 7;
+  if (i >= per + (x < rem ? 1 : 0)) return false;
+  place = x * per + (x < rem ? x : rem) + i;
+  return true;
 }
 
 // ---- groups of rows ---------------------------------------------------------
