@@ -10,39 +10,11 @@
 // two 16-bit numbers, its rounded value and the rest, so that H keeps at least
 // 16 bits and the rounding of the output stays the only one that shows.
 #include "half_products.hpp"
+#include "ozaki25.h"
 
 namespace oz {
 namespace half {
 namespace {
-
-typedef float v4f __attribute__((ext_vector_type(4)));
-
-template <int TYPE>
-__device__ __forceinline__ v4f mfma16(v4i a, v4i b, v4f c) {
-  if constexpr (TYPE == kBF16)
-    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(v8b, a), __builtin_bit_cast(v8b, b), c, 0, 0,
-                                                   0);
-  else
-    return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(v8h, a), __builtin_bit_cast(v8h, b), c, 0, 0,
-                                                  0);
-}
-
-// Elements c .. c + 7 of a row of `cols`; zeros past its end.
-__device__ __forceinline__ v4i load8(const char* row, int c, int cols) {
-  v4i v{};
-  const int have = cols - c;
-  const char* q = row + (int64_t)c * 2;
-  if (have >= 8) {
-    __builtin_memcpy(&v, q, 16);
-  } else if (have > 0) {
-    v8s e{};
-#pragma unroll
-    for (int j = 0; j < 7; ++j)
-      if (j < have) e[j] = ((const short*)q)[j];
-    v = __builtin_bit_cast(v4i, e);
-  }
-  return v;
-}
 
 // The least adapter above `after` among `count` ids (at most 64 N) in LDS;
 // `adapters` where there is none.  Ids outside [0, adapters) name none.
@@ -222,6 +194,105 @@ __global__ __launch_bounds__(T::THREADS, 1) void adapter_kernel(Adapter p) {
   store<T>(acc, lds, (char*)p.y + (r0 * p.ldy + c0) * 2, p.ldy, rows, cols, p.vec);
 }
 
+// ---- few rows (serving): the weights are read once ------------------------------
+// First launch: the projection's partial sums over parts of the depth, and
+// beside them H[t, :], a block per row, 16 ranks and part.
+constexpr int kServeWaves = 4;
+
+template <int TYPE, int NB, int TB>
+__global__ __launch_bounds__(kServeWaves * 64) void serve_partials_kernel(Adapter p, uint32_t shrink_blocks,
+                                                                          uint32_t tiles_n) {
+  __shared__ v4f lds[kServeWaves * TB * 16 * NB * 4];
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int steps = (p.k + 31) / 32;
+  auto range = [&](int part, int parts, int& s0, int& s1) {
+    const int q = part * kServeWaves + wave;
+    s0 = (int)((int64_t)steps * q / (parts * kServeWaves));
+    s1 = (int)((int64_t)steps * (q + 1) / (parts * kServeWaves));
+  };
+  int s0, s1;
+  if (blockIdx.x < shrink_blocks) {
+    const uint32_t chunks = (uint32_t)p.rank_pad / 16;
+    const int t = (int)(blockIdx.x / (chunks * p.splits)), in = (int)(blockIdx.x % (chunks * p.splits));
+    const int chunk = in % chunks, split = in / chunks;
+    const int a = p.ids[t];
+    if (a < 0 || a >= p.adapters) return;
+    const int ranks = p.rank - chunk * 16 < 16 ? p.rank - chunk * 16 : 16;
+    range(split, p.splits, s0, s1);
+    v4f acc[1][1] = {};
+    skinny<TYPE, 1, 1>((const char*)p.a + ((int64_t)a * p.a_stride + chunk * 16 * p.lda) * 2, p.lda, ranks,
+                       (const char*)p.x + t * p.ldx * 2, p.ldx, 1, p.k, s0, s1, acc);
+    skinny_join<1, 1, kServeWaves>(acc, lds, [&](int row, int r, v4f v) {
+      if (row > 0) return;
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        p.h[((int64_t)split * p.rows + t) * p.rank_pad + chunk * 16 + r + e] = r + e < ranks ? v[e] : 0.0f;
+    });
+    return;
+  }
+  const uint32_t place = blockIdx.x - shrink_blocks, per = tiles_n * p.base_splits;
+  const int t0 = (int)(place / per) * (16 * TB), in = (int)(place % per);
+  const int split = in % p.base_splits, c0 = in / p.base_splits * (16 * NB);
+  const int rows = p.rows - t0 < 16 * TB ? p.rows - t0 : 16 * TB, cols = p.n - c0 < 16 * NB ? p.n - c0 : 16 * NB;
+  range(split, p.base_splits, s0, s1);
+  v4f acc[NB][TB] = {};
+  skinny<TYPE, NB, TB>((const char*)p.w + c0 * p.ldw * 2, p.ldw, cols, (const char*)p.x + t0 * p.ldx * 2, p.ldx, rows,
+                       p.k, s0, s1, acc);
+  float* const out = p.partials + (int64_t)split * p.rows * p.n_pad;
+  skinny_join<NB, TB, kServeWaves>(acc, lds, [&](int row, int c, v4f v) {
+    if (row < rows && c < cols) *(v4f*)(out + (int64_t)(t0 + row) * p.n_pad + c0 + c) = v;  // n_pad: a multiple of 4
+  });
+}
+
+// Second launch: the partial sums in their order, then the row's adapter: a
+// thread per output, s_a H and the sum over the ranks in FP32.
+// grid (columns / 256, rows)
+template <int TYPE>
+__global__ __launch_bounds__(256) void serve_join_kernel(Adapter p) {
+  using O = typename Out<TYPE>::type;
+  typedef O v8o __attribute__((ext_vector_type(8)));
+  __shared__ float h[OZAKI25_MAX_RANK];
+  const int t = blockIdx.y, c = blockIdx.x * 256 + threadIdx.x;
+  const int a = p.rank > 0 ? p.ids[t] : -1;
+  const bool any = a >= 0 && a < p.adapters;
+  if (any && (int)threadIdx.x < p.rank_pad) {
+    float v = 0;
+    for (int s = 0; s < p.splits; ++s) v += p.h[((int64_t)s * p.rows + t) * p.rank_pad + threadIdx.x];
+    h[threadIdx.x] = v * (p.scales ? p.scales[a] : 1.0f);
+  }
+  float y = 0;
+  if (c < p.n)
+    for (int s = 0; s < p.base_splits; ++s) y += p.partials[((int64_t)s * p.rows + t) * p.n_pad + c];
+  __syncthreads();
+  if (c >= p.n) return;
+  if (any) {
+    const char* const B = (const char*)p.b + ((int64_t)a * p.b_stride + (int64_t)c * p.ldb) * 2;
+    for (int r = 0; r < p.rank; r += 8) {
+      const v8o b = __builtin_bit_cast(v8o, load8(B, r, p.rank));
+#pragma unroll
+      for (int e = 0; e < 8; ++e) y += h[r + e] * (float)b[e];
+    }
+  }
+  ((O*)p.y)[(int64_t)t * p.ldy + c] = (O)y;
+}
+
+template <int TYPE, int NB, int TB>
+hipError_t serve_tiles(const Adapter& p, hipStream_t s) {
+  const uint32_t tiles_n = (uint32_t)(p.n + 16 * NB - 1) / (16 * NB), tiles_t = (uint32_t)(p.rows + 16 * TB - 1) / (16 * TB);
+  const uint32_t shrinks = p.rank > 0 ? (uint32_t)p.rows * (p.rank_pad / 16) * p.splits : 0;
+  serve_partials_kernel<TYPE, NB, TB><<<dim3(shrinks + tiles_n * tiles_t * p.base_splits), dim3(kServeWaves * 64), 0, s>>>(
+      p, shrinks, tiles_n);
+  serve_join_kernel<TYPE><<<dim3((p.n + 255) / 256, p.rows), dim3(256), 0, s>>>(p);
+  return hipGetLastError();
+}
+
+template <int TYPE>
+hipError_t serve(const Adapter& p, hipStream_t s) {
+  if (p.rows <= 16) return serve_tiles<TYPE, 4, 1>(p, s);
+  if (p.rows <= 32) return serve_tiles<TYPE, 4, 2>(p, s);
+  return serve_tiles<TYPE, 4, 4>(p, s);
+}
+
 template <class T>
 hipError_t run(const Adapter& p, hipStream_t s) {
   const int64_t tiles = (int64_t)((p.rows + T::BM - 1) / T::BM) * ((p.n + T::BN - 1) / T::BN);
@@ -242,6 +313,7 @@ hipError_t shrink(const Adapter& p, hipStream_t s) {
 
 template <int TYPE>
 hipError_t of_type(const Adapter& p, bool dma, hipStream_t s) {
+  if (p.base_splits > 0) return serve<TYPE>(p, s);
   if (p.rank > 0 && p.k > 0) {
     const hipError_t e = p.rank <= 16 ? shrink<TYPE, 1>(p, s) : p.rank <= 32 ? shrink<TYPE, 2>(p, s) : shrink<TYPE, 4>(p, s);
     if (e != hipSuccess) return e;

@@ -131,10 +131,11 @@ struct Room {
 extern "C" {
 
 size_t ozaki25_adapter_matmul_workspace_size(int64_t rows, int64_t n, int64_t k, int64_t adapters, int64_t rank) {
-  if (rows <= 0 || n <= 0 || k <= 0 || adapters <= 0 || rank <= 0 || rank > OZAKI25_MAX_RANK ||
+  if (rows <= 0 || n <= 0 || k < 0 || adapters < 0 || rank < 0 || rank > OZAKI25_MAX_RANK ||
       too_large(rows, n, k, adapters))
     return 0;
-  return align_up((size_t)oz::half::adapter_splits(rows, k) * rows * pad16(rank) * sizeof(float));
+  const oz::half::AdapterPlan a = oz::half::adapter_plan(rows, n, k, pad16(rank));
+  return a.h_bytes + a.partial_bytes;
 }
 
 ozaki25_status ozaki25_adapter_matmul(int64_t rows, int64_t n, int64_t k, int64_t adapters, int64_t rank, const void* X,
@@ -161,7 +162,7 @@ ozaki25_status ozaki25_adapter_matmul(int64_t rows, int64_t n, int64_t k, int64_
                            span(adapters, a_stride, rank, lda, k, 2),
                            span(adapters, b_stride, n, ldb, rank, 2),
                            (size_t)adapters * 4};
-  const size_t need = any ? ozaki25_adapter_matmul_workspace_size(rows, n, k, adapters, rank) : 0;
+  const size_t need = ozaki25_adapter_matmul_workspace_size(rows, n, k, adapters, rank);
   for (int i = 0; i < 6; ++i)
     if (in[i] && (overlaps(Y, yb, in[i], bytes[i]) || (workspace && overlaps(workspace, need, in[i], bytes[i]))))
       return OZAKI25_ERR_INVALID_VALUE;
@@ -176,7 +177,10 @@ ozaki25_status ozaki25_adapter_matmul(int64_t rows, int64_t n, int64_t k, int64_
   p.a = A, p.lda = lda, p.a_stride = a_stride, p.b = B, p.ldb = ldb, p.b_stride = b_stride;
   p.scales = scales, p.y = Y, p.ldy = ldy;
   p.rows = (int)rows, p.n = (int)n, p.k = (int)k, p.adapters = any ? (int)adapters : 0, p.rank = any ? (int)rank : 0;
-  p.h = (float*)room.p, p.rank_pad = (int)pad16(rank), p.splits = oz::half::adapter_splits(rows, k);
+  const oz::half::AdapterPlan plan = oz::half::adapter_plan(rows, n, k, pad16(rank));
+  p.h = (float*)room.p, p.partials = (float*)(room.p + plan.h_bytes);
+  p.rank_pad = (int)pad16(rank), p.n_pad = (int)((n + 3) / 4 * 4);
+  p.splits = plan.splits, p.base_splits = plan.base_splits;
   return room.give(status_of(oz::half::launch_adapter(p, (int)type, (hipStream_t)stream)));
 }
 

@@ -524,6 +524,115 @@ __device__ __forceinline__ void store(const v16f (&acc)[T::MB][T::NB], char* lds
   }
 }
 
+// ---- few rows ----------------------------------------------------------------
+// The weights' columns as MFMA rows: 16 NB output columns x 16 TB rows of X,
+// operands straight from memory into fragments.  Each weight is read once per
+// block, so a block has few rows and its wavefronts split the depth.
+typedef float v4f __attribute__((ext_vector_type(4)));
+
+template <int TYPE>
+__device__ __forceinline__ v4f mfma16(v4i a, v4i b, v4f c) {
+  if constexpr (TYPE == kBF16)
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(v8b, a), __builtin_bit_cast(v8b, b), c, 0, 0,
+                                                   0);
+  else
+    return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(v8h, a), __builtin_bit_cast(v8h, b), c, 0, 0,
+                                                  0);
+}
+
+// Elements c .. c + 7 of a row of `cols`; zeros past its end.  Any alignment.
+__device__ __forceinline__ v4i load8(const char* row, int c, int cols) {
+  v4i v{};
+  const int have = cols - c;
+  const char* q = row + (int64_t)c * 2;
+  if (have >= 8) {
+    __builtin_memcpy(&v, q, 16);
+  } else if (have > 0) {
+    v8s e{};
+#pragma unroll
+    for (int j = 0; j < 7; ++j)
+      if (j < have) e[j] = ((const short*)q)[j];
+    v = __builtin_bit_cast(v4i, e);
+  }
+  return v;
+}
+
+__device__ __forceinline__ v4i load_whole(const char* q) {
+  v4i v;
+  __builtin_memcpy(&v, q, 16);
+  return v;
+}
+
+// acc[i][j] += 16 columns of W (rows of its cols x k matrix, from w on) times
+// 16 rows of X, over the depths 32 s0 .. 32 s1 (below k).  Rows past the last
+// are read as the last one; their sums are not used.  Lane l of a block: row of
+// X l % 16, columns 4 (l / 16) .. + 3.
+template <int TYPE, int NB, int TB>
+__device__ __forceinline__ void skinny(const char* w, int64_t ldw, int cols, const char* x, int64_t ldx, int rows,
+                                       int k, int s0, int s1, v4f (&acc)[NB][TB]) {
+  const int lane = threadIdx.x & 63, at = lane & 15, c0 = (lane >> 4) * 8;
+  const char *pw[NB], *px[TB];
+#pragma unroll
+  for (int i = 0; i < NB; ++i) pw[i] = w + (int64_t)(i * 16 + at < cols ? i * 16 + at : cols - 1) * ldw * 2;
+#pragma unroll
+  for (int j = 0; j < TB; ++j) px[j] = x + (int64_t)(j * 16 + at < rows ? j * 16 + at : rows - 1) * ldx * 2;
+  const int whole = k / 32 < s1 ? k / 32 : s1;  // steps without an end inside
+  constexpr int U = NB + TB <= 2 ? 8 : NB + TB <= 5 ? 4 : 2;
+  int s = s0;
+  for (; s + U <= whole; s += U) {
+    v4i fw[U][NB], fx[U][TB];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int64_t o = ((int64_t)(s + u) * 32 + c0) * 2;
+#pragma unroll
+      for (int i = 0; i < NB; ++i) fw[u][i] = load_whole(pw[i] + o);
+#pragma unroll
+      for (int j = 0; j < TB; ++j) fx[u][j] = load_whole(px[j] + o);
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+#pragma unroll
+      for (int i = 0; i < NB; ++i)
+#pragma unroll
+        for (int j = 0; j < TB; ++j) acc[i][j] = mfma16<TYPE>(fw[u][i], fx[u][j], acc[i][j]);
+  }
+  for (; s < s1; ++s) {
+    v4i fw[NB], fx[TB];
+#pragma unroll
+    for (int i = 0; i < NB; ++i) fw[i] = load8(pw[i], s * 32 + c0, k);
+#pragma unroll
+    for (int j = 0; j < TB; ++j) fx[j] = load8(px[j], s * 32 + c0, k);
+#pragma unroll
+    for (int i = 0; i < NB; ++i)
+#pragma unroll
+      for (int j = 0; j < TB; ++j) acc[i][j] = mfma16<TYPE>(fw[i], fx[j], acc[i][j]);
+  }
+}
+
+// The WAVES wavefronts' sums added up in their order: calls f(row, column,
+// four sums) once for every row and group of four columns of the block.
+template <int NB, int TB, int WAVES, class F>
+__device__ __forceinline__ void skinny_join(const v4f (&acc)[NB][TB], v4f* lds, F f) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  // [wave][row][column / 4], columns rotated by the row
+  constexpr int Q = NB * 4;
+#pragma unroll
+  for (int i = 0; i < NB; ++i)
+#pragma unroll
+    for (int j = 0; j < TB; ++j) {
+      const int row = j * 16 + (lane & 15), q = i * 4 + (lane >> 4);
+      lds[(wave * TB * 16 + row) * Q + ((q + row) & (Q - 1))] = acc[i][j];
+    }
+  __syncthreads();
+  for (int o = threadIdx.x; o < TB * 16 * Q; o += WAVES * 64) {
+    const int row = o / Q, q = o % Q;
+    v4f v{};
+#pragma unroll
+    for (int w = 0; w < WAVES; ++w) v += lds[(w * TB * 16 + row) * Q + ((q + row) & (Q - 1))];
+    f(row, q * 4, v);
+  }
+}
+
 // ---- order of the tiles ------------------------------------------------------
 // Place -> (row tile, column tile): row tiles in sets of kSet, column by column
 // inside a set, so that the blocks an XCD runs at a time share panels.
