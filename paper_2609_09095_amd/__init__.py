@@ -503,43 +503,73 @@ def ozaki25_dgemm_noalloc(A, B, C=None, subtract: bool = False, set: int = S12, 
 
 
 # ----------------------------------------------------------------- 16-bit products
+# A decode step's kernels take a few microseconds, as much as careless checks
+# would: one look at each property of each tensor.
+_HALF = None      # torch dtype -> ozaki25_dtype
+
+
 def _half_types():
+    global _HALF
     torch = _torch or _tensors()
-    return {torch.bfloat16: BF16, torch.float16: F16}
+    if _HALF is None:
+        _HALF = {torch.bfloat16: BF16, torch.float16: F16}
+    return _HALF
 
 
 def _pitched(t, name, dims, types, shape=None):
     """A `dims`-dimensional tensor of one of `types`, elements of a row
-    contiguous; returns (t, row pitch, matrix pitch)."""
-    torch = _torch or _tensors()
-    if not (isinstance(t, torch.Tensor) and t.dtype in types and t.dim() == dims):
+    contiguous; returns (shape, row pitch, matrix pitch)."""
+    if not (isinstance(t, _torch.Tensor) and t.dtype in types and t.dim() == dims):
         raise ValueError(f"{name} must be a {dims}-D tensor of dtype {' or '.join(str(d) for d in types)}")
-    if shape is not None and tuple(t.shape) != tuple(shape):
-        raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {tuple(shape)}")
-    rows, cols = t.shape[-2:]
-    s0, s1 = t.stride()[-2:]
-    if s1 != 1 and cols > 1:
+    size = t.shape
+    if shape is not None and size != shape:
+        raise ValueError(f"{name} has shape {tuple(size)}, expected {tuple(shape)}")
+    if dims == 3:
+        count, rows, cols = size
+    else:
+        rows, cols = size
+    if t.is_contiguous():
+        ld = cols or 1
+        return size, ld, rows * ld
+    stride = t.stride()
+    s0 = stride[-2]
+    if stride[-1] != 1 and cols > 1:
         raise ValueError(f"{name} must be row-major (unit column stride)")
     if rows > 1 and s0 < cols:
         raise ValueError(f"{name} rows overlap (row stride below the row length)")
     ld = max(s0 if rows > 1 else cols, 1)
-    if dims == 2:
-        return t, ld, 0
-    return t, ld, t.stride(0) if t.shape[0] > 1 else rows * ld
+    return size, ld, stride[0] if dims == 3 and count > 1 else rows * ld
 
 
-def _ends(ends, groups):
-    torch = _torch or _tensors()
-    if not (isinstance(ends, torch.Tensor) and ends.dtype == torch.int32 and ends.dim() == 1 and ends.is_contiguous()):
-        raise ValueError("ends must be a contiguous 1-D int32 tensor")
-    if ends.numel() != groups:
-        raise ValueError(f"ends holds {ends.numel()} groups, expected {groups}")
-    return ends
+def _vector(t, name, dtype, count):
+    """A contiguous vector of `count` elements of dtype."""
+    if not (isinstance(t, _torch.Tensor) and t.dtype == dtype and t.dim() == 1 and t.is_contiguous()):
+        raise ValueError(f"{name} must be a contiguous 1-D {str(dtype).replace('torch.', '')} tensor")
+    if t.numel() != count:
+        raise ValueError(f"{name} holds {t.numel()} elements, expected {count}")
+
+
+def _room(workspace):
+    """Address and bytes of a workspace, 0 and 0 for none."""
+    if workspace is None:
+        return 0, 0
+    if not (isinstance(workspace, _torch.Tensor) and workspace.dtype in (_torch.uint8, _torch.int8)
+            and workspace.is_contiguous()):
+        raise ValueError("workspace must be a contiguous tensor of dtype torch.uint8 or torch.int8")
+    return workspace.data_ptr(), workspace.numel()
+
+
+def _together(first, names, *others):
+    """Every tensor on the first one's GPU (checked after shapes and sizes)."""
+    dev = first.get_device()
+    for t in others:
+        if t is not None and (dev < 0 or t.get_device() != dev):
+            _on_gpu(zip(names, (first, *others)))
 
 
 def _new(shape, dtype, device, stream):
     """An output of the call, allocated on the stream that writes it."""
-    torch = _torch or _tensors()
+    torch = _torch
     if stream is None or device.type != "cuda":
         return torch.empty(shape, dtype=dtype, device=device)
     s = stream if hasattr(stream, "cuda_stream") else torch.cuda.ExternalStream(int(stream), device=device)
@@ -553,19 +583,19 @@ def ozaki25_grouped_matmul(X, W, ends, Y=None, stream=None):
     row (read on the device).  bfloat16 or float16; rows past the last end are
     zeros.  Returns Y, rows x n."""
     types = _half_types()
-    X, ldx, _ = _pitched(X, "X", 2, types)
-    rows, k = X.shape
-    W, ldw, stride = _pitched(W, "W", 3, (X.dtype,))
-    groups, n = W.shape[0], W.shape[1]
-    if W.shape[2] != k:
-        raise ValueError(f"W has {W.shape[2]} columns, X has {k}")
-    _ends(ends, groups)
+    (rows, k), ldx, _ = _pitched(X, "X", 2, types)
+    kind = (X.dtype,)
+    (groups, n, kw), ldw, stride = _pitched(W, "W", 3, kind)
+    if kw != k:
+        raise ValueError(f"W has {kw} columns, X has {k}")
+    _vector(ends, "ends", _torch.int32, groups)
     if Y is None:
         Y = _new((rows, n), X.dtype, X.device, stream)
-    Y, ldy, _ = _pitched(Y, "Y", 2, (X.dtype,), (rows, n))
-    _on_gpu([("X", X), ("W", W), ("ends", ends), ("Y", Y)])
-    _check(lib().ozaki25_grouped_matmul(rows, n, k, groups, _ptr(X), ldx, _ptr(W), ldw, stride, _ptr(ends), _ptr(Y),
-                                        ldy, types[X.dtype], _stream(stream)), "ozaki25_grouped_matmul")
+    _, ldy, _ = _pitched(Y, "Y", 2, kind, (rows, n))
+    _together(X, ("X", "W", "ends", "Y"), W, ends, Y)
+    _check(lib().ozaki25_grouped_matmul(rows, n, k, groups, X.data_ptr(), ldx, W.data_ptr(), ldw, stride,
+                                        ends.data_ptr(), Y.data_ptr(), ldy, types[X.dtype], _stream(stream)),
+           "ozaki25_grouped_matmul")
     return Y
 
 
@@ -573,19 +603,18 @@ def ozaki25_grouped_matmul_dx(dY, W, ends, dX=None, stream=None):
     """dX[r] = dY[r] W[g], the gradient of ozaki25_grouped_matmul's input.
     Returns dX, rows x k."""
     types = _half_types()
-    dY, lddy, _ = _pitched(dY, "dY", 2, types)
-    rows, n = dY.shape
-    W, ldw, stride = _pitched(W, "W", 3, (dY.dtype,))
-    groups, k = W.shape[0], W.shape[2]
-    if W.shape[1] != n:
-        raise ValueError(f"W has {W.shape[1]} rows, dY has {n} columns")
-    _ends(ends, groups)
+    (rows, n), lddy, _ = _pitched(dY, "dY", 2, types)
+    kind = (dY.dtype,)
+    (groups, nw, k), ldw, stride = _pitched(W, "W", 3, kind)
+    if nw != n:
+        raise ValueError(f"W has {nw} rows, dY has {n} columns")
+    _vector(ends, "ends", _torch.int32, groups)
     if dX is None:
         dX = _new((rows, k), dY.dtype, dY.device, stream)
-    dX, lddx, _ = _pitched(dX, "dX", 2, (dY.dtype,), (rows, k))
-    _on_gpu([("dY", dY), ("W", W), ("ends", ends), ("dX", dX)])
-    _check(lib().ozaki25_grouped_matmul_dx(rows, n, k, groups, _ptr(dY), lddy, _ptr(W), ldw, stride, _ptr(ends),
-                                           _ptr(dX), lddx, types[dY.dtype], _stream(stream)),
+    _, lddx, _ = _pitched(dX, "dX", 2, kind, (rows, k))
+    _together(dY, ("dY", "W", "ends", "dX"), W, ends, dX)
+    _check(lib().ozaki25_grouped_matmul_dx(rows, n, k, groups, dY.data_ptr(), lddy, W.data_ptr(), ldw, stride,
+                                           ends.data_ptr(), dX.data_ptr(), lddx, types[dY.dtype], _stream(stream)),
            "ozaki25_grouped_matmul_dx")
     return dX
 
@@ -594,27 +623,22 @@ def ozaki25_grouped_matmul_dw(dY, X, ends, dW=None, out_dtype=None, stream=None)
     """dW[g] = sum of dY[r]^T X[r] over the rows r of group g, the gradient of
     ozaki25_grouped_matmul's weights; zeros for an empty group.  out_dtype:
     the inputs' (the default) or float32.  Returns dW, groups x n x k."""
-    torch = _torch or _tensors()
     types = _half_types()
-    dY, lddy, _ = _pitched(dY, "dY", 2, types)
-    rows, n = dY.shape
-    X, ldx, _ = _pitched(X, "X", 2, (dY.dtype,))
-    k = X.shape[1]
-    if X.shape[0] != rows:
-        raise ValueError(f"X has {X.shape[0]} rows, dY has {rows}")
-    if not isinstance(ends, torch.Tensor):
-        raise ValueError("ends must be a contiguous 1-D int32 tensor")
-    groups = ends.numel()
-    _ends(ends, groups)
+    (rows, n), lddy, _ = _pitched(dY, "dY", 2, types)
+    (rx, k), ldx, _ = _pitched(X, "X", 2, (dY.dtype,))
+    if rx != rows:
+        raise ValueError(f"X has {rx} rows, dY has {rows}")
+    groups = ends.numel() if isinstance(ends, _torch.Tensor) else 0
+    _vector(ends, "ends", _torch.int32, groups)
     if dW is None:
         dW = _new((groups, n, k), out_dtype or dY.dtype, dY.device, stream)
     elif out_dtype is not None and dW.dtype != out_dtype:
         raise ValueError(f"dW has dtype {dW.dtype}, out_dtype is {out_dtype}")
-    dW, lddw, stride = _pitched(dW, "dW", 3, (dY.dtype, torch.float32), (groups, n, k))
-    _on_gpu([("dY", dY), ("X", X), ("ends", ends), ("dW", dW)])
-    out = F32 if dW.dtype == torch.float32 else types[dY.dtype]
-    _check(lib().ozaki25_grouped_matmul_dw(rows, n, k, groups, _ptr(dY), lddy, _ptr(X), ldx, _ptr(ends), _ptr(dW),
-                                           lddw, stride, types[dY.dtype], out, _stream(stream)),
+    _, lddw, stride = _pitched(dW, "dW", 3, (dY.dtype, _torch.float32), (groups, n, k))
+    _together(dY, ("dY", "X", "ends", "dW"), X, ends, dW)
+    out = F32 if dW.dtype == _torch.float32 else types[dY.dtype]
+    _check(lib().ozaki25_grouped_matmul_dw(rows, n, k, groups, dY.data_ptr(), lddy, X.data_ptr(), ldx, ends.data_ptr(),
+                                           dW.data_ptr(), lddw, stride, types[dY.dtype], out, _stream(stream)),
            "ozaki25_grouped_matmul_dw")
     return dW
 
@@ -628,33 +652,28 @@ def ozaki25_adapter_matmul(X, W, ids, A, B, scales=None, Y=None, workspace=None,
     whose id is outside [0, adapters) get the projection alone.  X: rows x k,
     W: n x k, ids: int32 [rows], A: adapters x rank x k, B: adapters x n x rank,
     bfloat16 or float16; scales: float32 [adapters].  Returns Y, rows x n."""
-    torch = _torch or _tensors()
     types = _half_types()
-    X, ldx, _ = _pitched(X, "X", 2, types)
-    rows, k = X.shape
-    W, ldw, _ = _pitched(W, "W", 2, (X.dtype,))
-    n = W.shape[0]
-    if W.shape[1] != k:
-        raise ValueError(f"W has {W.shape[1]} columns, X has {k}")
-    A, lda, a_stride = _pitched(A, "A", 3, (X.dtype,))
-    adapters, rank = A.shape[0], A.shape[1]
-    if A.shape[2] != k:
-        raise ValueError(f"A has {A.shape[2]} columns, X has {k}")
-    B, ldb, b_stride = _pitched(B, "B", 3, (X.dtype,), (adapters, n, rank))
-    if not (isinstance(ids, torch.Tensor) and ids.dtype == torch.int32 and ids.is_contiguous() and ids.shape == (rows,)):
-        raise ValueError(f"ids must be a contiguous int32 tensor of {rows} elements")
-    if scales is not None and not (isinstance(scales, torch.Tensor) and scales.dtype == torch.float32
-                                   and scales.is_contiguous() and scales.shape == (adapters,)):
-        raise ValueError(f"scales must be a contiguous float32 tensor of {adapters} elements")
+    (rows, k), ldx, _ = _pitched(X, "X", 2, types)
+    kind = (X.dtype,)
+    (n, kw), ldw, _ = _pitched(W, "W", 2, kind)
+    if kw != k:
+        raise ValueError(f"W has {kw} columns, X has {k}")
+    (adapters, rank, ka), lda, a_stride = _pitched(A, "A", 3, kind)
+    if ka != k:
+        raise ValueError(f"A has {ka} columns, X has {k}")
+    _, ldb, b_stride = _pitched(B, "B", 3, kind, (adapters, n, rank))
+    _vector(ids, "ids", _torch.int32, rows)
+    if scales is not None:
+        _vector(scales, "scales", _torch.float32, adapters)
     if Y is None:
         Y = _new((rows, n), X.dtype, X.device, stream)
-    Y, ldy, _ = _pitched(Y, "Y", 2, (X.dtype,), (rows, n))
-    ws_ptr, ws_bytes = _workspace(workspace)
-    _on_gpu([("X", X), ("W", W), ("ids", ids), ("A", A), ("B", B), ("scales", scales), ("Y", Y),
-             ("workspace", workspace)])
-    _check(lib().ozaki25_adapter_matmul(rows, n, k, adapters, rank, _ptr(X), ldx, _ptr(W), ldw, _ptr(ids), _ptr(A), lda,
-                                        a_stride, _ptr(B), ldb, b_stride, _ptr(scales), _ptr(Y), ldy, types[X.dtype],
-                                        ws_ptr, ws_bytes, _stream(stream)), "ozaki25_adapter_matmul")
+    _, ldy, _ = _pitched(Y, "Y", 2, kind, (rows, n))
+    ws_ptr, ws_bytes = _room(workspace)
+    _together(X, ("X", "W", "ids", "A", "B", "scales", "Y", "workspace"), W, ids, A, B, scales, Y, workspace)
+    _check(lib().ozaki25_adapter_matmul(rows, n, k, adapters, rank, X.data_ptr(), ldx, W.data_ptr(), ldw,
+                                        ids.data_ptr(), A.data_ptr(), lda, a_stride, B.data_ptr(), ldb, b_stride,
+                                        _ptr(scales), Y.data_ptr(), ldy, types[X.dtype], ws_ptr, ws_bytes,
+                                        _stream(stream)), "ozaki25_adapter_matmul")
     return Y
 
 
@@ -667,20 +686,19 @@ def ozaki25_orthogonalise(G, X=None, steps: int = 5, coefficients=(3.4445, -4.77
     """The matrices of G (count x m x n, or one m x n; bfloat16, float16 or
     float32) orthogonalised by `steps` Newton-Schulz products.  Returns X,
     bfloat16, of G's shape."""
-    torch = _torch or _tensors()
-    if not isinstance(G, torch.Tensor) or G.dim() not in (2, 3):
+    types = _half_types()
+    if not (isinstance(G, _torch.Tensor) and G.dim() in (2, 3)):
         raise ValueError("G must be a 2-D or 3-D tensor")
-    types = {**_half_types(), torch.float32: F32}
-    G, ldg, g_stride = _pitched(G, "G", G.dim(), tuple(types))
-    count = G.shape[0] if G.dim() == 3 else 1
-    m, n = G.shape[-2:]
+    dims = G.dim()
+    size, ldg, g_stride = _pitched(G, "G", dims, (*types, _torch.float32))
+    m, n = size[-2:]
     a, b, c = coefficients
     if X is None:
-        X = _new(G.shape, torch.bfloat16, G.device, stream)
-    X, ldx, x_stride = _pitched(X, "X", G.dim(), (torch.bfloat16,), G.shape)
-    ws_ptr, ws_bytes = _workspace(workspace)
-    _on_gpu([("G", G), ("X", X), ("workspace", workspace)])
-    _check(lib().ozaki25_orthogonalise(count, m, n, _ptr(G), ldg, g_stride, types[G.dtype], _ptr(X), ldx, x_stride,
-                                       steps, a, b, c, eps, ws_ptr, ws_bytes, _stream(stream)),
-           "ozaki25_orthogonalise")
+        X = _new(size, _torch.bfloat16, G.device, stream)
+    _, ldx, x_stride = _pitched(X, "X", dims, (_torch.bfloat16,), size)
+    ws_ptr, ws_bytes = _room(workspace)
+    _together(G, ("G", "X", "workspace"), X, workspace)
+    _check(lib().ozaki25_orthogonalise(size[0] if dims == 3 else 1, m, n, G.data_ptr(), ldg, g_stride,
+                                       types.get(G.dtype, F32), X.data_ptr(), ldx, x_stride, steps, a, b, c, eps,
+                                       ws_ptr, ws_bytes, _stream(stream)), "ozaki25_orthogonalise")
     return X

@@ -187,7 +187,7 @@ __global__ __launch_bounds__(T::THREADS, 1) void adapter_kernel(Adapter p) {
   const int rows = p.rows - r0 < T::BM ? p.rows - r0 : T::BM, cols = p.n - c0 < T::BN ? p.n - c0 : T::BN;
   for (int i = threadIdx.x; i < T::BM; i += T::THREADS) ids[i] = i < rows ? p.ids[r0 + i] : -1;
   v16f acc[T::MB][T::NB] = {};
-  product<T>(Operand{(const char*)p.x + r0 * p.ldx * 2, p.ldx, rows}, Operand{(const char*)p.w + c0 * p.ldw * 2, p.ldw, cols},
+  product<T>(Operand{(const char*)p.x + r0 * p.ldx * 2, p.ldx, rows, p.k}, Operand{(const char*)p.w + c0 * p.ldw * 2, p.ldw, cols, p.k},
              p.k, lds, acc);
   __syncthreads();
   if (p.rank > 0) expand<T>(p, r0, rows, c0, cols, ids, lds, acc);

@@ -10,6 +10,7 @@
 // from the ends with two wavefront scans per 64 groups; blocks past the last
 // tile leave at once.
 #include "half_products.hpp"
+#include "half_rules.hpp"
 
 namespace oz {
 namespace half {
@@ -31,11 +32,49 @@ __global__ __launch_bounds__(T::THREADS, 1) void grouped_rows_kernel(GroupedRows
   const int cols = g.cols - c0 < T::BN ? g.cols - c0 : T::BN;
   const bool none = t.group == g.groups;  // rows of no group: zeros
   const char* w = (const char*)g.w + (none ? 0 : t.group * g.group_stride * 2);
-  const Operand a{(const char*)g.x + t.row * g.ldx * 2, g.ldx, t.rows};
-  const Operand b{w + (T::LB == kAlong ? c0 * g.ldw : (int64_t)c0) * 2, g.ldw, cols};
+  const Operand a{(const char*)g.x + t.row * g.ldx * 2, g.ldx, t.rows, g.depth};
+  const Operand b{w + (T::LB == kAlong ? c0 * g.ldw : (int64_t)c0) * 2, g.ldw, cols,
+                  T::LB == kAlong ? g.depth : g.cols};
   v16f acc[T::MB][T::NB] = {};
   product<T>(a, b, none ? 0 : g.depth, lds, acc);
   store<T>(acc, lds, (char*)g.y + (t.row * g.ldy + c0) * 2, g.ldy, t.rows, cols, g.vec);
+}
+
+// The same for few rows per group (serving): a block reads 16 NB columns of a
+// group's weights once, for at most 16 TB of its rows.
+template <int TYPE, int NB, int TB, int WAVES>
+__global__ __launch_bounds__(WAVES * 64) void grouped_few_kernel(GroupedRows g) {
+  using O = typename Out<TYPE>::type;
+  __shared__ v4f lds[WAVES * TB * 16 * NB * 4];
+  const uint32_t tiles_n = ((uint32_t)g.cols + 16 * NB - 1) / (16 * NB);
+  const uint32_t tiles_m = count_row_tiles<16 * TB>(g.ends, g.groups, g.rows);
+  uint32_t place;
+  if (!block_place(blockIdx.x, tiles_m * tiles_n, place)) return;
+  // a group's row tiles side by side: they share the weights
+  const uint32_t tn = place / tiles_m, tm = place - tn * tiles_m;
+  RowTile t;
+  if (!find_row_tile<16 * TB>(g.ends, g.groups, g.rows, (int)tm, t)) return;
+  const int c0 = (int)tn * (16 * NB), cols = g.cols - c0 < 16 * NB ? g.cols - c0 : 16 * NB;
+  v4f acc[NB][TB] = {};
+  if (t.group < g.groups && g.depth > 0) {
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int steps = (g.depth + 31) / 32;
+    const char* w = (const char*)g.w + (t.group * g.group_stride + c0 * g.ldw) * 2;
+    skinny<TYPE, NB, TB>(w, g.ldw, cols, (const char*)g.x + t.row * g.ldx * 2, g.ldx, t.rows, g.depth,
+                         steps * wave / WAVES, steps * (wave + 1) / WAVES, acc);
+  }
+  O* const y = (O*)g.y + t.row * g.ldy + c0;
+  skinny_join<NB, TB, WAVES>(acc, lds, [&](int row, int c, v4f v) {
+    if (row >= t.rows || c >= cols) return;
+    O* const q = y + row * g.ldy + c;
+    if (g.vec) {
+      *(uint2*)q = pack4<TYPE>(v[0], v[1], v[2], v[3]);
+    } else {
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        if (c + e < cols) q[e] = (O)v[e];
+    }
+  });
 }
 
 // dW_g (n x k) = dY_g^T X_g; a group without rows gets zeros.
@@ -56,8 +95,8 @@ __global__ __launch_bounds__(T::THREADS, 1) void grouped_weights_kernel(GroupedW
   end = __builtin_amdgcn_readlane(end, group & 63);
   const int r0 = (int)tm * T::BM, c0 = (int)tn * T::BN;
   const int rows = g.n - r0 < T::BM ? g.n - r0 : T::BM, cols = g.k - c0 < T::BN ? g.k - c0 : T::BN;
-  const Operand a{(const char*)g.dy + (first * g.lddy + r0) * 2, g.lddy, rows};
-  const Operand b{(const char*)g.x + (first * g.ldx + c0) * 2, g.ldx, cols};
+  const Operand a{(const char*)g.dy + (first * g.lddy + r0) * 2, g.lddy, rows, g.n};
+  const Operand b{(const char*)g.x + (first * g.ldx + c0) * 2, g.ldx, cols, g.k};
   v16f acc[T::MB][T::NB] = {};
   product<T>(a, b, end - first, lds, acc);
   constexpr int E = sizeof(typename Out<T::OUT>::type);
@@ -72,6 +111,16 @@ hipError_t run_rows(const GroupedRows& g, hipStream_t s) {
   return hipGetLastError();
 }
 
+template <int TYPE, int NB, int TB, int WAVES>
+hipError_t run_few(const GroupedRows& g, hipStream_t s) {
+  // a tile holds at least one row, and all but each group's last (and that of no group) are full
+  const int64_t most = (int64_t)g.rows / (16 * TB) + g.groups + 1;
+  const int64_t tiles = (most < g.rows ? most : g.rows) * ((g.cols + 16 * NB - 1) / (16 * NB));
+  if (tiles * WAVES * 64 >= ((int64_t)1 << 32)) return hipErrorInvalidConfiguration;
+  grouped_few_kernel<TYPE, NB, TB, WAVES><<<dim3((uint32_t)((tiles + 7) & ~(int64_t)7)), dim3(WAVES * 64), 0, s>>>(g);
+  return hipGetLastError();
+}
+
 template <class T>
 hipError_t run_weights(const GroupedWeights& g, hipStream_t s) {
   const int64_t each = (int64_t)((g.n + T::BM - 1) / T::BM) * ((g.k + T::BN - 1) / T::BN);
@@ -83,14 +132,36 @@ hipError_t run_weights(const GroupedWeights& g, hipStream_t s) {
 
 template <int TYPE, int LB>
 hipError_t rows_of_type(const GroupedRows& g, bool dma, hipStream_t s) {
-  if (dma) return run_rows<Tile<TYPE, kAlong, LB, 2, 4, 4, 2, true, TYPE>>(g, s);
-  return run_rows<Tile<TYPE, kAlong, LB, 2, 2, 2, 2, false, TYPE>>(g, s);
+  if (LB == kAlong && few_rows(g.rows, g.groups)) switch (few_form(g.rows, g.groups, g.cols)) {
+      case kFew16: return run_few<TYPE, 1, 1, 8>(g, s);
+      case kFew32: return run_few<TYPE, 2, 2, 8>(g, s);
+      case kFew64x32: return run_few<TYPE, 4, 2, 4>(g, s);
+      case kFew64x64: return run_few<TYPE, 4, 4, 4>(g, s);
+    }
+  if (!dma) {
+    if (masked_small(false, expected_row_tiles(g.rows, g.groups, 128) * ceil_div(g.cols, 128)))
+      return run_rows<Tile<TYPE, kAlong, LB, 2, 2, 1, 1, false, TYPE>>(g, s);
+    return run_rows<Tile<TYPE, kAlong, LB, 2, 4, 2, 1, false, TYPE>>(g, s);
+  }
+  switch (rows_tile(g.rows, g.groups, g.cols)) {
+    case kSmallTile: return run_rows<Tile<TYPE, kAlong, LB, 2, 2, 1, 1, true, TYPE>>(g, s);
+    case kMiddleTile: return run_rows<Tile<TYPE, kAlong, LB, 2, 2, 2, 2, true, TYPE>>(g, s);
+    default: return run_rows<Tile<TYPE, kAlong, LB, 2, 4, 4, 2, true, TYPE>>(g, s);
+  }
 }
 
 template <int TYPE, int OUT>
 hipError_t weights_of_type(const GroupedWeights& g, bool dma, hipStream_t s) {
-  if (dma) return run_weights<Tile<TYPE, kAcross, kAcross, 2, 4, 4, 2, true, OUT>>(g, s);
-  return run_weights<Tile<TYPE, kAcross, kAcross, 2, 2, 2, 2, false, OUT>>(g, s);
+  if (!dma) {
+    if (masked_small(true, g.groups * ceil_div(g.n, 128) * ceil_div(g.k, 128)))
+      return run_weights<Tile<TYPE, kAcross, kAcross, 2, 2, 1, 1, false, OUT>>(g, s);
+    return run_weights<Tile<TYPE, kAcross, kAcross, 2, 4, 2, 1, false, OUT>>(g, s);
+  }
+  switch (weights_tile(g.n, g.k, g.groups)) {
+    case kSmallTile: return run_weights<Tile<TYPE, kAcross, kAcross, 2, 2, 1, 1, true, OUT>>(g, s);
+    case kMiddleTile: return run_weights<Tile<TYPE, kAcross, kAcross, 2, 2, 2, 2, true, OUT>>(g, s);
+    default: return run_weights<Tile<TYPE, kAcross, kAcross, 2, 4, 4, 2, true, OUT>>(g, s);
+  }
 }
 
 }  // namespace

@@ -1,0 +1,81 @@
+// The rules by which the 16-bit products choose their tiles, from sizes alone.
+// Plain C++, so that they also compile for the host's tests.  Measured on the
+// whole card (256 CUs); times in us, bfloat16.
+#pragma once
+
+#include <cstdint>
+
+namespace oz {
+namespace half {
+
+// Tiles: large 256 x 256 (one block per CU), middle 128 x 128 (two), small 64 x 64.
+enum TileSize { kSmallTile, kMiddleTile, kLargeTile };
+
+constexpr int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+
+// Row tiles of `bm` rows that a grouped product is expected to have: every
+// group's last tile is partly filled, and most groups have rows.
+constexpr int64_t expected_row_tiles(int64_t rows, int64_t groups, int64_t bm) {
+  const int64_t filled = groups < rows ? groups : rows;
+  const int64_t t = rows / bm + (groups * 3 + 4) / 5;
+  return t > filled ? t : filled;
+}
+
+// Large or middle tiles for `large` and `middle` tiles of either, by the
+// measured cost of a round (all CUs busy once) per 64 depths: a large round 1.4
+// if it is the only one, two rounds 3.2 whatever the second one's size, more 1.7
+// each and half a round lost; a middle one 1.0 if alone, else 1.05 each and
+// half a round lost.  Large / middle: rows, groups, n, k = 16384, 16, 4096, 2048
+// 310 / 339; 2048, 8, 4096, 2048 47 / 54; its input gradient 75 / 51; 4096, 8,
+// 4096, 2048 96 / 85; 16384, 8, 1024, 1024 56 / 48; 20000, 2, 4096, 2048 294 / 324.
+constexpr TileSize large_or_middle(int64_t large, int64_t middle) {
+  const double l = large / 256.0, m = middle / 512.0;
+  const double cl = l <= 1 ? 1.4 : l <= 2 ? 3.2 : 1.7 * (l + 0.5);
+  const double cm = m <= 1 ? 1.0 : 1.05 * (m + 0.5);
+  return cl < cm ? kLargeTile : kMiddleTile;
+}
+
+// A product by rows.  Small tiles where middle ones would leave every other
+// slot empty: 512, 8, 4096, 2048 small 26 / middle 29, 512, 8, 1024, 1024 8.2 /
+// 11.4; beyond 1024, 8, 4096, 2048 44 / 30.
+constexpr TileSize rows_tile(int64_t rows, int64_t groups, int64_t cols) {
+  const int64_t middle = expected_row_tiles(rows, groups, 128) * ceil_div(cols, 128);
+  if (middle <= 256) return kSmallTile;
+  return large_or_middle(expected_row_tiles(rows, groups, 256) * ceil_div(cols, 256), middle);
+}
+
+// The weights' gradient, whose groups differ in depth: large tiles only where
+// several rounds even that out.  Large / middle, 32-bit output: 4096, 8, 4096,
+// 2048 102 / 127, 16384, 16, 4096, 2048 340 / 396; 8192, 16, 2048, 1024 71 / 58,
+// 20000, 2, 4096, 2048 381 / 312; small / middle: 700, 2, 512, 256 6.4 / 10, 512,
+// 8, 1024, 1024 12.7 / 11.3.
+constexpr TileSize weights_tile(int64_t n, int64_t k, int64_t groups) {
+  if (groups * ceil_div(n, 128) * ceil_div(k, 128) <= 256) return kSmallTile;
+  return groups * ceil_div(n, 256) * ceil_div(k, 256) >= 768 ? kLargeTile : kMiddleTile;
+}
+
+// Operands that cannot go to LDS by DMA take middle tiles of eight wavefronts
+// (more loads in flight), and small ones sooner for the weights' gradient.
+// 4999, 7, 1031, 777 small / middle: forward 48 / 40, weights' gradient 40 / 49;
+// 16384, 8, 1031, 2049: weights' gradient 230 / 159.
+constexpr bool masked_small(bool weights, int64_t middle_tiles) { return middle_tiles <= (weights ? 512 : 256); }
+
+// Few rows per group: the weights go straight into fragments (at most 48 rows
+// a group on average).  Few-row form / tiles: 256, 8, 4096, 2048 42 / 51, 384,
+// 8, 2048, 2048 32 / 32, 512, 8, 4096, 2048 62 / 30.
+constexpr bool few_rows(int64_t rows, int64_t groups) { return groups > 0 && rows <= 48 * groups; }
+
+// Its blocks: 64 columns where that gives at least a block per CU (with 32 or,
+// above 16 rows a group, 64 rows each), else 16 columns (32 above 16 rows a
+// group, with 32 rows).  16 / 64 columns: 2, 8, 2048, 1024 4.0 / 6.8, 16, 1,
+// 4096, 4096 10.5 / 22; 256, 64, 1024, 2048 57 / 53, 64, 8, 4096, 2048 38 / 31.
+enum FewForm { kFew16, kFew32, kFew64x32, kFew64x64 };
+constexpr FewForm few_form(int64_t rows, int64_t groups, int64_t cols) {
+  const int64_t filled = groups < rows ? groups : rows;
+  const bool many = rows > 16 * groups;
+  if (filled * ceil_div(cols, 64) >= 256) return many ? kFew64x64 : kFew64x32;
+  return many ? kFew32 : kFew16;
+}
+
+}  // namespace half
+}  // namespace oz

@@ -43,6 +43,7 @@ typedef __bf16 v8b __attribute__((ext_vector_type(8)));
 typedef _Float16 v8h __attribute__((ext_vector_type(8)));
 typedef float v16f __attribute__((ext_vector_type(16)));
 using lds_ptr = __attribute__((address_space(3))) void*;
+using global_bytes = const __attribute__((address_space(1))) char*;
 using lds_bytes = const __attribute__((address_space(3))) char*;
 
 constexpr int kBF16 = 0, kF16 = 1, kF32 = 2;  // element types (ozaki25_dtype)
@@ -90,6 +91,7 @@ struct Operand {
   const char* p;
   int64_t ld;  // elements
   int vecs;    // vectors that exist, at most the tile's
+  int width;   // elements of a whole memory row
 };
 
 template <class T>
@@ -215,16 +217,34 @@ struct DmaLoads {
   }
 };
 
+// Chunks of 8 elements at any alignment.  A chunk that the row's end cuts is
+// read as the row's last 8 elements and shifted when it is put into LDS (one
+// load like the others: reading it element by element cost the edge tiles
+// three times the whole product's time).  Rows of fewer than 8 elements are
+// read element by element.
 template <int L, int V, int N>
 struct MaskedSide {
   v4i reg[N];
-  const char* p;
-  int64_t ld;
+  int have[N];      // elements of the chunk that exist
+  int64_t from[N];  // bytes from a stage's first element to the chunk
+  global_bytes p;
+  int64_t step;  // bytes from stage to stage
+  int64_t safe;  // bytes from the stage's first element to 8 elements that always exist
   int vecs;
-  __device__ __forceinline__ void init(const Operand& op) {
-    p = uniform(op.p);
-    ld = op.ld;
+  bool narrow;
+  __device__ __forceinline__ void init(const Operand& op, int depth, int wave, int lane) {
+    p = (global_bytes)uniform(op.p);
+    step = (L == kAlong ? kDepth : op.ld * kDepth) * 2;
     vecs = op.vecs;
+    narrow = op.width < 8;
+    const int first = L == kAlong ? depth : vecs;  // of the first row, from here on
+    safe = first < 8 ? (first - 8) * 2 : 0;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      int r, c;
+      chunk_at<L, V>((wave * N + i) * 1024 + lane * 16, r, c);
+      from[i] = (r * op.ld + c * 8) * 2;
+    }
   }
   __device__ __forceinline__ void load(int wave, int lane, int left) {
 #pragma unroll
@@ -232,26 +252,39 @@ struct MaskedSide {
       int r, c;
       chunk_at<L, V>((wave * N + i) * 1024 + lane * 16, r, c);
       const int rows = L == kAlong ? vecs : left, cols = L == kAlong ? left : vecs;
-      const int have = r < rows ? cols - c * 8 : 0;
-      v4i v{};
-      if (have > 0) {
-        const char* q = p + ((int64_t)r * ld + c * 8) * 2;
-        if (have >= 8) {
-          __builtin_memcpy(&v, q, 16);
-        } else {
-          v8s e{};
-#pragma unroll
-          for (int j = 0; j < 7; ++j)
-            if (j < have) e[j] = ((const short*)q)[j];
-          v = __builtin_bit_cast(v4i, e);
-        }
-      }
-      reg[i] = v;
+      const int n = cols - c * 8;
+      have[i] = r < rows ? (n < 0 ? 0 : n < 8 ? n : 8) : 0;
     }
-    p += L == kAlong ? kDepth * 2 : ld * kDepth * 2;
+    if (!narrow) {
+      // no branch around a load: its end would wait for the data
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        const int64_t at = have[i] > 0 ? from[i] - (8 - have[i]) * 2 : safe;
+        __builtin_memcpy(&reg[i], (const __attribute__((address_space(1))) void*)(p + at), 16);
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        v8s e{};
+#pragma unroll
+        for (int j = 0; j < 7; ++j)
+          if (j < have[i]) e[j] = ((const __attribute__((address_space(1))) short*)(p + from[i]))[j];
+        reg[i] = __builtin_bit_cast(v4i, e);
+        have[i] = 8;
+      }
+    }
+    p += step;
+    safe -= step;
   }
   __device__ __forceinline__ void put(int i, char* lds, int wave, int lane) const {
-    *(v4i*)(lds + (wave * N + i) * 1024 + lane * 16) = reg[i];
+    const int s = 16 * (8 - have[i]);  // bits to drop; 128: all
+    const uint4 x = __builtin_bit_cast(uint4, reg[i]);
+    uint64_t lo = (uint64_t)x.y << 32 | x.x, hi = (uint64_t)x.w << 32 | x.z;
+    const uint64_t up = hi << 1 << (63 - (s & 63));  // hi << (64 - s), also for s = 0
+    lo = s < 64 ? lo >> (s & 63) | up : hi >> (s & 63);
+    hi = s < 64 ? hi >> (s & 63) : 0;
+    if (s == 128) lo = 0;
+    *(v4i*)(lds + (wave * N + i) * 1024 + lane * 16) = v4i{(int)lo, (int)(lo >> 32), (int)hi, (int)(hi >> 32)};
   }
 };
 
@@ -260,9 +293,9 @@ struct MaskedLoads {
   MaskedSide<T::LA, T::BM, T::ADMA> a;
   MaskedSide<T::LB, T::BN, T::BDMA> b;
   int left;
-  __device__ __forceinline__ void init(const Operand& oa, const Operand& ob, int depth, int, int) {
-    a.init(oa);
-    b.init(ob);
+  __device__ __forceinline__ void init(const Operand& oa, const Operand& ob, int depth, int wave, int lane) {
+    a.init(oa, depth, wave, lane);
+    b.init(ob, depth, wave, lane);
     left = depth;
   }
   __device__ __forceinline__ void early(int wave, int lane) {
@@ -544,14 +577,14 @@ __device__ __forceinline__ v4f mfma16(v4i a, v4i b, v4f c) {
 __device__ __forceinline__ v4i load8(const char* row, int c, int cols) {
   v4i v{};
   const int have = cols - c;
-  const char* q = row + (int64_t)c * 2;
+  const global_bytes q = (global_bytes)row + (int64_t)c * 2;
   if (have >= 8) {
-    __builtin_memcpy(&v, q, 16);
+    __builtin_memcpy(&v, (const __attribute__((address_space(1))) void*)q, 16);
   } else if (have > 0) {
     v8s e{};
 #pragma unroll
     for (int j = 0; j < 7; ++j)
-      if (j < have) e[j] = ((const short*)q)[j];
+      if (j < have) e[j] = ((const __attribute__((address_space(1))) short*)q)[j];
     v = __builtin_bit_cast(v4i, e);
   }
   return v;
@@ -559,7 +592,7 @@ __device__ __forceinline__ v4i load8(const char* row, int c, int cols) {
 
 __device__ __forceinline__ v4i load_whole(const char* q) {
   v4i v;
-  __builtin_memcpy(&v, q, 16);
+  __builtin_memcpy(&v, (const __attribute__((address_space(1))) void*)(global_bytes)q, 16);
   return v;
 }
 

@@ -92,7 +92,7 @@ __global__ __launch_bounds__(T::THREADS, 1) void gram_kernel(Orthogonalise o, co
   if constexpr (SQUARE) a = in + blockIdx.y * ((int64_t)s * s * 2);
   const int64_t step = T::LA == kAlong ? ld : 1;
   v16f acc[T::MB][T::NB] = {};
-  product<T>(Operand{a + r0 * step * 2, ld, rows}, Operand{a + c0 * step * 2, ld, cols}, depth, lds, acc);
+  product<T>(Operand{a + r0 * step * 2, ld, rows, (int)ld}, Operand{a + c0 * step * 2, ld, cols, (int)ld}, depth, lds, acc);
   char* const o16 = out + blockIdx.y * ((int64_t)s * s * 2);
   const _Float16* const S = (const _Float16*)a;
   store_wide<T>(acc, lds, o16 + ((int64_t)r0 * s + c0) * 2, s, rows, cols, true, [&](int r, int q, float* v) {
@@ -144,9 +144,9 @@ __global__ __launch_bounds__(T::THREADS, 1) void update_kernel(Orthogonalise o, 
   const char* const P = (const char*)o.p16 + blockIdx.y * ((int64_t)s * s * 2);
   v16f acc[T::MB][T::NB] = {};
   if constexpr (TALL)
-    product<T>(Operand{X + (int64_t)r0 * o.np * 2, o.np, rows}, Operand{P + (int64_t)c0 * s * 2, s, cols}, s, lds, acc);
+    product<T>(Operand{X + (int64_t)r0 * o.np * 2, o.np, rows, o.np}, Operand{P + (int64_t)c0 * s * 2, s, cols, s}, s, lds, acc);
   else
-    product<T>(Operand{P + (int64_t)r0 * s * 2, s, rows}, Operand{X + (int64_t)c0 * 2, o.np, cols}, s, lds, acc);
+    product<T>(Operand{P + (int64_t)r0 * s * 2, s, rows, s}, Operand{X + (int64_t)c0 * 2, o.np, cols, o.np}, s, lds, acc);
   float* const x32 = o.x32 + blockIdx.y * each + (int64_t)r0 * o.np + c0;
   auto value = [&](int r, int q, float* v) {
     if (r < rows && q < cols) {
