@@ -2,14 +2,21 @@
 //
 //   Y[t, :] = X[t, :] W^T + s_a (X[t, :] A_a^T) B_a^T,   a = ids[t]
 //
-// Two launches.  The first forms H[t, :] = X[t, :] A_a^T, partial sums of a
-// split depth, in FP32.  The second runs the projection's tiles and, before a
-// tile is stored, adds for each adapter that its rows name the product of
-// those rows of H with that adapter's B_a: the projection's
-// output is written once and never read.  s_a H goes into that product as
-// two 16-bit numbers, its rounded value and the rest, so that H keeps at least
-// 16 bits and the rounding of the output stays the only one that shows.
+// Many rows: H[t, :] = X[t, :] A_a^T is formed first, in partial sums of a
+// split depth, and s_a H written as two 16-bit numbers, its rounded value and
+// the rest, so that it keeps at least 16 bits.  Then the projection's tiles
+// run and, before a tile is stored, add for each adapter that its rows name
+// the product of those rows of H with that adapter's B_a: the projection's
+// output is written once and never read.
+//
+// Few rows: the projection's weights are what has to be read.  One launch
+// reads them once into partial sums over parts of the depth and forms H beside
+// it; a second one adds the parts up and the adapters' share, in FP32.
+//
+// A few rows that would cost the tiles a round of their own take the few-row
+// form behind them.
 #include "half_products.hpp"
+#include "half_rules.hpp"
 #include "ozaki25.h"
 
 namespace oz {
@@ -33,142 +40,130 @@ __device__ __forceinline__ int next_adapter(const int* ids, int count, int after
   return adapters - __builtin_amdgcn_readlane(most, 63);
 }
 
-// H partial sums.  A block: TB tiles of 16 rows, 16 RB ranks, one part of the
-// depth split again over its four wavefronts, the adapters of its rows in
-// turn (every gridDim.y-th).  grid (row tiles, adapter slots, splits x rank
-// chunks)
-template <int TYPE, int RB, int TB>
+// ---- many rows: whole tiles --------------------------------------------------
+// Partial sums of X A_a^T: a block has 32 rows, 16 RB ranks and a part of the
+// depth, split again over its wavefronts; the adapters that its rows name in
+// turn.  grid (row tiles, parts x rank chunks)
+constexpr int kShrinkRows = 32;
+
+template <int TYPE, int RB>
 __global__ __launch_bounds__(256) void shrink_kernel(Adapter p) {
-  constexpr int ROWS = 16 * TB;
-  __shared__ int ids[64];
-  __shared__ float part[4][TB][RB][16][17];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int t0 = blockIdx.x * ROWS;
-  const int rows = p.rows - t0 < ROWS ? p.rows - t0 : ROWS;
-  const int split = blockIdx.z % p.splits, rank0 = blockIdx.z / p.splits * (16 * RB);
-  if (threadIdx.x < ROWS) ids[threadIdx.x] = (int)threadIdx.x < rows ? p.ids[t0 + threadIdx.x] : -1;
+  constexpr int TB = kShrinkRows / 16;
+  __shared__ int ids[kShrinkRows];
+  __shared__ v4f lds[4 * TB * 16 * RB * 4];
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int t0 = blockIdx.x * kShrinkRows;
+  const int rows = p.rows - t0 < kShrinkRows ? p.rows - t0 : kShrinkRows;
+  const int split = blockIdx.y % p.splits, rank0 = blockIdx.y / p.splits * (16 * RB);
+  const int ranks = p.rank - rank0 < 16 * RB ? p.rank - rank0 : 16 * RB;
+  if (threadIdx.x < kShrinkRows) ids[threadIdx.x] = (int)threadIdx.x < rows ? p.ids[t0 + threadIdx.x] : -1;
   __syncthreads();
-  // whole K steps of 32: this wavefront's range
   const int steps = (p.k + 31) / 32, q = split * 4 + wave;
   const int s0 = (int)((int64_t)steps * q / (p.splits * 4)), s1 = (int)((int64_t)steps * (q + 1) / (p.splits * 4));
-  const int row = lane & 15, half = lane >> 4;
-  int a = -1;
-  for (uint32_t slot = 0;; ++slot) {
-    a = next_adapter<1>(ids, ROWS, a, p.adapters);
+  for (int a = -1;;) {
+    a = next_adapter<1>(ids, rows, a, p.adapters);
     if (a == p.adapters) break;
-    if (slot % gridDim.y != blockIdx.y) continue;
     v4f acc[RB][TB] = {};
-    const char* const A = (const char*)p.a + (int64_t)a * p.a_stride * 2;
-    for (int s = s0; s < s1; ++s) {
-      const int c = s * 32 + half * 8;
-      v4i fa[RB], fx[TB];
+    skinny<TYPE, RB, TB>((const char*)p.a + (a * p.a_stride + rank0 * p.lda) * 2, p.lda, ranks,
+                         (const char*)p.x + t0 * p.ldx * 2, p.ldx, rows, p.k, s0, s1, acc);
+    skinny_join<RB, TB, 4>(acc, lds, [&](int t, int r, v4f v) {
+      if (t >= rows || ids[t] != a || rank0 + r >= p.rank_pad) return;
 #pragma unroll
-      for (int i = 0; i < RB; ++i) {
-        const int r = rank0 + i * 16 + row;
-        fa[i] = r < p.rank ? load8(A + (int64_t)r * p.lda * 2, c, p.k) : v4i{};
-      }
-#pragma unroll
-      for (int j = 0; j < TB; ++j) {
-        const int t = j * 16 + row;
-        fx[j] = t < rows && ids[t] == a ? load8((const char*)p.x + (t0 + t) * p.ldx * 2, c, p.k) : v4i{};
-      }
-#pragma unroll
-      for (int i = 0; i < RB; ++i)
-#pragma unroll
-        for (int j = 0; j < TB; ++j) acc[i][j] = mfma16<TYPE>(fa[i], fx[j], acc[i][j]);
-    }
-    // lane l of a 16 x 16 block: row tile's row l % 16, ranks 4 (l / 16) .. + 3
-#pragma unroll
-    for (int i = 0; i < RB; ++i)
-#pragma unroll
-      for (int j = 0; j < TB; ++j)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) part[wave][j][i][row][half * 4 + e] = acc[i][j][e];
-    __syncthreads();
-    for (int o = threadIdx.x; o < TB * 16 * RB * 16; o += 256) {
-      const int r = o % (RB * 16), t = o / (RB * 16);
-      if (t < rows && ids[t] == a && rank0 + r < p.rank_pad) {
-        float v = 0;
-#pragma unroll
-        for (int w = 0; w < 4; ++w) v += part[w][t >> 4][r >> 4][t & 15][r & 15];
-        p.h[((int64_t)split * p.rows + t0 + t) * p.rank_pad + rank0 + r] = v;
-      }
-    }
+      for (int e = 0; e < 4; ++e) v[e] = r + e < ranks ? v[e] : 0.0f;
+      *(v4f*)(p.h + ((int64_t)split * p.rows + t0 + t) * p.rank_pad + rank0 + r) = v;
+    });
     __syncthreads();
   }
 }
 
-// The adapters' share of a tile, added to its sums.  ids: the tile's rows.
+// s_a H from its partial sums, as the rounded values (rank_pad of a row) and
+// the rests (rank_pad more); rows without an adapter are not written.
+template <int TYPE>
+__global__ __launch_bounds__(256) void split_kernel(Adapter p) {
+  using O = typename Out<TYPE>::type;
+  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  const int quads = p.rank_pad / 4;
+  const int64_t t = i / quads;
+  const int r = (int)(i - t * quads) * 4;
+  if (t >= p.rows) return;
+  const int a = p.ids[t];
+  if (a < 0 || a >= p.adapters) return;
+  v4f v{};
+  for (int s = 0; s < p.splits; ++s) v += *(const v4f*)(p.h + ((int64_t)s * p.rows + t) * p.rank_pad + r);
+  v *= p.scales ? p.scales[a] : 1.0f;
+  float rest[4];
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    const float hi = (float)(O)v[e];
+    // an overflowing value has no rest: it stays an infinity
+    rest[e] = __builtin_isfinite(hi) ? v[e] - hi : 0.0f;
+  }
+  char* const out = (char*)p.h16 + (t * 2 * p.rank_pad + r) * 2;
+  *(uint2*)out = pack4<TYPE>(v[0], v[1], v[2], v[3]);
+  *(uint2*)(out + p.rank_pad * 2) = pack4<TYPE>(rest[0], rest[1], rest[2], rest[3]);
+}
+
+// The adapters' share of a tile, added to its sums: 64 ranks at a time, H's
+// rounded values, its rests and B_a in LDS.  A lane's outputs of a block lie in
+// one row (WIDE): it takes the sums where that row names this adapter.  (Rows
+// of other adapters as zeros would do without that choice, but pass on an
+// infinity of this adapter's B.)
 template <class T>
 __device__ __forceinline__ void expand(const Adapter& p, int r0, int rows, int c0, int cols, const int* ids, char* lds,
                                        v16f (&acc)[T::MB][T::NB]) {
-  static_assert(T::LA == kAlong && T::LB == kAlong && T::BM <= 256);
+  static_assert(T::LA == kAlong && T::LB == kAlong && T::WIDE);
+  static_assert(2 * T::A_BYTES + T::B_BYTES <= T::LDS);
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int wr = wave / T::WC, wc = wave % T::WC;
   Fragments<kAlong, T::BM, T::MB> fa;
   Fragments<kAlong, T::BN, T::NB> fb;
-  fa.init(wave / T::WC * T::MB, lane);
-  fb.init(wave % T::WC * T::NB, lane);
-  using O = typename Out<T::TYPE>::type;
-  typedef O v8o __attribute__((ext_vector_type(8)));
-  const int depth = 2 * p.rank_pad;  // the rounded values, then the rests
-  int a = -1;
-  for (;;) {
-    a = next_adapter<T::BM / 64>(ids, rows, a, p.adapters);
+  fa.init(wr * T::MB, lane);
+  fb.init(wc * T::NB, lane);
+  char* const rests = lds + T::A_BYTES;
+  char* const bs = lds + 2 * T::A_BYTES;
+  for (int a = -1;;) {
+    a = next_adapter<(T::BM + 63) / 64>(ids, rows, a, p.adapters);
     if (a == p.adapters) break;
-    const float scale = p.scales ? p.scales[a] : 1.0f;
-    const char* const B = (const char*)p.b + ((int64_t)a * p.b_stride + (int64_t)c0 * p.ldb) * 2;
-    for (int d0 = 0; d0 < depth; d0 += kDepth) {
-      const int chunks = (depth - d0 < kDepth ? depth - d0 : kDepth) / 8;
-      for (int o = threadIdx.x; o < T::BM * chunks; o += T::THREADS) {
-        const int r = o / chunks, c = o - r * chunks, d = d0 + c * 8;
-        const bool rest = d >= p.rank_pad;
-        v8o e{};
-        if (r < rows && ids[r] == a) {
-          const float* h = p.h + (int64_t)(r0 + r) * p.rank_pad + (rest ? d - p.rank_pad : d);
-          float v[8] = {};
-          for (int s = 0; s < p.splits; ++s) {
-            const float4 x = *(const float4*)h, y = *(const float4*)(h + 4);
-            v[0] += x.x, v[1] += x.y, v[2] += x.z, v[3] += x.w;
-            v[4] += y.x, v[5] += y.y, v[6] += y.z, v[7] += y.w;
-            h += (int64_t)p.rows * p.rank_pad;
-          }
+    const char* const B = (const char*)p.b + (a * p.b_stride + c0 * p.ldb) * 2;
+    for (int d0 = 0; d0 < p.rank_pad; d0 += kDepth) {
+      const int left = p.rank_pad - d0 < kDepth ? p.rank_pad - d0 : kDepth;
+      const char* const h = (const char*)p.h16 + ((int64_t)r0 * 2 * p.rank_pad + d0) * 2;
+      MaskedSide<kAlong, T::BM, T::ADMA> hi, lo;
+      MaskedSide<kAlong, T::BN, T::BDMA> b;
+      hi.init(Operand{h, 2 * p.rank_pad, rows, 2 * p.rank_pad}, left, wave, lane);
+      lo.init(Operand{h + p.rank_pad * 2, 2 * p.rank_pad, rows, 2 * p.rank_pad}, left, wave, lane);
+      b.init(Operand{B + d0 * 2, p.ldb, cols, p.rank}, p.rank - d0, wave, lane);
+      hi.load(wave, lane, left);
+      lo.load(wave, lane, left);
+      b.load(wave, lane, p.rank - d0);
 #pragma unroll
-          for (int j = 0; j < 8; ++j) {
-            const float x = v[j] * scale;
-            const O hi = (O)x;
-            // an overflowing value has no rest: it stays an infinity
-            e[j] = !rest ? hi : __builtin_isfinite((float)hi) ? (O)(x - (float)hi) : (O)0.0f;
-          }
-        }
-        *(v4i*)(lds + r * 128 + ((c ^ swz_along(r)) << 4)) = __builtin_bit_cast(v4i, e);
+      for (int i = 0; i < T::ADMA; ++i) {
+        hi.put(i, lds, wave, lane);
+        lo.put(i, rests, wave, lane);
       }
-      for (int o = threadIdx.x; o < T::BN * chunks; o += T::THREADS) {
-        const int v = o / chunks, c = o - v * chunks, d = d0 + c * 8;
-        const int r = d >= p.rank_pad ? d - p.rank_pad : d;
-        v4i e{};
-        if (v < cols) e = load8(B + (int64_t)v * p.ldb * 2, r, p.rank);
-        *(v4i*)(lds + T::A_BYTES + v * 128 + ((c ^ swz_along(v)) << 4)) = e;
-      }
+#pragma unroll
+      for (int i = 0; i < T::BDMA; ++i) b.put(i, bs, wave, lane);
       __syncthreads();
-      // a lane's outputs of a block lie in one row: it takes the sums where
-      // that row names this adapter (a product with zeros instead would pass
-      // on an infinity of this adapter's B)
+      const int ks_end = left / 16;
 #pragma unroll
       for (int x = 0; x < T::MB; ++x) {
-        const bool mine = ids[(wave / T::WC * T::MB + x) * 32 + (lane & 31)] == a;
-        v4i xa[kDepth / 16];
+        const bool mine = ids[(wr * T::MB + x) * 32 + (lane & 31)] == a;
+        v16f t[T::NB] = {};
+        for (int ks = 0; ks < ks_end; ++ks) {
+          // the swizzle's K step term, as Fragments has it
+          const v4i xh = *(const v4i*)(lds + fa.at(ks) + x * 4096), xl = *(const v4i*)(rests + fa.at(ks) + x * 4096);
 #pragma unroll
-        for (int ks = 0; ks < kDepth / 16; ++ks) xa[ks] = ks * 2 < chunks ? fa.read((lds_bytes)lds, ks, x) : v4i{};
-#pragma unroll
-        for (int y = 0; y < T::NB; ++y) {
-          v16f t{};
-#pragma unroll
-          for (int ks = 0; ks < kDepth / 16; ++ks)
-            if (ks * 2 < chunks) t = mfma<T::TYPE>(fb.read((lds_bytes)lds + T::A_BYTES, ks, y), xa[ks], t);
-#pragma unroll
-          for (int i = 0; i < 16; ++i) acc[x][y][i] += mine ? t[i] : 0.0f;
+          for (int y = 0; y < T::NB; ++y) {
+            const v4i xb = *(const v4i*)(bs + fb.at(ks) + y * 4096);
+            t[y] = mfma<T::TYPE>(xb, xh, t[y]);
+            t[y] = mfma<T::TYPE>(xb, xl, t[y]);
+          }
         }
+#pragma unroll
+        for (int y = 0; y < T::NB; ++y)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) acc[x][y][i] += mine ? t[y][i] : 0.0f;
       }
       __syncthreads();
     }
@@ -177,19 +172,21 @@ __device__ __forceinline__ void expand(const Adapter& p, int r0, int rows, int c
 
 template <class T>
 __global__ __launch_bounds__(T::THREADS, 1) void adapter_kernel(Adapter p) {
-  __shared__ __attribute__((aligned(1024))) char lds[T::LDS];
-  __shared__ int ids[T::BM];
+  // one array: with two, the compiler would tell them apart by alias scopes of
+  // its own and wait for the loads into LDS before every fragment
+  __shared__ __attribute__((aligned(1024))) char lds[T::LDS + T::BM * 4];
+  int* const ids = (int*)(lds + T::LDS);
   const uint32_t tiles_n = ((uint32_t)p.n + T::BN - 1) / T::BN, tiles_m = ((uint32_t)p.rows + T::BM - 1) / T::BM;
   uint32_t place, tm, tn;
   if (!block_place(blockIdx.x, tiles_m * tiles_n, place)) return;
   place_to_tile(place, tiles_m, tiles_n, tm, tn);
   const int r0 = (int)tm * T::BM, c0 = (int)tn * T::BN;
   const int rows = p.rows - r0 < T::BM ? p.rows - r0 : T::BM, cols = p.n - c0 < T::BN ? p.n - c0 : T::BN;
-  for (int i = threadIdx.x; i < T::BM; i += T::THREADS) ids[i] = i < rows ? p.ids[r0 + i] : -1;
+  if (p.rank > 0)
+    for (int i = threadIdx.x; i < T::BM; i += T::THREADS) ids[i] = i < rows ? p.ids[r0 + i] : -1;
   v16f acc[T::MB][T::NB] = {};
-  product<T>(Operand{(const char*)p.x + r0 * p.ldx * 2, p.ldx, rows, p.k}, Operand{(const char*)p.w + c0 * p.ldw * 2, p.ldw, cols, p.k},
-             p.k, lds, acc);
-  __syncthreads();
+  product<T>(Operand{(const char*)p.x + r0 * p.ldx * 2, p.ldx, rows, p.k},
+             Operand{(const char*)p.w + c0 * p.ldw * 2, p.ldw, cols, p.k}, p.k, lds, acc);
   if (p.rank > 0) expand<T>(p, r0, rows, c0, cols, ids, lds, acc);
   store<T>(acc, lds, (char*)p.y + (r0 * p.ldy + c0) * 2, p.ldy, rows, cols, p.vec);
 }
@@ -295,40 +292,68 @@ hipError_t serve(const Adapter& p, hipStream_t s) {
 
 template <class T>
 hipError_t run(const Adapter& p, hipStream_t s) {
-  const int64_t tiles = (int64_t)((p.rows + T::BM - 1) / T::BM) * ((p.n + T::BN - 1) / T::BN);
+  const int64_t tiles = ceil_div(p.rows, T::BM) * ceil_div(p.n, T::BN);
   if (tiles * T::THREADS >= ((int64_t)1 << 32)) return hipErrorInvalidConfiguration;
-  adapter_kernel<T><<<dim3((uint32_t)((tiles + 7) & ~(int64_t)7)), dim3(T::THREADS), 0, s>>>(p);
+  const dim3 grid((uint32_t)((tiles + 7) & ~(int64_t)7));
+  adapter_kernel<T><<<grid, dim3(T::THREADS), 0, s>>>(p);
   return hipGetLastError();
 }
 
 template <int TYPE, int RB>
 hipError_t shrink(const Adapter& p, hipStream_t s) {
-  const uint32_t chunks = (uint32_t)(p.rank + 16 * RB - 1) / (16 * RB);
-  if (p.rows <= 256)
-    shrink_kernel<TYPE, RB, 1><<<dim3((p.rows + 15) / 16, 16, p.splits * chunks), dim3(256), 0, s>>>(p);
-  else
-    shrink_kernel<TYPE, RB, 4><<<dim3((p.rows + 63) / 64, 4, p.splits * chunks), dim3(256), 0, s>>>(p);
+  const dim3 grid((uint32_t)ceil_div(p.rows, kShrinkRows), (uint32_t)(p.splits * ceil_div(p.rank, 16 * RB)));
+  shrink_kernel<TYPE, RB><<<grid, dim3(256), 0, s>>>(p);
+  split_kernel<TYPE><<<dim3((uint32_t)ceil_div((int64_t)p.rows * (p.rank_pad / 4), 256)), dim3(256), 0, s>>>(p);
   return hipGetLastError();
 }
 
 template <int TYPE>
-hipError_t of_type(const Adapter& p, bool dma, hipStream_t s) {
-  if (p.base_splits > 0) return serve<TYPE>(p, s);
-  if (p.rank > 0 && p.k > 0) {
+hipError_t tiles(const Adapter& p, hipStream_t s) {
+  if (p.rank > 0) {
     const hipError_t e = p.rank <= 16 ? shrink<TYPE, 1>(p, s) : p.rank <= 32 ? shrink<TYPE, 2>(p, s) : shrink<TYPE, 4>(p, s);
     if (e != hipSuccess) return e;
   }
-  if (dma) return run<Tile<TYPE, kAlong, kAlong, 2, 4, 4, 2, true, TYPE>>(p, s);
-  return run<Tile<TYPE, kAlong, kAlong, 2, 2, 2, 2, false, TYPE>>(p, s);
+  const int64_t middle = ceil_div(p.rows, 128) * ceil_div(p.n, 128);
+  if (!(dma_operand(p.x, p.ldx, p.k) && dma_operand(p.w, p.ldw, p.k))) {
+    if (masked_small(false, middle)) return run<Tile<TYPE, kAlong, kAlong, 2, 2, 1, 1, false, TYPE>>(p, s);
+    return run<Tile<TYPE, kAlong, kAlong, 2, 4, 2, 1, false, TYPE>>(p, s);
+  }
+  switch (tile_of(middle, ceil_div(p.rows, 256) * ceil_div(p.n, 256))) {
+    case kSmallTile: return run<Tile<TYPE, kAlong, kAlong, 2, 2, 1, 1, true, TYPE>>(p, s);
+    case kMiddleTile: return run<Tile<TYPE, kAlong, kAlong, 2, 2, 2, 2, true, TYPE>>(p, s);
+    default: return run<Tile<TYPE, kAlong, kAlong, 2, 4, 4, 2, true, TYPE>>(p, s);
+  }
+}
+
+template <int TYPE>
+hipError_t both(Adapter p, int serve_rows, hipStream_t s) {
+  const int whole = p.rows - serve_rows;
+  if (whole > 0) {
+    Adapter t = p;
+    t.rows = whole;
+    const hipError_t e = tiles<TYPE>(t, s);
+    if (e != hipSuccess) return e;
+  }
+  if (serve_rows == 0) return hipSuccess;
+  p.rows = serve_rows;
+  p.x = (const char*)p.x + whole * p.ldx * 2;
+  p.y = (char*)p.y + whole * p.ldy * 2;
+  if (p.ids) p.ids += whole;
+  p.splits = p.serve_splits;
+  return serve<TYPE>(p, s);
 }
 
 }  // namespace
 
-hipError_t launch_adapter(Adapter p, int type, hipStream_t s) {
-  const bool dma = dma_operand(p.x, p.ldx, p.k) && dma_operand(p.w, p.ldw, p.k);
+hipError_t launch_adapter(Adapter p, const AdapterPlan& plan, char* room, int type, hipStream_t s) {
   p.vec = (uintptr_t)p.y % 16 == 0 && p.ldy % 8 == 0 && p.n % 8 == 0;
   if (p.k == 0 || p.adapters == 0) p.rank = 0;  // X A^T is zero
-  return type == kBF16 ? of_type<kBF16>(p, dma, s) : of_type<kF16>(p, dma, s);
+  // the two parts run one after the other and share the room of their partial sums of H
+  p.h = (float*)room;
+  p.h16 = room + plan.h_bytes;
+  p.partials = (float*)(room + plan.h_bytes + plan.h16_bytes);
+  p.splits = plan.splits, p.serve_splits = plan.serve_splits, p.base_splits = plan.base_splits;
+  return type == kBF16 ? both<kBF16>(p, plan.serve_rows, s) : both<kF16>(p, plan.serve_rows, s);
 }
 
 }  // namespace half

@@ -135,7 +135,7 @@ size_t ozaki25_adapter_matmul_workspace_size(int64_t rows, int64_t n, int64_t k,
       too_large(rows, n, k, adapters))
     return 0;
   const oz::half::AdapterPlan a = oz::half::adapter_plan(rows, n, k, pad16(rank));
-  return a.h_bytes + a.partial_bytes;
+  return a.h_bytes + a.h16_bytes + a.partial_bytes;
 }
 
 ozaki25_status ozaki25_adapter_matmul(int64_t rows, int64_t n, int64_t k, int64_t adapters, int64_t rank, const void* X,
@@ -177,11 +177,9 @@ ozaki25_status ozaki25_adapter_matmul(int64_t rows, int64_t n, int64_t k, int64_
   p.a = A, p.lda = lda, p.a_stride = a_stride, p.b = B, p.ldb = ldb, p.b_stride = b_stride;
   p.scales = scales, p.y = Y, p.ldy = ldy;
   p.rows = (int)rows, p.n = (int)n, p.k = (int)k, p.adapters = any ? (int)adapters : 0, p.rank = any ? (int)rank : 0;
-  const oz::half::AdapterPlan plan = oz::half::adapter_plan(rows, n, k, pad16(rank));
-  p.h = (float*)room.p, p.partials = (float*)(room.p + plan.h_bytes);
   p.rank_pad = (int)pad16(rank), p.n_pad = (int)((n + 3) / 4 * 4);
-  p.splits = plan.splits, p.base_splits = plan.base_splits;
-  return room.give(status_of(oz::half::launch_adapter(p, (int)type, (hipStream_t)stream)));
+  const oz::half::AdapterPlan plan = oz::half::adapter_plan(rows, n, k, pad16(rank));
+  return room.give(status_of(oz::half::launch_adapter(p, plan, room.p, (int)type, (hipStream_t)stream)));
 }
 
 size_t ozaki25_orthogonalise_workspace_size(int64_t count, int64_t m, int64_t n) {

@@ -2,6 +2,7 @@
 // orthogonalise.hip).  Arguments were checked by the entry points.
 #pragma once
 
+#include "half_rules.hpp"
 #include "half_tile.hpp"
 
 namespace oz {
@@ -45,44 +46,17 @@ struct Adapter {
   void* y;              // rows x n
   int64_t ldy;
   int rows, n, k, adapters, rank;
-  // workspace, as adapter_plan lays it out
-  float* h;         // splits x rows x rank_pad
-  float* partials;  // base_splits x rows x n_pad
-  int rank_pad;     // rank rounded up to 16
-  int n_pad;        // n rounded up to 4
-  int splits;       // parts of the depth of X A^T
-  int base_splits;  // parts of the depth of X W^T in the few-row form; 0: whole tiles
-  bool vec;         // 16-byte stores of y (set by the launch)
+  // workspace (set by the launch)
+  float* h;          // parts x rows x rank_pad
+  void* h16;         // rows x 2 rank_pad
+  float* partials;   // base_splits x rows x n_pad
+  int rank_pad;      // rank rounded up to 16
+  int n_pad;         // n rounded up to 4
+  int splits;        // parts of the depth of X A^T
+  int serve_splits;  // the same in the few-row form
+  int base_splits;   // parts of the depth of X W^T in the few-row form
+  bool vec;          // 16-byte stores of y
 };
-
-// How a call runs: at most kServeRows rows read the weights once and split the
-// depth over blocks (partial sums in the workspace), more rows take whole tiles.
-constexpr int64_t kServeRows = 64;
-struct AdapterPlan {
-  int splits, base_splits;
-  size_t h_bytes, partial_bytes;
-};
-inline AdapterPlan adapter_plan(int64_t rows, int64_t n, int64_t k, int64_t rank_pad) {
-  AdapterPlan a{};
-  if (rows <= kServeRows) {
-    // about two blocks per CU, at least 256 depths (two steps of 32 per wavefront) each
-    const int64_t tiles = (n + 63) / 64, most = (k + 255) / 256;
-    int64_t b = (512 + tiles - 1) / tiles;
-    b = b < most ? b : most;
-    a.base_splits = (int)(b < 1 ? 1 : b > 8 ? 8 : b);
-    const int64_t h = (k + 1023) / 1024;
-    a.splits = (int)(h < 1 ? 1 : h > 8 ? 8 : h);
-  } else {
-    const int64_t tiles = rows <= 256 ? (rows + 15) / 16 * 4 : (rows + 63) / 64;
-    int64_t s = (512 + tiles - 1) / tiles;
-    const int64_t most = (k + 511) / 512;
-    s = s < most ? s : most;
-    a.splits = (int)(s < 1 ? 1 : s > 8 ? 8 : s);
-  }
-  a.h_bytes = ((size_t)a.splits * rows * rank_pad * sizeof(float) + 255) / 256 * 256;
-  a.partial_bytes = ((size_t)a.base_splits * rows * ((n + 3) / 4 * 4) * sizeof(float) + 255) / 256 * 256;
-  return a;
-}
 
 struct Orthogonalise {
   const void* g;  // count matrices m x n
@@ -115,7 +89,7 @@ inline bool dma_operand(const void* p, int64_t ld, int64_t cols) {
 
 hipError_t launch_grouped_rows(GroupedRows g, int type, bool transposed, hipStream_t s);
 hipError_t launch_grouped_weights(GroupedWeights g, int type, int out, hipStream_t s);
-hipError_t launch_adapter(Adapter p, int type, hipStream_t s);
+hipError_t launch_adapter(Adapter p, const AdapterPlan& plan, char* room, int type, hipStream_t s);
 hipError_t launch_orthogonalise(Orthogonalise o, int type, int steps, hipStream_t s);
 
 }  // namespace half

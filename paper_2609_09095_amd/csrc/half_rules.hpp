@@ -3,6 +3,7 @@
 // whole card (256 CUs); times in us, bfloat16.
 #pragma once
 
+#include <cstddef>
 #include <cstdint>
 
 namespace oz {
@@ -17,8 +18,8 @@ constexpr int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 // group's last tile is partly filled, and most groups have rows.
 constexpr int64_t expected_row_tiles(int64_t rows, int64_t groups, int64_t bm) {
   const int64_t filled = groups < rows ? groups : rows;
-  const int64_t t = rows / bm + (groups * 3 + 4) / 5;
-  return t > filled ? t : filled;
+  const int64_t t = rows / bm + groups * 3 / 5, least = ceil_div(rows, bm) > filled ? ceil_div(rows, bm) : filled;
+  return t > least ? t : least;
 }
 
 // Large or middle tiles for `large` and `middle` tiles of either, by the
@@ -35,13 +36,17 @@ constexpr TileSize large_or_middle(int64_t large, int64_t middle) {
   return cl < cm ? kLargeTile : kMiddleTile;
 }
 
-// A product by rows.  Small tiles where middle ones would leave every other
-// slot empty: 512, 8, 4096, 2048 small 26 / middle 29, 512, 8, 1024, 1024 8.2 /
-// 11.4; beyond 1024, 8, 4096, 2048 44 / 30.
+// Small tiles where middle ones would leave every other slot empty: 512, 8,
+// 4096, 2048 small 26 / middle 29, 512, 8, 1024, 1024 8.2 / 11.4; beyond 1024, 8,
+// 4096, 2048 44 / 30.
+constexpr TileSize tile_of(int64_t middle, int64_t large) {
+  return middle <= 256 ? kSmallTile : large_or_middle(large, middle);
+}
+
+// A grouped product by rows.
 constexpr TileSize rows_tile(int64_t rows, int64_t groups, int64_t cols) {
-  const int64_t middle = expected_row_tiles(rows, groups, 128) * ceil_div(cols, 128);
-  if (middle <= 256) return kSmallTile;
-  return large_or_middle(expected_row_tiles(rows, groups, 256) * ceil_div(cols, 256), middle);
+  return tile_of(expected_row_tiles(rows, groups, 128) * ceil_div(cols, 128),
+                 expected_row_tiles(rows, groups, 256) * ceil_div(cols, 256));
 }
 
 // The weights' gradient, whose groups differ in depth: large tiles only where
@@ -75,6 +80,44 @@ constexpr FewForm few_form(int64_t rows, int64_t groups, int64_t cols) {
   const bool many = rows > 16 * groups;
   if (filled * ceil_div(cols, 64) >= 256) return many ? kFew64x64 : kFew64x32;
   return many ? kFew32 : kFew16;
+}
+
+// How an adapter product runs: `rows - serve_rows` rows in whole tiles, the
+// last serve_rows in the few-row form, which reads the weights once per 64 rows.
+struct AdapterPlan {
+  int serve_rows;
+  int splits, serve_splits;  // parts of the depth of X A^T in either
+  int base_splits;           // of X W^T in the few-row form
+  size_t h_bytes, h16_bytes, partial_bytes;
+};
+
+constexpr int clamp_parts(int64_t parts, int64_t most) {
+  const int64_t p = parts < most ? parts : most;
+  return (int)(p < 1 ? 1 : p > 8 ? 8 : p);
+}
+
+constexpr int64_t kServeRows = 64;
+
+constexpr AdapterPlan adapter_plan(int64_t rows, int64_t n, int64_t k, int64_t rank_pad) {
+  AdapterPlan a{};
+  const int64_t over = rows % 256;
+  if (rows <= kServeRows) {
+    a.serve_rows = (int)rows;
+  } else if (over > 0 && over <= kServeRows && rows > 256) {
+    // rows that would take large tiles a round of their own
+    const int64_t with = ceil_div(rows, 256) * ceil_div(n, 256), without = rows / 256 * ceil_div(n, 256);
+    if (ceil_div(with, 256) > ceil_div(without, 256)) a.serve_rows = (int)over;
+  }
+  const int64_t tile_rows = rows - a.serve_rows;
+  // about two blocks per CU; at least 256 depths (two steps of 32 per wavefront) each
+  a.base_splits = a.serve_rows > 0 ? clamp_parts(ceil_div(512, ceil_div(n, 64) * ceil_div(a.serve_rows, 64)), ceil_div(k, 256)) : 0;
+  a.serve_splits = clamp_parts(ceil_div(k, 1024), 8);
+  a.splits = clamp_parts(ceil_div(1024, ceil_div(tile_rows > 0 ? tile_rows : 1, 32)), ceil_div(k, 512));
+  const size_t h1 = (size_t)a.splits * tile_rows, h2 = (size_t)a.serve_splits * a.serve_rows;
+  a.h_bytes = ((h1 > h2 ? h1 : h2) * rank_pad * sizeof(float) + 255) / 256 * 256;
+  a.h16_bytes = ((size_t)tile_rows * 2 * rank_pad * 2 + 255) / 256 * 256;
+  a.partial_bytes = ((size_t)a.base_splits * a.serve_rows * (ceil_div(n, 4) * 4) * sizeof(float) + 255) / 256 * 256;
+  return a;
 }
 
 }  // namespace half

@@ -342,6 +342,11 @@ struct Fragments {
       }
     }
   }
+  // kAlong: the offset of block 0 for a K step known at run time only
+  __device__ __forceinline__ int at(int ks) const {
+    static_assert(L == kAlong);
+    return base[0] ^ (ks << 5);
+  }
   // block x, K step ks of the stage at lds
   __device__ __forceinline__ v4i read(lds_bytes lds, int ks, int x) const {
     if constexpr (L == kAlong) {
