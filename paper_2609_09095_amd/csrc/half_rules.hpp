@@ -55,7 +55,9 @@ constexpr TileSize rows_tile(int64_t rows, int64_t groups, int64_t cols) {
 // 20000, 2, 4096, 2048 381 / 312; small / middle: 700, 2, 512, 256 6.4 / 10, 512,
 // 8, 1024, 1024 12.7 / 11.3.
 constexpr TileSize weights_tile(int64_t n, int64_t k, int64_t groups) {
-  if (groups * ceil_div(n, 128) * ceil_div(k, 128) <= 256) return kSmallTile;
+  const int64_t middle = groups * ceil_div(n, 128) * ceil_div(k, 128);
+  if (groups == 1) return tile_of(middle, ceil_div(n, 256) * ceil_div(k, 256));
+  if (middle <= 256) return kSmallTile;
   return groups * ceil_div(n, 256) * ceil_div(k, 256) >= 768 ? kLargeTile : kMiddleTile;
 }
 
@@ -96,14 +98,17 @@ constexpr int clamp_parts(int64_t parts, int64_t most) {
   return (int)(p < 1 ? 1 : p > 8 ? 8 : p);
 }
 
-constexpr int64_t kServeRows = 64;
+// Few-row form / tiles, eight adapters (rows, n, k, rank): 65, 4096, 4096, 16 25 /
+// 60; 128, 4096, 4096, 64 53 / 54; 256, 1024, 1024, 16 12 / 17; beyond 200, 4096,
+// 4096, 16 47 / 50, 512, 1024, 1024, 16 19 / 16, 512, 4096, 4096, 64 157 / 49.
+constexpr int64_t kServeRows = 128, kServeOutputs = 1 << 18;
 
 constexpr AdapterPlan adapter_plan(int64_t rows, int64_t n, int64_t k, int64_t rank_pad) {
   AdapterPlan a{};
   const int64_t over = rows % 256;
-  if (rows <= kServeRows) {
+  if (rows <= kServeRows || rows * n <= kServeOutputs) {
     a.serve_rows = (int)rows;
-  } else if (over > 0 && over <= kServeRows && rows > 256) {
+  } else if (over > 0 && over <= 64 && rows > 256) {
     // rows that would take large tiles a round of their own
     const int64_t with = ceil_div(rows, 256) * ceil_div(n, 256), without = rows / 256 * ceil_div(n, 256);
     if (ceil_div(with, 256) > ceil_div(without, 256)) a.serve_rows = (int)over;
@@ -112,7 +117,7 @@ constexpr AdapterPlan adapter_plan(int64_t rows, int64_t n, int64_t k, int64_t r
   // about two blocks per CU; at least 256 depths (two steps of 32 per wavefront) each
   a.base_splits = a.serve_rows > 0 ? clamp_parts(ceil_div(512, ceil_div(n, 64) * ceil_div(a.serve_rows, 64)), ceil_div(k, 256)) : 0;
   a.serve_splits = clamp_parts(ceil_div(k, 1024), 8);
-  a.splits = clamp_parts(ceil_div(1024, ceil_div(tile_rows > 0 ? tile_rows : 1, 32)), ceil_div(k, 512));
+  a.splits = clamp_parts(ceil_div(1024, ceil_div(tile_rows > 0 ? tile_rows : 1, 32)), ceil_div(k, tile_rows > 2048 ? 1024 : 512));
   const size_t h1 = (size_t)a.splits * tile_rows, h2 = (size_t)a.serve_splits * a.serve_rows;
   a.h_bytes = ((h1 > h2 ? h1 : h2) * rank_pad * sizeof(float) + 255) / 256 * 256;
   a.h16_bytes = ((size_t)tile_rows * 2 * rank_pad * 2 + 255) / 256 * 256;

@@ -217,6 +217,18 @@ struct DmaLoads {
   }
 };
 
+// The upper `have` (0 to 8) of 8 elements moved down, zeros above them.
+__device__ __forceinline__ v4i keep_upper(v4i v, int have) {
+  const int s = 16 * (8 - have);  // bits to drop; 128: all
+  const uint4 x = __builtin_bit_cast(uint4, v);
+  uint64_t lo = (uint64_t)x.y << 32 | x.x, hi = (uint64_t)x.w << 32 | x.z;
+  const uint64_t up = hi << 1 << (63 - (s & 63));  // hi << (64 - s), also for s = 0
+  lo = s < 64 ? lo >> (s & 63) | up : hi >> (s & 63);
+  hi = s < 64 ? hi >> (s & 63) : 0;
+  if (s == 128) lo = 0;
+  return v4i{(int)lo, (int)(lo >> 32), (int)hi, (int)(hi >> 32)};
+}
+
 // Chunks of 8 elements at any alignment.  A chunk that the row's end cuts is
 // read as the row's last 8 elements and shifted when it is put into LDS (one
 // load like the others: reading it element by element cost the edge tiles
@@ -277,14 +289,7 @@ struct MaskedSide {
     safe -= step;
   }
   __device__ __forceinline__ void put(int i, char* lds, int wave, int lane) const {
-    const int s = 16 * (8 - have[i]);  // bits to drop; 128: all
-    const uint4 x = __builtin_bit_cast(uint4, reg[i]);
-    uint64_t lo = (uint64_t)x.y << 32 | x.x, hi = (uint64_t)x.w << 32 | x.z;
-    const uint64_t up = hi << 1 << (63 - (s & 63));  // hi << (64 - s), also for s = 0
-    lo = s < 64 ? lo >> (s & 63) | up : hi >> (s & 63);
-    hi = s < 64 ? hi >> (s & 63) : 0;
-    if (s == 128) lo = 0;
-    *(v4i*)(lds + (wave * N + i) * 1024 + lane * 16) = v4i{(int)lo, (int)(lo >> 32), (int)hi, (int)(hi >> 32)};
+    *(v4i*)(lds + (wave * N + i) * 1024 + lane * 16) = keep_upper(reg[i], have[i]);
   }
 };
 
@@ -578,27 +583,23 @@ __device__ __forceinline__ v4f mfma16(v4i a, v4i b, v4f c) {
                                                   0);
 }
 
-// Elements c .. c + 7 of a row of `cols`; zeros past its end.  Any alignment.
-__device__ __forceinline__ v4i load8(const char* row, int c, int cols) {
-  v4i v{};
-  const int have = cols - c;
-  const global_bytes q = (global_bytes)row + (int64_t)c * 2;
-  if (have >= 8) {
-    __builtin_memcpy(&v, (const __attribute__((address_space(1))) void*)q, 16);
-  } else if (have > 0) {
-    v8s e{};
-#pragma unroll
-    for (int j = 0; j < 7; ++j)
-      if (j < have) e[j] = ((const __attribute__((address_space(1))) short*)q)[j];
-    v = __builtin_bit_cast(v4i, e);
-  }
-  return v;
-}
-
 __device__ __forceinline__ v4i load_whole(const char* q) {
   v4i v;
   __builtin_memcpy(&v, (const __attribute__((address_space(1))) void*)(global_bytes)q, 16);
   return v;
+}
+
+// Elements c .. c + 7 of a row of `cols`; zeros past its end.  Any alignment;
+// no branch around the load where rows have 8 elements.
+__device__ __forceinline__ v4i load8(const char* row, int c, int cols) {
+  const int n = cols - c, have = n < 0 ? 0 : n < 8 ? n : 8;
+  if (cols >= 8) return keep_upper(load_whole(row + (int64_t)(have > 0 ? c - (8 - have) : 0) * 2), have);
+  v8s e{};
+  const auto q = (const __attribute__((address_space(1))) short*)(global_bytes)row;
+#pragma unroll
+  for (int j = 0; j < 7; ++j)
+    if (j < have) e[j] = q[c + j];
+  return __builtin_bit_cast(v4i, e);
 }
 
 // acc[i][j] += 16 columns of W (rows of its cols x k matrix, from w on) times
@@ -615,7 +616,7 @@ __device__ __forceinline__ void skinny(const char* w, int64_t ldw, int cols, con
 #pragma unroll
   for (int j = 0; j < TB; ++j) px[j] = x + (int64_t)(j * 16 + at < rows ? j * 16 + at : rows - 1) * ldx * 2;
   const int whole = k / 32 < s1 ? k / 32 : s1;  // steps without an end inside
-  constexpr int U = NB + TB <= 2 ? 8 : NB + TB <= 5 ? 4 : 2;
+  constexpr int U = NB + TB <= 2 ? 8 : NB + TB <= 6 ? 4 : 2;
   int s = s0;
   for (; s + U <= whole; s += U) {
     v4i fw[U][NB], fx[U][TB];
@@ -634,7 +635,28 @@ __device__ __forceinline__ void skinny(const char* w, int64_t ldw, int cols, con
 #pragma unroll
         for (int j = 0; j < TB; ++j) acc[i][j] = mfma16<TYPE>(fw[u][i], fx[u][j], acc[i][j]);
   }
-  for (; s < s1; ++s) {
+  if (s < whole) {  // fewer than U: all loads, then all products
+    v4i fw[U - 1][NB], fx[U - 1][TB];
+#pragma unroll
+    for (int u = 0; u < U - 1; ++u)
+      if (s + u < whole) {
+        const int64_t o = ((int64_t)(s + u) * 32 + c0) * 2;
+#pragma unroll
+        for (int i = 0; i < NB; ++i) fw[u][i] = load_whole(pw[i] + o);
+#pragma unroll
+        for (int j = 0; j < TB; ++j) fx[u][j] = load_whole(px[j] + o);
+      }
+#pragma unroll
+    for (int u = 0; u < U - 1; ++u)
+      if (s + u < whole) {
+#pragma unroll
+        for (int i = 0; i < NB; ++i)
+#pragma unroll
+          for (int j = 0; j < TB; ++j) acc[i][j] = mfma16<TYPE>(fw[u][i], fx[u][j], acc[i][j]);
+      }
+    s = whole;
+  }
+  if (s < s1) {  // the step that the depth's end cuts
     v4i fw[NB], fx[TB];
 #pragma unroll
     for (int i = 0; i < NB; ++i) fw[i] = load8(pw[i], s * 32 + c0, k);
