@@ -319,7 +319,7 @@ hipError_t tiles(const Adapter& p, hipStream_t s) {
     return run<Tile<TYPE, kAlong, kAlong, 2, 4, 2, 1, false, TYPE>>(p, s);
   }
   switch (tile_of(middle, ceil_div(p.rows, 256) * ceil_div(p.n, 256))) {
-    case kSmallTile: return run<Tile<TYPE, kAlong, kAlong, 2, 2, 1, 1, true, TYPE>>(p, s);
+    case kSmallTile: return run<Tile<TYPE, kAlong, kAlong, 2, 2, 1, 1, true, TYPE, 4>>(p, s);
     case kMiddleTile: return run<Tile<TYPE, kAlong, kAlong, 2, 2, 2, 2, true, TYPE>>(p, s);
     default: return run<Tile<TYPE, kAlong, kAlong, 2, 4, 4, 2, true, TYPE>>(p, s);
   }

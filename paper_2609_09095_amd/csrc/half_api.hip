@@ -67,7 +67,7 @@ int64_t pad16(int64_t x) { return (x + 15) / 16 * 16; }
 
 // Workspace of the orthogonalisation: offsets from its start.
 struct OrthRoom {
-  size_t squares, x32, x16[2], s16, p16, total;
+  size_t squares, x32, x16[2], s16, p16, d32, p32, total;
 };
 
 OrthRoom orth_room(int64_t count, int64_t m, int64_t n) {
@@ -85,6 +85,8 @@ OrthRoom orth_room(int64_t count, int64_t m, int64_t n) {
   r.x16[1] = take(each * 2);
   r.s16 = take(ss * 2);
   r.p16 = take(ss * 2);
+  r.d32 = take(s * count * 4);
+  r.p32 = take(s * count * 4);
   r.total = off;
   return r;
 }
@@ -219,6 +221,7 @@ ozaki25_status ozaki25_orthogonalise(int64_t count, int64_t m, int64_t n, const 
   o.x32 = (float*)(room.p + r.x32);
   o.x16[0] = room.p + r.x16[0], o.x16[1] = room.p + r.x16[1];
   o.s16 = room.p + r.s16, o.p16 = room.p + r.p16;
+  o.d32 = (float*)(room.p + r.d32), o.p32 = (float*)(room.p + r.p32);
   return room.give(status_of(oz::half::launch_orthogonalise(o, (int)type, steps, (hipStream_t)stream)));
 }
 

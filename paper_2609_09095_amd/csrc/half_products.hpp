@@ -70,15 +70,17 @@ struct Orthogonalise {
   double* squares;  // count x orthogonalise_parts
   float* x32;       // count x mp x np
   void* x16[2];     // the same
-  void* s16;        // count x s x s, s the shorter padded side
+  void* s16;        // count x s x s, s the shorter padded side; zero diagonal
   void* p16;        // the same
+  float* d32;       // count x s: the diagonal of S
+  float* p32;       // the same of P
   bool vec;         // 16-byte stores of x (set by the launch)
 };
 
 // Blocks (and partial sums) per matrix of the norm.
 inline int orthogonalise_parts(int64_t m, int64_t n) {
-  const int64_t p = (m * n + 16383) / 16384;
-  return (int)(p < 1 ? 1 : p > 128 ? 128 : p);
+  const int64_t p = m * ((n + 7) / 8) / 1024;
+  return (int)(p < 1 ? 1 : p > 256 ? 256 : p);
 }
 
 // Whether a matrix of `cols` columns can go to LDS by DMA: 16-byte rows, and a

@@ -25,7 +25,6 @@
 //          past the depth are sent outside it.
 //  masked: through registers with element bounds, for any pitch, size and
 //          2-byte alignment.
-// Two stages; a stage's loads are issued while the previous one is multiplied.
 #pragma once
 
 #include <hip/hip_runtime.h>
@@ -102,14 +101,15 @@ struct MaskedLoads;
 // A tile's shape: WR x WC wavefronts, each MB x NB blocks of 32 x 32 outputs.
 // OUT: the output type.  A 16-bit output's blocks are multiplied transposed
 // (WIDE), which gives a lane four consecutive columns of one row.
-template <int TYPE_, int LA_, int LB_, int WR_, int WC_, int MB_, int NB_, bool DMA_, int OUT_>
+// BUFS: stages in LDS.
+template <int TYPE_, int LA_, int LB_, int WR_, int WC_, int MB_, int NB_, bool DMA_, int OUT_, int BUFS_ = 2>
 struct Tile {
   static constexpr int TYPE = TYPE_, LA = LA_, LB = LB_, WR = WR_, WC = WC_, MB = MB_, NB = NB_, OUT = OUT_;
   static constexpr bool DMA = DMA_, WIDE = OUT_ != kF32;
   static constexpr int BM = WR * MB * 32, BN = WC * NB * 32;
   static constexpr int WAVES = WR * WC, THREADS = WAVES * 64;
   static constexpr int A_BYTES = BM * kDepth * 2, B_BYTES = BN * kDepth * 2;
-  static constexpr int STAGE = A_BYTES + B_BYTES, LDS = 2 * STAGE;
+  static constexpr int BUFS = BUFS_, STAGE = A_BYTES + B_BYTES, LDS = BUFS * STAGE;
   static constexpr int ADMA = A_BYTES / 1024 / WAVES, BDMA = B_BYTES / 1024 / WAVES;
   using Loads = std::conditional_t<DMA, DmaLoads<Tile>, MaskedLoads<Tile>>;
   static_assert(ADMA * WAVES * 1024 == A_BYTES && BDMA * WAVES * 1024 == B_BYTES, "whole slabs per wavefront");
@@ -129,11 +129,19 @@ __device__ __forceinline__ void chunk_at(int o, int& r, int& c) {
   }
 }
 
-// vmcnt(n) alone
+// At most N vector loads in flight, no LDS access.
 template <int N>
-__device__ __forceinline__ void wait_loads() {
+__device__ __forceinline__ void wait_loads_and_lds() {
   static_assert(N < 64);
-  __builtin_amdgcn_s_waitcnt((N & 15) | ((N >> 4) << 14) | (7 << 4) | (15 << 8));
+  __builtin_amdgcn_s_waitcnt((N & 15) | ((N >> 4) << 14));
+}
+
+// A barrier that waits for nothing but the other wavefronts; no memory access
+// moves over it.
+__device__ __forceinline__ void block_barrier() {
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
 }
 
 // ---- loaders ----------------------------------------------------------------
@@ -206,15 +214,19 @@ struct DmaLoads {
   __device__ __forceinline__ void early(int, int) {}
   __device__ __forceinline__ void prologue(char* lds, int wave, int lane) {
 #pragma unroll
-    for (int s = 0; s < 2; ++s) {
+    for (int s = 0; s < T::BUFS; ++s) {
       begin();
 #pragma unroll
       for (int j = 0; j < T::ADMA + T::BDMA; ++j) late(j, lds + s * T::STAGE, wave, lane);
       end();
     }
-    wait_loads<T::ADMA + T::BDMA>();
-    __syncthreads();
+    wait();
+    block_barrier();
   }
+  // the first stage's loads have landed, or (a stage's own were the oldest) the
+  // next one's; those of the stages behind it may be in flight
+  __device__ __forceinline__ void wait() { wait_loads_and_lds<(T::BUFS - 1) * (T::ADMA + T::BDMA)>(); }
+  __device__ __forceinline__ void wait_next() { wait_loads_and_lds<(T::BUFS - 2) * (T::ADMA + T::BDMA)>(); }
 };
 
 // The upper `have` (0 to 8) of 8 elements moved down, zeros above them.
@@ -318,13 +330,14 @@ struct MaskedLoads {
   __device__ __forceinline__ void end() {}
   __device__ __forceinline__ void prologue(char* lds, int wave, int lane) {
 #pragma unroll
-    for (int s = 0; s < 2; ++s) {
+    for (int s = 0; s < T::BUFS; ++s) {
       early(wave, lane);
 #pragma unroll
       for (int j = 0; j < T::ADMA + T::BDMA; ++j) late(j, lds + s * T::STAGE, wave, lane);
     }
     __syncthreads();
   }
+  __device__ __forceinline__ void wait_next() { wait_loads_and_lds<0>(); }
 };
 
 // Fragments of a wavefront's N blocks of 32 vectors from block w0 on.
@@ -366,6 +379,12 @@ struct Fragments {
   }
 };
 
+template <class T>
+__device__ __forceinline__ int next_buffer(int cur) {
+  if constexpr (T::BUFS == 2) return cur ^ T::STAGE;
+  return cur + T::STAGE < T::LDS ? cur + T::STAGE : 0;
+}
+
 // One stage's products; on entry the fragments of its first K step are in
 // af[0], bf[0].  cur, next: this stage's and the next one's buffer; freed: cur,
 // as the target of the loads.  The three are declared not to alias, or the
@@ -382,8 +401,8 @@ __device__ __forceinline__ void stage_products(Loader& ld, const FA& fa, const F
   for (int ks = 0; ks < KS; ++ks) {
     const bool last = ks + 1 == KS;
     if (last) {
-      __builtin_amdgcn_s_waitcnt(0);
-      __syncthreads();
+      ld.wait_next();
+      block_barrier();
       ld.begin();
     }
     __builtin_amdgcn_sched_barrier(0);
@@ -412,12 +431,13 @@ __device__ __forceinline__ void stage_products(Loader& ld, const FA& fa, const F
 
 // acc += A B over `depth`; lds: T::LDS bytes, 1024-aligned.
 //
-// Two stages in LDS.  The last K step's products of a stage run behind the
-// barrier that hands over to the next stage: their fragments are in registers
-// by then, so the matrix cores work while the next stage's first fragments
-// are read, and the buffer just freed takes the loads of the stage after
-// next, which then have a whole stage's products to arrive.  The order of
-// reads, loads and products is the written one (sched_barrier).
+// Two stages in LDS (four for small tiles).  The last K step's products of a
+// stage run behind the barrier that hands over to the next stage: their
+// fragments are in registers by then, so the matrix cores work while the next
+// stage's first fragments are read, and the buffer just freed takes the loads
+// of the stage that comes BUFS later, which then have BUFS - 1 stages' products
+// to arrive.  The order of reads, loads and products is the written one
+// (sched_barrier).
 //
 // Wavefronts whose rows all lie past the tile's edge load and wait like the
 // others, but multiply nothing (the matrix cores and the clock are theirs).
@@ -439,13 +459,13 @@ __device__ __forceinline__ void product(const Operand& a, const Operand& b, int 
     int cur = 0;
     for (int s = 0; s < nst; ++s) {
       ld.early(wave, lane);
-      __builtin_amdgcn_s_waitcnt(0);
-      __syncthreads();
+      ld.wait_next();
+      block_barrier();
       ld.begin();
 #pragma unroll
       for (int j = 0; j < ND; ++j) ld.late(j, lds + cur, wave, lane);
       ld.end();
-      cur ^= T::STAGE;
+      cur = next_buffer<T>(cur);
     }
   } else {
     Fragments<T::LA, T::BM, T::MB> fa;
@@ -460,8 +480,9 @@ __device__ __forceinline__ void product(const Operand& a, const Operand& b, int 
     for (int x = 0; x < T::NB; ++x) bf[0][x] = fb.read(l3 + T::A_BYTES, 0, x);
     int cur = 0;
     for (int s = 0; s < nst; ++s) {
-      stage_products<T>(ld, fa, fb, l3 + cur, l3 + (cur ^ T::STAGE), lds + cur, wave, lane, af, bf, acc);
-      cur ^= T::STAGE;
+      const int next = next_buffer<T>(cur);
+      stage_products<T>(ld, fa, fb, l3 + cur, l3 + next, lds + cur, wave, lane, af, bf, acc);
+      cur = next;
     }
   }
   __builtin_amdgcn_s_waitcnt(0);  // the look-ahead past the end (zeros) lands before LDS is used again

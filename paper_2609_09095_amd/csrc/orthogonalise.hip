@@ -14,6 +14,12 @@
 // in half's range, and its 11 bits round eight times finer than the bfloat16
 // of the result.  Stored as X 2^8, S 2^10, P 2^8.
 //
+// S and P come close to multiples of the identity, and a rounding of their
+// diagonals would be an error of every vector: the diagonals d and p are kept
+// in 32 bits beside the matrices, whose own diagonals are stored as zeros, and
+//   (S^2)_ij = (So^2)_ij + (d_i + d_j) So_ij,  (S^2)_ii = (So^2)_ii + d_i^2,
+//   (P X)_ij = (Po X)_ij + p_i X_ij.
+//
 // Matrices are padded with zero rows and columns to multiples of 8 (zeros stay
 // zeros through every step), so all loads are DMA.
 #include "half_products.hpp"
@@ -24,24 +30,33 @@ namespace {
 
 constexpr float kScaleX = 256.0f, kScaleS = 1024.0f, kScaleP = 256.0f;
 
+// Elements c .. c + 7 of a row of n; zeros past its end.
 template <int TYPE>
-__device__ __forceinline__ float to_float(const void* p, int64_t i) {
-  using E = typename Out<TYPE>::type;
-  return (float)((const E*)p)[i];
+__device__ __forceinline__ void row8(const void* g, int64_t row, int c, int n, float (&x)[8]) {
+  if constexpr (TYPE == kF32) {
+    const auto q = (const __attribute__((address_space(1))) float*)(global_bytes)g + row + c;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) x[j] = c + j < n ? q[j] : 0.0f;
+  } else {
+    typedef typename Out<TYPE>::type v8 __attribute__((ext_vector_type(8)));
+    const v8 v = __builtin_bit_cast(v8, load8((const char*)g + row * 2, c, n));
+#pragma unroll
+    for (int j = 0; j < 8; ++j) x[j] = (float)v[j];
+  }
 }
 
 // Sums of squares of a matrix, one per block, in 64 bits: no overflow or
-// underflow for any 32-bit input.  grid (blocks, count)
+// underflow for any 32-bit input.  grid (parts, count)
 template <int TYPE>
 __global__ __launch_bounds__(256) void squares_kernel(Orthogonalise o) {
-  const int64_t total = (int64_t)o.m * o.n;
-  const int64_t per = (total + gridDim.x - 1) / gridDim.x;
-  const int64_t end = per * (blockIdx.x + 1) < total ? per * (blockIdx.x + 1) : total;
+  const uint32_t chunks = (uint32_t)o.np / 8, total = chunks * (uint32_t)o.m;
   double sum = 0;
-  for (int64_t i = per * blockIdx.x + threadIdx.x; i < end; i += 256) {
-    const int64_t r = i / o.n, c = i - r * o.n;
-    const double x = to_float<TYPE>(o.g, blockIdx.y * o.g_stride + r * o.ldg + c);
-    sum += x * x;
+  for (uint32_t i = blockIdx.x * 256 + threadIdx.x; i < total; i += gridDim.x * 256) {
+    const uint32_t r = i / chunks, c = (i - r * chunks) * 8;
+    float x[8];
+    row8<TYPE>(o.g, blockIdx.y * o.g_stride + r * o.ldg, c, o.n, x);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) sum += (double)x[j] * (double)x[j];
   }
   __shared__ double part[4];
   for (int d = 32; d; d >>= 1) sum += __shfl_xor(sum, d);
@@ -54,15 +69,24 @@ __global__ __launch_bounds__(256) void squares_kernel(Orthogonalise o) {
 template <int TYPE>
 __global__ __launch_bounds__(256) void start_kernel(Orthogonalise o, int parts) {
   double sum = 0;
-  for (int i = 0; i < parts; ++i) sum += o.squares[blockIdx.y * parts + i];
+  for (int i = threadIdx.x & 63; i < parts; i += 64) sum += o.squares[blockIdx.y * parts + i];
+  for (int d = 32; d; d >>= 1) sum += __shfl_xor(sum, d);
   const float scale = (float)(1.0 / (sqrt(sum) + (double)o.eps));
-  const int64_t total = (int64_t)o.mp * o.np;
-  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < total; i += (int64_t)gridDim.x * 256) {
-    const int64_t r = i / o.np, c = i - r * o.np;
-    float x = 0.0f;
-    if (r < o.m && c < o.n) x = to_float<TYPE>(o.g, blockIdx.y * o.g_stride + r * o.ldg + c) * scale;
-    o.x32[blockIdx.y * total + i] = x;
-    ((_Float16*)o.x16[0])[blockIdx.y * total + i] = (_Float16)(x * kScaleX);
+  const uint32_t chunks = (uint32_t)o.np / 8, total = chunks * (uint32_t)o.mp;
+  const int64_t each = (int64_t)o.mp * o.np;
+  for (uint32_t i = blockIdx.x * 256 + threadIdx.x; i < total; i += gridDim.x * 256) {
+    const uint32_t r = i / chunks, c = (i - r * chunks) * 8;
+    float x[8] = {};
+    if ((int)r < o.m) row8<TYPE>(o.g, blockIdx.y * o.g_stride + r * o.ldg, c, o.n, x);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) x[j] = (int)(c + j) < o.n && (int)r < o.m ? x[j] * scale : 0.0f;
+    float4* const p = (float4*)(o.x32 + blockIdx.y * each + (int64_t)i * 8);
+    p[0] = float4{x[0], x[1], x[2], x[3]};
+    p[1] = float4{x[4], x[5], x[6], x[7]};
+#pragma unroll
+    for (int j = 0; j < 8; ++j) x[j] *= kScaleX;
+    const uint2 lo = pack4<kF16>(x[0], x[1], x[2], x[3]), hi = pack4<kF16>(x[4], x[5], x[6], x[7]);
+    *(uint4*)((_Float16*)o.x16[0] + blockIdx.y * each + (int64_t)i * 8) = uint4{lo.x, lo.y, hi.x, hi.y};
   }
 }
 
@@ -76,153 +100,263 @@ __device__ __forceinline__ void triangle_tile(uint32_t t, uint32_t& tm, uint32_t
   tm = t - c * (c + 1) / 2;
 }
 
-// A symmetric product C = A A^T (kAlong, A s x depth) or A^T A (kAcross, A
-// depth x s), the tiles on and above the diagonal, each stored twice.  With
-// SQUARE, A = S and P = b S + c S^2 is stored.  grid (tiles, count)
+// The wavefront's place in a WIDE tile: a lane holds, of block (a, b), row
+// row0 + 32 a and the columns col0 + 32 b + 8 q .. + 3.
+template <class T>
+struct WidePlace {
+  int row0, col0;
+  __device__ __forceinline__ WidePlace() {
+    const int lane = threadIdx.x & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    row0 = wave / T::WC * T::MB * 32 + (lane & 31);
+    col0 = wave % T::WC * T::NB * 32 + 4 * (lane >> 5);
+  }
+};
+
+// A symmetric product A A^T (kAlong, A s x depth) or A^T A (kAcross, A
+// depth x s), the tiles on and above the diagonal, each stored twice: S, or with
+// SQUARE (A = So) P = b S + c S^2, their diagonals apart.  grid (tiles, count)
 template <class T, bool SQUARE>
-__global__ __launch_bounds__(T::THREADS, 1) void gram_kernel(Orthogonalise o, const char* in, char* out, int s,
-                                                            int depth, int64_t ld, float c) {
+__global__ __launch_bounds__(T::THREADS, 1) void gram_kernel(Orthogonalise o, const char* in, int s, int depth,
+                                                            int64_t ld, uint32_t first) {
   __shared__ __attribute__((aligned(1024))) char lds[T::LDS];
-  static_assert(T::BM == T::BN && T::LA == T::LB, "square tiles");
+  static_assert(T::BM == T::BN && T::LA == T::LB && T::OUT == kF16, "square tiles");
   uint32_t tm, tn;
-  triangle_tile(blockIdx.x, tm, tn);
+  triangle_tile(first + blockIdx.x, tm, tn);
   const int r0 = (int)tm * T::BM, c0 = (int)tn * T::BN;
   const int rows = s - r0 < T::BM ? s - r0 : T::BM, cols = s - c0 < T::BN ? s - c0 : T::BN;
-  const char* a = in + blockIdx.y * ((int64_t)o.mp * o.np * 2);
-  if constexpr (SQUARE) a = in + blockIdx.y * ((int64_t)s * s * 2);
+  const int64_t square = (int64_t)s * s;
+  const char* const a = in + blockIdx.y * (SQUARE ? square : (int64_t)o.mp * o.np) * 2;
+  _Float16* const out = (_Float16*)(SQUARE ? o.p16 : o.s16) + blockIdx.y * square + (int64_t)r0 * s + c0;
+  const float* const d = o.d32 + (int64_t)blockIdx.y * s;
+  float* const diagonal = (SQUARE ? o.p32 : o.d32) + (int64_t)blockIdx.y * s;
   const int64_t step = T::LA == kAlong ? ld : 1;
   v16f acc[T::MB][T::NB] = {};
-  product<T>(Operand{a + r0 * step * 2, ld, rows, (int)ld}, Operand{a + c0 * step * 2, ld, cols, (int)ld}, depth, lds, acc);
-  char* const o16 = out + blockIdx.y * ((int64_t)s * s * 2);
-  const _Float16* const S = (const _Float16*)a;
-  store_wide<T>(acc, lds, o16 + ((int64_t)r0 * s + c0) * 2, s, rows, cols, true, [&](int r, int q, float* v) {
-    if constexpr (SQUARE) {
-      const bool in = r < rows && q < cols;
+  product<T>(Operand{a + r0 * step * 2, ld, rows, (int)ld}, Operand{a + c0 * step * 2, ld, cols, (int)ld}, depth, lds,
+             acc);
+  const WidePlace<T> w;
+  if constexpr (SQUARE) {
+    // loads from clamped places and no branch, so that they are all in flight
+    const _Float16* const S = (const _Float16*)a + (int64_t)r0 * s + c0;
+    const float ks = kScaleP / kScaleS, kc = o.c * kScaleP / (kScaleS * kScaleS);
+    float4 dc[T::NB][4];
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const float x = in ? (float)S[(int64_t)(r0 + r) * s + c0 + q + j] : 0.0f;
-        v[j] = v[j] * c + x * (o.b * kScaleP / kScaleS);
+    for (int b = 0; b < T::NB; ++b)
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const int c = w.col0 + 32 * b + 8 * q;
+        dc[b][q] = *(const float4*)(d + c0 + (c < cols ? c : 0));
       }
-    } else {
 #pragma unroll
-      for (int j = 0; j < 4; ++j) v[j] *= c;
+    for (int x = 0; x < T::MB; ++x) {
+      const int r = w.row0 + 32 * x < rows ? w.row0 + 32 * x : rows - 1;
+      const float di = d[r0 + r];
+      uint2 v[T::NB][4];
+#pragma unroll
+      for (int b = 0; b < T::NB; ++b)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          const int c = w.col0 + 32 * b + 8 * q;
+          v[b][q] = *(const uint2*)(S + (int64_t)r * s + (c < cols ? c : 0));
+        }
+#pragma unroll
+      for (int b = 0; b < T::NB; ++b)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          typedef _Float16 h4 __attribute__((ext_vector_type(4)));
+          const h4 e = __builtin_bit_cast(h4, v[b][q]);
+          const float dj[4] = {dc[b][q].x, dc[b][q].y, dc[b][q].z, dc[b][q].w};
+#pragma unroll
+          for (int j = 0; j < 4; ++j)
+            acc[x][b][4 * q + j] = kc * acc[x][b][4 * q + j] + (o.b + o.c * (di + dj[j])) * ks * (float)e[j];
+        }
     }
-  });
+  } else {
+#pragma unroll
+    for (int x = 0; x < T::MB; ++x)
+#pragma unroll
+      for (int b = 0; b < T::NB; ++b) acc[x][b] *= kScaleS / (kScaleX * kScaleX);
+  }
+  if (tm == tn) {
+#pragma unroll
+    for (int x = 0; x < T::MB; ++x)
+#pragma unroll
+      for (int b = 0; b < T::NB; ++b)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          const int r = w.row0 + 32 * x;
+          if (r != w.col0 + 32 * b + 8 * (i >> 2) + (i & 3)) continue;
+          if (r < rows) {
+            // acc: S_ii 2^10, or c (So^2)_ii 2^8 (So_ii is zero)
+            if constexpr (SQUARE) {
+              const float di = d[r0 + r];
+              diagonal[r0 + r] = (o.b + o.c * di) * di + acc[x][b][i] * (1.0f / kScaleP);
+            } else {
+              diagonal[r0 + r] = acc[x][b][i] * (1.0f / kScaleS);
+            }
+          }
+          acc[x][b][i] = 0.0f;
+        }
+  }
+  store_wide<T>(acc, lds, out, s, rows, cols, true, [](int, int, float*) {});
   if (tm == tn) return;
-  // the mirror image: the wavefront's blocks transposed, 32 rows at a time
-  const int lane = threadIdx.x & 63;
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int wr = wave / T::WC * T::MB * 32, wc = wave % T::WC * T::NB * 32;
-  _Float16* const m16 = (_Float16*)o16 + (int64_t)(c0 + wc) * s + r0 + wr;
+  // the mirror image: a half wavefront has 32 consecutive rows of one column
+  _Float16* const mirror = (_Float16*)(SQUARE ? o.p16 : o.s16) + blockIdx.y * square + (int64_t)c0 * s + r0;
 #pragma unroll
   for (int x = 0; x < T::MB; ++x)
 #pragma unroll
-    for (int y = 0; y < T::NB; ++y)
+    for (int b = 0; b < T::NB; ++b)
 #pragma unroll
       for (int i = 0; i < 16; ++i) {
-        const int r = x * 32 + (lane & 31), q = y * 32 + 8 * (i >> 2) + 4 * (lane >> 5) + (i & 3);
-        if (wr + r < rows && wc + q < cols) {
-          float v = acc[x][y][i] * c;
-          if constexpr (SQUARE) v += (float)S[(int64_t)(r0 + wr + r) * s + c0 + wc + q] * (o.b * kScaleP / kScaleS);
-          m16[(int64_t)q * s + r] = (_Float16)v;
-        }
+        const int r = w.row0 + 32 * x, c = w.col0 + 32 * b + 8 * (i >> 2) + (i & 3);
+        if (r < rows && c < cols) mirror[(int64_t)c * s + r] = (_Float16)acc[x][b][i];
       }
 }
 
-// X <- a X + P X (WIDE_ matrices, kAlong x kAcross) or a X + X P (kAlong x
-// kAlong: P is symmetric).  LAST: the result to the caller's matrix.
-// grid (tiles, count)
+// X <- a X + P X (kAlong x kAcross) or, TALL, a X + X P (kAlong x kAlong: P is
+// symmetric).  LAST: the result to the caller's matrix.  grid (tiles, count)
 template <class T, bool TALL, bool LAST>
 __global__ __launch_bounds__(T::THREADS, 1) void update_kernel(Orthogonalise o, const char* x16, char* next) {
   __shared__ __attribute__((aligned(1024))) char lds[T::LDS];
   const int s = TALL ? o.np : o.mp;
-  const uint32_t tiles_n = ((uint32_t)o.np + T::BN - 1) / T::BN;
-  const int r0 = (int)(blockIdx.x / tiles_n) * T::BM, c0 = (int)(blockIdx.x % tiles_n) * T::BN;
+  const uint32_t tiles_n = ((uint32_t)o.np + T::BN - 1) / T::BN, tiles_m = ((uint32_t)o.mp + T::BM - 1) / T::BM;
+  uint32_t place, tm, tn;
+  if (!block_place(blockIdx.x, tiles_m * tiles_n, place)) return;
+  place_to_tile(place, tiles_m, tiles_n, tm, tn);
+  const int r0 = (int)tm * T::BM, c0 = (int)tn * T::BN;
   const int rows = o.mp - r0 < T::BM ? o.mp - r0 : T::BM, cols = o.np - c0 < T::BN ? o.np - c0 : T::BN;
   const int64_t each = (int64_t)o.mp * o.np;
   const char* const X = x16 + blockIdx.y * each * 2;
   const char* const P = (const char*)o.p16 + blockIdx.y * ((int64_t)s * s * 2);
+  const float* const p = o.p32 + (int64_t)blockIdx.y * s;
   v16f acc[T::MB][T::NB] = {};
   if constexpr (TALL)
-    product<T>(Operand{X + (int64_t)r0 * o.np * 2, o.np, rows, o.np}, Operand{P + (int64_t)c0 * s * 2, s, cols, s}, s, lds, acc);
+    product<T>(Operand{X + (int64_t)r0 * o.np * 2, o.np, rows, o.np}, Operand{P + (int64_t)c0 * s * 2, s, cols, s}, s,
+               lds, acc);
   else
-    product<T>(Operand{P + (int64_t)r0 * s * 2, s, rows, s}, Operand{X + (int64_t)c0 * 2, o.np, cols, o.np}, s, lds, acc);
+    product<T>(Operand{P + (int64_t)r0 * s * 2, s, rows, s}, Operand{X + (int64_t)c0 * 2, o.np, cols, o.np}, s, lds,
+               acc);
   float* const x32 = o.x32 + blockIdx.y * each + (int64_t)r0 * o.np + c0;
-  auto value = [&](int r, int q, float* v) {
-    if (r < rows && q < cols) {
-      float4* const p = (float4*)(x32 + (int64_t)r * o.np + q);
-      const float4 x = *p;
-      const float k = 1.0f / (kScaleX * kScaleP);
-      v[0] = o.a * x.x + k * v[0];
-      v[1] = o.a * x.y + k * v[1];
-      v[2] = o.a * x.z + k * v[2];
-      v[3] = o.a * x.w + k * v[3];
-      if constexpr (!LAST) {
-        *p = float4{v[0], v[1], v[2], v[3]};
+  const WidePlace<T> w;
+  const float k = 1.0f / (kScaleX * kScaleP);
 #pragma unroll
-        for (int j = 0; j < 4; ++j) v[j] *= kScaleX;
+  for (int x = 0; x < T::MB; ++x) {
+    const int r = w.row0 + 32 * x < rows ? w.row0 + 32 * x : rows - 1;
+    const float pi = TALL ? 0.0f : p[r0 + r];
+    float4 v[T::NB][4], pj[T::NB][4];
+#pragma unroll
+    for (int b = 0; b < T::NB; ++b)
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const int c = w.col0 + 32 * b + 8 * q < cols ? w.col0 + 32 * b + 8 * q : 0;
+        v[b][q] = *(const float4*)(x32 + (int64_t)r * o.np + c);
+        pj[b][q] = TALL ? *(const float4*)(p + c0 + c) : float4{pi, pi, pi, pi};
       }
-    }
-  };
+#pragma unroll
+    for (int b = 0; b < T::NB; ++b)
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        float4 y;
+        y.x = (o.a + pj[b][q].x) * v[b][q].x + k * acc[x][b][4 * q];
+        y.y = (o.a + pj[b][q].y) * v[b][q].y + k * acc[x][b][4 * q + 1];
+        y.z = (o.a + pj[b][q].z) * v[b][q].z + k * acc[x][b][4 * q + 2];
+        y.w = (o.a + pj[b][q].w) * v[b][q].w + k * acc[x][b][4 * q + 3];
+        const int c = w.col0 + 32 * b + 8 * q;
+        if constexpr (!LAST)
+          if (w.row0 + 32 * x < rows && c < cols) *(float4*)(x32 + (int64_t)r * o.np + c) = y;
+        const float scale = LAST ? 1.0f : kScaleX;
+        acc[x][b][4 * q] = y.x * scale;
+        acc[x][b][4 * q + 1] = y.y * scale;
+        acc[x][b][4 * q + 2] = y.z * scale;
+        acc[x][b][4 * q + 3] = y.w * scale;
+      }
+  }
+  auto as_is = [](int, int, float*) {};
   if constexpr (LAST)
     store_wide<T>(acc, lds, (char*)o.x + (blockIdx.y * o.x_stride + r0 * o.ldx + c0) * 2, o.ldx, o.m - r0, o.n - c0,
-                  o.vec, value);
+                  o.vec, as_is);
   else
-    store_wide<T>(acc, lds, next + (blockIdx.y * each + (int64_t)r0 * o.np + c0) * 2, o.np, rows, cols, true, value);
+    store_wide<T>(acc, lds, next + (blockIdx.y * each + (int64_t)r0 * o.np + c0) * 2, o.np, rows, cols, true, as_is);
 }
 
 template <int TYPE>
 hipError_t start(const Orthogonalise& o, hipStream_t s) {
-  const int64_t total = (int64_t)o.mp * o.np;
   const int parts = orthogonalise_parts(o.m, o.n);
   squares_kernel<TYPE><<<dim3(parts, o.count), dim3(256), 0, s>>>(o);
-  const int blocks = (int)((total + 2047) / 2048 < 4096 ? (total + 2047) / 2048 : 4096);
-  start_kernel<TYPE><<<dim3(blocks, o.count), dim3(256), 0, s>>>(o, parts);
+  const int64_t chunks = (int64_t)o.mp * o.np / 8, blocks = ceil_div(chunks, 256);
+  start_kernel<TYPE><<<dim3((uint32_t)(blocks < 2048 ? blocks : 2048), o.count), dim3(256), 0, s>>>(o, parts);
   return hipGetLastError();
 }
 
-template <int WR, int WC, int MB, int NB>
-hipError_t steps(const Orthogonalise& o, int steps, hipStream_t s) {
-  const bool tall = o.m > o.n;
-  const int sh = tall ? o.np : o.mp, lo = tall ? o.mp : o.np;
-  using G0 = Tile<kF16, kAlong, kAlong, WR, WC, MB, NB, true, kF16>;
-  using G1 = Tile<kF16, kAcross, kAcross, WR, WC, MB, NB, true, kF16>;
-  const uint32_t t = (uint32_t)((sh + G0::BM - 1) / G0::BM);
-  const dim3 tri(t * (t + 1) / 2, o.count), block(G0::THREADS);
-  const dim3 all((uint32_t)((o.mp + G0::BM - 1) / G0::BM) * (uint32_t)((o.np + G0::BN - 1) / G0::BN), o.count);
-  for (int i = 0; i < steps; ++i) {
+// tile shapes: WR, WC, MB, NB, stages
+template <int WR, int WC, int MB, int NB, int BUFS>
+struct Shape {
+  template <int LA, int LB, int OUT>
+  using Of = Tile<kF16, LA, LB, WR, WC, MB, NB, true, OUT, BUFS>;
+};
+using Large = Shape<2, 4, 4, 2, 2>;
+using Middle = Shape<2, 2, 2, 2, 2>;
+using Small = Shape<2, 2, 1, 1, 4>;
+
+template <class H, int L, bool SQUARE>
+void gram(const Orthogonalise& o, const char* in, int s, int depth, int64_t ld, hipStream_t st) {
+  using T = typename H::template Of<L, L, kF16>;
+  const uint32_t t = (uint32_t)ceil_div(s, T::BM);
+  gram_kernel<T, SQUARE><<<dim3(t * (t + 1) / 2, o.count), dim3(T::THREADS), 0, st>>>(o, in, s, depth, ld, 0u);
+}
+
+template <int L, bool SQUARE>
+void gram(const Orthogonalise& o, const char* in, int s, int depth, int64_t ld, hipStream_t st) {
+  auto tiles = [&](int64_t b) { return o.count * ceil_div(s, b) * (ceil_div(s, b) + 1) / 2; };
+  switch (tile_of(tiles(128), tiles(256))) {
+    case kSmallTile: return gram<Small, L, SQUARE>(o, in, s, depth, ld, st);
+    case kMiddleTile: return gram<Middle, L, SQUARE>(o, in, s, depth, ld, st);
+    default: return gram<Large, L, SQUARE>(o, in, s, depth, ld, st);
+  }
+}
+
+template <class H, bool TALL, bool LAST>
+void update(const Orthogonalise& o, const char* x, char* next, hipStream_t st) {
+  using T = typename H::template Of<kAlong, TALL ? kAlong : kAcross, LAST ? kBF16 : kF16>;
+  const int64_t tiles = ceil_div(o.mp, T::BM) * ceil_div(o.np, T::BN);
+  update_kernel<T, TALL, LAST><<<dim3((uint32_t)((tiles + 7) & ~(int64_t)7), o.count), dim3(T::THREADS), 0, st>>>(o, x, next);
+}
+
+template <bool TALL, bool LAST>
+void update(const Orthogonalise& o, const char* x, char* next, hipStream_t st) {
+  auto tiles = [&](int64_t b) { return o.count * ceil_div(o.mp, b) * ceil_div(o.np, b); };
+  switch (tile_of(tiles(128), tiles(256))) {
+    case kSmallTile: return update<Small, TALL, LAST>(o, x, next, st);
+    case kMiddleTile: return update<Middle, TALL, LAST>(o, x, next, st);
+    default: return update<Large, TALL, LAST>(o, x, next, st);
+  }
+}
+
+template <bool TALL>
+hipError_t steps(const Orthogonalise& o, int count, hipStream_t st) {
+  const int s = TALL ? o.np : o.mp, l = TALL ? o.mp : o.np;
+  for (int i = 0; i < count; ++i) {
     const char* x = (const char*)o.x16[i & 1];
     char* next = (char*)o.x16[(i + 1) & 1];
-    const float cs = kScaleS / (kScaleX * kScaleX), cp = o.c * kScaleP / (kScaleS * kScaleS);
-    if (tall)
-      gram_kernel<G1, false><<<tri, block, 0, s>>>(o, x, (char*)o.s16, sh, lo, o.np, cs);
+    gram<TALL ? kAcross : kAlong, false>(o, x, s, l, o.np, st);
+    gram<kAlong, true>(o, (const char*)o.s16, s, s, s, st);
+    if (i + 1 < count)
+      update<TALL, false>(o, x, next, st);
     else
-      gram_kernel<G0, false><<<tri, block, 0, s>>>(o, x, (char*)o.s16, sh, lo, o.np, cs);
-    gram_kernel<G0, true><<<tri, block, 0, s>>>(o, (const char*)o.s16, (char*)o.p16, sh, sh, sh, cp);
-    const bool last = i + 1 == steps;
-    using U0 = Tile<kF16, kAlong, kAcross, WR, WC, MB, NB, true, kF16>;
-    using L0 = Tile<kF16, kAlong, kAcross, WR, WC, MB, NB, true, kBF16>;
-    using L1 = Tile<kF16, kAlong, kAlong, WR, WC, MB, NB, true, kBF16>;
-    if (tall && last)
-      update_kernel<L1, true, true><<<all, block, 0, s>>>(o, x, next);
-    else if (tall)
-      update_kernel<G0, true, false><<<all, block, 0, s>>>(o, x, next);
-    else if (last)
-      update_kernel<L0, false, true><<<all, block, 0, s>>>(o, x, next);
-    else
-      update_kernel<U0, false, false><<<all, block, 0, s>>>(o, x, next);
+      update<TALL, true>(o, x, next, st);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
   }
-  return hipGetLastError();
+  return hipSuccess;
 }
 
 }  // namespace
 
 hipError_t launch_orthogonalise(Orthogonalise o, int type, int count_steps, hipStream_t s) {
   o.vec = (uintptr_t)o.x % 16 == 0 && o.ldx % 8 == 0 && o.x_stride % 8 == 0 && o.n % 8 == 0;
-  hipError_t e = type == kBF16 ? start<kBF16>(o, s) : type == kF16 ? start<kF16>(o, s) : start<kF32>(o, s);
+  const hipError_t e = type == kBF16 ? start<kBF16>(o, s) : type == kF16 ? start<kF16>(o, s) : start<kF32>(o, s);
   if (e != hipSuccess) return e;
-  const int64_t big = (int64_t)((o.mp + 255) / 256) * ((o.np + 255) / 256) * o.count;
-  return big >= 256 ? steps<2, 4, 4, 2>(o, count_steps, s) : steps<2, 2, 2, 2>(o, count_steps, s);
+  return o.m > o.n ? steps<true>(o, count_steps, s) : steps<false>(o, count_steps, s);
 }
 
 }  // namespace half
