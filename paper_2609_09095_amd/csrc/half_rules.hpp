@@ -43,6 +43,14 @@ constexpr TileSize tile_of(int64_t middle, int64_t large) {
   return middle <= 256 ? kSmallTile : large_or_middle(large, middle);
 }
 
+// Large tiles beyond whole rounds that are worth a launch of their own in small
+// tiles (16 each): few, so that they fill no more than a round and a half of
+// those; 0: none.  2 x 4096 x 4096, a symmetric product's 272 tiles: OVER
+constexpr int64_t large_tiles_over(int64_t large) {
+  const int64_t over = large % 256;
+  return large > 256 && over <= 48 ? over : 0;
+}
+
 // A grouped product by rows.
 constexpr TileSize rows_tile(int64_t rows, int64_t groups, int64_t cols) {
   return tile_of(expected_row_tiles(rows, groups, 128) * ceil_div(cols, 128),

@@ -115,29 +115,55 @@ struct WidePlace {
 
 // A symmetric product A A^T (kAlong, A s x depth) or A^T A (kAcross, A
 // depth x s), the tiles on and above the diagonal, each stored twice: S, or with
-// SQUARE (A = So) P = b S + c S^2, their diagonals apart.  grid (tiles, count)
+// SQUARE (A = So) P = b S + c S^2, their diagonals apart.  Block b takes the
+// (b / sub^2)-th tile from `first` on, of the matrices' triangles of tiles one
+// after the other, or its b % sub^2-th part where tiles of sub^2 times this size
+// are meant.
 template <class T, bool SQUARE>
 __global__ __launch_bounds__(T::THREADS, 1) void gram_kernel(Orthogonalise o, const char* in, int s, int depth,
-                                                            int64_t ld, uint32_t first) {
+                                                            int64_t ld, uint32_t first, uint32_t sub) {
   __shared__ __attribute__((aligned(1024))) char lds[T::LDS];
   static_assert(T::BM == T::BN && T::LA == T::LB && T::OUT == kF16, "square tiles");
+  const uint32_t side = ((uint32_t)s + T::BM * sub - 1) / (T::BM * sub), triangle = side * (side + 1) / 2;
+  const uint32_t tile = first + blockIdx.x / (sub * sub), part = blockIdx.x % (sub * sub);
+  const uint32_t z = tile / triangle;
   uint32_t tm, tn;
-  triangle_tile(first + blockIdx.x, tm, tn);
+  triangle_tile(tile - z * triangle, tm, tn);
+  tm = tm * sub + part / sub;
+  tn = tn * sub + part % sub;
   const int r0 = (int)tm * T::BM, c0 = (int)tn * T::BN;
+  if (tm > tn || c0 >= s) return;  // parts below the diagonal or past the edge
   const int rows = s - r0 < T::BM ? s - r0 : T::BM, cols = s - c0 < T::BN ? s - c0 : T::BN;
   const int64_t square = (int64_t)s * s;
-  const char* const a = in + blockIdx.y * (SQUARE ? square : (int64_t)o.mp * o.np) * 2;
-  _Float16* const out = (_Float16*)(SQUARE ? o.p16 : o.s16) + blockIdx.y * square + (int64_t)r0 * s + c0;
-  const float* const d = o.d32 + (int64_t)blockIdx.y * s;
-  float* const diagonal = (SQUARE ? o.p32 : o.d32) + (int64_t)blockIdx.y * s;
+  const char* const a = in + z * (SQUARE ? square : (int64_t)o.mp * o.np) * 2;
+  _Float16* const out = (_Float16*)(SQUARE ? o.p16 : o.s16) + z * square + (int64_t)r0 * s + c0;
+  const float* const d = o.d32 + (int64_t)z * s;
+  float* const diagonal = (SQUARE ? o.p32 : o.d32) + (int64_t)z * s;
   const int64_t step = T::LA == kAlong ? ld : 1;
+  const WidePlace<T> w;
+  // So of the tile's own outputs, from clamped places and without a branch, so
+  // that all loads are in flight; before the product where registers allow
+  constexpr bool EARLY = T::MB * T::NB <= 4;
+  const _Float16* const S = (const _Float16*)a + (int64_t)r0 * s + c0;
+  uint2 own[EARLY ? T::MB : 1][T::NB][4];
+  auto load_own = [&](int x, uint2 (&v)[T::NB][4]) __attribute__((always_inline)) {
+    const int r = w.row0 + 32 * x < rows ? w.row0 + 32 * x : rows - 1;
+#pragma unroll
+    for (int b = 0; b < T::NB; ++b)
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const int c = w.col0 + 32 * b + 8 * q;
+        v[b][q] = *(const uint2*)(S + (int64_t)r * s + (c < cols ? c : 0));
+      }
+  };
+  if constexpr (SQUARE && EARLY) {
+#pragma unroll
+    for (int x = 0; x < T::MB; ++x) load_own(x, own[x]);
+  }
   v16f acc[T::MB][T::NB] = {};
   product<T>(Operand{a + r0 * step * 2, ld, rows, (int)ld}, Operand{a + c0 * step * 2, ld, cols, (int)ld}, depth, lds,
              acc);
-  const WidePlace<T> w;
   if constexpr (SQUARE) {
-    // loads from clamped places and no branch, so that they are all in flight
-    const _Float16* const S = (const _Float16*)a + (int64_t)r0 * s + c0;
     const float ks = kScaleP / kScaleS, kc = o.c * kScaleP / (kScaleS * kScaleS);
     float4 dc[T::NB][4];
 #pragma unroll
@@ -149,22 +175,14 @@ __global__ __launch_bounds__(T::THREADS, 1) void gram_kernel(Orthogonalise o, co
       }
 #pragma unroll
     for (int x = 0; x < T::MB; ++x) {
-      const int r = w.row0 + 32 * x < rows ? w.row0 + 32 * x : rows - 1;
-      const float di = d[r0 + r];
-      uint2 v[T::NB][4];
-#pragma unroll
-      for (int b = 0; b < T::NB; ++b)
-#pragma unroll
-        for (int q = 0; q < 4; ++q) {
-          const int c = w.col0 + 32 * b + 8 * q;
-          v[b][q] = *(const uint2*)(S + (int64_t)r * s + (c < cols ? c : 0));
-        }
+      const float di = d[r0 + (w.row0 + 32 * x < rows ? w.row0 + 32 * x : rows - 1)];
+      if constexpr (!EARLY) load_own(x, own[0]);
 #pragma unroll
       for (int b = 0; b < T::NB; ++b)
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
           typedef _Float16 h4 __attribute__((ext_vector_type(4)));
-          const h4 e = __builtin_bit_cast(h4, v[b][q]);
+          const h4 e = __builtin_bit_cast(h4, own[EARLY ? x : 0][b][q]);
           const float dj[4] = {dc[b][q].x, dc[b][q].y, dc[b][q].z, dc[b][q].w};
 #pragma unroll
           for (int j = 0; j < 4; ++j)
@@ -201,7 +219,7 @@ __global__ __launch_bounds__(T::THREADS, 1) void gram_kernel(Orthogonalise o, co
   store_wide<T>(acc, lds, out, s, rows, cols, true, [](int, int, float*) {});
   if (tm == tn) return;
   // the mirror image: a half wavefront has 32 consecutive rows of one column
-  _Float16* const mirror = (_Float16*)(SQUARE ? o.p16 : o.s16) + blockIdx.y * square + (int64_t)c0 * s + r0;
+  _Float16* const mirror = (_Float16*)(SQUARE ? o.p16 : o.s16) + z * square + (int64_t)c0 * s + r0;
 #pragma unroll
   for (int x = 0; x < T::MB; ++x)
 #pragma unroll
@@ -229,6 +247,24 @@ __global__ __launch_bounds__(T::THREADS, 1) void update_kernel(Orthogonalise o, 
   const char* const X = x16 + blockIdx.y * each * 2;
   const char* const P = (const char*)o.p16 + blockIdx.y * ((int64_t)s * s * 2);
   const float* const p = o.p32 + (int64_t)blockIdx.y * s;
+  float* const x32 = o.x32 + blockIdx.y * each + (int64_t)r0 * o.np + c0;
+  const WidePlace<T> w;
+  constexpr bool EARLY = T::MB * T::NB <= 4;
+  float4 own[EARLY ? T::MB : 1][T::NB][4];
+  auto load_own = [&](int x, float4 (&v)[T::NB][4]) __attribute__((always_inline)) {
+    const int r = w.row0 + 32 * x < rows ? w.row0 + 32 * x : rows - 1;
+#pragma unroll
+    for (int b = 0; b < T::NB; ++b)
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const int c = w.col0 + 32 * b + 8 * q;
+        v[b][q] = *(const float4*)(x32 + (int64_t)r * o.np + (c < cols ? c : 0));
+      }
+  };
+  if constexpr (EARLY) {
+#pragma unroll
+    for (int x = 0; x < T::MB; ++x) load_own(x, own[x]);
+  }
   v16f acc[T::MB][T::NB] = {};
   if constexpr (TALL)
     product<T>(Operand{X + (int64_t)r0 * o.np * 2, o.np, rows, o.np}, Operand{P + (int64_t)c0 * s * 2, s, cols, s}, s,
@@ -236,32 +272,24 @@ __global__ __launch_bounds__(T::THREADS, 1) void update_kernel(Orthogonalise o, 
   else
     product<T>(Operand{P + (int64_t)r0 * s * 2, s, rows, s}, Operand{X + (int64_t)c0 * 2, o.np, cols, o.np}, s, lds,
                acc);
-  float* const x32 = o.x32 + blockIdx.y * each + (int64_t)r0 * o.np + c0;
-  const WidePlace<T> w;
   const float k = 1.0f / (kScaleX * kScaleP);
 #pragma unroll
   for (int x = 0; x < T::MB; ++x) {
     const int r = w.row0 + 32 * x < rows ? w.row0 + 32 * x : rows - 1;
     const float pi = TALL ? 0.0f : p[r0 + r];
-    float4 v[T::NB][4], pj[T::NB][4];
+    if constexpr (!EARLY) load_own(x, own[0]);
 #pragma unroll
     for (int b = 0; b < T::NB; ++b)
 #pragma unroll
       for (int q = 0; q < 4; ++q) {
-        const int c = w.col0 + 32 * b + 8 * q < cols ? w.col0 + 32 * b + 8 * q : 0;
-        v[b][q] = *(const float4*)(x32 + (int64_t)r * o.np + c);
-        pj[b][q] = TALL ? *(const float4*)(p + c0 + c) : float4{pi, pi, pi, pi};
-      }
-#pragma unroll
-    for (int b = 0; b < T::NB; ++b)
-#pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        float4 y;
-        y.x = (o.a + pj[b][q].x) * v[b][q].x + k * acc[x][b][4 * q];
-        y.y = (o.a + pj[b][q].y) * v[b][q].y + k * acc[x][b][4 * q + 1];
-        y.z = (o.a + pj[b][q].z) * v[b][q].z + k * acc[x][b][4 * q + 2];
-        y.w = (o.a + pj[b][q].w) * v[b][q].w + k * acc[x][b][4 * q + 3];
         const int c = w.col0 + 32 * b + 8 * q;
+        const float4 v = own[EARLY ? x : 0][b][q];
+        const float4 pj = TALL ? *(const float4*)(p + c0 + (c < cols ? c : 0)) : float4{pi, pi, pi, pi};
+        float4 y;
+        y.x = (o.a + pj.x) * v.x + k * acc[x][b][4 * q];
+        y.y = (o.a + pj.y) * v.y + k * acc[x][b][4 * q + 1];
+        y.z = (o.a + pj.z) * v.z + k * acc[x][b][4 * q + 2];
+        y.w = (o.a + pj.w) * v.w + k * acc[x][b][4 * q + 3];
         if constexpr (!LAST)
           if (w.row0 + 32 * x < rows && c < cols) *(float4*)(x32 + (int64_t)r * o.np + c) = y;
         const float scale = LAST ? 1.0f : kScaleX;
@@ -298,20 +326,27 @@ using Large = Shape<2, 4, 4, 2, 2>;
 using Middle = Shape<2, 2, 2, 2, 2>;
 using Small = Shape<2, 2, 1, 1, 4>;
 
+// `tiles` tiles of sub times the shape's side, from `first` on
 template <class H, int L, bool SQUARE>
-void gram(const Orthogonalise& o, const char* in, int s, int depth, int64_t ld, hipStream_t st) {
+void gram(const Orthogonalise& o, const char* in, int s, int depth, int64_t ld, int64_t first, int64_t tiles, int sub,
+          hipStream_t st) {
   using T = typename H::template Of<L, L, kF16>;
-  const uint32_t t = (uint32_t)ceil_div(s, T::BM);
-  gram_kernel<T, SQUARE><<<dim3(t * (t + 1) / 2, o.count), dim3(T::THREADS), 0, st>>>(o, in, s, depth, ld, 0u);
+  gram_kernel<T, SQUARE><<<dim3((uint32_t)(tiles * sub * sub)), dim3(T::THREADS), 0, st>>>(
+      o, in, s, depth, ld, (uint32_t)first, (uint32_t)sub);
 }
 
 template <int L, bool SQUARE>
 void gram(const Orthogonalise& o, const char* in, int s, int depth, int64_t ld, hipStream_t st) {
   auto tiles = [&](int64_t b) { return o.count * ceil_div(s, b) * (ceil_div(s, b) + 1) / 2; };
-  switch (tile_of(tiles(128), tiles(256))) {
-    case kSmallTile: return gram<Small, L, SQUARE>(o, in, s, depth, ld, st);
-    case kMiddleTile: return gram<Middle, L, SQUARE>(o, in, s, depth, ld, st);
-    default: return gram<Large, L, SQUARE>(o, in, s, depth, ld, st);
+  const int64_t large = tiles(256), over = large_tiles_over(large);
+  if (over > 0) {
+    gram<Large, L, SQUARE>(o, in, s, depth, ld, 0, large - over, 1, st);
+    return gram<Small, L, SQUARE>(o, in, s, depth, ld, large - over, over, 4, st);
+  }
+  switch (tile_of(tiles(128), large)) {
+    case kSmallTile: return gram<Small, L, SQUARE>(o, in, s, depth, ld, 0, tiles(64), 1, st);
+    case kMiddleTile: return gram<Middle, L, SQUARE>(o, in, s, depth, ld, 0, tiles(128), 1, st);
+    default: return gram<Large, L, SQUARE>(o, in, s, depth, ld, 0, large, 1, st);
   }
 }
 
