@@ -37,7 +37,7 @@ __global__ __launch_bounds__(T::THREADS, 1) void grouped_rows_kernel(GroupedRows
                   T::LB == kAlong ? g.depth : g.cols};
   v16f acc[T::MB][T::NB] = {};
   product<T>(a, b, none ? 0 : g.depth, lds, acc);
-  store<T>(acc, lds, (char*)g.y + (t.row * g.ldy + c0) * 2, g.ldy, t.rows, cols, g.vec);
+  store<T>(acc, lds, (char*)g.y + (t.row * g.ldy + c0) * 2, g.ldy, t.rows, cols, g.vec, g.stream);
 }
 
 // The same for few rows per group (serving): a block reads 16 NB columns of a
@@ -100,7 +100,7 @@ __global__ __launch_bounds__(T::THREADS, 1) void grouped_weights_kernel(GroupedW
   v16f acc[T::MB][T::NB] = {};
   product<T>(a, b, end - first, lds, acc);
   constexpr int E = sizeof(typename Out<T::OUT>::type);
-  store<T>(acc, lds, (char*)g.dw + (group * g.group_stride + r0 * g.lddw + c0) * E, g.lddw, rows, cols, g.vec);
+  store<T>(acc, lds, (char*)g.dw + (group * g.group_stride + r0 * g.lddw + c0) * E, g.lddw, rows, cols, g.vec, g.stream);
 }
 
 template <class T>
@@ -168,6 +168,7 @@ hipError_t weights_of_type(const GroupedWeights& g, bool dma, hipStream_t s) {
 
 hipError_t launch_grouped_rows(GroupedRows g, int type, bool transposed, hipStream_t s) {
   g.vec = (uintptr_t)g.y % 16 == 0 && g.ldy % 8 == 0 && g.cols % 8 == 0;
+  g.stream = past_caches((int64_t)g.rows * g.cols * 2);
   const bool dma = dma_operand(g.x, g.ldx, g.depth) && dma_operand(g.w, g.ldw, transposed ? g.cols : g.depth) &&
                    g.group_stride % 8 == 0 && g.cols % 8 == 0 && g.depth % 8 == 0;
   if (type == kBF16)
@@ -177,6 +178,7 @@ hipError_t launch_grouped_rows(GroupedRows g, int type, bool transposed, hipStre
 
 hipError_t launch_grouped_weights(GroupedWeights g, int type, int out, hipStream_t s) {
   g.vec = (uintptr_t)g.dw % 16 == 0 && g.lddw % 8 == 0 && g.group_stride % 8 == 0 && g.k % 8 == 0;
+  g.stream = past_caches((int64_t)g.groups * g.n * g.k * 2);
   const bool dma = dma_operand(g.dy, g.lddy, g.n) && dma_operand(g.x, g.ldx, g.k);
   if (type == kBF16)
     return out == kF32 ? weights_of_type<kBF16, kF32>(g, dma, s) : weights_of_type<kBF16, kBF16>(g, dma, s);

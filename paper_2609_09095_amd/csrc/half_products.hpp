@@ -17,7 +17,7 @@ struct GroupedRows {
   void* y;  // rows x cols
   int64_t ldy;
   int rows, cols, depth, groups;
-  bool vec;  // 16-byte stores of y (set by the launch)
+  bool vec, stream;  // 16-byte stores of y, past the caches (set by the launch)
 };
 
 struct GroupedWeights {
@@ -29,7 +29,7 @@ struct GroupedWeights {
   void* dw;  // a stack of n x k
   int64_t lddw, group_stride;
   int rows, n, k, groups;
-  bool vec;  // 16-byte stores of a 16-bit dw (set by the launch)
+  bool vec, stream;  // 16-byte stores of a 16-bit dw, past the caches (set by the launch)
 };
 
 struct Adapter {
@@ -55,7 +55,7 @@ struct Adapter {
   int splits;        // parts of the depth of X A^T
   int serve_splits;  // the same in the few-row form
   int base_splits;   // parts of the depth of X W^T in the few-row form
-  bool vec;          // 16-byte stores of y
+  bool vec, stream;  // 16-byte stores of y, past the caches
 };
 
 struct Orthogonalise {
@@ -79,9 +79,12 @@ struct Orthogonalise {
 
 // Blocks (and partial sums) per matrix of the norm.
 inline int orthogonalise_parts(int64_t m, int64_t n) {
-  const int64_t p = m * ((n + 7) / 8) / 1024;
-  return (int)(p < 1 ? 1 : p > 256 ? 256 : p);
+  const int64_t p = m * ((n + 7) / 8) / 512;
+  return (int)(p < 1 ? 1 : p > 1024 ? 1024 : p);
 }
+
+// Outputs that the 32 MiB of L2 do not hold are stored past it.
+inline bool past_caches(int64_t bytes) { return bytes > ((int64_t)32 << 20); }
 
 // Whether a matrix of `cols` columns can go to LDS by DMA: 16-byte rows, and a
 // tile's offsets below 2^31.

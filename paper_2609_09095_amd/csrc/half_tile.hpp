@@ -509,10 +509,11 @@ __device__ __forceinline__ void wave_lds_ready() {
 // after the last stage, to a row-major 16-bit matrix: 16 bytes per lane, whole
 // runs of 64 bytes.  rows, cols: what exists of the tile.  `vec`: rows start
 // on 16 bytes and cols is a multiple of 8; else single elements are stored.
+// `stream`: past the caches, for outputs that do not fit them.
 // value(r, c, v): the four outputs from row r, column c on, given the sums.
 template <class T, class F>
 __device__ __forceinline__ void store_wide(const v16f (&acc)[T::MB][T::NB], char* lds, void* out, int64_t ld, int rows,
-                                           int cols, bool vec, F value) {
+                                           int cols, bool vec, bool stream, F value) {
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int r0 = wave / T::WC * T::MB * 32, c0 = wave % T::WC * T::NB * 32;
@@ -543,7 +544,11 @@ __device__ __forceinline__ void store_wide(const v16f (&acc)[T::MB][T::NB], char
     v[i] = *(const v4i*)(mine + r * PITCH + ((ch ^ (r & (CH - 1))) << 4));
   }
   const int rleft = cleft > 0 ? rows - r0 - lr : 0;
-  if (vec) {
+  if (vec && stream) {
+#pragma unroll
+    for (int i = 0; i < ROUNDS; ++i)
+      if (i * RPI < rleft) __builtin_nontemporal_store(v[i], (v4i*)(o + (int64_t)(i * RPI) * ld));
+  } else if (vec) {
 #pragma unroll
     for (int i = 0; i < ROUNDS; ++i)
       if (i * RPI < rleft) *(v4i*)(o + (int64_t)(i * RPI) * ld) = v[i];
@@ -561,12 +566,14 @@ __device__ __forceinline__ void store_wide(const v16f (&acc)[T::MB][T::NB], char
 }
 
 // The tile to a row-major matrix of type T::OUT, rounded once.  32-bit outputs
-// are stored straight from registers, 32 consecutive columns per half wavefront.
+// are stored straight from registers, 32 consecutive columns per half wavefront,
+// and always past the caches.  16384, 16, 4096, 2048 with and without: forward 275 /
+// 287 us, weights' gradient in 32 bits 274 / 330, in 16 bits 249 / 287.
 template <class T>
 __device__ __forceinline__ void store(const v16f (&acc)[T::MB][T::NB], char* lds, void* out, int64_t ld, int rows,
-                                      int cols, bool vec) {
+                                      int cols, bool vec, bool stream) {
   if constexpr (T::WIDE) {
-    store_wide<T>(acc, lds, out, ld, rows, cols, vec, [](int, int, float*) {});
+    store_wide<T>(acc, lds, out, ld, rows, cols, vec, stream, [](int, int, float*) {});
   } else {
     const int lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -582,7 +589,7 @@ __device__ __forceinline__ void store(const v16f (&acc)[T::MB][T::NB], char* lds
         if (row + r < rows) {
 #pragma unroll
           for (int b = 0; b < T::NB; ++b)
-            if (col + b * 32 < cols) p[b * 32] = acc[a][b][i];
+            if (col + b * 32 < cols) __builtin_nontemporal_store(acc[a][b][i], p + b * 32);
         }
       }
   }
@@ -716,8 +723,11 @@ __device__ __forceinline__ void skinny_join(const v4f (&acc)[NB][TB], v4f* lds, 
 
 // ---- order of the tiles ------------------------------------------------------
 // Place -> (row tile, column tile): row tiles in sets of kSet, column by column
-// inside a set, so that the blocks an XCD runs at a time share panels.
-constexpr uint32_t kSet = 4;
+// inside a set, so that the blocks an XCD runs at a time share panels.  Sets of
+// 1, 2, 4, 8: 32768, 32, 2048, 4096 forward 535 / 540 / 560 / 562 us, 16384, 16,
+// 4096, 2048 279 / 277 / 272 / 280, its input gradient 298 / 304 / 320 / 298, 8192^3
+// 844 / 820 / 820 / 820.
+constexpr uint32_t kSet = 2;
 __device__ __forceinline__ void place_to_tile(uint32_t place, uint32_t tiles_m, uint32_t tiles_n, uint32_t& tm,
                                               uint32_t& tn) {
   const uint32_t per = kSet * tiles_n;

@@ -34,9 +34,18 @@ constexpr float kScaleX = 256.0f, kScaleS = 1024.0f, kScaleP = 256.0f;
 template <int TYPE>
 __device__ __forceinline__ void row8(const void* g, int64_t row, int c, int n, float (&x)[8]) {
   if constexpr (TYPE == kF32) {
-    const auto q = (const __attribute__((address_space(1))) float*)(global_bytes)g + row + c;
+    const auto q = (const __attribute__((address_space(1))) float*)(global_bytes)g + row;
+    if (__builtin_amdgcn_ballot_w64(c + 8 > n) == 0) {
+      const char* const at = (const char*)g + (row + c) * 4;
+      const float4 lo = __builtin_bit_cast(float4, load_whole(at)), hi = __builtin_bit_cast(float4, load_whole(at + 16));
+      x[0] = lo.x, x[1] = lo.y, x[2] = lo.z, x[3] = lo.w, x[4] = hi.x, x[5] = hi.y, x[6] = hi.z, x[7] = hi.w;
+    } else {
 #pragma unroll
-    for (int j = 0; j < 8; ++j) x[j] = c + j < n ? q[j] : 0.0f;
+      for (int j = 0; j < 8; ++j) {
+        const float v = q[c + j < n ? c + j : n - 1];
+        x[j] = c + j < n ? v : 0.0f;
+      }
+    }
   } else {
     typedef typename Out<TYPE>::type v8 __attribute__((ext_vector_type(8)));
     const v8 v = __builtin_bit_cast(v8, load8((const char*)g + row * 2, c, n));
@@ -51,6 +60,7 @@ template <int TYPE>
 __global__ __launch_bounds__(256) void squares_kernel(Orthogonalise o) {
   const uint32_t chunks = (uint32_t)o.np / 8, total = chunks * (uint32_t)o.m;
   double sum = 0;
+#pragma unroll 4
   for (uint32_t i = blockIdx.x * 256 + threadIdx.x; i < total; i += gridDim.x * 256) {
     const uint32_t r = i / chunks, c = (i - r * chunks) * 8;
     float x[8];
@@ -216,7 +226,7 @@ __global__ __launch_bounds__(T::THREADS, 1) void gram_kernel(Orthogonalise o, co
           acc[x][b][i] = 0.0f;
         }
   }
-  store_wide<T>(acc, lds, out, s, rows, cols, true, [](int, int, float*) {});
+  store_wide<T>(acc, lds, out, s, rows, cols, true, false, [](int, int, float*) {});
   if (tm == tn) return;
   // the mirror image: a half wavefront has 32 consecutive rows of one column
   _Float16* const mirror = (_Float16*)(SQUARE ? o.p16 : o.s16) + z * square + (int64_t)c0 * s + r0;
@@ -302,9 +312,9 @@ __global__ __launch_bounds__(T::THREADS, 1) void update_kernel(Orthogonalise o, 
   auto as_is = [](int, int, float*) {};
   if constexpr (LAST)
     store_wide<T>(acc, lds, (char*)o.x + (blockIdx.y * o.x_stride + r0 * o.ldx + c0) * 2, o.ldx, o.m - r0, o.n - c0,
-                  o.vec, as_is);
+                  o.vec, true, as_is);
   else
-    store_wide<T>(acc, lds, next + (blockIdx.y * each + (int64_t)r0 * o.np + c0) * 2, o.np, rows, cols, true, as_is);
+    store_wide<T>(acc, lds, next + (blockIdx.y * each + (int64_t)r0 * o.np + c0) * 2, o.np, rows, cols, true, false, as_is);
 }
 
 template <int TYPE>
