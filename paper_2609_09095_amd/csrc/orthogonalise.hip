@@ -123,6 +123,20 @@ struct WidePlace {
   }
 };
 
+// The diagonal element that the lane holds of a WIDE block on the diagonal, set
+// to zero there; false: it holds none.
+__device__ __forceinline__ bool take_diagonal(v16f& v, float& mine) {
+  const int lane = threadIdx.x & 63, r = lane & 31, c0 = 4 * (lane >> 5);
+  mine = 0.0f;
+#pragma unroll
+  for (int i = 0; i < 16; ++i) {
+    const bool here = r == c0 + 8 * (i >> 2) + (i & 3);
+    mine = here ? v[i] : mine;
+    v[i] = here ? 0.0f : v[i];
+  }
+  return (r >> 2 & 1) == lane >> 5;
+}
+
 // A symmetric product A A^T (kAlong, A s x depth) or A^T A (kAcross, A
 // depth x s), the tiles on and above the diagonal, each stored twice: S, or with
 // SQUARE (A = So) P = b S + c S^2, their diagonals apart.  Block b takes the
@@ -206,25 +220,20 @@ __global__ __launch_bounds__(T::THREADS, 1) void gram_kernel(Orthogonalise o, co
       for (int b = 0; b < T::NB; ++b) acc[x][b] *= kScaleS / (kScaleX * kScaleX);
   }
   if (tm == tn) {
+    const int at = w.row0 - (threadIdx.x & 31), to = w.col0 - 4 * (threadIdx.x >> 5 & 1);  // the wavefront's blocks
 #pragma unroll
     for (int x = 0; x < T::MB; ++x)
 #pragma unroll
-      for (int b = 0; b < T::NB; ++b)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          const int r = w.row0 + 32 * x;
-          if (r != w.col0 + 32 * b + 8 * (i >> 2) + (i & 3)) continue;
-          if (r < rows) {
-            // acc: S_ii 2^10, or c (So^2)_ii 2^8 (So_ii is zero)
-            if constexpr (SQUARE) {
-              const float di = d[r0 + r];
-              diagonal[r0 + r] = (o.b + o.c * di) * di + acc[x][b][i] * (1.0f / kScaleP);
-            } else {
-              diagonal[r0 + r] = acc[x][b][i] * (1.0f / kScaleS);
-            }
-          }
-          acc[x][b][i] = 0.0f;
+      for (int b = 0; b < T::NB; ++b) {
+        if (at + 32 * x != to + 32 * b) continue;
+        // S_ii 2^10, or c (So^2)_ii 2^8 (So_ii is zero)
+        float mine;
+        const int r = w.row0 + 32 * x;
+        if (take_diagonal(acc[x][b], mine) && r < rows) {
+          const float di = SQUARE ? d[r0 + r] : 0.0f;
+          diagonal[r0 + r] = SQUARE ? (o.b + o.c * di) * di + mine * (1.0f / kScaleP) : mine * (1.0f / kScaleS);
         }
+      }
   }
   store_wide<T>(acc, lds, out, s, rows, cols, true, false, [](int, int, float*) {});
   if (tm == tn) return;
@@ -317,6 +326,161 @@ __global__ __launch_bounds__(T::THREADS, 1) void update_kernel(Orthogonalise o, 
     store_wide<T>(acc, lds, next + (blockIdx.y * each + (int64_t)r0 * o.np + c0) * 2, o.np, rows, cols, true, false, as_is);
 }
 
+// ---- matrices of at most 128 x 128: all steps in one block ---------------------
+// Eight wavefronts of 64 x 32 outputs; X in registers (32 bits) and, as the
+// operands are needed, in LDS, one array for X and one for S and then P.  Their
+// rows of 256 bytes have their 16-byte chunks XOR-swizzled by the row and are
+// read both ways, along a row and (transposing loads) across rows.  Tall
+// matrices are transposed as they are read and written.  32 x 128 x 128: a launch
+// of BLOCK us where the steps' launches took 95.
+constexpr int kSide = 128, kRow = kSide * 2;
+
+__device__ __forceinline__ int block_offset(int row, int col) {
+  return row * kRow + (((col >> 3) ^ (row & 15)) << 4) + (col & 7) * 2;
+}
+
+// acc = A B over `depth` from LDS: A's rows along, B's rows along or across.
+template <bool ACROSS>
+__device__ __forceinline__ void block_product(lds_bytes a, lds_bytes b, int row0, int col0, int depth, v16f (&acc)[2]) {
+  const int lane = threadIdx.x & 63;
+  acc[0] = acc[1] = v16f{};
+#pragma unroll 4
+  for (int k = 0; k < depth; k += 16) {
+    v4i fa[2], fb;
+    const int d = k + 8 * (lane >> 5);
+#pragma unroll
+    for (int x = 0; x < 2; ++x)
+      fa[x] = *(const __attribute__((address_space(3))) v4i*)(a + block_offset(row0 + 32 * x + (lane & 31), d));
+    if constexpr (ACROSS) {
+      using tr = __attribute__((address_space(3))) v4s*;
+      const int r = d + ((lane >> 2) & 3), c = col0 + (lane & 16) + 4 * (lane & 3);
+      const v4s lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((tr)(b + block_offset(r, c)));
+      const v4s hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((tr)(b + block_offset(r + 4, c)));
+      fb = __builtin_bit_cast(v4i, v8s{lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]});
+    } else {
+      fb = *(const __attribute__((address_space(3))) v4i*)(b + block_offset(col0 + (lane & 31), d));
+    }
+#pragma unroll
+    for (int x = 0; x < 2; ++x) acc[x] = mfma<kF16>(fb, fa[x], acc[x]);  // as WIDE tiles
+  }
+}
+
+template <int TYPE>
+__global__ __launch_bounds__(512, 1) void small_kernel(Orthogonalise o, int steps) {
+  using E = typename Out<TYPE>::type;
+  __shared__ __attribute__((aligned(1024))) char lds[2 * kSide * kRow + 2 * kSide * 4 + 8 * 8];
+  char* const xs = lds;
+  char* const ss = lds + kSide * kRow;
+  float* const diag_s = (float*)(lds + 2 * kSide * kRow);
+  float* const diag_p = diag_s + kSide;
+  double* const sums = (double*)(diag_p + kSide);
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int row0 = (wave >> 2) * 64, col0 = (wave & 3) * 32;
+  const int row = row0 + (lane & 31), col = col0 + 4 * (lane >> 5);
+  const bool tall = o.m > o.n;
+  const int s = tall ? o.n : o.m, l = tall ? o.m : o.n;
+  const int64_t along = tall ? o.ldg : 1, across = tall ? 1 : o.ldg;  // strides of X's columns and rows in G
+  const auto g = (const __attribute__((address_space(1))) E*)(global_bytes)o.g + blockIdx.x * o.g_stride;
+  v16f X[2];
+  double sum = 0;
+#pragma unroll
+  for (int x = 0; x < 2; ++x)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      const int r = row + 32 * x, c = col + 8 * (i >> 2) + (i & 3);
+      const bool in = r < s && c < l;
+      const float v = (float)g[(in ? r : 0) * across + (in ? c : 0) * along];
+      X[x][i] = in ? v : 0.0f;
+      sum += (double)X[x][i] * (double)X[x][i];
+    }
+  for (int d = 32; d; d >>= 1) sum += __shfl_xor(sum, d);
+  if (lane == 0) sums[wave] = sum;
+  __syncthreads();
+  const double square =
+      ((sums[0] + sums[1]) + (sums[2] + sums[3])) + ((sums[4] + sums[5]) + (sums[6] + sums[7]));
+  const float scale = (float)(1.0 / (sqrt(square) + (double)o.eps));
+#pragma unroll
+  for (int x = 0; x < 2; ++x)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      // (not by the product alone: padding stays zero for an infinite or NaN scale)
+      const bool in = row + 32 * x < s && col + 8 * (i >> 2) + (i & 3) < l;
+      X[x][i] = in ? X[x][i] * scale : 0.0f;
+    }
+  // the four outputs of group q of block x to LDS
+  auto put = [&](char* to, int x, int q, float v0, float v1, float v2, float v3) __attribute__((always_inline)) {
+    *(uint2*)(to + block_offset(row + 32 * x, col + 8 * q)) = pack4<kF16>(v0, v1, v2, v3);
+  };
+  const auto x3 = (lds_bytes)xs, s3 = (lds_bytes)ss;
+  const int depth_s = (s + 15) / 16 * 16, depth_l = (l + 15) / 16 * 16;
+  v16f acc[2];
+  for (int step = 0; step < steps; ++step) {
+#pragma unroll
+    for (int x = 0; x < 2; ++x)
+#pragma unroll
+      for (int q = 0; q < 4; ++q)
+        put(xs, x, q, X[x][4 * q] * kScaleX, X[x][4 * q + 1] * kScaleX, X[x][4 * q + 2] * kScaleX,
+            X[x][4 * q + 3] * kScaleX);
+    __syncthreads();
+    block_product<false>(x3, x3, row0, col0, depth_l, acc);
+#pragma unroll
+    for (int x = 0; x < 2; ++x) {
+      acc[x] *= kScaleS / (kScaleX * kScaleX);
+      float mine;
+      if (row0 + 32 * x == col0 && take_diagonal(acc[x], mine)) diag_s[row + 32 * x] = mine * (1.0f / kScaleS);
+#pragma unroll
+      for (int q = 0; q < 4; ++q)
+        put(ss, x, q, acc[x][4 * q], acc[x][4 * q + 1], acc[x][4 * q + 2], acc[x][4 * q + 3]);
+    }
+    __syncthreads();
+    block_product<false>(s3, s3, row0, col0, depth_s, acc);
+    const float ks = kScaleP / kScaleS, kc = o.c * kScaleP / (kScaleS * kScaleS);
+#pragma unroll
+    for (int x = 0; x < 2; ++x) {
+      const int r = row + 32 * x;
+      const float di = diag_s[r];
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        typedef _Float16 h4 __attribute__((ext_vector_type(4)));
+        const int c = col + 8 * q;
+        const h4 e = *(const h4*)(ss + block_offset(r, c));
+        const float4 dj = *(const float4*)(diag_s + c);
+        const float d[4] = {dj.x, dj.y, dj.z, dj.w};
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+          acc[x][4 * q + j] = kc * acc[x][4 * q + j] + (o.b + o.c * (di + d[j])) * ks * (float)e[j];
+      }
+      float mine;
+      if (row0 + 32 * x == col0 && take_diagonal(acc[x], mine))
+        diag_p[r] = (o.b + o.c * di) * di + mine * (1.0f / kScaleP);
+    }
+    __syncthreads();
+#pragma unroll
+    for (int x = 0; x < 2; ++x)
+#pragma unroll
+      for (int q = 0; q < 4; ++q)
+        put(ss, x, q, acc[x][4 * q], acc[x][4 * q + 1], acc[x][4 * q + 2], acc[x][4 * q + 3]);
+    __syncthreads();
+    block_product<true>(s3, x3, row0, col0, depth_s, acc);
+#pragma unroll
+    for (int x = 0; x < 2; ++x) {
+      const float a = o.a + diag_p[row + 32 * x];
+#pragma unroll
+      for (int i = 0; i < 16; ++i) X[x][i] = a * X[x][i] + (1.0f / (kScaleX * kScaleP)) * acc[x][i];
+    }
+    __syncthreads();
+  }
+  const int64_t out_c = tall ? o.ldx : 1, out_r = tall ? 1 : o.ldx;
+  __bf16* const out = (__bf16*)o.x + blockIdx.x * o.x_stride;
+#pragma unroll
+  for (int x = 0; x < 2; ++x)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      const int r = row + 32 * x, c = col + 8 * (i >> 2) + (i & 3);
+      if (r < s && c < l) out[r * out_r + c * out_c] = (__bf16)X[x][i];
+    }
+}
+
 template <int TYPE>
 hipError_t start(const Orthogonalise& o, hipStream_t s) {
   const int parts = orthogonalise_parts(o.m, o.n);
@@ -399,6 +563,15 @@ hipError_t steps(const Orthogonalise& o, int count, hipStream_t st) {
 
 hipError_t launch_orthogonalise(Orthogonalise o, int type, int count_steps, hipStream_t s) {
   o.vec = (uintptr_t)o.x % 16 == 0 && o.ldx % 8 == 0 && o.x_stride % 8 == 0 && o.n % 8 == 0;
+  if (o.m <= kSide && o.n <= kSide) {
+    if (type == kBF16)
+      small_kernel<kBF16><<<dim3(o.count), dim3(512), 0, s>>>(o, count_steps);
+    else if (type == kF16)
+      small_kernel<kF16><<<dim3(o.count), dim3(512), 0, s>>>(o, count_steps);
+    else
+      small_kernel<kF32><<<dim3(o.count), dim3(512), 0, s>>>(o, count_steps);
+    return hipGetLastError();
+  }
   const hipError_t e = type == kBF16 ? start<kBF16>(o, s) : type == kF16 ? start<kF16>(o, s) : start<kF32>(o, s);
   if (e != hipSuccess) return e;
   return o.m > o.n ? steps<true>(o, count_steps, s) : steps<false>(o, count_steps, s);
