@@ -188,7 +188,7 @@ __global__ __launch_bounds__(T::THREADS, 1) void adapter_kernel(Adapter p) {
   product<T>(Operand{(const char*)p.x + r0 * p.ldx * 2, p.ldx, rows, p.k},
              Operand{(const char*)p.w + c0 * p.ldw * 2, p.ldw, cols, p.k}, p.k, lds, acc);
   if (p.rank > 0) expand<T>(p, r0, rows, c0, cols, ids, lds, acc);
-  store<T>(acc, lds, (char*)p.y + (r0 * p.ldy + c0) * 2, p.ldy, rows, cols, p.vec, p.stream);
+  store<T>(acc, lds, (char*)p.y + (r0 * p.ldy + c0) * 2, p.ldy, rows, cols, p.stream);
 }
 
 // ---- few rows (serving): the weights are read once ------------------------------
@@ -346,7 +346,6 @@ hipError_t both(Adapter p, int serve_rows, hipStream_t s) {
 }  // namespace
 
 hipError_t launch_adapter(Adapter p, const AdapterPlan& plan, char* room, int type, hipStream_t s) {
-  p.vec = (uintptr_t)p.y % 16 == 0 && p.ldy % 8 == 0 && p.n % 8 == 0;
   p.stream = past_caches((int64_t)p.rows * p.n * 2);
   if (p.k == 0 || p.adapters == 0) p.rank = 0;  // X A^T is zero
   // the two parts run one after the other and share the room of their partial sums of H

@@ -37,7 +37,7 @@ __global__ __launch_bounds__(T::THREADS, 1) void grouped_rows_kernel(GroupedRows
                   T::LB == kAlong ? g.depth : g.cols};
   v16f acc[T::MB][T::NB] = {};
   product<T>(a, b, none ? 0 : g.depth, lds, acc);
-  store<T>(acc, lds, (char*)g.y + (t.row * g.ldy + c0) * 2, g.ldy, t.rows, cols, g.vec, g.stream);
+  store<T>(acc, lds, (char*)g.y + (t.row * g.ldy + c0) * 2, g.ldy, t.rows, cols, g.stream);
 }
 
 // The same for few rows per group (serving): a block reads 16 NB columns of a
@@ -67,11 +67,12 @@ __global__ __launch_bounds__(WAVES * 64) void grouped_few_kernel(GroupedRows g) 
   skinny_join<NB, TB, WAVES>(acc, lds, [&](int row, int c, v4f v) {
     if (row >= t.rows || c >= cols) return;
     O* const q = y + row * g.ldy + c;
-    if (g.vec) {
-      *(uint2*)q = pack4<TYPE>(v[0], v[1], v[2], v[3]);
+    if (c + 4 <= cols) {
+      const uint2 w = pack4<TYPE>(v[0], v[1], v[2], v[3]);
+      __builtin_memcpy(q, &w, 8);  // any alignment
     } else {
 #pragma unroll
-      for (int e = 0; e < 4; ++e)
+      for (int e = 0; e < 3; ++e)
         if (c + e < cols) q[e] = (O)v[e];
     }
   });
@@ -100,7 +101,7 @@ __global__ __launch_bounds__(T::THREADS, 1) void grouped_weights_kernel(GroupedW
   v16f acc[T::MB][T::NB] = {};
   product<T>(a, b, end - first, lds, acc);
   constexpr int E = sizeof(typename Out<T::OUT>::type);
-  store<T>(acc, lds, (char*)g.dw + (group * g.group_stride + r0 * g.lddw + c0) * E, g.lddw, rows, cols, g.vec, g.stream);
+  store<T>(acc, lds, (char*)g.dw + (group * g.group_stride + r0 * g.lddw + c0) * E, g.lddw, rows, cols, g.stream);
 }
 
 template <class T>
@@ -167,7 +168,6 @@ hipError_t weights_of_type(const GroupedWeights& g, bool dma, hipStream_t s) {
 }  // namespace
 
 hipError_t launch_grouped_rows(GroupedRows g, int type, bool transposed, hipStream_t s) {
-  g.vec = (uintptr_t)g.y % 16 == 0 && g.ldy % 8 == 0 && g.cols % 8 == 0;
   g.stream = past_caches((int64_t)g.rows * g.cols * 2);
   const bool dma = dma_operand(g.x, g.ldx, g.depth) && dma_operand(g.w, g.ldw, transposed ? g.cols : g.depth) &&
                    g.group_stride % 8 == 0 && g.cols % 8 == 0 && g.depth % 8 == 0;
@@ -177,7 +177,6 @@ hipError_t launch_grouped_rows(GroupedRows g, int type, bool transposed, hipStre
 }
 
 hipError_t launch_grouped_weights(GroupedWeights g, int type, int out, hipStream_t s) {
-  g.vec = (uintptr_t)g.dw % 16 == 0 && g.lddw % 8 == 0 && g.group_stride % 8 == 0 && g.k % 8 == 0;
   g.stream = past_caches((int64_t)g.groups * g.n * g.k * 2);
   const bool dma = dma_operand(g.dy, g.lddy, g.n) && dma_operand(g.x, g.ldx, g.k);
   if (type == kBF16)

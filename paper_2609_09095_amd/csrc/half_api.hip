@@ -231,7 +231,7 @@ ozaki25_status ozaki25_grouped_matmul(int64_t rows, int64_t n, int64_t k, int64_
   const ozaki25_status st =
       check_rows(rows, n, k, groups, X, ldx, k, W, ldw, group_stride, ends, Y, ldy, n, type);
   if (st != OZAKI25_SUCCESS || rows == 0 || n == 0) return st;
-  const oz::half::GroupedRows g{X, ldx, W, ldw, group_stride, ends, Y, ldy, (int)rows, (int)n, (int)k, (int)groups, false, false};
+  const oz::half::GroupedRows g{X, ldx, W, ldw, group_stride, ends, Y, ldy, (int)rows, (int)n, (int)k, (int)groups, false};
   return status_of(oz::half::launch_grouped_rows(g, (int)type, false, (hipStream_t)stream));
 }
 
@@ -242,7 +242,7 @@ ozaki25_status ozaki25_grouped_matmul_dx(int64_t rows, int64_t n, int64_t k, int
   const ozaki25_status st =
       check_rows(rows, n, k, groups, dY, lddy, n, W, ldw, group_stride, ends, dX, lddx, k, type);
   if (st != OZAKI25_SUCCESS || rows == 0 || k == 0) return st;
-  const oz::half::GroupedRows g{dY, lddy, W, ldw, group_stride, ends, dX, lddx, (int)rows, (int)k, (int)n, (int)groups, false, false};
+  const oz::half::GroupedRows g{dY, lddy, W, ldw, group_stride, ends, dX, lddx, (int)rows, (int)k, (int)n, (int)groups, false};
   return status_of(oz::half::launch_grouped_rows(g, (int)type, true, (hipStream_t)stream));
 }
 
@@ -266,7 +266,7 @@ ozaki25_status ozaki25_grouped_matmul_dw(int64_t rows, int64_t n, int64_t k, int
       overlaps(dW, ob, ends, (size_t)groups * sizeof(int32_t)))
     return OZAKI25_ERR_INVALID_VALUE;
   const oz::half::GroupedWeights g{dY,   lddy,         X,         ldx,    ends,   dW,
-                                   lddw, group_stride, (int)rows, (int)n, (int)k, (int)groups, false, false};
+                                   lddw, group_stride, (int)rows, (int)n, (int)k, (int)groups, false};
   return status_of(oz::half::launch_grouped_weights(g, (int)type, (int)out_type, (hipStream_t)stream));
 }
 

@@ -17,7 +17,7 @@ struct GroupedRows {
   void* y;  // rows x cols
   int64_t ldy;
   int rows, cols, depth, groups;
-  bool vec, stream;  // 16-byte stores of y, past the caches (set by the launch)
+  bool stream;  // y past the caches (set by the launch)
 };
 
 struct GroupedWeights {
@@ -29,7 +29,7 @@ struct GroupedWeights {
   void* dw;  // a stack of n x k
   int64_t lddw, group_stride;
   int rows, n, k, groups;
-  bool vec, stream;  // 16-byte stores of a 16-bit dw, past the caches (set by the launch)
+  bool stream;  // a 16-bit dw past the caches (set by the launch)
 };
 
 struct Adapter {
@@ -55,7 +55,7 @@ struct Adapter {
   int splits;        // parts of the depth of X A^T
   int serve_splits;  // the same in the few-row form
   int base_splits;   // parts of the depth of X W^T in the few-row form
-  bool vec, stream;  // 16-byte stores of y, past the caches
+  bool stream;       // y past the caches
 };
 
 struct Orthogonalise {
@@ -74,7 +74,6 @@ struct Orthogonalise {
   void* p16;        // the same
   float* d32;       // count x s: the diagonal of S
   float* p32;       // the same of P
-  bool vec;         // 16-byte stores of x (set by the launch)
 };
 
 // Blocks (and partial sums) per matrix of the norm.

@@ -250,15 +250,24 @@ template <int L, int V, int N>
 struct MaskedSide {
   v4i reg[N];
   int have[N];      // elements of the chunk that exist
-  int64_t from[N];  // bytes from a stage's first element to the chunk
+  int64_t whole[N];  // a stage with all 64 depths: bytes from its first element to what is read
   global_bytes p;
-  int64_t step;  // bytes from stage to stage
+  int64_t ld;
   int64_t safe;  // bytes from the stage's first element to 8 elements that always exist
   int vecs;
   bool narrow;
+  bool cuts;  // some lane's chunk is not whole
+  __device__ __forceinline__ int existing(int r, int c, int left) const {
+    const int rows = L == kAlong ? vecs : left, cols = L == kAlong ? left : vecs;
+    const int n = cols - c * 8;
+    return r < rows ? (n < 0 ? 0 : n < 8 ? n : 8) : 0;
+  }
+  __device__ __forceinline__ int64_t place(int r, int c, int n) const {
+    return n > 0 ? (r * ld + c * 8 - (8 - n)) * 2 : safe;
+  }
   __device__ __forceinline__ void init(const Operand& op, int depth, int wave, int lane) {
     p = (global_bytes)uniform(op.p);
-    step = (L == kAlong ? kDepth : op.ld * kDepth) * 2;
+    ld = op.ld;
     vecs = op.vecs;
     narrow = op.width < 8;
     const int first = L == kAlong ? depth : vecs;  // of the first row, from here on
@@ -267,41 +276,61 @@ struct MaskedSide {
     for (int i = 0; i < N; ++i) {
       int r, c;
       chunk_at<L, V>((wave * N + i) * 1024 + lane * 16, r, c);
-      from[i] = (r * op.ld + c * 8) * 2;
+      // kAcross: a chunk that does not exist reads its row's last 8 elements,
+      // wherever the stage is (kAlong: the first row's first ones, which `safe`
+      // would move away from)
+      have[i] = existing(r, c, kDepth);
+      whole[i] = L == kAcross || have[i] > 0 ? (r * ld + (have[i] > 0 ? c * 8 - (8 - have[i]) : vecs - 8)) * 2 : 0;
     }
   }
   __device__ __forceinline__ void load(int wave, int lane, int left) {
+    int64_t at[N];
+    if (left >= kDepth) {
+      // the common stage: nothing depends on how far the depth goes
+      int least = 8;
 #pragma unroll
-    for (int i = 0; i < N; ++i) {
-      int r, c;
-      chunk_at<L, V>((wave * N + i) * 1024 + lane * 16, r, c);
-      const int rows = L == kAlong ? vecs : left, cols = L == kAlong ? left : vecs;
-      const int n = cols - c * 8;
-      have[i] = r < rows ? (n < 0 ? 0 : n < 8 ? n : 8) : 0;
+      for (int i = 0; i < N; ++i) {
+        at[i] = whole[i];
+        least = have[i] < least ? have[i] : least;
+      }
+      cuts = __builtin_amdgcn_ballot_w64(least < 8) != 0;
+    } else {
+      cuts = true;
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        int r, c;
+        chunk_at<L, V>((wave * N + i) * 1024 + lane * 16, r, c);
+        have[i] = existing(r, c, left);
+        at[i] = place(r, c, have[i]);
+      }
     }
     if (!narrow) {
       // no branch around a load: its end would wait for the data
 #pragma unroll
-      for (int i = 0; i < N; ++i) {
-        const int64_t at = have[i] > 0 ? from[i] - (8 - have[i]) * 2 : safe;
-        __builtin_memcpy(&reg[i], (const __attribute__((address_space(1))) void*)(p + at), 16);
-      }
+      for (int i = 0; i < N; ++i)
+        __builtin_memcpy(&reg[i], (const __attribute__((address_space(1))) void*)(p + at[i]), 16);
     } else {
 #pragma unroll
       for (int i = 0; i < N; ++i) {
+        int r, c;
+        chunk_at<L, V>((wave * N + i) * 1024 + lane * 16, r, c);
+        const int n = existing(r, c, left < kDepth ? left : kDepth);
         v8s e{};
 #pragma unroll
         for (int j = 0; j < 7; ++j)
-          if (j < have[i]) e[j] = ((const __attribute__((address_space(1))) short*)(p + from[i]))[j];
+          if (j < n) e[j] = ((const __attribute__((address_space(1))) short*)(p + (r * ld + c * 8) * 2))[j];
         reg[i] = __builtin_bit_cast(v4i, e);
-        have[i] = 8;
       }
+      cuts = false;
     }
+    const int64_t step = (L == kAlong ? kDepth : ld * kDepth) * 2;
     p += step;
     safe -= step;
   }
   __device__ __forceinline__ void put(int i, char* lds, int wave, int lane) const {
-    *(v4i*)(lds + (wave * N + i) * 1024 + lane * 16) = keep_upper(reg[i], have[i]);
+    v4i v = reg[i];
+    if (cuts) v = keep_upper(v, have[i]);
+    *(v4i*)(lds + (wave * N + i) * 1024 + lane * 16) = v;
   }
 };
 
@@ -507,13 +536,11 @@ __device__ __forceinline__ void wave_lds_ready() {
 
 // The wavefront's blocks (WIDE tiles) through its part of LDS, which is free
 // after the last stage, to a row-major 16-bit matrix: 16 bytes per lane, whole
-// runs of 64 bytes.  rows, cols: what exists of the tile.  `vec`: rows start
-// on 16 bytes and cols is a multiple of 8; else single elements are stored.
-// `stream`: past the caches, for outputs that do not fit them.
+// runs of 64 bytes.  rows, cols: what exists of the tile.  `stream`: past the caches, for outputs that do not fit them.
 // value(r, c, v): the four outputs from row r, column c on, given the sums.
 template <class T, class F>
 __device__ __forceinline__ void store_wide(const v16f (&acc)[T::MB][T::NB], char* lds, void* out, int64_t ld, int rows,
-                                           int cols, bool vec, bool stream, F value) {
+                                           int cols, bool stream, F value) {
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int r0 = wave / T::WC * T::MB * 32, c0 = wave % T::WC * T::NB * 32;
@@ -544,22 +571,27 @@ __device__ __forceinline__ void store_wide(const v16f (&acc)[T::MB][T::NB], char
     v[i] = *(const v4i*)(mine + r * PITCH + ((ch ^ (r & (CH - 1))) << 4));
   }
   const int rleft = cleft > 0 ? rows - r0 - lr : 0;
-  if (vec && stream) {
+  // 16 bytes at any alignment; single elements where the row's end cuts them
+  typedef v4i any_v4i __attribute__((aligned(2)));
+  using to = __attribute__((address_space(1))) any_v4i*;
+  if (cleft >= 8) {
+    if (stream) {
 #pragma unroll
-    for (int i = 0; i < ROUNDS; ++i)
-      if (i * RPI < rleft) __builtin_nontemporal_store(v[i], (v4i*)(o + (int64_t)(i * RPI) * ld));
-  } else if (vec) {
+      for (int i = 0; i < ROUNDS; ++i)
+        if (i * RPI < rleft) __builtin_nontemporal_store((any_v4i)v[i], (to)(o + (int64_t)(i * RPI) * ld));
+    } else {
 #pragma unroll
-    for (int i = 0; i < ROUNDS; ++i)
-      if (i * RPI < rleft) *(v4i*)(o + (int64_t)(i * RPI) * ld) = v[i];
-  } else {
+      for (int i = 0; i < ROUNDS; ++i)
+        if (i * RPI < rleft) *(to)(o + (int64_t)(i * RPI) * ld) = v[i];
+    }
+  } else if (cleft > 0) {
 #pragma unroll
     for (int i = 0; i < ROUNDS; ++i)
       if (i * RPI < rleft) {
         short* const q = o + (int64_t)(i * RPI) * ld;
         const v8s e = __builtin_bit_cast(v8s, v[i]);
 #pragma unroll
-        for (int j = 0; j < 8; ++j)
+        for (int j = 0; j < 7; ++j)
           if (j < cleft) q[j] = e[j];
       }
   }
@@ -571,9 +603,9 @@ __device__ __forceinline__ void store_wide(const v16f (&acc)[T::MB][T::NB], char
 // 287 us, weights' gradient in 32 bits 274 / 330, in 16 bits 249 / 287.
 template <class T>
 __device__ __forceinline__ void store(const v16f (&acc)[T::MB][T::NB], char* lds, void* out, int64_t ld, int rows,
-                                      int cols, bool vec, bool stream) {
+                                      int cols, bool stream) {
   if constexpr (T::WIDE) {
-    store_wide<T>(acc, lds, out, ld, rows, cols, vec, stream, [](int, int, float*) {});
+    store_wide<T>(acc, lds, out, ld, rows, cols, stream, [](int, int, float*) {});
   } else {
     const int lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);

@@ -235,7 +235,7 @@ __global__ __launch_bounds__(T::THREADS, 1) void gram_kernel(Orthogonalise o, co
         }
       }
   }
-  store_wide<T>(acc, lds, out, s, rows, cols, true, false, [](int, int, float*) {});
+  store_wide<T>(acc, lds, out, s, rows, cols, false, [](int, int, float*) {});
   if (tm == tn) return;
   // the mirror image: a half wavefront has 32 consecutive rows of one column
   _Float16* const mirror = (_Float16*)(SQUARE ? o.p16 : o.s16) + z * square + (int64_t)c0 * s + r0;
@@ -321,9 +321,9 @@ __global__ __launch_bounds__(T::THREADS, 1) void update_kernel(Orthogonalise o, 
   auto as_is = [](int, int, float*) {};
   if constexpr (LAST)
     store_wide<T>(acc, lds, (char*)o.x + (blockIdx.y * o.x_stride + r0 * o.ldx + c0) * 2, o.ldx, o.m - r0, o.n - c0,
-                  o.vec, true, as_is);
+                  true, as_is);
   else
-    store_wide<T>(acc, lds, next + (blockIdx.y * each + (int64_t)r0 * o.np + c0) * 2, o.np, rows, cols, true, false, as_is);
+    store_wide<T>(acc, lds, next + (blockIdx.y * each + (int64_t)r0 * o.np + c0) * 2, o.np, rows, cols, false, as_is);
 }
 
 // ---- matrices of at most 128 x 128: all steps in one block ---------------------
@@ -562,7 +562,6 @@ hipError_t steps(const Orthogonalise& o, int count, hipStream_t st) {
 }  // namespace
 
 hipError_t launch_orthogonalise(Orthogonalise o, int type, int count_steps, hipStream_t s) {
-  o.vec = (uintptr_t)o.x % 16 == 0 && o.ldx % 8 == 0 && o.x_stride % 8 == 0 && o.n % 8 == 0;
   if (o.m <= kSide && o.n <= kSide) {
     if (type == kBF16)
       small_kernel<kBF16><<<dim3(o.count), dim3(512), 0, s>>>(o, count_steps);
