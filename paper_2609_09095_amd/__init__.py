@@ -565,16 +565,17 @@ def _together(first, names, *others):
     for t in others:
         if t is not None and (dev < 0 or t.get_device() != dev):
             _on_gpu(zip(names, (first, *others)))
+            return
 
 
-def _new(shape, dtype, device, stream):
-    """An output of the call, allocated on the stream that writes it."""
-    torch = _torch
-    if stream is None or device.type != "cuda":
-        return torch.empty(shape, dtype=dtype, device=device)
-    s = stream if hasattr(stream, "cuda_stream") else torch.cuda.ExternalStream(int(stream), device=device)
-    with torch.cuda.stream(s):
-        return torch.empty(shape, dtype=dtype, device=device)
+def _new(like, shape, stream, dtype=None):
+    """An output of the call beside `like`, of its dtype if none is given,
+    allocated on the stream that writes it."""
+    if stream is None or not like.is_cuda:
+        return like.new_empty(shape, dtype=dtype)
+    s = stream if hasattr(stream, "cuda_stream") else _torch.cuda.ExternalStream(int(stream), device=like.device)
+    with _torch.cuda.stream(s):
+        return like.new_empty(shape, dtype=dtype)
 
 
 def ozaki25_grouped_matmul(X, W, ends, Y=None, stream=None):
@@ -590,9 +591,11 @@ def ozaki25_grouped_matmul(X, W, ends, Y=None, stream=None):
         raise ValueError(f"W has {kw} columns, X has {k}")
     _vector(ends, "ends", _torch.int32, groups)
     if Y is None:
-        Y = _new((rows, n), X.dtype, X.device, stream)
-    _, ldy, _ = _pitched(Y, "Y", 2, kind, (rows, n))
-    _together(X, ("X", "W", "ends", "Y"), W, ends, Y)
+        _together(X, ("X", "W", "ends"), W, ends)
+        Y, ldy = _new(X, (rows, n), stream), n or 1
+    else:
+        _, ldy, _ = _pitched(Y, "Y", 2, kind, (rows, n))
+        _together(X, ("X", "W", "ends", "Y"), W, ends, Y)
     _check(lib().ozaki25_grouped_matmul(rows, n, k, groups, X.data_ptr(), ldx, W.data_ptr(), ldw, stride,
                                         ends.data_ptr(), Y.data_ptr(), ldy, types[X.dtype], _stream(stream)),
            "ozaki25_grouped_matmul")
@@ -610,9 +613,11 @@ def ozaki25_grouped_matmul_dx(dY, W, ends, dX=None, stream=None):
         raise ValueError(f"W has {nw} rows, dY has {n} columns")
     _vector(ends, "ends", _torch.int32, groups)
     if dX is None:
-        dX = _new((rows, k), dY.dtype, dY.device, stream)
-    _, lddx, _ = _pitched(dX, "dX", 2, kind, (rows, k))
-    _together(dY, ("dY", "W", "ends", "dX"), W, ends, dX)
+        _together(dY, ("dY", "W", "ends"), W, ends)
+        dX, lddx = _new(dY, (rows, k), stream), k or 1
+    else:
+        _, lddx, _ = _pitched(dX, "dX", 2, kind, (rows, k))
+        _together(dY, ("dY", "W", "ends", "dX"), W, ends, dX)
     _check(lib().ozaki25_grouped_matmul_dx(rows, n, k, groups, dY.data_ptr(), lddy, W.data_ptr(), ldw, stride,
                                            ends.data_ptr(), dX.data_ptr(), lddx, types[dY.dtype], _stream(stream)),
            "ozaki25_grouped_matmul_dx")
@@ -631,7 +636,7 @@ def ozaki25_grouped_matmul_dw(dY, X, ends, dW=None, out_dtype=None, stream=None)
     groups = ends.numel() if isinstance(ends, _torch.Tensor) else 0
     _vector(ends, "ends", _torch.int32, groups)
     if dW is None:
-        dW = _new((groups, n, k), out_dtype or dY.dtype, dY.device, stream)
+        dW = _new(dY, (groups, n, k), stream, out_dtype)
     elif out_dtype is not None and dW.dtype != out_dtype:
         raise ValueError(f"dW has dtype {dW.dtype}, out_dtype is {out_dtype}")
     _, lddw, stride = _pitched(dW, "dW", 3, (dY.dtype, _torch.float32), (groups, n, k))
@@ -665,11 +670,13 @@ def ozaki25_adapter_matmul(X, W, ids, A, B, scales=None, Y=None, workspace=None,
     _vector(ids, "ids", _torch.int32, rows)
     if scales is not None:
         _vector(scales, "scales", _torch.float32, adapters)
-    if Y is None:
-        Y = _new((rows, n), X.dtype, X.device, stream)
-    _, ldy, _ = _pitched(Y, "Y", 2, kind, (rows, n))
     ws_ptr, ws_bytes = _room(workspace)
-    _together(X, ("X", "W", "ids", "A", "B", "scales", "Y", "workspace"), W, ids, A, B, scales, Y, workspace)
+    if Y is None:
+        _together(X, ("X", "W", "ids", "A", "B", "scales", "workspace"), W, ids, A, B, scales, workspace)
+        Y, ldy = _new(X, (rows, n), stream), n or 1
+    else:
+        _, ldy, _ = _pitched(Y, "Y", 2, kind, (rows, n))
+        _together(X, ("X", "W", "ids", "A", "B", "scales", "Y", "workspace"), W, ids, A, B, scales, Y, workspace)
     _check(lib().ozaki25_adapter_matmul(rows, n, k, adapters, rank, X.data_ptr(), ldx, W.data_ptr(), ldw,
                                         ids.data_ptr(), A.data_ptr(), lda, a_stride, B.data_ptr(), ldb, b_stride,
                                         _ptr(scales), Y.data_ptr(), ldy, types[X.dtype], ws_ptr, ws_bytes,
@@ -694,7 +701,7 @@ def ozaki25_orthogonalise(G, X=None, steps: int = 5, coefficients=(3.4445, -4.77
     m, n = size[-2:]
     a, b, c = coefficients
     if X is None:
-        X = _new(size, _torch.bfloat16, G.device, stream)
+        X = _new(G, size, stream, _torch.bfloat16)
     _, ldx, x_stride = _pitched(X, "X", dims, (_torch.bfloat16,), size)
     ws_ptr, ws_bytes = _room(workspace)
     _together(G, ("G", "X", "workspace"), X, workspace)
