@@ -311,7 +311,6 @@ hipError_t serve(const Adapter& p, hipStream_t s) {
 template <class T>
 hipError_t run(const Adapter& p, hipStream_t s) {
   const int64_t tiles = ceil_div(p.rows, T::BM) * ceil_div(p.n, T::BN);
-  if (tiles * T::THREADS >= ((int64_t)1 << 32)) return hipErrorInvalidConfiguration;
   const dim3 grid((uint32_t)((tiles + 7) & ~(int64_t)7));
   adapter_kernel<T><<<grid, dim3(T::THREADS), 0, s>>>(p);
   return hipGetLastError();
@@ -364,6 +363,11 @@ hipError_t both(Adapter p, int serve_rows, hipStream_t s) {
 }  // namespace
 
 hipError_t launch_adapter(Adapter p, const AdapterPlan& plan, char* room, int type, hipStream_t s) {
+  // more work-items than a launch holds (by the smallest tiles): before anything runs
+  constexpr int64_t kMost = ((int64_t)1 << 32) - 4096;
+  if (ceil_div(p.rows, 64) * ceil_div(p.n, 64) * 256 > kMost || ceil_div(p.rows, kShrinkRows) * 256 > kMost ||
+      (int64_t)p.rows * (p.rank_pad / 4) > kMost)
+    return hipErrorInvalidConfiguration;
   p.stream = past_caches((int64_t)p.rows * p.n * 2);
   if (p.k == 0 || p.adapters == 0) p.rank = 0;  // X A^T is zero
   // the two parts run one after the other and share the room of their partial sums of H

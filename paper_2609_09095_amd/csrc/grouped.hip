@@ -22,12 +22,13 @@ template <class T>
 __global__ __launch_bounds__(T::THREADS, 1) void grouped_rows_kernel(GroupedRows g) {
   __shared__ __attribute__((aligned(1024))) char lds[T::LDS];
   const uint32_t tiles_n = ((uint32_t)g.cols + T::BN - 1) / T::BN;
-  const uint32_t tiles_m = count_row_tiles<T::BM>(g.ends, g.groups, g.rows);
+  RowTiles<T::BM> all;
+  const uint32_t tiles_m = all.init(g.ends, g.groups, g.rows);
   uint32_t place, tm, tn;
   if (!block_place(blockIdx.x, tiles_m * tiles_n, place)) return;
   place_to_tile(place, tiles_m, tiles_n, tm, tn);
   RowTile t;
-  if (!find_row_tile<T::BM>(g.ends, g.groups, g.rows, (int)tm, t)) return;
+  if (!all.find((int)tm, t)) return;
   const int c0 = (int)tn * T::BN;
   const int cols = g.cols - c0 < T::BN ? g.cols - c0 : T::BN;
   const bool none = t.group == g.groups;  // rows of no group: zeros
@@ -47,13 +48,14 @@ __global__ __launch_bounds__(WAVES * 64) void grouped_few_kernel(GroupedRows g) 
   using O = typename Out<TYPE>::type;
   __shared__ v4f lds[WAVES * TB * 16 * NB * 4];
   const uint32_t tiles_n = ((uint32_t)g.cols + 16 * NB - 1) / (16 * NB);
-  const uint32_t tiles_m = count_row_tiles<16 * TB>(g.ends, g.groups, g.rows);
+  RowTiles<16 * TB> all;
+  const uint32_t tiles_m = all.init(g.ends, g.groups, g.rows);
   uint32_t place;
   if (!block_place(blockIdx.x, tiles_m * tiles_n, place)) return;
   // a group's row tiles side by side: they share the weights
   const uint32_t tn = place / tiles_m, tm = place - tn * tiles_m;
   RowTile t;
-  if (!find_row_tile<16 * TB>(g.ends, g.groups, g.rows, (int)tm, t)) return;
+  if (!all.find((int)tm, t)) return;
   const int c0 = (int)tn * (16 * NB), cols = g.cols - c0 < 16 * NB ? g.cols - c0 : 16 * NB;
   v4f acc[NB][TB] = {};
   if (t.group < g.groups && g.depth > 0) {
@@ -91,7 +93,8 @@ __global__ __launch_bounds__(T::THREADS, 1) void grouped_weights_kernel(GroupedW
   place_to_tile(place, tiles_m, tiles_n, tm, tn);
   const int lane = threadIdx.x & 63;
   int last = 0, first = 0, end = 0;
-  for (int g0 = 0; g0 <= (int)group; g0 += 64) group_rows(g.ends, g.groups, g.rows, g0, lane, last, first, end);
+  for (int g0 = 0; g0 <= (int)group; g0 += 64)
+    group_rows(group_end(g.ends, g.groups, g.rows, g0, lane), lane, last, first, end);
   first = __builtin_amdgcn_readlane(first, group & 63);
   end = __builtin_amdgcn_readlane(end, group & 63);
   const int r0 = (int)tm * T::BM, c0 = (int)tn * T::BN;

@@ -114,7 +114,7 @@ constexpr int64_t kServeRows = 128, kServeOutputs = 1 << 18;
 constexpr AdapterPlan adapter_plan(int64_t rows, int64_t n, int64_t k, int64_t rank_pad) {
   AdapterPlan a{};
   const int64_t over = rows % 256;
-  if (rows <= kServeRows || rows * n <= kServeOutputs) {
+  if (rows <= kServeRows || (rows <= 4 * kServeRows && rows * n <= kServeOutputs)) {
     a.serve_rows = (int)rows;
   } else if (over > 0 && over <= 64 && rows > 256) {
     // rows that would take large tiles a round of their own

@@ -795,11 +795,12 @@ __device__ __forceinline__ int scan64(int v, F f) {
 // 64 groups from g0: the lane's group's rows [first, end), ends clamped to
 // [the previous end, rows] whatever the array holds.  Group number `groups`
 // is what no group covers, [last end, rows).  `last` carries from call to call.
-__device__ __forceinline__ void group_rows(const int32_t* ends, int groups, int rows, int g0, int lane, int& last,
-                                           int& first, int& end) {
+__device__ __forceinline__ int group_end(const int32_t* ends, int groups, int rows, int g0, int lane) {
   const int g = g0 + lane;
-  int e = g < groups ? ends[g] : rows;
-  e = e < 0 ? 0 : (e > rows ? rows : e);
+  const int e = g < groups ? ends[g] : rows;
+  return e < 0 ? 0 : (e > rows ? rows : e);
+}
+__device__ __forceinline__ void group_rows(int e, int lane, int& last, int& first, int& end) {
   e = scan64(e > last ? e : last, [](int a, int b) { return a > b ? a : b; });
   const int before = __builtin_amdgcn_update_dpp(0, e, 0x138, 0xf, 0xf, false);  // wave_shr:1
   first = lane == 0 ? last : before;
@@ -807,49 +808,78 @@ __device__ __forceinline__ void group_rows(const int32_t* ends, int groups, int 
   last = __builtin_amdgcn_readlane(e, 63);
 }
 
-// The row tile number t of a grouped product with tiles of BM rows: its group
-// (`groups` for rows of no group), first row and number of rows; false past
-// the last tile.  total: the number of row tiles.
-template <int BM>
-__device__ __forceinline__ int count_row_tiles(const int32_t* ends, int groups, int rows) {
-  const int lane = threadIdx.x & 63;
-  int last = 0, total = 0;
-  for (int g0 = 0; g0 <= groups; g0 += 64) {
-    int first, end;
-    group_rows(ends, groups, rows, g0, lane, last, first, end);
-    const int t = (end - first + BM - 1) / BM;
-    total += __builtin_amdgcn_readlane(scan64(t, [](int a, int b) { return a + b; }), 63);
-  }
-  return total;
-}
-
+// The row tiles of a grouped product with tiles of BM rows.  Up to 255 groups
+// are read once, all loads in flight, and stay in registers.
 struct RowTile {
   int group, row, rows;
 };
 
 template <int BM>
-__device__ __forceinline__ bool find_row_tile(const int32_t* ends, int groups, int rows, int t, RowTile& out) {
-  const int lane = threadIdx.x & 63;
-  int last = 0, before = 0;
-  for (int g0 = 0; g0 <= groups; g0 += 64) {
-    int first, end;
-    group_rows(ends, groups, rows, g0, lane, last, first, end);
-    const int mine = (end - first + BM - 1) / BM;
-    const int incl = scan64(mine, [](int a, int b) { return a + b; });
-    const uint64_t past = __builtin_amdgcn_ballot_w64(before + incl > t);
-    if (past) {
-      const int l = __builtin_ctzll(past);
-      const int in = t - before - __builtin_amdgcn_readlane(incl - mine, l);
-      out.group = g0 + l;
-      out.row = __builtin_amdgcn_readlane(first, l) + in * BM;
-      const int left = __builtin_amdgcn_readlane(end, l) - out.row;
-      out.rows = left < BM ? left : BM;
-      return true;
+struct RowTiles {
+  static constexpr int HELD = 4;
+  const int32_t* ends;
+  int groups, rows, lane;
+  int first[HELD], end[HELD];
+
+  // calls f(first group, first rows, ends) for each 64 groups until it returns true
+  template <class F>
+  __device__ __forceinline__ bool each(F f) {
+    if (groups < HELD * 64) {
+#pragma unroll
+      for (int i = 0; i < HELD; ++i)
+        if (i * 64 <= groups && f(i * 64, first[i], end[i])) return true;
+      return false;
     }
-    before += __builtin_amdgcn_readlane(incl, 63);
+    int last = 0;
+    for (int g0 = 0; g0 <= groups; g0 += 64) {
+      int a, b;
+      group_rows(group_end(ends, groups, rows, g0, lane), lane, last, a, b);
+      if (f(g0, a, b)) return true;
+    }
+    return false;
   }
-  return false;
-}
+  // returns the number of tiles
+  __device__ __forceinline__ int init(const int32_t* e, int ng, int nr) {
+    ends = e;
+    groups = ng;
+    rows = nr;
+    lane = threadIdx.x & 63;
+    if (groups < HELD * 64) {
+      int v[HELD], last = 0;
+#pragma unroll
+      for (int i = 0; i < HELD; ++i) v[i] = i * 64 <= groups ? group_end(ends, groups, rows, i * 64, lane) : rows;
+#pragma unroll
+      for (int i = 0; i < HELD; ++i)
+        if (i * 64 <= groups) group_rows(v[i], lane, last, first[i], end[i]);
+    }
+    int total = 0;
+    each([&](int, int a, int b) {
+      total += __builtin_amdgcn_readlane(scan64((b - a + BM - 1) / BM, [](int x, int y) { return x + y; }), 63);
+      return false;
+    });
+    return total;
+  }
+  // tile number t: its group (`groups` for rows of no group), first row and
+  // number of rows; false past the last
+  __device__ __forceinline__ bool find(int t, RowTile& out) {
+    int before = 0;
+    return each([&](int g0, int a, int b) {
+      const int mine = (b - a + BM - 1) / BM;
+      const int incl = scan64(mine, [](int x, int y) { return x + y; });
+      const uint64_t past = __builtin_amdgcn_ballot_w64(before + incl > t);
+      if (past) {
+        const int l = __builtin_ctzll(past);
+        out.group = g0 + l;
+        out.row = __builtin_amdgcn_readlane(a, l) + (t - before - __builtin_amdgcn_readlane(incl - mine, l)) * BM;
+        const int left = __builtin_amdgcn_readlane(b, l) - out.row;
+        out.rows = left < BM ? left : BM;
+        return true;
+      }
+      before += __builtin_amdgcn_readlane(incl, 63);
+      return false;
+    });
+  }
+};
 
 }  // namespace half
 }  // namespace oz
