@@ -64,7 +64,7 @@ __global__ __launch_bounds__(256) void shrink_kernel(Adapter p) {
     a = next_adapter<1>(ids, rows, a, p.adapters);
     if (a == p.adapters) break;
     v4f acc[RB][TB] = {};
-    skinny<TYPE, RB, TB>((const char*)p.a + (a * p.a_stride + rank0 * p.lda) * 2, p.lda, ranks,
+    skinny<TYPE, RB, TB, 4>((const char*)p.a + (a * p.a_stride + rank0 * p.lda) * 2, p.lda, ranks,
                          (const char*)p.x + t0 * p.ldx * 2, p.ldx, rows, p.k, s0, s1, acc);
     skinny_join<RB, TB, 4>(acc, lds, [&](int t, int r, v4f v) {
       if (t >= rows || ids[t] != a || rank0 + r >= p.rank_pad) return;
@@ -217,7 +217,7 @@ __global__ __launch_bounds__(kServeWaves * 64) void serve_partials_kernel(Adapte
     const int ranks = p.rank - chunk * 16 < 16 ? p.rank - chunk * 16 : 16;
     range(split, p.splits, s0, s1);
     v4f acc[1][1] = {};
-    skinny<TYPE, 1, 1>((const char*)p.a + ((int64_t)a * p.a_stride + chunk * 16 * p.lda) * 2, p.lda, ranks,
+    skinny<TYPE, 1, 1, 8>((const char*)p.a + ((int64_t)a * p.a_stride + chunk * 16 * p.lda) * 2, p.lda, ranks,
                        (const char*)p.x + t * p.ldx * 2, p.ldx, 1, p.k, s0, s1, acc);
     skinny_join<1, 1, kServeWaves>(acc, lds, [&](int row, int r, v4f v) {
       if (row > 0) return;
@@ -233,7 +233,7 @@ __global__ __launch_bounds__(kServeWaves * 64) void serve_partials_kernel(Adapte
   const int rows = p.rows - t0 < 16 * TB ? p.rows - t0 : 16 * TB, cols = p.n - c0 < 16 * NB ? p.n - c0 : 16 * NB;
   range(split, p.base_splits, s0, s1);
   v4f acc[NB][TB] = {};
-  skinny<TYPE, NB, TB>((const char*)p.w + c0 * p.ldw * 2, p.ldw, cols, (const char*)p.x + t0 * p.ldx * 2, p.ldx, rows,
+  skinny<TYPE, NB, TB, (NB + TB <= 6 ? 4 : 2)>((const char*)p.w + c0 * p.ldw * 2, p.ldw, cols, (const char*)p.x + t0 * p.ldx * 2, p.ldx, rows,
                        p.k, s0, s1, acc);
   float* const out = p.partials + (int64_t)split * p.rows * p.n_pad;
   skinny_join<NB, TB, kServeWaves>(acc, lds, [&](int row, int c, v4f v) {

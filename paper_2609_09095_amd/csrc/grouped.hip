@@ -43,7 +43,7 @@ __global__ __launch_bounds__(T::THREADS, 1) void grouped_rows_kernel(GroupedRows
 
 // The same for few rows per group (serving): a block reads 16 NB columns of a
 // group's weights once, for at most 16 TB of its rows.
-template <int TYPE, int NB, int TB, int WAVES>
+template <int TYPE, int NB, int TB, int WAVES, int U>
 __global__ __launch_bounds__(WAVES * 64) void grouped_few_kernel(GroupedRows g) {
   using O = typename Out<TYPE>::type;
   __shared__ v4f lds[WAVES * TB * 16 * NB * 4];
@@ -62,7 +62,7 @@ __global__ __launch_bounds__(WAVES * 64) void grouped_few_kernel(GroupedRows g) 
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int steps = (g.depth + 31) / 32;
     const char* w = (const char*)g.w + (t.group * g.group_stride + c0 * g.ldw) * 2;
-    skinny<TYPE, NB, TB>(w, g.ldw, cols, (const char*)g.x + t.row * g.ldx * 2, g.ldx, t.rows, g.depth,
+    skinny<TYPE, NB, TB, U>(w, g.ldw, cols, (const char*)g.x + t.row * g.ldx * 2, g.ldx, t.rows, g.depth,
                          steps * wave / WAVES, steps * (wave + 1) / WAVES, acc);
   }
   O* const y = (O*)g.y + t.row * g.ldy + c0;
@@ -115,13 +115,13 @@ hipError_t run_rows(const GroupedRows& g, hipStream_t s) {
   return hipGetLastError();
 }
 
-template <int TYPE, int NB, int TB, int WAVES>
+template <int TYPE, int NB, int TB, int WAVES, int U>
 hipError_t run_few(const GroupedRows& g, hipStream_t s) {
   // a tile holds at least one row, and all but each group's last (and that of no group) are full
   const int64_t most = (int64_t)g.rows / (16 * TB) + g.groups + 1;
   const int64_t tiles = (most < g.rows ? most : g.rows) * ((g.cols + 16 * NB - 1) / (16 * NB));
   if (tiles * WAVES * 64 >= ((int64_t)1 << 32)) return hipErrorInvalidConfiguration;
-  grouped_few_kernel<TYPE, NB, TB, WAVES><<<dim3((uint32_t)((tiles + 7) & ~(int64_t)7)), dim3(WAVES * 64), 0, s>>>(g);
+  grouped_few_kernel<TYPE, NB, TB, WAVES, U><<<dim3((uint32_t)((tiles + 7) & ~(int64_t)7)), dim3(WAVES * 64), 0, s>>>(g);
   return hipGetLastError();
 }
 
@@ -137,10 +137,10 @@ hipError_t run_weights(const GroupedWeights& g, hipStream_t s) {
 template <int TYPE, int LB>
 hipError_t rows_of_type(const GroupedRows& g, bool dma, hipStream_t s) {
   if (LB == kAlong && few_rows(g.rows, g.groups)) switch (few_form(g.rows, g.groups, g.cols)) {
-      case kFew16: return run_few<TYPE, 1, 1, 8>(g, s);
-      case kFew32: return run_few<TYPE, 2, 2, 8>(g, s);
-      case kFew64x32: return run_few<TYPE, 4, 2, 4>(g, s);
-      case kFew64x64: return run_few<TYPE, 4, 4, 4>(g, s);
+      case kFew16: return run_few<TYPE, 1, 1, 8, 8>(g, s);
+      case kFew32: return run_few<TYPE, 2, 2, 8, 4>(g, s);
+      case kFew64x32: return run_few<TYPE, 4, 2, 4, 2>(g, s);
+      case kFew64x64: return run_few<TYPE, 4, 4, 4, 2>(g, s);
     }
   if (!dma) {
     if (masked_small(false, expected_row_tiles(g.rows, g.groups, 128) * ceil_div(g.cols, 128)))

@@ -83,7 +83,7 @@ constexpr bool few_rows(int64_t rows, int64_t groups) { return groups > 0 && row
 // Its blocks: 64 columns where that gives at least a block per CU (with 32 or,
 // above 16 rows a group, 64 rows each), else 16 columns (32 above 16 rows a
 // group, with 32 rows).  16 / 64 columns: 2, 8, 2048, 1024 4.0 / 6.8, 16, 1,
-// 4096, 4096 10.5 / 22; 256, 64, 1024, 2048 57 / 53, 64, 8, 4096, 2048 38 / 31.
+// 4096, 4096 10.5 / 22; 256, 64, 1024, 2048 57 / 51, 64, 8, 4096, 2048 38 / 30.
 enum FewForm { kFew16, kFew32, kFew64x32, kFew64x64 };
 constexpr FewForm few_form(int64_t rows, int64_t groups, int64_t cols) {
   const int64_t filled = groups < rows ? groups : rows;

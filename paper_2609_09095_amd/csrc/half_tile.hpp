@@ -664,9 +664,9 @@ __device__ __forceinline__ v4i load8(const char* row, int c, int cols) {
 
 // acc[i][j] += 16 columns of W (rows of its cols x k matrix, from w on) times
 // 16 rows of X, over the depths 32 s0 .. 32 s1 (below k).  Rows past the last
-// are read as the last one; their sums are not used.  Lane l of a block: row of
+// are read as the last one; their sums are not used.  U steps in flight.  Lane l of a block: row of
 // X l % 16, columns 4 (l / 16) .. + 3.
-template <int TYPE, int NB, int TB>
+template <int TYPE, int NB, int TB, int U>
 __device__ __forceinline__ void skinny(const char* w, int64_t ldw, int cols, const char* x, int64_t ldx, int rows,
                                        int k, int s0, int s1, v4f (&acc)[NB][TB]) {
   const int lane = threadIdx.x & 63, at = lane & 15, c0 = (lane >> 4) * 8;
@@ -676,7 +676,6 @@ __device__ __forceinline__ void skinny(const char* w, int64_t ldw, int cols, con
 #pragma unroll
   for (int j = 0; j < TB; ++j) px[j] = x + (int64_t)(j * 16 + at < rows ? j * 16 + at : rows - 1) * ldx * 2;
   const int whole = k / 32 < s1 ? k / 32 : s1;  // steps without an end inside
-  constexpr int U = NB + TB <= 2 ? 8 : NB + TB <= 6 ? 4 : 2;
   int s = s0;
   for (; s + U <= whole; s += U) {
     v4i fw[U][NB], fx[U][TB];
