@@ -44,7 +44,7 @@ __device__ __forceinline__ int next_adapter(const int* ids, int count, int after
 // Partial sums of X A_a^T: a block has 32 rows, 16 RB ranks and a part of the
 // depth, split again over its wavefronts; the adapters that its rows name in
 // turn.  grid (row tiles, parts x rank chunks)
-constexpr int kShrinkRows = 32;
+constexpr int kShrinkRows = 32, kShrinkTiles = 1024;  // rows of a block; from how many rows on tiles
 
 template <int TYPE, int RB>
 __global__ __launch_bounds__(256) void shrink_kernel(Adapter p) {
@@ -73,6 +73,48 @@ __global__ __launch_bounds__(256) void shrink_kernel(Adapter p) {
       *(v4f*)(p.h + ((int64_t)split * p.rows + t0 + t) * p.rank_pad + rank0 + r) = v;
     });
     __syncthreads();
+  }
+}
+
+// The same with whole tiles, 64 rows x 64 ranks, for many rows whose operands
+// can go to LDS by DMA: k = 4096, rank 64, 4096 rows 19 us against 32, the whole
+// call with 8192 rows 262 / 277; with 512 rows of rank 16 17.8 / 16.2.
+// grid (row tiles, parts x rank chunks)
+template <class T>
+__global__ __launch_bounds__(T::THREADS, 1) void shrink_tiles_kernel(Adapter p) {
+  static_assert(!T::WIDE && T::BM == 64);
+  __shared__ __attribute__((aligned(1024))) char lds[T::LDS + T::BM * 4];
+  int* const ids = (int*)(lds + T::LDS);
+  const int t0 = blockIdx.x * T::BM;
+  const int rows = p.rows - t0 < T::BM ? p.rows - t0 : T::BM;
+  const int split = blockIdx.y % p.splits, rank0 = blockIdx.y / p.splits * T::BN;
+  const int ranks = p.rank - rank0 < T::BN ? p.rank - rank0 : T::BN;
+  const int stages = (p.k + kDepth - 1) / kDepth;
+  const int d0 = stages * split / p.splits * kDepth, d1 = stages * (split + 1) / p.splits * kDepth;
+  const int depth = (d1 < p.k ? d1 : p.k) - d0;
+  if ((int)threadIdx.x < T::BM) ids[threadIdx.x] = (int)threadIdx.x < rows ? p.ids[t0 + threadIdx.x] : -1;
+  __syncthreads();
+  const int lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int row = wave / T::WC * T::MB * 32 + 4 * (lane >> 5), col = wave % T::WC * T::NB * 32 + (lane & 31);
+  for (int a = -1;;) {
+    a = next_adapter<1>(ids, rows, a, p.adapters);
+    if (a == p.adapters) break;
+    v16f acc[T::MB][T::NB] = {};
+    product<T>(Operand{(const char*)p.x + (t0 * p.ldx + d0) * 2, p.ldx, rows, p.k},
+               Operand{(const char*)p.a + (a * p.a_stride + rank0 * p.lda + d0) * 2, p.lda, ranks, p.k}, depth, lds, acc);
+    // lane l of a block: rank l % 32, rows 8 (i / 4) + 4 (l / 32) + i % 4; ranks past the last are zeros
+#pragma unroll
+    for (int x = 0; x < T::MB; ++x)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        const int t = row + 32 * x + 8 * (i >> 2) + (i & 3);
+        if (ids[t] != a) continue;
+#pragma unroll
+        for (int y = 0; y < T::NB; ++y)
+          if (rank0 + col + 32 * y < p.rank_pad)
+            p.h[((int64_t)split * p.rows + t0 + t) * p.rank_pad + rank0 + col + 32 * y] = acc[x][y][i];
+      }
   }
 }
 
@@ -318,8 +360,14 @@ hipError_t run(const Adapter& p, hipStream_t s) {
 
 template <int TYPE, int RB>
 hipError_t shrink(const Adapter& p, hipStream_t s) {
-  const dim3 grid((uint32_t)ceil_div(p.rows, kShrinkRows), (uint32_t)(p.splits * ceil_div(p.rank, 16 * RB)));
-  shrink_kernel<TYPE, RB><<<grid, dim3(256), 0, s>>>(p);
+  if (p.rows >= kShrinkTiles && dma_operand(p.x, p.ldx, p.k) && dma_operand(p.a, p.lda, p.k) && p.a_stride % 8 == 0) {
+    using T = Tile<TYPE, kAlong, kAlong, 2, 2, 1, 1, true, kF32, 4>;
+    const dim3 grid((uint32_t)ceil_div(p.rows, T::BM), (uint32_t)(p.splits * ceil_div(p.rank, T::BN)));
+    shrink_tiles_kernel<T><<<grid, dim3(T::THREADS), 0, s>>>(p);
+  } else {
+    const dim3 grid((uint32_t)ceil_div(p.rows, kShrinkRows), (uint32_t)(p.splits * ceil_div(p.rank, 16 * RB)));
+    shrink_kernel<TYPE, RB><<<grid, dim3(256), 0, s>>>(p);
+  }
   split_kernel<TYPE><<<dim3((uint32_t)ceil_div((int64_t)p.rows * (p.rank_pad / 4), 256)), dim3(256), 0, s>>>(p);
   return hipGetLastError();
 }

@@ -114,6 +114,18 @@ def test_adapter_forms(dtype, rows, n, k, tile, serve):
     check_adapter(rows, n, k, 5, 24, ids_of(rows, 5), dtype)
 
 
+# The products X A^T in tiles: ranks that fill no tile of 64, rows of many
+# adapters in any order, depths that end inside a stage.
+@pytest.mark.parametrize("rows, n, k, rank, order", [
+    (1024, 264, 520, 1, "any"), (1031, 520, 2056, 65, "any"), (1100, 512, 1032, 24, "sorted"),
+    (2049, 136, 8, 128, "any"), (1087, 264, 1096, 200, "sorted")])
+def test_adapter_many_rows(rows, n, k, rank, order):
+    ids = ids_of(rows, 9)
+    if order == "any":
+        ids = np.random.default_rng(rank).permutation(ids)
+    check_adapter(rows, n, k, 9, rank, ids, torch.bfloat16)
+
+
 @pytest.mark.parametrize("rows, n, k, small", [(400, 1000, 111, True), (2048, 2049, 137, False)])
 def test_adapter_masked(rows, n, k, small):
     assert bool(rules().rule_masked_small(0, -(-rows // 128) * -(-n // 128))) == small
