@@ -361,7 +361,7 @@ hipError_t run(const Adapter& p, hipStream_t s) {
 template <int TYPE, int RB>
 hipError_t shrink(const Adapter& p, hipStream_t s) {
   if (p.rows >= kShrinkTiles && dma_operand(p.x, p.ldx, p.k) && dma_operand(p.a, p.lda, p.k) && p.a_stride % 8 == 0) {
-    using T = Tile<TYPE, kAlong, kAlong, 2, 2, 1, 1, true, kF32, 4>;
+    using T = Tile<TYPE, kAlong, kAlong, 2, 2, 1, 1, true, kF32, 3>;
     const dim3 grid((uint32_t)ceil_div(p.rows, T::BM), (uint32_t)(p.splits * ceil_div(p.rank, T::BN)));
     shrink_tiles_kernel<T><<<grid, dim3(T::THREADS), 0, s>>>(p);
   } else {
@@ -384,7 +384,7 @@ hipError_t tiles(const Adapter& p, hipStream_t s) {
     return run<Tile<TYPE, kAlong, kAlong, 2, 4, 2, 1, false, TYPE>>(p, s);
   }
   switch (tile_of(middle, ceil_div(p.rows, 256) * ceil_div(p.n, 256))) {
-    case kSmallTile: return run<Tile<TYPE, kAlong, kAlong, 2, 2, 1, 1, true, TYPE, 4>>(p, s);
+    case kSmallTile: return run<Tile<TYPE, kAlong, kAlong, 2, 2, 1, 1, true, TYPE, 3>>(p, s);
     case kMiddleTile: return run<Tile<TYPE, kAlong, kAlong, 2, 2, 2, 2, true, TYPE>>(p, s);
     default: return run<Tile<TYPE, kAlong, kAlong, 2, 4, 4, 2, true, TYPE>>(p, s);
   }

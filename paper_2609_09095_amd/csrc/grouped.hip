@@ -148,7 +148,7 @@ hipError_t rows_of_type(const GroupedRows& g, bool dma, hipStream_t s) {
     return run_rows<Tile<TYPE, kAlong, LB, 2, 4, 2, 1, false, TYPE>>(g, s);
   }
   switch (rows_tile(g.rows, g.groups, g.cols)) {
-    case kSmallTile: return run_rows<Tile<TYPE, kAlong, LB, 2, 2, 1, 1, true, TYPE, 4>>(g, s);
+    case kSmallTile: return run_rows<Tile<TYPE, kAlong, LB, 2, 2, 1, 1, true, TYPE, 3>>(g, s);
     case kMiddleTile: return run_rows<Tile<TYPE, kAlong, LB, 2, 2, 2, 2, true, TYPE>>(g, s);
     default: return run_rows<Tile<TYPE, kAlong, LB, 2, 4, 4, 2, true, TYPE>>(g, s);
   }
@@ -162,7 +162,7 @@ hipError_t weights_of_type(const GroupedWeights& g, bool dma, hipStream_t s) {
     return run_weights<Tile<TYPE, kAcross, kAcross, 2, 4, 2, 1, false, OUT>>(g, s);
   }
   switch (weights_tile(g.n, g.k, g.groups)) {
-    case kSmallTile: return run_weights<Tile<TYPE, kAcross, kAcross, 2, 2, 1, 1, true, OUT, 4>>(g, s);
+    case kSmallTile: return run_weights<Tile<TYPE, kAcross, kAcross, 2, 2, 1, 1, true, OUT, 3>>(g, s);
     case kMiddleTile: return run_weights<Tile<TYPE, kAcross, kAcross, 2, 2, 2, 2, true, OUT>>(g, s);
     default: return run_weights<Tile<TYPE, kAcross, kAcross, 2, 4, 4, 2, true, OUT>>(g, s);
   }

@@ -36,36 +36,44 @@ constexpr TileSize large_or_middle(int64_t large, int64_t middle) {
   return cl < cm ? kLargeTile : kMiddleTile;
 }
 
-// Small tiles where middle ones would leave every other slot empty: 512, 8,
-// 4096, 2048 small 26 / middle 29, 512, 8, 1024, 1024 8.2 / 11.4; beyond 1024, 8,
+// Small tiles where middle ones would fill less than four fifths of the CUs.
+// Small / middle: rows, groups, n, k = 512, 8, 1024, 1024 8.5 / 11.4; 1536, 1,
+// 2048, 2048 (192 middle tiles) 24 / 25; beyond (224 to 256) 3584, 2, 1024, 1024
+// 18.5 / 13.9, 2048, 1, 2048, 2048 32 / 27, weights' gradient 34 / 27, 1024, 8,
 // 4096, 2048 44 / 30.
+constexpr int64_t kMiddleLeast = 205;
 constexpr TileSize tile_of(int64_t middle, int64_t large) {
-  return middle <= 256 ? kSmallTile : large_or_middle(large, middle);
+  return middle < kMiddleLeast ? kSmallTile : large_or_middle(large, middle);
 }
 
 // Large tiles beyond whole rounds that are worth a launch of their own in small
 // tiles (16 each): few, so that they fill no more than a round and a half of
-// those; 0: none.  2 x 4096 x 4096, a symmetric product's 272 tiles: OVER
+// those; 0: none.  2 x 4096 x 4096, a symmetric product's 272 tiles: 129 + 25 (S)
+// and 139 + 27 (P), middle tiles 180 and 191.
 constexpr int64_t large_tiles_over(int64_t large) {
   const int64_t over = large % 256;
   return large > 256 && over <= 48 ? over : 0;
 }
 
-// A grouped product by rows.
+// A grouped product by rows.  Middle tiles that are half empty on average have
+// to fill all CUs: 512, 8, 4096, 2048 small 23.5 / middle 25.6, but 640, 8, 4096,
+// 2048 29 / 27.
 constexpr TileSize rows_tile(int64_t rows, int64_t groups, int64_t cols) {
-  return tile_of(expected_row_tiles(rows, groups, 128) * ceil_div(cols, 128),
-                 expected_row_tiles(rows, groups, 256) * ceil_div(cols, 256));
+  const int64_t middle = expected_row_tiles(rows, groups, 128) * ceil_div(cols, 128);
+  if (rows <= 64 * groups && middle <= 256) return kSmallTile;
+  return tile_of(middle, expected_row_tiles(rows, groups, 256) * ceil_div(cols, 256));
 }
 
 // The weights' gradient, whose groups differ in depth: large tiles only where
 // several rounds even that out.  Large / middle, 32-bit output: 4096, 8, 4096,
 // 2048 102 / 127, 16384, 16, 4096, 2048 340 / 396; 8192, 16, 2048, 1024 71 / 58,
-// 20000, 2, 4096, 2048 381 / 312; small / middle: 700, 2, 512, 256 6.4 / 10, 512,
-// 8, 1024, 1024 12.7 / 11.3.
+// 20000, 2, 4096, 2048 381 / 312; small / middle: 700, 2, 512, 256 5.3 / 10,
+// beyond 205 middle tiles 4096, 7, 1024, 512 14.5 / 11.5, 2048, 2, 2048, 1024 19.9
+// / 16.8.
 constexpr TileSize weights_tile(int64_t n, int64_t k, int64_t groups) {
   const int64_t middle = groups * ceil_div(n, 128) * ceil_div(k, 128);
   if (groups == 1) return tile_of(middle, ceil_div(n, 256) * ceil_div(k, 256));
-  if (middle <= 256) return kSmallTile;
+  if (middle < kMiddleLeast) return kSmallTile;
   return groups * ceil_div(n, 256) * ceil_div(k, 256) >= 768 ? kLargeTile : kMiddleTile;
 }
 

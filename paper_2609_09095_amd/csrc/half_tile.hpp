@@ -460,7 +460,7 @@ __device__ __forceinline__ void stage_products(Loader& ld, const FA& fa, const F
 
 // acc += A B over `depth`; lds: T::LDS bytes, 1024-aligned.
 //
-// Two stages in LDS (four for small tiles).  The last K step's products of a
+// Two stages in LDS (three for small tiles).  The last K step's products of a
 // stage run behind the barrier that hands over to the next stage: their
 // fragments are in registers by then, so the matrix cores work while the next
 // stage's first fragments are read, and the buffer just freed takes the loads

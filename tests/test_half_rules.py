@@ -67,3 +67,11 @@ def test_expected_row_tiles():
     for rows, groups, bm in itertools.product((1, 2, 63, 64, 65, 1000, 4096, 1 << 30), (1, 2, 8, 64, 65536), (64, 128, 256)):
         t = L.rule_row_tiles(rows, groups, bm)
         assert -(-rows // bm) <= t <= rows // bm + groups + 1 and t >= min(groups, rows)
+
+
+def test_small_tiles_below_four_fifths_of_the_cus():
+    L = rules()
+    for c, want in (((1536, 1, 2048), SMALL), ((2048, 1, 2048), MIDDLE), ((3584, 2, 1024), MIDDLE),
+                    ((512, 8, 4096), SMALL), ((640, 8, 4096), MIDDLE)):
+        assert L.rule_rows_tile(*c) == want, c
+    assert L.rule_weights_tile(2048, 1024, 2) == MIDDLE and L.rule_weights_tile(1024, 512, 6) == SMALL
