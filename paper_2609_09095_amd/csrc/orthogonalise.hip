@@ -137,6 +137,33 @@ __device__ __forceinline__ bool take_diagonal(v16f& v, float& mine) {
   return (r >> 2 & 1) == lane >> 5;
 }
 
+// What store_wide left in LDS, transposed: out[c, r], whose rows have `rows`
+// elements (a multiple of 8, at 16 bytes).  Transposing loads give a lane 8 of
+// them, and 4 lanes a run of 64 bytes.
+template <class T>
+__device__ __forceinline__ void mirror_wide(char* lds, _Float16* out, int64_t ld, int rows, int cols) {
+  const int lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int r0 = wave / T::WC * T::MB * 32, c0 = wave % T::WC * T::NB * 32;
+  constexpr int PITCH = T::NB * 64, CH = T::NB * 4;
+  const auto mine = (lds_bytes)lds + wave * (T::MB * 32 * PITCH);
+  const int group = 8 * (lane >> 4), r = group + (lane >> 2 & 3), c = 4 * (lane & 3);
+  using tr = __attribute__((address_space(3))) v4s*;
+  auto at = [&](int row, int col) { return (tr)(mine + row * PITCH + (((col >> 3) ^ (row & (CH - 1))) << 4) + (col & 7) * 2); };
+#pragma unroll
+  for (int b = 0; b < T::NB * 2; ++b) {
+    const int col = c0 + b * 16 + (lane & 15);
+#pragma unroll
+    for (int a = 0; a < T::MB; ++a) {
+      const v4s lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16(at(a * 32 + r, b * 16 + c));
+      const v4s hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16(at(a * 32 + r + 4, b * 16 + c));
+      const int row = r0 + a * 32 + group;
+      if (row < rows && col < cols)
+        *(v4i*)(out + (int64_t)col * ld + row) = __builtin_bit_cast(v4i, v8s{lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]});
+    }
+  }
+}
+
 // A symmetric product A A^T (kAlong, A s x depth) or A^T A (kAcross, A
 // depth x s), the tiles on and above the diagonal, each stored twice: S, or with
 // SQUARE (A = So) P = b S + c S^2, their diagonals apart.  Block b takes the
@@ -145,11 +172,13 @@ __device__ __forceinline__ bool take_diagonal(v16f& v, float& mine) {
 // are meant.
 template <class T, bool SQUARE>
 __global__ __launch_bounds__(T::THREADS, 1) void gram_kernel(Orthogonalise o, const char* in, int s, int depth,
-                                                            int64_t ld, uint32_t first, uint32_t sub) {
+                                                            int64_t ld, uint32_t first, uint32_t tiles, uint32_t sub) {
   __shared__ __attribute__((aligned(1024))) char lds[T::LDS];
   static_assert(T::BM == T::BN && T::LA == T::LB && T::OUT == kF16, "square tiles");
   const uint32_t side = ((uint32_t)s + T::BM * sub - 1) / (T::BM * sub), triangle = side * (side + 1) / 2;
-  const uint32_t tile = first + blockIdx.x / (sub * sub), part = blockIdx.x % (sub * sub);
+  uint32_t place;
+  if (!block_place(blockIdx.x, tiles * sub * sub, place)) return;
+  const uint32_t tile = first + place / (sub * sub), part = place % (sub * sub);
   const uint32_t z = tile / triangle;
   uint32_t tm, tn;
   triangle_tile(tile - z * triangle, tm, tn);
@@ -237,17 +266,7 @@ __global__ __launch_bounds__(T::THREADS, 1) void gram_kernel(Orthogonalise o, co
   }
   store_wide<T>(acc, lds, out, s, rows, cols, false, [](int, int, float*) {});
   if (tm == tn) return;
-  // the mirror image: a half wavefront has 32 consecutive rows of one column
-  _Float16* const mirror = (_Float16*)(SQUARE ? o.p16 : o.s16) + z * square + (int64_t)c0 * s + r0;
-#pragma unroll
-  for (int x = 0; x < T::MB; ++x)
-#pragma unroll
-    for (int b = 0; b < T::NB; ++b)
-#pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        const int r = w.row0 + 32 * x, c = w.col0 + 32 * b + 8 * (i >> 2) + (i & 3);
-        if (r < rows && c < cols) mirror[(int64_t)c * s + r] = (_Float16)acc[x][b][i];
-      }
+  mirror_wide<T>(lds, (_Float16*)(SQUARE ? o.p16 : o.s16) + z * square + (int64_t)c0 * s + r0, s, rows, cols);
 }
 
 // X <- a X + P X (kAlong x kAcross) or, TALL, a X + X P (kAlong x kAlong: P is
@@ -506,8 +525,9 @@ template <class H, int L, bool SQUARE>
 void gram(const Orthogonalise& o, const char* in, int s, int depth, int64_t ld, int64_t first, int64_t tiles, int sub,
           hipStream_t st) {
   using T = typename H::template Of<L, L, kF16>;
-  gram_kernel<T, SQUARE><<<dim3((uint32_t)(tiles * sub * sub)), dim3(T::THREADS), 0, st>>>(
-      o, in, s, depth, ld, (uint32_t)first, (uint32_t)sub);
+  const uint32_t blocks = ((uint32_t)(tiles * sub * sub) + 7) & ~7u;
+  gram_kernel<T, SQUARE><<<dim3(blocks), dim3(T::THREADS), 0, st>>>(o, in, s, depth, ld, (uint32_t)first,
+                                                                    (uint32_t)tiles, (uint32_t)sub);
 }
 
 template <int L, bool SQUARE>
