@@ -217,18 +217,20 @@ __global__ __launch_bounds__(T::THREADS, 1) void gram_kernel(Orthogonalise o, co
   product<T>(Operand{a + r0 * step * 2, ld, rows, (int)ld}, Operand{a + c0 * step * 2, ld, cols, (int)ld}, depth, lds,
              acc);
   if constexpr (SQUARE) {
-    const float ks = kScaleP / kScaleS, kc = o.c * kScaleP / (kScaleS * kScaleS);
+    // (b + c (d_i + d_j)) So_ij in the operands' scales
+    const float ks = kScaleP / kScaleS, cs = o.c * ks, kc = o.c * kScaleP / (kScaleS * kScaleS);
     float4 dc[T::NB][4];
 #pragma unroll
     for (int b = 0; b < T::NB; ++b)
 #pragma unroll
       for (int q = 0; q < 4; ++q) {
         const int c = w.col0 + 32 * b + 8 * q;
-        dc[b][q] = *(const float4*)(d + c0 + (c < cols ? c : 0));
+        const float4 v = *(const float4*)(d + c0 + (c < cols ? c : 0));
+        dc[b][q] = float4{cs * v.x, cs * v.y, cs * v.z, cs * v.w};
       }
 #pragma unroll
     for (int x = 0; x < T::MB; ++x) {
-      const float di = d[r0 + (w.row0 + 32 * x < rows ? w.row0 + 32 * x : rows - 1)];
+      const float di = o.b * ks + cs * d[r0 + (w.row0 + 32 * x < rows ? w.row0 + 32 * x : rows - 1)];
       if constexpr (!EARLY) load_own(x, own[0]);
 #pragma unroll
       for (int b = 0; b < T::NB; ++b)
@@ -239,7 +241,7 @@ __global__ __launch_bounds__(T::THREADS, 1) void gram_kernel(Orthogonalise o, co
           const float dj[4] = {dc[b][q].x, dc[b][q].y, dc[b][q].z, dc[b][q].w};
 #pragma unroll
           for (int j = 0; j < 4; ++j)
-            acc[x][b][4 * q + j] = kc * acc[x][b][4 * q + j] + (o.b + o.c * (di + dj[j])) * ks * (float)e[j];
+            acc[x][b][4 * q + j] = __builtin_fmaf(di + dj[j], (float)e[j], kc * acc[x][b][4 * q + j]);
         }
     }
   } else {
@@ -248,24 +250,30 @@ __global__ __launch_bounds__(T::THREADS, 1) void gram_kernel(Orthogonalise o, co
 #pragma unroll
       for (int b = 0; b < T::NB; ++b) acc[x][b] *= kScaleS / (kScaleX * kScaleX);
   }
+  // the diagonal apart as the tile is stored: at most one element per lane and row of blocks
+  float mine[T::MB] = {};
+  int call = 0;  // block row a, block b and quad q in order: known when unrolled
+  store_wide<T>(acc, lds, out, s, rows, cols, false, [&](int r, int c, float* v) {
+    const int x = call++ / (T::NB * 4);
+    if (tm != tn) return;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      mine[x] = r == c + j ? v[j] : mine[x];
+      v[j] = r == c + j ? 0.0f : v[j];
+    }
+  });
   if (tm == tn) {
-    const int at = w.row0 - (threadIdx.x & 31), to = w.col0 - 4 * (threadIdx.x >> 5 & 1);  // the wavefront's blocks
+    // S_ii 2^10, or c (So^2)_ii 2^8 (So_ii is zero)
 #pragma unroll
-    for (int x = 0; x < T::MB; ++x)
-#pragma unroll
-      for (int b = 0; b < T::NB; ++b) {
-        if (at + 32 * x != to + 32 * b) continue;
-        // S_ii 2^10, or c (So^2)_ii 2^8 (So_ii is zero)
-        float mine;
-        const int r = w.row0 + 32 * x;
-        if (take_diagonal(acc[x][b], mine) && r < rows) {
-          const float di = SQUARE ? d[r0 + r] : 0.0f;
-          diagonal[r0 + r] = SQUARE ? (o.b + o.c * di) * di + mine * (1.0f / kScaleP) : mine * (1.0f / kScaleS);
-        }
-      }
+    for (int x = 0; x < T::MB; ++x) {
+      const int r = w.row0 + 32 * x;
+      const bool here = r >= w.col0 && r < w.col0 + T::NB * 32 && (r - w.col0 & 4) == 0;
+      const float di = SQUARE ? d[r0 + (r < rows ? r : rows - 1)] : 0.0f;
+      if (here && r < rows)
+        diagonal[r0 + r] = SQUARE ? (o.b + o.c * di) * di + mine[x] * (1.0f / kScaleP) : mine[x] * (1.0f / kScaleS);
+    }
+    return;
   }
-  store_wide<T>(acc, lds, out, s, rows, cols, false, [](int, int, float*) {});
-  if (tm == tn) return;
   mirror_wide<T>(lds, (_Float16*)(SQUARE ? o.p16 : o.s16) + z * square + (int64_t)c0 * s + r0, s, rows, cols);
 }
 
@@ -381,10 +389,10 @@ __global__ __launch_bounds__(T::THREADS, 1) void update_kernel(Orthogonalise o, 
           v = *whole.at(lane_row + 32 * (x & 1), lane_col + 32 * b + 8 * q);
         const float4 pj = TALL ? *(const float4*)(p + c0 + (c < cols ? c : 0)) : float4{pi, pi, pi, pi};
         float4 y;
-        y.x = (o.a + pj.x) * v.x + k * acc[x][b][4 * q];
-        y.y = (o.a + pj.y) * v.y + k * acc[x][b][4 * q + 1];
-        y.z = (o.a + pj.z) * v.z + k * acc[x][b][4 * q + 2];
-        y.w = (o.a + pj.w) * v.w + k * acc[x][b][4 * q + 3];
+        y.x = __builtin_fmaf(o.a + pj.x, v.x, k * acc[x][b][4 * q]);
+        y.y = __builtin_fmaf(o.a + pj.y, v.y, k * acc[x][b][4 * q + 1]);
+        y.z = __builtin_fmaf(o.a + pj.z, v.z, k * acc[x][b][4 * q + 2]);
+        y.w = __builtin_fmaf(o.a + pj.w, v.w, k * acc[x][b][4 * q + 3]);
         if constexpr (!LAST && !EARLY) *whole.at(lane_row + 32 * (x & 1), lane_col + 32 * b + 8 * q) = y;
         if constexpr (!LAST && EARLY)
           if (w.row0 + 32 * x < rows && c < cols) *(float4*)(x32 + (int64_t)r * o.np + c) = y;
@@ -411,8 +419,10 @@ __global__ __launch_bounds__(T::THREADS, 1) void update_kernel(Orthogonalise o, 
 // rows of 256 bytes have their 16-byte chunks XOR-swizzled by the row and are
 // read both ways, along a row and (transposing loads) across rows.  Tall
 // matrices are transposed as they are read and written.  32 x 128 x 128: a launch
-// of 39 us where the steps' launches took 95.
+// of 37 us where the steps' launches took 95.
 constexpr int kSide = 128, kRow = kSide * 2;
+constexpr float kBlockX = 32.0f;  // X's scale here, whose square is S's
+static_assert(kBlockX * kBlockX == kScaleS);
 
 __device__ __forceinline__ int block_offset(int row, int col) {
   return row * kRow + (((col >> 3) ^ (row & 15)) << 4) + (col & 7) * 2;
@@ -486,7 +496,7 @@ __global__ __launch_bounds__(512, 1) void small_kernel(Orthogonalise o, int step
     for (int i = 0; i < 16; ++i) {
       // (not by the product alone: padding stays zero for an infinite or NaN scale)
       const bool in = row + 32 * x < s && col + 8 * (i >> 2) + (i & 3) < l;
-      X[x][i] = in ? X[x][i] * scale : 0.0f;
+      X[x][i] = in ? X[x][i] * scale * kBlockX : 0.0f;
     }
   // the four outputs of group q of block x to LDS
   auto put = [&](char* to, int x, int q, float v0, float v1, float v2, float v3) __attribute__((always_inline)) {
@@ -495,7 +505,7 @@ __global__ __launch_bounds__(512, 1) void small_kernel(Orthogonalise o, int step
   const auto x3 = (lds_bytes)xs, s3 = (lds_bytes)ss;
   const int depth_s = (s + 15) / 16 * 16, depth_l = (l + 15) / 16 * 16;
   v16f acc[2];
-  const float ks = kScaleP / kScaleS, kc = o.c * kScaleP / (kScaleS * kScaleS);
+  const float ks = kScaleP / kScaleS, cs = o.c * ks, kc = o.c * kScaleP / (kScaleS * kScaleS);
   // Wavefronts whose outputs all lie past the edge only wait.  (Blocks of 32 rows
   // past it that share a wavefront may then hold anything: they are nobody's
   // depth and not stored.)
@@ -506,15 +516,13 @@ __global__ __launch_bounds__(512, 1) void small_kernel(Orthogonalise o, int step
       for (int x = 0; x < 2; ++x)
 #pragma unroll
         for (int q = 0; q < 4; ++q)
-          put(xs, x, q, X[x][4 * q] * kScaleX, X[x][4 * q + 1] * kScaleX, X[x][4 * q + 2] * kScaleX,
-              X[x][4 * q + 3] * kScaleX);
+          put(xs, x, q, X[x][4 * q], X[x][4 * q + 1], X[x][4 * q + 2], X[x][4 * q + 3]);
     }
     __syncthreads();
     if (in_s) {
       block_product<false>(x3, x3, row0, col0, depth_l, acc);
 #pragma unroll
       for (int x = 0; x < 2; ++x) {
-        acc[x] *= kScaleS / (kScaleX * kScaleX);
         float mine;
         if (row0 + 32 * x == col0 && take_diagonal(acc[x], mine)) diag_s[row + 32 * x] = mine * (1.0f / kScaleS);
 #pragma unroll
@@ -528,21 +536,21 @@ __global__ __launch_bounds__(512, 1) void small_kernel(Orthogonalise o, int step
 #pragma unroll
       for (int x = 0; x < 2; ++x) {
         const int r = row + 32 * x;
-        const float di = diag_s[r];
+        const float d = diag_s[r], di = o.b * ks + cs * d;
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
           typedef _Float16 h4 __attribute__((ext_vector_type(4)));
           const int c = col + 8 * q;
           const h4 e = *(const h4*)(ss + block_offset(r, c));
           const float4 dj = *(const float4*)(diag_s + c);
-          const float d[4] = {dj.x, dj.y, dj.z, dj.w};
+          const float dc[4] = {cs * dj.x, cs * dj.y, cs * dj.z, cs * dj.w};
 #pragma unroll
           for (int j = 0; j < 4; ++j)
-            acc[x][4 * q + j] = kc * acc[x][4 * q + j] + (o.b + o.c * (di + d[j])) * ks * (float)e[j];
+            acc[x][4 * q + j] = __builtin_fmaf(di + dc[j], (float)e[j], kc * acc[x][4 * q + j]);
         }
         float mine;
         if (row0 + 32 * x == col0 && take_diagonal(acc[x], mine))
-          diag_p[r] = (o.b + o.c * di) * di + mine * (1.0f / kScaleP);
+          diag_p[r] = (o.b + o.c * d) * d + mine * (1.0f / kScaleP);
       }
     }
     __syncthreads();
@@ -560,7 +568,7 @@ __global__ __launch_bounds__(512, 1) void small_kernel(Orthogonalise o, int step
       for (int x = 0; x < 2; ++x) {
         const float a = o.a + diag_p[row + 32 * x];
 #pragma unroll
-        for (int i = 0; i < 16; ++i) X[x][i] = a * X[x][i] + (1.0f / (kScaleX * kScaleP)) * acc[x][i];
+        for (int i = 0; i < 16; ++i) X[x][i] = __builtin_fmaf(a, X[x][i], (1.0f / kScaleP) * acc[x][i]);
       }
     }
     __syncthreads();
@@ -572,7 +580,7 @@ __global__ __launch_bounds__(512, 1) void small_kernel(Orthogonalise o, int step
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
       const int r = row + 32 * x, c = col + 8 * (i >> 2) + (i & 3);
-      if (r < s && c < l) out[r * out_r + c * out_c] = (__bf16)X[x][i];
+      if (r < s && c < l) out[r * out_r + c * out_c] = (__bf16)(X[x][i] * (1.0f / kBlockX));
     }
 }
 
