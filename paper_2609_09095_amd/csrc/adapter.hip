@@ -227,8 +227,9 @@ __global__ __launch_bounds__(T::THREADS, 1) void adapter_kernel(Adapter p) {
   if (p.rank > 0)
     for (int i = threadIdx.x; i < T::BM; i += T::THREADS) ids[i] = i < rows ? p.ids[r0 + i] : -1;
   v16f acc[T::MB][T::NB] = {};
-  product<T>(Operand{(const char*)p.x + r0 * p.ldx * 2, p.ldx, rows, p.k},
-             Operand{(const char*)p.w + c0 * p.ldw * 2, p.ldw, cols, p.k}, p.k, lds, acc);
+  if (!product<T>(Operand{(const char*)p.x + r0 * p.ldx * 2, p.ldx, rows, p.k},
+                  Operand{(const char*)p.w + c0 * p.ldw * 2, p.ldw, cols, p.k}, p.k, lds, acc))
+    return;
   if (p.rank > 0) expand<T>(p, r0, rows, c0, cols, ids, lds, acc);
   store<T>(acc, lds, (char*)p.y + (r0 * p.ldy + c0) * 2, p.ldy, rows, cols, p.stream);
 }
@@ -380,6 +381,8 @@ hipError_t tiles(const Adapter& p, hipStream_t s) {
   }
   const int64_t middle = ceil_div(p.rows, 128) * ceil_div(p.n, 128);
   if (!(dma_operand(p.x, p.ldx, p.k) && dma_operand(p.w, p.ldw, p.k))) {
+    if (masked_sets(ceil_div(p.rows, 64) * ceil_div(p.n, 64), p.k))
+      return run<Tile<TYPE, kAlong, kAlong, 2, 2, 1, 1, false, TYPE, 2, 4>>(p, s);
     if (masked_small(false, middle)) return run<Tile<TYPE, kAlong, kAlong, 2, 2, 1, 1, false, TYPE>>(p, s);
     return run<Tile<TYPE, kAlong, kAlong, 2, 4, 2, 1, false, TYPE>>(p, s);
   }

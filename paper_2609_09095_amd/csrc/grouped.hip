@@ -37,7 +37,7 @@ __global__ __launch_bounds__(T::THREADS, 1) void grouped_rows_kernel(GroupedRows
   const Operand b{w + (T::LB == kAlong ? c0 * g.ldw : (int64_t)c0) * 2, g.ldw, cols,
                   T::LB == kAlong ? g.depth : g.cols};
   v16f acc[T::MB][T::NB] = {};
-  product<T>(a, b, none ? 0 : g.depth, lds, acc);
+  if (!product<T>(a, b, none ? 0 : g.depth, lds, acc)) return;
   store<T>(acc, lds, (char*)g.y + (t.row * g.ldy + c0) * 2, g.ldy, t.rows, cols, g.stream);
 }
 
@@ -102,7 +102,7 @@ __global__ __launch_bounds__(T::THREADS, 1) void grouped_weights_kernel(GroupedW
   const Operand a{(const char*)g.dy + (first * g.lddy + r0) * 2, g.lddy, rows, g.n};
   const Operand b{(const char*)g.x + (first * g.ldx + c0) * 2, g.ldx, cols, g.k};
   v16f acc[T::MB][T::NB] = {};
-  product<T>(a, b, end - first, lds, acc);
+  if (!product<T>(a, b, end - first, lds, acc)) return;
   constexpr int E = sizeof(typename Out<T::OUT>::type);
   store<T>(acc, lds, (char*)g.dw + (group * g.group_stride + r0 * g.lddw + c0) * E, g.lddw, rows, cols, g.stream);
 }
@@ -143,6 +143,8 @@ hipError_t rows_of_type(const GroupedRows& g, bool dma, hipStream_t s) {
       case kFew64x64: return run_few<TYPE, 4, 4, 4, 2>(g, s);
     }
   if (!dma) {
+    if (masked_sets(expected_row_tiles(g.rows, g.groups, 64) * ceil_div(g.cols, 64), g.depth))
+      return run_rows<Tile<TYPE, kAlong, LB, 2, 2, 1, 1, false, TYPE, 2, 4>>(g, s);
     if (masked_small(false, expected_row_tiles(g.rows, g.groups, 128) * ceil_div(g.cols, 128)))
       return run_rows<Tile<TYPE, kAlong, LB, 2, 2, 1, 1, false, TYPE>>(g, s);
     return run_rows<Tile<TYPE, kAlong, LB, 2, 4, 2, 1, false, TYPE>>(g, s);
@@ -157,6 +159,8 @@ hipError_t rows_of_type(const GroupedRows& g, bool dma, hipStream_t s) {
 template <int TYPE, int OUT>
 hipError_t weights_of_type(const GroupedWeights& g, bool dma, hipStream_t s) {
   if (!dma) {
+    if (masked_sets(g.groups * ceil_div(g.n, 64) * ceil_div(g.k, 64), g.rows / g.groups))  // their average depth
+      return run_weights<Tile<TYPE, kAcross, kAcross, 2, 2, 1, 1, false, OUT, 2, 4>>(g, s);
     if (masked_small(true, g.groups * ceil_div(g.n, 128) * ceil_div(g.k, 128)))
       return run_weights<Tile<TYPE, kAcross, kAcross, 2, 2, 1, 1, false, OUT>>(g, s);
     return run_weights<Tile<TYPE, kAcross, kAcross, 2, 4, 2, 1, false, OUT>>(g, s);

@@ -83,6 +83,14 @@ constexpr TileSize weights_tile(int64_t n, int64_t k, int64_t groups) {
 // 16384, 8, 1031, 2049: weights' gradient 230 / 159.
 constexpr bool masked_small(bool weights, int64_t middle_tiles) { return middle_tiles <= (weights ? 512 : 256); }
 
+// Small tiles of such operands with four sets of wavefronts that share the depth
+// (a stage waits for loads into registers), where no CU has a second tile: one
+// set / four: weights' gradient of 8704, 4, 389, 263 39 / 25, input gradient of 300,
+// 3, 1000, 777 16.7 / 12.8, but 700, 2, 513, 257 12 / 12, weights' gradient 9.8 /
+// 10.8.  (With loads into LDS one set already takes what a CU can: 1024, 1, 512,
+// 4096 22.1 / 21.2, 1024, 1, 1024, 1024 8.7 / 9.6.)
+constexpr bool masked_sets(int64_t small_tiles, int64_t depth) { return small_tiles <= 256 && depth > 640; }
+
 // Few rows per group: the weights go straight into fragments (at most 48 rows
 // a group on average).  Few-row form / tiles: 256, 8, 4096, 2048 42 / 51, 384,
 // 8, 2048, 2048 32 / 32, 512, 8, 4096, 2048 62 / 30.

@@ -101,17 +101,20 @@ struct MaskedLoads;
 // A tile's shape: WR x WC wavefronts, each MB x NB blocks of 32 x 32 outputs.
 // OUT: the output type.  A 16-bit output's blocks are multiplied transposed
 // (WIDE), which gives a lane four consecutive columns of one row.
-// BUFS: stages in LDS.
-template <int TYPE_, int LA_, int LB_, int WR_, int WC_, int MB_, int NB_, bool DMA_, int OUT_, int BUFS_ = 2>
+// BUFS: stages in LDS.  KG: sets of such wavefronts, each with its own stages and
+// a part of the depth; the first set adds up the sums and stores.
+template <int TYPE_, int LA_, int LB_, int WR_, int WC_, int MB_, int NB_, bool DMA_, int OUT_, int BUFS_ = 2,
+          int KG_ = 1>
 struct Tile {
   static constexpr int TYPE = TYPE_, LA = LA_, LB = LB_, WR = WR_, WC = WC_, MB = MB_, NB = NB_, OUT = OUT_;
   static constexpr bool DMA = DMA_, WIDE = OUT_ != kF32;
   static constexpr int BM = WR * MB * 32, BN = WC * NB * 32;
-  static constexpr int WAVES = WR * WC, THREADS = WAVES * 64;
+  static constexpr int WAVES = WR * WC, KG = KG_, THREADS = KG * WAVES * 64;
   static constexpr int A_BYTES = BM * kDepth * 2, B_BYTES = BN * kDepth * 2;
-  static constexpr int BUFS = BUFS_, STAGE = A_BYTES + B_BYTES, LDS = BUFS * STAGE;
+  static constexpr int BUFS = BUFS_, STAGE = A_BYTES + B_BYTES, SET = BUFS * STAGE, LDS = KG * SET;
   static constexpr int ADMA = A_BYTES / 1024 / WAVES, BDMA = B_BYTES / 1024 / WAVES;
   using Loads = std::conditional_t<DMA, DmaLoads<Tile>, MaskedLoads<Tile>>;
+  static_assert(KG == 1 || BM * BN * 4 <= SET, "a set's sums fit its stages' LDS");
   static_assert(ADMA * WAVES * 1024 == A_BYTES && BDMA * WAVES * 1024 == B_BYTES, "whole slabs per wavefront");
 };
 
@@ -411,7 +414,7 @@ struct Fragments {
 template <class T>
 __device__ __forceinline__ int next_buffer(int cur) {
   if constexpr (T::BUFS == 2) return cur ^ T::STAGE;
-  return cur + T::STAGE < T::LDS ? cur + T::STAGE : 0;
+  return cur + T::STAGE < T::SET ? cur + T::STAGE : 0;
 }
 
 // One stage's products; on entry the fragments of its first K step are in
@@ -470,14 +473,27 @@ __device__ __forceinline__ void stage_products(Loader& ld, const FA& fa, const F
 //
 // Wavefronts whose rows all lie past the tile's edge load and wait like the
 // others, but multiply nothing (the matrix cores and the clock are theirs).
+//
+// With KG sets of wavefronts all run the same number of stages (a set whose part
+// is empty repeats the first one's and is left out of the sum).  The sums are
+// added in the sets' order.  False: the wavefront's set is done.
 template <class T>
-__device__ __forceinline__ void product(const Operand& a, const Operand& b, int depth, char* lds,
-                                        v16f (&acc)[T::MB][T::NB]) {
+__device__ __forceinline__ bool product(Operand a, Operand b, int depth, char* lds, v16f (&acc)[T::MB][T::NB]) {
   const int lane = threadIdx.x & 63;
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int all = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), set = all / T::WAVES, wave = all % T::WAVES;
   const int wr = wave / T::WC, wc = wave % T::WC;
-  const int nst = (depth + kDepth - 1) / kDepth;
-  if (nst == 0) return;
+  int nst = (depth + kDepth - 1) / kDepth;
+  if (nst == 0) return set == 0;
+  const int parts = nst;
+  char* const sets = lds;
+  if constexpr (T::KG > 1) {
+    nst = (nst + T::KG - 1) / T::KG;
+    const int first = set * nst < parts ? set * nst * kDepth : 0;
+    a.p += (T::LA == kAlong ? (int64_t)first : first * a.ld) * 2;
+    b.p += (T::LB == kAlong ? (int64_t)first : first * b.ld) * 2;
+    depth -= first;
+    lds += set * T::SET;
+  }
   constexpr int ND = T::ADMA + T::BDMA;
   using Loader = typename T::Loads;
   Loader ld;
@@ -516,6 +532,32 @@ __device__ __forceinline__ void product(const Operand& a, const Operand& b, int 
   }
   __builtin_amdgcn_s_waitcnt(0);  // the look-ahead past the end (zeros) lands before LDS is used again
   __syncthreads();
+  if constexpr (T::KG > 1) {
+    constexpr int EACH = T::WAVES * 64;
+    float* const mine = (float*)lds + wave * 64 + lane;
+    if (set > 0) {
+#pragma unroll
+      for (int x = 0; x < T::MB; ++x)
+#pragma unroll
+        for (int y = 0; y < T::NB; ++y)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) mine[((x * T::NB + y) * 16 + i) * EACH] = acc[x][y][i];
+    }
+    __syncthreads();
+    if (set > 0) return false;
+#pragma unroll
+    for (int g = 1; g < T::KG; ++g) {
+      if (g * nst >= parts) break;
+      const float* const other = mine + g * (T::SET / 4);
+#pragma unroll
+      for (int x = 0; x < T::MB; ++x)
+#pragma unroll
+        for (int y = 0; y < T::NB; ++y)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) acc[x][y][i] += other[((x * T::NB + y) * 16 + i) * EACH];
+    }
+  }
+  return true;
 }
 
 // Four consecutive outputs of a row, rounded to 16 bits.

@@ -13,6 +13,7 @@ int rule_few_form(int64_t rows, int64_t groups, int64_t cols) { return few_form(
 int rule_masked_small(int weights, int64_t middle) { return masked_small(weights != 0, middle); }
 int64_t rule_row_tiles(int64_t rows, int64_t groups, int64_t bm) { return expected_row_tiles(rows, groups, bm); }
 int64_t rule_tiles_over(int64_t large) { return large_tiles_over(large); }
+int rule_masked_sets(int64_t tiles, int64_t depth) { return masked_sets(tiles, depth); }
 int rule_serve_rows(int64_t rows, int64_t n, int64_t k) { return adapter_plan(rows, n, k, 16).serve_rows; }
 int rule_serve_parts(int64_t rows, int64_t n, int64_t k) { return adapter_plan(rows, n, k, 16).base_splits; }
 int rule_shrink_parts(int64_t rows, int64_t n, int64_t k) { return adapter_plan(rows, n, k, 16).splits; }

@@ -52,6 +52,26 @@ def test_grouped_rows_masked(rows, groups, n, k, small):
     check_all(rows, n, k, sizes_of(rows, groups), torch.bfloat16)
 
 
+# Unaligned operands of a long depth in few tiles: sets of wavefronts share it.
+# Groups of fewer stages than sets (and of none) leave sets without a part.
+@pytest.mark.parametrize("sizes, n, k", [([2100, 0, 1, 70, 130, 1700], 70, 65), ([641, 700], 129, 33), ([2000], 5, 3)])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+def test_weights_of_long_groups_masked(sizes, n, k, dtype):
+    assert rules().rule_masked_sets(len(sizes) * -(-n // 64) * -(-k // 64), sum(sizes) // len(sizes))
+    check_all(sum(sizes), n, k, sizes, dtype)
+
+
+@pytest.mark.parametrize("rows, groups, n, k", [(300, 3, 129, 777), (200, 1, 641, 1500), (130, 2, 1001, 643)])
+def test_rows_of_long_depths_masked(rows, groups, n, k):
+    assert rules().rule_masked_sets(rules().rule_row_tiles(rows, groups, 64) * -(-n // 64), k)
+    check_all(rows, n, k, sizes_of(rows, groups), torch.bfloat16)
+
+
+def test_adapter_of_long_depths_masked():
+    assert adapter(450, 600, 777)[1] == 0 and rules().rule_masked_sets(8 * 10, 777)
+    check_adapter(450, 600, 777, 5, 20, ids_of(450, 5), torch.bfloat16)
+
+
 @pytest.mark.parametrize("rows, groups, n, k, want", [(700, 2, 512, 256, SMALL), (900, 8, 1024, 1024, MIDDLE),
                                                        (900, 12, 2048, 2048, LARGE), (300, 1, 2048, 2304, MIDDLE),
                                                        (300, 1, 4096, 4096, LARGE)])
