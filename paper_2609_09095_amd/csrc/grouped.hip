@@ -18,6 +18,12 @@ namespace {
 
 // Y (rows x cols) = X (rows x depth) times the group's weights: kAlong for
 // weights cols x depth, kAcross for depth x cols.
+//
+// 2 rows cols depth operations on operands read about once per XCD: bound by the
+// matrix cores and the clock they leave.  8192 x 8192 x 8192, one group: 815 us (1350
+// TFLOP/s) in either layout, the library's own product of that size 765 us.
+// 16384 rows of 16 uneven groups, 4096 x 2048: 294 us (935 TFLOP/s): each group's
+// last tile is partly filled, and the tiles are 4.3 rounds of the CUs.
 template <class T>
 __global__ __launch_bounds__(T::THREADS, 1) void grouped_rows_kernel(GroupedRows g) {
   __shared__ __attribute__((aligned(1024))) char lds[T::LDS];
@@ -42,7 +48,10 @@ __global__ __launch_bounds__(T::THREADS, 1) void grouped_rows_kernel(GroupedRows
 }
 
 // The same for few rows per group (serving): a block reads 16 NB columns of a
-// group's weights once, for at most 16 TB of its rows.
+// group's weights once, for at most 16 TB of its rows.  Bound by that read: 256
+// rows of 64 groups, 1024 x 2048: 50 us (5.4 TB/s, a large copy's rate).  With
+// little to read by the launch and the chain of loads: 2 rows, two of 8 groups,
+// 2048 x 1024: 4.0 us.
 template <int TYPE, int NB, int TB, int WAVES, int U>
 __global__ __launch_bounds__(WAVES * 64) void grouped_few_kernel(GroupedRows g) {
   using O = typename Out<TYPE>::type;
@@ -80,7 +89,11 @@ __global__ __launch_bounds__(WAVES * 64) void grouped_few_kernel(GroupedRows g) 
   });
 }
 
-// dW_g (n x k) = dY_g^T X_g; a group without rows gets zeros.
+// dW_g (n x k) = dY_g^T X_g; a group without rows gets zeros.  One tile sums over
+// all of its group's rows, so nothing is joined between blocks.  8192 x 8192 x
+// 8192: 820 us (1340 TFLOP/s).  32768 rows of 32 groups, 2048 x 4096, 32-bit
+// output: about 610 us (900 TFLOP/s): 1 GB of outputs leave past the caches
+// between the tiles' products.
 template <class T>
 __global__ __launch_bounds__(T::THREADS, 1) void grouped_weights_kernel(GroupedWeights g) {
   __shared__ __attribute__((aligned(1024))) char lds[T::LDS];
