@@ -342,9 +342,10 @@ ozaki25_status ozaki25_dgemm_noalloc(int64_t m, int64_t n, int64_t k, const doub
  * (to nearest even).  Row-major matrices with pitches in elements; device
  * pointers aligned to their element; any pitch of at least the row length up
  * to OZAKI25_MAX_LD.  Rows that start on 16 bytes and sizes that are multiples
- * of 8 take the faster loads.  Nothing is allocated, and every call may be
- * captured into a graph.  Sums run in an order fixed by the sizes and group
- * ends: the same inputs give the same bits. */
+ * of 8 take the faster loads.  The grouped products need no memory of their
+ * own; the others allocate only where no workspace is given.  With one, every
+ * call may be captured into a graph.  Sums run in an order fixed by the sizes
+ * and group ends: the same inputs give the same bits. */
 typedef enum { OZAKI25_BF16 = 0, OZAKI25_F16 = 1, OZAKI25_F32 = 2 } ozaki25_dtype;
 
 #define OZAKI25_MAX_ROWS 1073741824  /* 2^30: rows of an activation */
