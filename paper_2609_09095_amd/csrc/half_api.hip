@@ -136,7 +136,7 @@ size_t ozaki25_adapter_matmul_workspace_size(int64_t rows, int64_t n, int64_t k,
   if (rows <= 0 || n <= 0 || k < 0 || adapters < 0 || rank < 0 || rank > OZAKI25_MAX_RANK ||
       too_large(rows, n, k, adapters))
     return 0;
-  const oz::half::AdapterPlan a = oz::half::adapter_plan(rows, n, k, pad16(rank));
+  const oz::half::AdapterPlan a = oz::half::adapter_plan(rows, n, k, pad16(rank), adapters);
   return a.h_bytes + a.h16_bytes + a.partial_bytes;
 }
 
@@ -180,7 +180,7 @@ ozaki25_status ozaki25_adapter_matmul(int64_t rows, int64_t n, int64_t k, int64_
   p.scales = scales, p.y = Y, p.ldy = ldy;
   p.rows = (int)rows, p.n = (int)n, p.k = (int)k, p.adapters = any ? (int)adapters : 0, p.rank = any ? (int)rank : 0;
   p.rank_pad = (int)pad16(rank), p.n_pad = (int)((n + 3) / 4 * 4);
-  const oz::half::AdapterPlan plan = oz::half::adapter_plan(rows, n, k, pad16(rank));
+  const oz::half::AdapterPlan plan = oz::half::adapter_plan(rows, n, k, pad16(rank), adapters);
   return room.give(status_of(oz::half::launch_adapter(p, plan, room.p, (int)type, (hipStream_t)stream)));
 }
 

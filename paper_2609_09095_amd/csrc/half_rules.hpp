@@ -127,10 +127,23 @@ constexpr int clamp_parts(int64_t parts, int64_t most) {
 // 4096, 16 47 / 50, 512, 1024, 1024, 16 19 / 16, 512, 4096, 4096, 64 157 / 49.
 constexpr int64_t kServeRows = 128, kServeOutputs = 1 << 18;
 
-constexpr AdapterPlan adapter_plan(int64_t rows, int64_t n, int64_t k, int64_t rank_pad) {
+// Rows whose adapters the tiles would go through one after the other, up to 64 in
+// a tile of 64 rows.  Few-row form / tiles, an adapter of its own choice for each
+// row (rows, n, k, rank, adapters): 256, 4096, 4096, 16, 8 47 / 60; the same of 16
+// 47 / 87; rank 64 of 64 92 / 185; 512, 1024, 1024, 16, 32 19 / 103; 333, 1000, 1111,
+// 16, 16 22 / 89; 512, 2048, 2048, 64, 32 76 / 152, but the same in runs of 16 rows
+// 75 / 45 and 512, 4096, 4096, 16, 16 85 / 95, in runs 85 / 57.
+constexpr bool serve_many(int64_t rows, int64_t n, int64_t k, int64_t rank_pad, int64_t adapters) {
+  if (rank_pad == 0) return false;
+  if (rows <= 2 * kServeRows) return 2 * adapters >= rank_pad;
+  return rows <= 4 * kServeRows && adapters >= 16 && rows * n * k <= (adapters < 64 ? adapters : 64) << 26;
+}
+
+constexpr AdapterPlan adapter_plan(int64_t rows, int64_t n, int64_t k, int64_t rank_pad, int64_t adapters = 0) {
   AdapterPlan a{};
   const int64_t over = rows % 256;
-  if (rows <= kServeRows || (rows <= 4 * kServeRows && rows * n <= kServeOutputs)) {
+  if (rows <= kServeRows || (rows <= 4 * kServeRows && rows * n <= kServeOutputs) ||
+      serve_many(rows, n, k, rank_pad, adapters)) {
     a.serve_rows = (int)rows;
   } else if (over > 0 && over <= 64 && rows > 256) {
     // rows that would take large tiles a round of their own

@@ -134,6 +134,18 @@ def test_adapter_forms(dtype, rows, n, k, tile, serve):
     check_adapter(rows, n, k, 5, 24, ids_of(rows, 5), dtype)
 
 
+# Rows of many adapters, each its own choice: few of them in the few-row form,
+# more in tiles that go through up to 64 adapters each.
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("rows, n, k, adapters, rank, many", [
+    (129, 4100, 520, 16, 24, 1), (256, 2056, 777, 70, 130, 0), (255, 2056, 777, 130, 256, 1), (333, 1000, 1111, 16, 16, 1),
+    (512, 1024, 264, 64, 65, 1), (500, 1025, 264, 15, 8, 0), (512, 3000, 4096, 64, 16, 0)])
+def test_many_adapters(dtype, rows, n, k, adapters, rank, many):
+    assert rules().rule_serve_many(rows, n, k, -(-rank // 16) * 16, adapters) == many
+    ids = np.random.default_rng(rows).integers(-1, adapters + 1, rows)
+    check_adapter(rows, n, k, adapters, rank, ids, dtype)
+
+
 # The products X A^T in tiles: ranks that fill no tile of 64, rows of many
 # adapters in any order, depths that end inside a stage.
 @pytest.mark.parametrize("rows, n, k, rank, order", [
