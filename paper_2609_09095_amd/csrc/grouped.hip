@@ -149,7 +149,8 @@ hipError_t run_weights(const GroupedWeights& g, hipStream_t s) {
 
 template <int TYPE, int LB>
 hipError_t rows_of_type(const GroupedRows& g, bool dma, hipStream_t s) {
-  if (LB == kAlong && few_rows(g.rows, g.groups)) switch (few_form(g.rows, g.groups, g.cols)) {
+  const bool few = few_rows(g.rows, g.groups) && (dma || few_rows_masked(g.rows, g.groups, g.cols, g.depth));
+  if (LB == kAlong && few) switch (few_form(g.rows, g.groups, g.cols)) {
       case kFew16: return run_few<TYPE, 1, 1, 8, 8>(g, s);
       case kFew32: return run_few<TYPE, 2, 2, 8, 4>(g, s);
       case kFew64x32: return run_few<TYPE, 4, 2, 4, 2>(g, s);

@@ -96,6 +96,19 @@ constexpr bool masked_sets(int64_t small_tiles, int64_t depth) { return small_ti
 // 8, 2048, 2048 32 / 32, 512, 8, 4096, 2048 62 / 30.
 constexpr bool few_rows(int64_t rows, int64_t groups) { return groups > 0 && rows <= 48 * groups; }
 
+// The same for operands that cannot go to LDS by DMA: a fragment's rows then start
+// anywhere in a cache line, and the tiles read them in longer pieces.  Few-row form /
+// tiles: 960, 29, 1024, 1971 74 / 35, 3000, 64, 1000, 777 77 / 27, 500, 16, 3001, 3000
+// 96 / 75; with at most 16 rows a group 100, 29, 1024, 1971 50 / 37, 64, 8, 2048,
+// 2047 37 / 24, but short depths, many tiles or few of them 128, 8, 512, 513 9.0 /
+// 10.3, 300, 64, 4000, 777 127 / 135, 250, 16, 3001, 3000 63 / 74, 16, 1, 4096, 4095
+// 27 / 30.  (One or two rows a group: the tiles would be empty.)
+constexpr bool few_rows_masked(int64_t rows, int64_t groups, int64_t cols, int64_t depth) {
+  if (rows <= 2 * groups) return true;
+  const int64_t tiles = expected_row_tiles(rows, groups, 64) * ceil_div(cols, 64);
+  return rows <= 16 * groups && (depth <= 640 || tiles > 512 || tiles <= 64);
+}
+
 // Its blocks: 64 columns where that gives at least a block per CU (with 32 or,
 // above 16 rows a group, 64 rows each), else 16 columns (32 above 16 rows a
 // group, with 32 rows).  16 / 64 columns: 2, 8, 2048, 1024 4.0 / 6.8, 16, 1,

@@ -34,7 +34,7 @@ def rules():
                                 ("rule_few_form", 3, ctypes.c_int), ("rule_row_tiles", 3, i64),
                                 ("rule_tiles_over", 1, i64), ("rule_serve_rows", 3, ctypes.c_int),
                                 ("rule_serve_parts", 3, ctypes.c_int), ("rule_shrink_parts", 3, ctypes.c_int),
-                                ("rule_serve_many", 5, ctypes.c_int)):
+                                ("rule_serve_many", 5, ctypes.c_int), ("rule_few_rows_masked", 4, ctypes.c_int)):
             f = getattr(L, name)
             f.argtypes = [i64] * args
             f.restype = res

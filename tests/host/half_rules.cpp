@@ -9,6 +9,9 @@ int rule_rows_tile(int64_t rows, int64_t groups, int64_t cols) { return rows_til
 int rule_weights_tile(int64_t n, int64_t k, int64_t groups) { return weights_tile(n, k, groups); }
 int rule_tile_of(int64_t middle, int64_t large) { return tile_of(middle, large); }
 int rule_few_rows(int64_t rows, int64_t groups) { return few_rows(rows, groups); }
+int rule_few_rows_masked(int64_t rows, int64_t groups, int64_t cols, int64_t depth) {
+  return few_rows_masked(rows, groups, cols, depth);
+}
 int rule_few_form(int64_t rows, int64_t groups, int64_t cols) { return few_form(rows, groups, cols); }
 int rule_masked_small(int weights, int64_t middle) { return masked_small(weights != 0, middle); }
 int64_t rule_row_tiles(int64_t rows, int64_t groups, int64_t bm) { return expected_row_tiles(rows, groups, bm); }

@@ -52,6 +52,16 @@ def test_grouped_rows_masked(rows, groups, n, k, small):
     check_all(rows, n, k, sizes_of(rows, groups), torch.bfloat16)
 
 
+# Few unaligned rows a group: straight into fragments or in tiles.
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("rows, groups, n, k, few", [
+    (16, 8, 2057, 777, 1), (100, 8, 300, 129, 1), (300, 64, 700, 901, 1), (9, 1, 100, 1027, 1), (70, 8, 1000, 999, 0),
+    (700, 29, 260, 1001, 0), (129, 8, 65, 7, 0)])
+def test_few_rows_masked(dtype, rows, groups, n, k, few):
+    assert rules().rule_few_rows(rows, groups) and rules().rule_few_rows_masked(rows, groups, n, k) == few
+    check_all(rows, n, k, sizes_of(rows, groups), dtype)
+
+
 # Unaligned operands of a long depth in few tiles: sets of wavefronts share it.
 # Groups of fewer stages than sets (and of none) leave sets without a part.
 @pytest.mark.parametrize("sizes, n, k", [([2100, 0, 1, 70, 130, 1700], 70, 65), ([641, 700], 129, 33), ([2000], 5, 3)])

@@ -30,6 +30,15 @@ def test_few_rows_on_the_measured_side():
         assert forward(*c) == want, c
 
 
+def test_few_rows_of_masked_operands_on_the_measured_side():
+    L = rules()
+    for c, want in (((960, 29, 1024, 1971), 0), ((3000, 64, 1000, 777), 0), ((500, 16, 3001, 3000), 0),
+                    ((100, 29, 1024, 1971), 0), ((64, 8, 2048, 2047), 0), ((128, 8, 512, 513), 1),
+                    ((300, 64, 4000, 777), 1), ((250, 16, 3001, 3000), 1), ((16, 1, 4096, 4095), 1),
+                    ((1, 1, 1, 1), 1), ((16, 8, 2048, 2047), 1), ((17, 8, 2048, 2047), 0)):
+        assert L.rule_few_rows_masked(*c) == want, c
+
+
 def test_adapter_forms():
     assert adapter(1, 4096, 4096) == (None, 1) and adapter(128, 4096, 4096) == (None, 128)
     assert adapter(256, 1024, 1024) == (None, 256) and adapter(512, 1024, 1024) == (SMALL, 0)
