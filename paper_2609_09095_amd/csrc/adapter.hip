@@ -9,7 +9,8 @@
 // the product of those rows of H with that adapter's B_a: the projection's
 // output is written once and never read.
 //
-// Few rows: the projection's weights are what has to be read.  One launch
+// Few rows, and some more that name many adapters (which a tile would go through
+// one by one): the projection's weights are what has to be read.  One launch
 // reads them once into partial sums over parts of the depth and forms H beside
 // it; a second one adds the parts up and the adapters' share, in FP32.
 //

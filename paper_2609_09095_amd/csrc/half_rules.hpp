@@ -146,9 +146,11 @@ constexpr int64_t kServeRows = 128, kServeOutputs = 1 << 18;
 // 47 / 87; rank 64 of 64 92 / 185; 512, 1024, 1024, 16, 32 19 / 103; 333, 1000, 1111,
 // 16, 16 22 / 89; 512, 2048, 2048, 64, 32 76 / 152, but the same in runs of 16 rows
 // 75 / 45 and 512, 4096, 4096, 16, 16 85 / 95, in runs 85 / 57.
+// Depths that cannot go to LDS by DMA: 256, 4096, 4095, 16, 16 129 / 149, in runs
+// 126 / 57.
 constexpr bool serve_many(int64_t rows, int64_t n, int64_t k, int64_t rank_pad, int64_t adapters) {
   if (rank_pad == 0) return false;
-  if (rows <= 2 * kServeRows) return 2 * adapters >= rank_pad;
+  if (rows <= 2 * kServeRows && k % 8 == 0) return 2 * adapters >= rank_pad;
   return rows <= 4 * kServeRows && adapters >= 16 && rows * n * k <= (adapters < 64 ? adapters : 64) << 26;
 }
 

@@ -148,7 +148,7 @@ def test_adapter_forms(dtype, rows, n, k, tile, serve):
 # more in tiles that go through up to 64 adapters each.
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
 @pytest.mark.parametrize("rows, n, k, adapters, rank, many", [
-    (129, 4100, 520, 16, 24, 1), (256, 2056, 777, 70, 130, 0), (255, 2056, 777, 130, 256, 1), (333, 1000, 1111, 16, 16, 1),
+    (129, 4100, 520, 16, 24, 1), (256, 2056, 777, 70, 130, 1), (250, 2056, 777, 12, 24, 0), (255, 2056, 777, 130, 256, 1), (333, 1000, 1111, 16, 16, 1),
     (512, 1024, 264, 64, 65, 1), (500, 1025, 264, 15, 8, 0), (512, 3000, 4096, 64, 16, 0)])
 def test_many_adapters(dtype, rows, n, k, adapters, rank, many):
     assert rules().rule_serve_many(rows, n, k, -(-rank // 16) * 16, adapters) == many

@@ -51,7 +51,8 @@ def test_adapter_forms():
 def test_many_adapters_in_few_rows():
     L = rules()
     for c, want in (((256, 4096, 4096, 16, 8), 1), ((256, 4096, 4096, 16, 7), 0), ((256, 4096, 4096, 64, 32), 1),
-                    ((256, 4096, 4096, 64, 31), 0), ((256, 4096, 4096, 0, 8), 0), ((512, 1024, 1024, 16, 16), 1),
+                    ((256, 4096, 4096, 64, 31), 0), ((256, 4096, 4096, 0, 8), 0), ((256, 4096, 4095, 16, 16), 0),
+                    ((256, 4096, 4095, 16, 64), 1), ((512, 1024, 1024, 16, 16), 1),
                     ((512, 1024, 1024, 16, 15), 0), ((512, 2048, 2048, 64, 32), 1), ((512, 2048, 2048, 64, 31), 0),
                     ((512, 4096, 4096, 16, 65536), 0), ((512, 1 << 22, 1 << 22, 256, 65536), 0),
                     ((513, 1, 1, 16, 64), 0)):
