@@ -139,6 +139,9 @@ __device__ __forceinline__ void wait_loads_and_lds() {
   __builtin_amdgcn_s_waitcnt((N & 15) | ((N >> 4) << 14));
 }
 
+// No LDS access in flight; any number of vector loads.
+__device__ __forceinline__ void wait_lds() { __builtin_amdgcn_s_waitcnt(15 | 7 << 4 | 3 << 14); }
+
 // A barrier that waits for nothing but the other wavefronts; no memory access
 // moves over it.
 __device__ __forceinline__ void block_barrier() {

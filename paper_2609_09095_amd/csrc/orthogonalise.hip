@@ -304,8 +304,12 @@ struct TileRows {
     row = lane >> 4, ch = lane & 15;
   }
   __device__ __forceinline__ int column(int i) const { return c0 + (ch ^ (4 * i + row & 15)) * 4; }
-  // rows `first` to first + 63 of the wavefront's part; places past the edge are clamped
+  // rows `first` to first + 63 of the wavefront's part; places past the edge are
+  // clamped.  What the wavefront still reads of the rows before them comes first:
+  // a load into LDS does not wait for reads that are queued.
   __device__ __forceinline__ void load(const float* tile, int first) const {
+    wave_lds_ready();
+    wait_lds();
     const auto rsrc = __builtin_amdgcn_make_buffer_rsrc((void*)uniform((const char*)tile), (short)0, 0x7ffffff0, 0x00020000);
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
