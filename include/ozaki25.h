@@ -397,9 +397,10 @@ ozaki25_status ozaki25_grouped_matmul_dw(int64_t rows, int64_t n, int64_t k, int
  *  [adapters], or NULL for 1;  Y: rows x n (ldy).  Adapters of lower rank are
  *  padded with zeros.
  *  type: OZAKI25_BF16 or OZAKI25_F16, of X, W, A, B and Y.  Both sums run in
- *    FP32; scales[a] X A_a^T enters the second product as two numbers of the
- *    type (the rounded value and the rest; beyond the type's range, in half
- *    65504, it is an infinity).
+ *    FP32.  With few rows scales[a] X A_a^T enters the second product in FP32,
+ *    with more as two numbers of the type, the rounded value and the rest: 16
+ *    bits of it in bfloat16, in half 22, or 2^-38 of the row's largest value
+ *    where that is more.  It may lie outside the type's range.
  *  workspace: NULL to allocate stream-ordered, else at least
  *    ozaki25_adapter_matmul_workspace_size() bytes, 256-byte aligned.
  * Y must not overlap the inputs.  rows == 0 or n == 0: no-op; k == 0: zeros.

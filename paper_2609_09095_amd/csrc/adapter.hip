@@ -4,7 +4,8 @@
 //
 // Many rows: H[t, :] = X[t, :] A_a^T is formed first, in partial sums of a
 // split depth, and s_a H written as two 16-bit numbers, its rounded value and
-// the rest, so that it keeps at least 16 bits.  Then the projection's tiles
+// the rest, so that it keeps 16 bits (bfloat16) or 22 (half, at a power of two
+// of each row's own).  Then the projection's tiles
 // run and, before a tile is stored, add for each adapter that its rows name
 // the product of those rows of H with that adapter's B_a: the projection's
 // output is written once and never read.
@@ -123,31 +124,53 @@ __global__ __launch_bounds__(T::THREADS, 1) void shrink_tiles_kernel(Adapter p) 
 // s_a H from its partial sums, as the rounded values (rank_pad of a row) and
 // the rests (rank_pad more); rows without an adapter are not written.  One 16-bit
 // number would round what the result's own rounding has not asked for; two keep
-// 16 bits or more and cost 64 more ranks of the matrix cores.  4096 rows, rank 64:
-// 5.6 us, mostly the launch.
+// 16 bits (bfloat16) or 22 (half) and cost 64 more ranks of the matrix cores.
+//
+// Half's range is not that of s_a H: a row's values are divided by a power of
+// two that brings its largest finite one to [2^14, 2^15), and the tiles multiply
+// its sums by that power in 32 bits.  No value overflows, and the rests' least
+// difference, 2^-24, is 2^-38 of the row's largest value or less.  bfloat16 has
+// float32's range; a value past its largest number leaves more to the rest.
+// `lanes`, a power of two, hold a row, four ranks each.
 template <int TYPE>
-__global__ __launch_bounds__(256) void split_kernel(Adapter p) {
+__global__ __launch_bounds__(256) void split_kernel(Adapter p, int lanes) {
   using O = typename Out<TYPE>::type;
-  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  const int quads = p.rank_pad / 4;
-  const int64_t t = i / quads;
-  const int r = (int)(i - t * quads) * 4;
-  if (t >= p.rows) return;
-  const int a = p.ids[t];
-  if (a < 0 || a >= p.adapters) return;
-  v4f v{};
-  for (int s = 0; s < p.splits; ++s) v += *(const v4f*)(p.h + ((int64_t)s * p.rows + t) * p.rank_pad + r);
-  v *= p.scales ? p.scales[a] : 1.0f;
-  float rest[4];
+  const int r = (int)(threadIdx.x & (lanes - 1)) * 4, per = 256 / lanes;
+  for (int64_t t = (int64_t)blockIdx.x * per + threadIdx.x / lanes; t < p.rows; t += (int64_t)gridDim.x * per) {
+    const int a = p.ids[t];
+    if (a < 0 || a >= p.adapters) continue;
+    v4f v{};
+    if (r < p.rank_pad)
+      for (int s = 0; s < p.splits; ++s) v += *(const v4f*)(p.h + ((int64_t)s * p.rows + t) * p.rank_pad + r);
+    v *= p.scales ? p.scales[a] : 1.0f;
+    if constexpr (TYPE == kF16) {
+      float most = 0.0f;
 #pragma unroll
-  for (int e = 0; e < 4; ++e) {
-    const float hi = (float)(O)v[e];
-    // an overflowing value has no rest: it stays an infinity
-    rest[e] = __builtin_isfinite(hi) ? v[e] - hi : 0.0f;
+      for (int e = 0; e < 4; ++e) {
+        const float size = __builtin_fabsf(v[e]);
+        most = size > most && __builtin_isfinite(size) ? size : most;
+      }
+      for (int d = lanes >> 1; d; d >>= 1) most = fmaxf(most, __shfl_xor(most, d));
+      // most in [2^(e - 1), 2^e); below 2^-100 nothing is left of it in any product
+      const int e = most > 0.0f ? __builtin_amdgcn_frexp_expf(most) : 0, power = (e < -100 ? -100 : e) - 15;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) v[i] = __builtin_ldexpf(v[i], -power);
+      if (r == 0) p.factors[t] = __builtin_ldexpf(1.0f, power);
+    }
+    if (r >= p.rank_pad) continue;
+    constexpr float kMost = TYPE == kF16 ? 65504.0f : 0x1.fep127f;
+    float hi[4], rest[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      hi[e] = (float)(O)v[e];
+      const bool finite = __builtin_isfinite(v[e]);
+      if (finite && !__builtin_isfinite(hi[e])) hi[e] = __builtin_copysignf(kMost, v[e]);
+      rest[e] = finite ? v[e] - hi[e] : 0.0f;
+    }
+    char* const out = (char*)p.h16 + (t * 2 * p.rank_pad + r) * 2;
+    *(uint2*)out = pack4<TYPE>(hi[0], hi[1], hi[2], hi[3]);
+    *(uint2*)(out + p.rank_pad * 2) = pack4<TYPE>(rest[0], rest[1], rest[2], rest[3]);
   }
-  char* const out = (char*)p.h16 + (t * 2 * p.rank_pad + r) * 2;
-  *(uint2*)out = pack4<TYPE>(v[0], v[1], v[2], v[3]);
-  *(uint2*)(out + p.rank_pad * 2) = pack4<TYPE>(rest[0], rest[1], rest[2], rest[3]);
 }
 
 // The adapters' share of a tile, added to its sums: 64 ranks at a time, H's
@@ -156,8 +179,8 @@ __global__ __launch_bounds__(256) void split_kernel(Adapter p) {
 // of other adapters as zeros would do without that choice, but pass on an
 // infinity of this adapter's B.)
 template <class T>
-__device__ __forceinline__ void expand(const Adapter& p, int r0, int rows, int c0, int cols, const int* ids, char* lds,
-                                       v16f (&acc)[T::MB][T::NB]) {
+__device__ __forceinline__ void expand(const Adapter& p, int r0, int rows, int c0, int cols, const int* ids,
+                                       const float* factors, char* lds, v16f (&acc)[T::MB][T::NB]) {
   static_assert(T::LA == kAlong && T::LB == kAlong && T::WIDE);
   static_assert(2 * T::A_BYTES + T::B_BYTES <= T::LDS);
   const int lane = threadIdx.x & 63;
@@ -195,7 +218,9 @@ __device__ __forceinline__ void expand(const Adapter& p, int r0, int rows, int c
       const int ks_end = left / 16;
 #pragma unroll
       for (int x = 0; x < T::MB; ++x) {
-        const bool mine = ids[(wr * T::MB + x) * 32 + (lane & 31)] == a;
+        const int row = (wr * T::MB + x) * 32 + (lane & 31);
+        const bool mine = ids[row] == a;
+        const float factor = T::TYPE == kF16 ? factors[row] : 1.0f;
         v16f t[T::NB] = {};
         for (int ks = 0; ks < ks_end; ++ks) {
           // the swizzle's K step term, as Fragments has it
@@ -210,7 +235,7 @@ __device__ __forceinline__ void expand(const Adapter& p, int r0, int rows, int c
 #pragma unroll
         for (int y = 0; y < T::NB; ++y)
 #pragma unroll
-          for (int i = 0; i < 16; ++i) acc[x][y][i] += mine ? t[y][i] : 0.0f;
+          for (int i = 0; i < 16; ++i) acc[x][y][i] += mine ? factor * t[y][i] : 0.0f;
       }
       __syncthreads();
     }
@@ -225,8 +250,9 @@ template <class T>
 __global__ __launch_bounds__(T::THREADS, 1) void adapter_kernel(Adapter p) {
   // one array: with two, the compiler would tell them apart by alias scopes of
   // its own and wait for the loads into LDS before every fragment
-  __shared__ __attribute__((aligned(1024))) char lds[T::LDS + T::BM * 4];
+  __shared__ __attribute__((aligned(1024))) char lds[T::LDS + T::BM * 8];
   int* const ids = (int*)(lds + T::LDS);
+  float* const factors = (float*)(ids + T::BM);
   const uint32_t tiles_n = ((uint32_t)p.n + T::BN - 1) / T::BN, tiles_m = ((uint32_t)p.rows + T::BM - 1) / T::BM;
   uint32_t place, tm, tn;
   if (!block_place(blockIdx.x, tiles_m * tiles_n, place)) return;
@@ -234,12 +260,15 @@ __global__ __launch_bounds__(T::THREADS, 1) void adapter_kernel(Adapter p) {
   const int r0 = (int)tm * T::BM, c0 = (int)tn * T::BN;
   const int rows = p.rows - r0 < T::BM ? p.rows - r0 : T::BM, cols = p.n - c0 < T::BN ? p.n - c0 : T::BN;
   if (p.rank > 0)
-    for (int i = threadIdx.x; i < T::BM; i += T::THREADS) ids[i] = i < rows ? p.ids[r0 + i] : -1;
+    for (int i = threadIdx.x; i < T::BM; i += T::THREADS) {
+      ids[i] = i < rows ? p.ids[r0 + i] : -1;
+      if constexpr (T::TYPE == kF16) factors[i] = i < rows ? p.factors[r0 + i] : 1.0f;
+    }
   v16f acc[T::MB][T::NB] = {};
   if (!product<T>(Operand{(const char*)p.x + r0 * p.ldx * 2, p.ldx, rows, p.k},
                   Operand{(const char*)p.w + c0 * p.ldw * 2, p.ldw, cols, p.k}, p.k, lds, acc))
     return;
-  if (p.rank > 0) expand<T>(p, r0, rows, c0, cols, ids, lds, acc);
+  if (p.rank > 0) expand<T>(p, r0, rows, c0, cols, ids, factors, lds, acc);
   store<T>(acc, lds, (char*)p.y + (r0 * p.ldy + c0) * 2, p.ldy, rows, cols, p.stream);
 }
 
@@ -383,7 +412,10 @@ hipError_t shrink(const Adapter& p, hipStream_t s) {
     const dim3 grid((uint32_t)ceil_div(p.rows, kShrinkRows), (uint32_t)(p.splits * ceil_div(p.rank, 16 * RB)));
     shrink_kernel<TYPE, RB><<<grid, dim3(256), 0, s>>>(p);
   }
-  split_kernel<TYPE><<<dim3((uint32_t)ceil_div((int64_t)p.rows * (p.rank_pad / 4), 256)), dim3(256), 0, s>>>(p);
+  int lanes = 4;  // of a row: 16 to 256 ranks
+  while (lanes * 4 < p.rank_pad) lanes *= 2;
+  const int64_t blocks = ceil_div((int64_t)p.rows * lanes, 256);
+  split_kernel<TYPE><<<dim3((uint32_t)(blocks < 1 << 20 ? blocks : 1 << 20)), dim3(256), 0, s>>>(p, lanes);
   return hipGetLastError();
 }
 
@@ -430,15 +462,15 @@ hipError_t both(Adapter p, int serve_rows, hipStream_t s) {
 hipError_t launch_adapter(Adapter p, const AdapterPlan& plan, char* room, int type, hipStream_t s) {
   // more work-items than a launch holds (by the smallest tiles): before anything runs
   constexpr int64_t kMost = ((int64_t)1 << 32) - 4096;
-  if (ceil_div(p.rows, 64) * ceil_div(p.n, 64) * 256 > kMost || ceil_div(p.rows, kShrinkRows) * 256 > kMost ||
-      (int64_t)p.rows * (p.rank_pad / 4) > kMost)
+  if (ceil_div(p.rows, 64) * ceil_div(p.n, 64) * 256 > kMost || ceil_div(p.rows, kShrinkRows) * 256 > kMost)
     return hipErrorInvalidConfiguration;
   p.stream = past_caches((int64_t)p.rows * p.n * 2);
   if (p.k == 0 || p.adapters == 0) p.rank = 0;  // X A^T is zero
   // the two parts run one after the other and share the room of their partial sums of H
   p.h = (float*)room;
   p.h16 = room + plan.h_bytes;
-  p.partials = (float*)(room + plan.h_bytes + plan.h16_bytes);
+  p.factors = (float*)(room + plan.h_bytes + plan.h16_bytes);
+  p.partials = (float*)(room + plan.h_bytes + plan.h16_bytes + plan.factor_bytes);
   p.splits = plan.splits, p.serve_splits = plan.serve_splits, p.base_splits = plan.base_splits;
   return type == kBF16 ? both<kBF16>(p, plan.serve_rows, s) : both<kF16>(p, plan.serve_rows, s);
 }

@@ -137,7 +137,7 @@ size_t ozaki25_adapter_matmul_workspace_size(int64_t rows, int64_t n, int64_t k,
       too_large(rows, n, k, adapters))
     return 0;
   const oz::half::AdapterPlan a = oz::half::adapter_plan(rows, n, k, pad16(rank), adapters);
-  return a.h_bytes + a.h16_bytes + a.partial_bytes;
+  return a.h_bytes + a.h16_bytes + a.factor_bytes + a.partial_bytes;
 }
 
 ozaki25_status ozaki25_adapter_matmul(int64_t rows, int64_t n, int64_t k, int64_t adapters, int64_t rank, const void* X,

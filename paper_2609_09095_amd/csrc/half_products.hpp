@@ -49,6 +49,7 @@ struct Adapter {
   // workspace (set by the launch)
   float* h;          // parts x rows x rank_pad
   void* h16;         // rows x 2 rank_pad
+  float* factors;    // rows: what a row's h16 was divided by (half)
   float* partials;   // base_splits x rows x n_pad
   int rank_pad;      // rank rounded up to 16
   int n_pad;         // n rounded up to 4

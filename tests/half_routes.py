@@ -34,7 +34,8 @@ def rules():
                                 ("rule_few_form", 3, ctypes.c_int), ("rule_row_tiles", 3, i64),
                                 ("rule_tiles_over", 1, i64), ("rule_serve_rows", 3, ctypes.c_int),
                                 ("rule_serve_parts", 3, ctypes.c_int), ("rule_shrink_parts", 3, ctypes.c_int),
-                                ("rule_serve_many", 5, ctypes.c_int), ("rule_few_rows_masked", 4, ctypes.c_int)):
+                                ("rule_serve_many", 5, ctypes.c_int), ("rule_plan_serve_rows", 5, ctypes.c_int),
+                                ("rule_few_rows_masked", 4, ctypes.c_int)):
             f = getattr(L, name)
             f.argtypes = [i64] * args
             f.restype = res
@@ -55,6 +56,16 @@ def adapter(rows, n, k):
     """(tile size or None, rows in the few-row form) of an adapter product."""
     L = rules()
     serve = L.rule_serve_rows(rows, n, k)
+    tiles = rows - serve
+    up = lambda b: -(-tiles // b) * -(-n // b)  # noqa: E731
+    return (L.rule_tile_of(up(128), up(256)) if tiles else None), serve
+
+
+def adapter_of(rows, n, k, adapters, rank):
+    """The same with the adapters and their rank, which move rows of many
+    adapters into the few-row form."""
+    L = rules()
+    serve = L.rule_plan_serve_rows(rows, n, k, -(-rank // 16) * 16, adapters)
     tiles = rows - serve
     up = lambda b: -(-tiles // b) * -(-n // b)  # noqa: E731
     return (L.rule_tile_of(up(128), up(256)) if tiles else None), serve

@@ -18,6 +18,9 @@ int64_t rule_row_tiles(int64_t rows, int64_t groups, int64_t bm) { return expect
 int64_t rule_tiles_over(int64_t large) { return large_tiles_over(large); }
 int rule_masked_sets(int64_t tiles, int64_t depth) { return masked_sets(tiles, depth); }
 int rule_serve_rows(int64_t rows, int64_t n, int64_t k) { return adapter_plan(rows, n, k, 16).serve_rows; }
+int rule_plan_serve_rows(int64_t rows, int64_t n, int64_t k, int64_t rank_pad, int64_t adapters) {
+  return adapter_plan(rows, n, k, rank_pad, adapters).serve_rows;
+}
 int rule_serve_many(int64_t rows, int64_t n, int64_t k, int64_t rank_pad, int64_t adapters) {
   return serve_many(rows, n, k, rank_pad, adapters);
 }
