@@ -173,14 +173,40 @@ __global__ __launch_bounds__(256) void split_kernel(Adapter p, int lanes) {
   }
 }
 
+// Infinities and NaN among 8 elements.
+template <int TYPE>
+__device__ __forceinline__ bool any_special(v4i v) {
+  constexpr uint32_t kExponent = TYPE == kF16 ? 0x7c00 : 0x7f80;
+  bool any = false;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const uint32_t lo = (uint32_t)v[i] & kExponent, hi = (uint32_t)v[i] >> 16 & kExponent;
+    any |= lo == kExponent || hi == kExponent;
+  }
+  return any;
+}
+
+// They as zeros.
+template <int TYPE>
+__device__ __forceinline__ v4i without_special(v4i v) {
+  constexpr short kExponent = TYPE == kF16 ? 0x7c00 : 0x7f80;
+  v8s e = __builtin_bit_cast(v8s, v);
+#pragma unroll
+  for (int i = 0; i < 8; ++i) e[i] = (e[i] & kExponent) == kExponent ? (short)0 : e[i];
+  return __builtin_bit_cast(v4i, e);
+}
+
 // The adapters' share of a tile, added to its sums: 64 ranks at a time, H's
 // rounded values, its rests and B_a in LDS.  A lane's outputs of a block lie in
 // one row (WIDE): it takes the sums where that row names this adapter.  (Rows
 // of other adapters as zeros would do without that choice, but pass on an
-// infinity of this adapter's B.)
+// infinity of this adapter's B.)  An infinity of the row's own B_a meets the
+// rounded values only: a rest has either sign, or is zero.  `special`, zero at
+// first, is set once any has been seen.
 template <class T>
 __device__ __forceinline__ void expand(const Adapter& p, int r0, int rows, int c0, int cols, const int* ids,
-                                       const float* factors, char* lds, v16f (&acc)[T::MB][T::NB]) {
+                                       const float* factors, int* special, char* lds,
+                                       v16f (&acc)[T::MB][T::NB]) {
   static_assert(T::LA == kAlong && T::LB == kAlong && T::WIDE);
   static_assert(2 * T::A_BYTES + T::B_BYTES <= T::LDS);
   const int lane = threadIdx.x & 63;
@@ -213,8 +239,12 @@ __device__ __forceinline__ void expand(const Adapter& p, int r0, int rows, int c
         lo.put(i, rests, wave, lane);
       }
 #pragma unroll
-      for (int i = 0; i < T::BDMA; ++i) b.put(i, bs, wave, lane);
+      for (int i = 0; i < T::BDMA; ++i) {
+        b.put(i, bs, wave, lane);
+        if (any_special<T::TYPE>(b.reg[i])) *special = 1;
+      }
       __syncthreads();
+      const bool finite = __builtin_amdgcn_readfirstlane(*special) == 0;
       const int ks_end = left / 16;
 #pragma unroll
       for (int x = 0; x < T::MB; ++x) {
@@ -229,7 +259,7 @@ __device__ __forceinline__ void expand(const Adapter& p, int r0, int rows, int c
           for (int y = 0; y < T::NB; ++y) {
             const v4i xb = *(const v4i*)(bs + fb.at(ks) + y * 4096);
             t[y] = mfma<T::TYPE>(xb, xh, t[y]);
-            t[y] = mfma<T::TYPE>(xb, xl, t[y]);
+            t[y] = mfma<T::TYPE>(finite ? xb : without_special<T::TYPE>(xb), xl, t[y]);
           }
         }
 #pragma unroll
@@ -250,15 +280,17 @@ template <class T>
 __global__ __launch_bounds__(T::THREADS, 1) void adapter_kernel(Adapter p) {
   // one array: with two, the compiler would tell them apart by alias scopes of
   // its own and wait for the loads into LDS before every fragment
-  __shared__ __attribute__((aligned(1024))) char lds[T::LDS + T::BM * 8];
+  __shared__ __attribute__((aligned(1024))) char lds[T::LDS + T::BM * 8 + 16];
   int* const ids = (int*)(lds + T::LDS);
   float* const factors = (float*)(ids + T::BM);
+  int* const special = (int*)(factors + T::BM);
   const uint32_t tiles_n = ((uint32_t)p.n + T::BN - 1) / T::BN, tiles_m = ((uint32_t)p.rows + T::BM - 1) / T::BM;
   uint32_t place, tm, tn;
   if (!block_place(blockIdx.x, tiles_m * tiles_n, place)) return;
   place_to_tile(place, tiles_m, tiles_n, tm, tn);
   const int r0 = (int)tm * T::BM, c0 = (int)tn * T::BN;
   const int rows = p.rows - r0 < T::BM ? p.rows - r0 : T::BM, cols = p.n - c0 < T::BN ? p.n - c0 : T::BN;
+  if (threadIdx.x == 0) *special = 0;
   if (p.rank > 0)
     for (int i = threadIdx.x; i < T::BM; i += T::THREADS) {
       ids[i] = i < rows ? p.ids[r0 + i] : -1;
@@ -268,7 +300,7 @@ __global__ __launch_bounds__(T::THREADS, 1) void adapter_kernel(Adapter p) {
   if (!product<T>(Operand{(const char*)p.x + r0 * p.ldx * 2, p.ldx, rows, p.k},
                   Operand{(const char*)p.w + c0 * p.ldw * 2, p.ldw, cols, p.k}, p.k, lds, acc))
     return;
-  if (p.rank > 0) expand<T>(p, r0, rows, c0, cols, ids, factors, lds, acc);
+  if (p.rank > 0) expand<T>(p, r0, rows, c0, cols, ids, factors, special, lds, acc);
   store<T>(acc, lds, (char*)p.y + (r0 * p.ldy + c0) * 2, p.ldy, rows, cols, p.stream);
 }
 

@@ -107,3 +107,28 @@ def test_bfloat16_past_its_largest_number(rows, n, k, tile):
     A[1, 0, 0], A[1, 0, 1], B[:] = 2.0 ** 64 * (2 - 2.0 ** -7), 2.0 ** 64 * 1.5 * 2.0 ** -8, 2.0 ** -120
     ids, scales = torch.ones(rows, dtype=torch.int32, device="cuda"), torch.ones(2, device="cuda")
     close(call(X, W, ids, A, B, scales), *reference(X, W, ids, A, B, scales))
+
+
+@pytest.mark.parametrize("dtype", [BF, HALF])
+@pytest.mark.parametrize("rows, n, k, tile", FORMS + [(4096, 4096, 72, LARGE), (2304, 2048, 72, 1)])
+def test_infinities_of_the_rows_own_adapter(dtype, rows, n, k, tile):
+    """An infinity in B_a is one, with the sign of its product, in the column
+    of every row of a (an h of either sign, from the first 64 ranks and the
+    ones behind)."""
+    takes(rows, n, k, 4, 72, tile)
+    X, W, ids = draw((rows, k), dtype, 1), draw((n, k), dtype, 2) * k ** -0.5, ids_of(rows, 4)
+    A, B = draw((4, 72, k), dtype, 3) * k ** -0.5, draw((4, n, 72), dtype, 4)
+    scales = torch.tensor([1.0, 0.5, -2.0, 1.0], device="cuda")
+    special = [(1, 5, 3, float("inf")), (2, 7, 0, float("-inf")), (2, n - 1, 71, float("inf")), (3, 0, 70, float("inf"))]
+    want, _ = reference(X, W, ids, A, B, scales)
+    sure = torch.ones_like(want, dtype=torch.bool)
+    for a, c, r, v in special:
+        B[a, c, r] = v
+        rows_of = ids == a
+        h = X[rows_of].double() @ A[a, r].double()
+        want[rows_of, c] = torch.sign(h) * float(scales[a]) * v
+        sure[rows_of, c] = h.abs() > k * 2.0 ** -22 * (X[rows_of].double().abs() @ A[a, r].double().abs())
+    Y = call(X, W, ids, A, B, scales).double()
+    finite = torch.isfinite(want)
+    assert torch.equal(torch.isfinite(Y)[sure], finite[sure])
+    assert torch.equal(Y[sure & ~finite], want[sure & ~finite])
