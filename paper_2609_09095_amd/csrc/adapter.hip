@@ -143,6 +143,9 @@ __global__ __launch_bounds__(256) void split_kernel(Adapter p, int lanes) {
     if (r < p.rank_pad)
       for (int s = 0; s < p.splits; ++s) v += *(const v4f*)(p.h + ((int64_t)s * p.rows + t) * p.rank_pad + r);
     v *= p.scales ? p.scales[a] : 1.0f;
+    // ranks past the last: zeros also behind an infinite scale or activation
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[e] = r + e < p.rank ? v[e] : 0.0f;
     if constexpr (TYPE == kF16) {
       float most = 0.0f;
 #pragma unroll
@@ -386,7 +389,7 @@ __global__ __launch_bounds__(256) void serve_join_kernel(Adapter p) {
     if ((int)threadIdx.x < p.rank_pad) {
       float v = 0;
       for (int s = 0; s < p.splits; ++s) v += p.h[((int64_t)s * p.rows + t) * p.rank_pad + threadIdx.x];
-      h[threadIdx.x] = v * (p.scales ? p.scales[a] : 1.0f);
+      h[threadIdx.x] = (int)threadIdx.x < p.rank ? v * (p.scales ? p.scales[a] : 1.0f) : 0.0f;
     }
   }
   float y = 0;

@@ -132,3 +132,22 @@ def test_infinities_of_the_rows_own_adapter(dtype, rows, n, k, tile):
     finite = torch.isfinite(want)
     assert torch.equal(torch.isfinite(Y)[sure], finite[sure])
     assert torch.equal(Y[sure & ~finite], want[sure & ~finite])
+
+
+@pytest.mark.parametrize("dtype", [BF, HALF])
+@pytest.mark.parametrize("rank", [1, 5, 20, 70])
+@pytest.mark.parametrize("rows, n, k, tile", FORMS)
+def test_infinite_scales_and_activations(dtype, rank, rows, n, k, tile):
+    """With positive operands every output that an infinity reaches is one: the
+    ranks that pad an adapter add nothing."""
+    takes(rows, n, k, 3, rank, tile)
+    positive = lambda s, seed: draw(s, dtype, seed).abs().clamp(min=2.0 ** -6)  # noqa: E731
+    X, W, A, B = positive((rows, k), 1), positive((n, k), 2), positive((3, rank, k), 3), positive((3, n, rank), 4)
+    ids, scales = ids_of(rows, 3), torch.tensor([1.0, float("inf"), 0.0], device="cuda")
+    scales[2] = 2.0 ** -6
+    X *= 2.0 ** -3
+    X[9, 0] = float("inf")
+    Y = call(X, W, ids, A, B, scales)
+    want = ids == 1
+    want[9] = True
+    assert torch.equal(torch.isposinf(Y), want[:, None].expand_as(Y)) and not torch.isnan(Y).any()
