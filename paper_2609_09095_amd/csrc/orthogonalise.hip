@@ -76,6 +76,11 @@ __global__ __launch_bounds__(256) void squares_kernel(Orthogonalise o) {
   if (threadIdx.x == 0) o.squares[blockIdx.y * gridDim.x + blockIdx.x] = part[0] + part[1] + part[2] + part[3];
 }
 
+// 1 / (|G|_F + eps): a matrix of zeros is divided by nothing, whatever eps is.
+__device__ __forceinline__ float reciprocal_norm(double squares, float eps) {
+  return squares == 0.0 ? 0.0f : (float)(1.0 / (sqrt(squares) + (double)eps));
+}
+
 // X_0 in both forms, padding included.  Bound by memory: 2 x 4096 x 4096 51 us
 // (268 MB: 5.3 TB/s).  grid (blocks, count)
 template <int TYPE>
@@ -83,7 +88,7 @@ __global__ __launch_bounds__(256) void start_kernel(Orthogonalise o, int parts) 
   double sum = 0;
   for (int i = threadIdx.x & 63; i < parts; i += 64) sum += o.squares[blockIdx.y * parts + i];
   for (int d = 32; d; d >>= 1) sum += __shfl_xor(sum, d);
-  const float scale = (float)(1.0 / (sqrt(sum) + (double)o.eps));
+  const float scale = reciprocal_norm(sum, o.eps);
   const uint32_t chunks = (uint32_t)o.np / 8, total = chunks * (uint32_t)o.mp;
   const int64_t each = (int64_t)o.mp * o.np;
   for (uint32_t i = blockIdx.x * 256 + threadIdx.x; i < total; i += gridDim.x * 256) {
@@ -503,7 +508,7 @@ __global__ __launch_bounds__(512, 1) void small_kernel(Orthogonalise o, int step
   __syncthreads();
   const double square =
       ((sums[0] + sums[1]) + (sums[2] + sums[3])) + ((sums[4] + sums[5]) + (sums[6] + sums[7]));
-  const float scale = (float)(1.0 / (sqrt(square) + (double)o.eps));
+  const float scale = reciprocal_norm(square, o.eps);
 #pragma unroll
   for (int x = 0; x < 2; ++x)
 #pragma unroll
