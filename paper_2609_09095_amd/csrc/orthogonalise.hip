@@ -76,10 +76,19 @@ __global__ __launch_bounds__(256) void squares_kernel(Orthogonalise o) {
   if (threadIdx.x == 0) o.squares[blockIdx.y * gridDim.x + blockIdx.x] = part[0] + part[1] + part[2] + part[3];
 }
 
-// 1 / (|G|_F + eps): a matrix of zeros is divided by nothing, whatever eps is.
-__device__ __forceinline__ float reciprocal_norm(double squares, float eps) {
-  return squares == 0.0 ? 0.0f : (float)(1.0 / (sqrt(squares) + (double)eps));
-}
+// Division by |G|_F + eps: its reciprocal may be no normal 32-bit number where
+// G's own elements are, so it is kept as a factor in [1/2, 1] and a power of two.
+// A matrix of zeros is divided by nothing, whatever eps is.
+struct Scaling {
+  float factor;
+  int power;
+  __device__ __forceinline__ Scaling(double squares, float eps) {
+    const double scale = squares == 0.0 ? 0.0 : 1.0 / (sqrt(squares) + (double)eps);
+    power = __builtin_amdgcn_frexp_exp(scale);
+    factor = (float)__builtin_amdgcn_frexp_mant(scale);
+  }
+  __device__ __forceinline__ float operator()(float x) const { return __builtin_ldexpf(x, power) * factor; }
+};
 
 // X_0 in both forms, padding included.  Bound by memory: 2 x 4096 x 4096 51 us
 // (268 MB: 5.3 TB/s).  grid (blocks, count)
@@ -88,7 +97,7 @@ __global__ __launch_bounds__(256) void start_kernel(Orthogonalise o, int parts) 
   double sum = 0;
   for (int i = threadIdx.x & 63; i < parts; i += 64) sum += o.squares[blockIdx.y * parts + i];
   for (int d = 32; d; d >>= 1) sum += __shfl_xor(sum, d);
-  const float scale = reciprocal_norm(sum, o.eps);
+  const Scaling scale(sum, o.eps);
   const uint32_t chunks = (uint32_t)o.np / 8, total = chunks * (uint32_t)o.mp;
   const int64_t each = (int64_t)o.mp * o.np;
   for (uint32_t i = blockIdx.x * 256 + threadIdx.x; i < total; i += gridDim.x * 256) {
@@ -96,7 +105,7 @@ __global__ __launch_bounds__(256) void start_kernel(Orthogonalise o, int parts) 
     float x[8] = {};
     if ((int)r < o.m) row8<TYPE>(o.g, blockIdx.y * o.g_stride + r * o.ldg, c, o.n, x);
 #pragma unroll
-    for (int j = 0; j < 8; ++j) x[j] = (int)(c + j) < o.n && (int)r < o.m ? x[j] * scale : 0.0f;
+    for (int j = 0; j < 8; ++j) x[j] = (int)(c + j) < o.n && (int)r < o.m ? scale(x[j]) : 0.0f;
     float4* const p = (float4*)(o.x32 + blockIdx.y * each + (int64_t)i * 8);
     p[0] = float4{x[0], x[1], x[2], x[3]};
     p[1] = float4{x[4], x[5], x[6], x[7]};
@@ -508,14 +517,14 @@ __global__ __launch_bounds__(512, 1) void small_kernel(Orthogonalise o, int step
   __syncthreads();
   const double square =
       ((sums[0] + sums[1]) + (sums[2] + sums[3])) + ((sums[4] + sums[5]) + (sums[6] + sums[7]));
-  const float scale = reciprocal_norm(square, o.eps);
+  const Scaling scale(square, o.eps);
 #pragma unroll
   for (int x = 0; x < 2; ++x)
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
       // (not by the product alone: padding stays zero for an infinite or NaN scale)
       const bool in = row + 32 * x < s && col + 8 * (i >> 2) + (i & 3) < l;
-      X[x][i] = in ? X[x][i] * scale * kBlockX : 0.0f;
+      X[x][i] = in ? scale(X[x][i]) * kBlockX : 0.0f;
     }
   // the four outputs of group q of block x to LDS
   auto put = [&](char* to, int x, int q, float v0, float v1, float v2, float v3) __attribute__((always_inline)) {

@@ -36,3 +36,13 @@ def test_zeros_stay_zeros(shape, dtype):
         G[0] = 0
         X = call(G, eps=eps)
         assert torch.count_nonzero(X[0]) == 0 and torch.isfinite(X).all()
+
+
+@pytest.mark.parametrize("exponent", [-149, -140, -120, 0, 100, 118])
+@pytest.mark.parametrize("shape", SHAPES)
+def test_norms_whose_reciprocal_is_no_normal_float(shape, exponent):
+    """Whole numbers up to 2^9 times a power of two, the least one float32's
+    least positive number: scaling is exact, so results are equal."""
+    G = (gradient(shape, torch.float32) * 6e4).round().clamp(-511, 511)
+    assert float(G.abs().max()) > 100
+    assert torch.equal(call(G, eps=0.0), call(torch.ldexp(G.double(), torch.tensor(exponent, device="cuda")).float(), eps=0.0))
