@@ -428,9 +428,10 @@ ozaki25_status ozaki25_adapter_matmul(int64_t rows, int64_t n, int64_t k, int64_
  *  a, b, c: e.g. 3.4445, -4.7750, 2.0315 with 5 steps, which brings singular
  *    values to about [0.7, 1.2].
  * X is carried from step to step in FP32; the products' operands are rounded
- * to half (11 bits; the diagonals of S and b S + c S^2 kept in FP32) and summed
- * in FP32; the norm is a 64-bit sum.  A matrix of
- * zeros gives zeros; one with a NaN or infinity gives NaN.
+ * to half (11 bits) and summed in FP32, whatever G's type; the diagonal of S is
+ * kept in FP32, and that of b S + c S^2 in rows of S that are mostly their
+ * diagonal, as they are unless G has few directions.  The norm is a 64-bit sum.
+ * A matrix of zeros gives zeros; one with a NaN or infinity gives NaN.
  *  workspace: NULL to allocate stream-ordered, else at least
  *    ozaki25_orthogonalise_workspace_size() bytes, 256-byte aligned (about 8
  *    bytes per element and 4 per element of the shorter side squared).

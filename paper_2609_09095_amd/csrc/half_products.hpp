@@ -67,14 +67,15 @@ struct Orthogonalise {
   int count, m, n;
   int mp, np;  // m, n padded to multiples of 8
   float a, b, c, eps;
+  float per_c;  // 1 / c, zero for c = 0
   // workspace
   double* squares;  // count x orthogonalise_parts
   float* x32;       // count x mp x np
   void* x16[2];     // the same
   void* s16;        // count x s x s, s the shorter padded side; zero diagonal
-  void* p16;        // the same
+  void* p16;        // the same; a share of the diagonal
   float* d32;       // count x s: the diagonal of S
-  float* p32;       // the same of P
+  float* p32;       // the rest of P's diagonal
 };
 
 // Blocks (and partial sums) per matrix of the norm.
