@@ -426,7 +426,10 @@ ozaki25_status ozaki25_adapter_matmul(int64_t rows, int64_t n, int64_t k, int64_
  *  G: count matrices m x n (ldg), g_stride elements apart, bfloat16, half or
  *    float32;  X: the same (ldx, x_stride >= (m - 1) ldx + n), bfloat16.
  *  a, b, c: e.g. 3.4445, -4.7750, 2.0315 with 5 steps, which brings singular
- *    values to about [0.7, 1.2].
+ *    values to about [0.7, 1.2].  X_0's are at most 1.  A polynomial that lets
+ *    them grow stays in half's range in every step that starts from singular
+ *    values s < 7.9 with |b s^2 + c s^4| < 255; past that results are infinities
+ *    or NaN.
  * X is carried from step to step in FP32; the products' operands are rounded
  * to half (11 bits) and summed in FP32, whatever G's type; the diagonal of S is
  * kept in FP32, and that of b S + c S^2 in rows of S that are mostly their

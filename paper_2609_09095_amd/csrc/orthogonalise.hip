@@ -10,9 +10,10 @@
 // multiplied by P, which is small where the singular values are.
 //
 // The operands X, S and P are IEEE half: their entries are bounded (|X| by the
-// polynomial's largest value, S by its square), so powers of two place them
-// in half's range, and its 11 bits round eight times finer than the bfloat16
-// of the result.  Stored as X 2^8, S 2^10, P 2^8.
+// polynomial's largest value, S by its square), so powers of two place those of a
+// polynomial that is meant to converge in half's range (singular values below 7.9,
+// |P| below 255; larger ones become infinities), and its 11 bits round eight times
+// finer than the bfloat16 of the result.  Stored as X 2^8, S 2^10, P 2^8.
 //
 // S and P come close to multiples of the identity, and a rounding of their
 // diagonals would be an error of every vector: the diagonals d and p are kept

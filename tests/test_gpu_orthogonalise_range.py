@@ -7,7 +7,7 @@ import torch
 
 import gpu_util
 import paper_2609_09095_amd as oz
-from test_gpu_orthogonalise import gradient
+from test_gpu_orthogonalise import MUON, exact, gradient
 
 pytestmark = pytest.mark.gpu
 
@@ -46,3 +46,39 @@ def test_norms_whose_reciprocal_is_no_normal_float(shape, exponent):
     G = (gradient(shape, torch.float32) * 6e4).round().clamp(-511, 511)
     assert float(G.abs().max()) > 100
     assert torch.equal(call(G, eps=0.0), call(torch.ldexp(G.double(), torch.tensor(exponent, device="cuda")).float(), eps=0.0))
+
+
+def rank_one(shape):
+    gen = torch.Generator(device="cuda").manual_seed(1)
+    n = lambda *s: torch.randn(s, device="cuda", generator=gen)  # noqa: E731
+    return n(*shape[:-1], 1) * n(*shape[:-2], 1, shape[-1])
+
+
+def rounded(x):
+    """To half's 11 bits at any exponent."""
+    m, e = torch.frexp(x)
+    return torch.ldexp(torch.round(m * 2048) / 2048, e)
+
+
+@pytest.mark.parametrize("coefficients, steps", [
+    ((7.9, 0.0, 0.0), 2),       # singular values of 7.9 before the last step
+    ((2.0, 250.0, 0.0), 1), ((-2.0, 0.0, -250.0), 1),  # |b s^2 + c s^4| of 250
+    ((2.0, 1.5, 0.5), 2), ((3.0, -4.0, 2.0), 6), ((-7.0, 3.0, 0.0), 2), ((1e-3, 0.0, 0.0), 3), (MUON, 5)])
+@pytest.mark.parametrize("shape", SHAPES)
+def test_polynomials_inside_the_stated_range(shape, coefficients, steps):
+    """Matrices of rank one, whose singular value is 1 at first: with operands
+    of 11 bits the results are as near as the model with such operands is,
+    twice, beside the result's rounding."""
+    G = rank_one(shape)
+    X = call(G, coefficients=coefficients, steps=steps)
+    for x, g in zip(X, G):
+        want = exact(g, steps, coefficients)
+        d = (exact(g, steps, coefficients, operand=rounded) - want).norm()
+        off = (x.double() - want).norm()
+        assert off <= 2 * d + (2.0 ** -9 + 1e-5) * want.norm(), (float(off / want.norm()), float(d / want.norm()))
+
+
+@pytest.mark.parametrize("coefficients, steps", [((1e4, 0.0, 0.0), 3), ((2.0, 1e5, 0.0), 2), ((0.0, 0.0, 1e6), 3)])
+@pytest.mark.parametrize("shape", SHAPES)
+def test_polynomials_past_the_stated_range_do_not_pass_for_results(shape, coefficients, steps):
+    assert not torch.isfinite(call(rank_one(shape), coefficients=coefficients, steps=steps)).any()
