@@ -437,7 +437,9 @@ ozaki25_status ozaki25_adapter_matmul(int64_t rows, int64_t n, int64_t k, int64_
  * A matrix of zeros gives zeros; one with a NaN or infinity gives NaN.
  *  workspace: NULL to allocate stream-ordered, else at least
  *    ozaki25_orthogonalise_workspace_size() bytes, 256-byte aligned (about 8
- *    bytes per element and 4 per element of the shorter side squared).
+ *    bytes per element and 4 per element of the shorter side squared; matrices of
+ *    at most 128 x 128 keep nothing there: 256 bytes are asked for, and NULL
+ *    allocates nothing).
  * X must not overlap G.  count, m or n == 0: no-op.  Errors: INVALID_VALUE,
  * UNSUPPORTED (a side beyond OZAKI25_MAX_SIDE), WORKSPACE, HIP. */
 size_t ozaki25_orthogonalise_workspace_size(int64_t count, int64_t m, int64_t n);

@@ -71,7 +71,9 @@ struct OrthRoom {
 };
 
 OrthRoom orth_room(int64_t count, int64_t m, int64_t n) {
-  OrthRoom r;
+  OrthRoom r{};
+  r.total = kAlign;  // the least that a caller's workspace is
+  if (oz::half::orthogonalise_in_one_launch(m, n)) return r;
   const size_t each = (size_t)(pad8(m) * pad8(n)) * count, s = (size_t)pad8(m < n ? m : n), ss = s * s * count;
   size_t off = 0;
   auto take = [&](size_t bytes) {
@@ -210,8 +212,10 @@ ozaki25_status ozaki25_orthogonalise(int64_t count, int64_t m, int64_t n, const 
   if (workspace && (overlaps(workspace, r.total, X, xb) || overlaps(workspace, r.total, G, gb)))
     return OZAKI25_ERR_INVALID_VALUE;
   Room room((hipStream_t)stream);
-  const ozaki25_status st = room.take(workspace, workspace_bytes, r.total);
-  if (st != OZAKI25_SUCCESS) return st;
+  if (workspace || !oz::half::orthogonalise_in_one_launch(m, n)) {
+    const ozaki25_status st = room.take(workspace, workspace_bytes, r.total);
+    if (st != OZAKI25_SUCCESS) return st;
+  }
   oz::half::Orthogonalise o{};
   o.g = G, o.ldg = ldg, o.g_stride = g_stride;
   o.x = X, o.ldx = ldx, o.x_stride = x_stride;

@@ -78,6 +78,10 @@ struct Orthogonalise {
   float* p32;       // the rest of P's diagonal
 };
 
+// Matrices of at most this side run in one launch that needs no workspace.
+constexpr int kOneLaunchSide = 128;
+inline bool orthogonalise_in_one_launch(int64_t m, int64_t n) { return m <= kOneLaunchSide && n <= kOneLaunchSide; }
+
 // Blocks (and partial sums) per matrix of the norm.
 inline int orthogonalise_parts(int64_t m, int64_t n) {
   const int64_t p = m * ((n + 7) / 8) / 512;

@@ -487,7 +487,7 @@ __global__ __launch_bounds__(T::THREADS, 1) void update_kernel(Orthogonalise o, 
 // read both ways, along a row and (transposing loads) across rows.  Tall
 // matrices are transposed as they are read and written.  32 x 128 x 128: a launch
 // of 37 us where the steps' launches took 95.
-constexpr int kSide = 128, kRow = kSide * 2;
+constexpr int kSide = kOneLaunchSide, kRow = kSide * 2;
 constexpr float kBlockX = 32.0f;  // X's scale here, whose square is S's
 static_assert(kBlockX * kBlockX == kScaleS);
 
@@ -738,7 +738,7 @@ hipError_t steps(const Orthogonalise& o, int count, hipStream_t st) {
 }  // namespace
 
 hipError_t launch_orthogonalise(Orthogonalise o, int type, int count_steps, hipStream_t s) {
-  if (o.m <= kSide && o.n <= kSide) {
+  if (orthogonalise_in_one_launch(o.m, o.n)) {
     if (type == kBF16)
       small_kernel<kBF16><<<dim3(o.count), dim3(512), 0, s>>>(o, count_steps);
     else if (type == kF16)
