@@ -65,6 +65,9 @@ size_t align_up(size_t x) { return (x + kAlign - 1) / kAlign * kAlign; }
 int64_t pad8(int64_t x) { return (x + 7) / 8 * 8; }
 int64_t pad16(int64_t x) { return (x + 15) / 16 * 16; }
 
+// The padded rank of an adapter product; zero where nothing reaches the adapters.
+int64_t used_rank(int64_t k, int64_t adapters, int64_t rank) { return k > 0 && adapters > 0 ? pad16(rank) : 0; }
+
 // Workspace of the orthogonalisation: offsets from its start.
 struct OrthRoom {
   size_t squares, x32, x16[2], s16, p16, d32, p32, total;
@@ -138,7 +141,7 @@ size_t ozaki25_adapter_matmul_workspace_size(int64_t rows, int64_t n, int64_t k,
   if (rows <= 0 || n <= 0 || k < 0 || adapters < 0 || rank < 0 || rank > OZAKI25_MAX_RANK ||
       too_large(rows, n, k, adapters))
     return 0;
-  const oz::half::AdapterPlan a = oz::half::adapter_plan(rows, n, k, pad16(rank), adapters);
+  const oz::half::AdapterPlan a = oz::half::adapter_plan(rows, n, k, used_rank(k, adapters, rank), adapters);
   return a.h_bytes + a.h16_bytes + a.factor_bytes + a.partial_bytes;
 }
 
@@ -181,8 +184,8 @@ ozaki25_status ozaki25_adapter_matmul(int64_t rows, int64_t n, int64_t k, int64_
   p.a = A, p.lda = lda, p.a_stride = a_stride, p.b = B, p.ldb = ldb, p.b_stride = b_stride;
   p.scales = scales, p.y = Y, p.ldy = ldy;
   p.rows = (int)rows, p.n = (int)n, p.k = (int)k, p.adapters = any ? (int)adapters : 0, p.rank = any ? (int)rank : 0;
-  p.rank_pad = (int)pad16(rank), p.n_pad = (int)((n + 3) / 4 * 4);
-  const oz::half::AdapterPlan plan = oz::half::adapter_plan(rows, n, k, pad16(rank), adapters);
+  p.rank_pad = (int)used_rank(k, adapters, rank), p.n_pad = (int)((n + 3) / 4 * 4);
+  const oz::half::AdapterPlan plan = oz::half::adapter_plan(rows, n, k, p.rank_pad, adapters);
   return room.give(status_of(oz::half::launch_adapter(p, plan, room.p, (int)type, (hipStream_t)stream)));
 }
 

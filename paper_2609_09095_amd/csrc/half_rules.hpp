@@ -173,7 +173,7 @@ constexpr AdapterPlan adapter_plan(int64_t rows, int64_t n, int64_t k, int64_t r
   const size_t h1 = (size_t)a.splits * tile_rows, h2 = (size_t)a.serve_splits * a.serve_rows;
   a.h_bytes = ((h1 > h2 ? h1 : h2) * rank_pad * sizeof(float) + 255) / 256 * 256;
   a.h16_bytes = ((size_t)tile_rows * 2 * rank_pad * 2 + 255) / 256 * 256;
-  a.factor_bytes = ((size_t)tile_rows * sizeof(float) + 255) / 256 * 256;
+  a.factor_bytes = ((size_t)(rank_pad > 0 ? tile_rows : 0) * sizeof(float) + 255) / 256 * 256;
   a.partial_bytes = ((size_t)a.base_splits * a.serve_rows * (ceil_div(n, 4) * 4) * sizeof(float) + 255) / 256 * 256;
   return a;
 }

@@ -4,6 +4,7 @@ import torch
 
 import gpu_util
 import paper_2609_09095_amd as oz
+from test_gpu_grouped import draw
 from test_gpu_orthogonalise import check, gradient
 
 pytestmark = pytest.mark.gpu
@@ -28,3 +29,14 @@ def test_one_launch_in_a_graph_without_a_workspace(shape):
         graph.replay()
         torch.cuda.synchronize()
         assert torch.equal(X, oz.ozaki25_orthogonalise(G))
+
+
+@pytest.mark.parametrize("rows, n", [(3, 64), (700, 520)])
+def test_no_depth_and_no_adapters(rows, n):
+    f = dict(dtype=torch.bfloat16, device="cuda")
+    ids = torch.zeros(rows, dtype=torch.int32, device="cuda")
+    E = torch.empty
+    assert not oz.ozaki25_adapter_matmul(E(rows, 0, **f), E(n, 0, **f), ids, E(2, 24, 0, **f), E(2, n, 24, **f)).any()
+    X, W = draw((rows, 64), torch.bfloat16, 0), draw((n, 64), torch.bfloat16, 1)
+    none = oz.ozaki25_adapter_matmul(X, W, ids, E(0, 24, 64, **f), E(0, n, 24, **f))
+    assert torch.equal(none, oz.ozaki25_adapter_matmul(X, W, ids - 1, E(2, 24, 64, **f).zero_(), E(2, n, 24, **f).zero_()))
