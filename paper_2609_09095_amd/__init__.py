@@ -14,6 +14,7 @@ from __future__ import annotations
 import ctypes
 import os
 import re
+import warnings
 
 __all__ = [
     "Ozaki25Error", "lib", "library_path", "exported_symbols",
@@ -504,7 +505,9 @@ def ozaki25_dgemm_noalloc(A, B, C=None, subtract: bool = False, set: int = S12, 
 
 # ----------------------------------------------------------------- 16-bit products
 # A decode step's kernels take a few microseconds, as much as careless checks
-# would: one look at each property of each tensor.
+# would: one look at each property of each tensor.  The calls are not recorded for
+# gradients (ozaki25_grouped_matmul's are calls of their own); they warn where an
+# input asks for one.
 _HALF = None      # torch dtype -> ozaki25_dtype
 
 
@@ -568,6 +571,14 @@ def _together(first, names, *others):
             return
 
 
+def _unrecorded(what):
+    """A warning, with an input that asks for a gradient, that none is recorded."""
+    if _torch.is_grad_enabled():
+        warnings.warn(f"{what} does not record gradients: its result is a constant to autograd, though an input requires "
+                      "them (call it under torch.no_grad(), or in a torch.autograd.Function with the products that are "
+                      "its gradients)", stacklevel=3)
+
+
 def _new(like, shape, stream, dtype=None):
     """An output of the call beside `like`, of its dtype if none is given,
     allocated on the stream that writes it."""
@@ -590,6 +601,8 @@ def ozaki25_grouped_matmul(X, W, ends, Y=None, stream=None):
     if kw != k:
         raise ValueError(f"W has {kw} columns, X has {k}")
     _vector(ends, "ends", _torch.int32, groups)
+    if X.requires_grad or W.requires_grad:
+        _unrecorded("ozaki25_grouped_matmul")
     if Y is None:
         _together(X, ("X", "W", "ends"), W, ends)
         Y, ldy = _new(X, (rows, n), stream), n or 1
@@ -612,6 +625,8 @@ def ozaki25_grouped_matmul_dx(dY, W, ends, dX=None, stream=None):
     if nw != n:
         raise ValueError(f"W has {nw} rows, dY has {n} columns")
     _vector(ends, "ends", _torch.int32, groups)
+    if dY.requires_grad or W.requires_grad:
+        _unrecorded("ozaki25_grouped_matmul_dx")
     if dX is None:
         _together(dY, ("dY", "W", "ends"), W, ends)
         dX, lddx = _new(dY, (rows, k), stream), k or 1
@@ -635,6 +650,8 @@ def ozaki25_grouped_matmul_dw(dY, X, ends, dW=None, out_dtype=None, stream=None)
         raise ValueError(f"X has {rx} rows, dY has {rows}")
     groups = ends.numel() if isinstance(ends, _torch.Tensor) else 0
     _vector(ends, "ends", _torch.int32, groups)
+    if dY.requires_grad or X.requires_grad:
+        _unrecorded("ozaki25_grouped_matmul_dw")
     if dW is None:
         dW = _new(dY, (groups, n, k), stream, out_dtype)
     elif out_dtype is not None and dW.dtype != out_dtype:
@@ -671,6 +688,9 @@ def ozaki25_adapter_matmul(X, W, ids, A, B, scales=None, Y=None, workspace=None,
     if scales is not None:
         _vector(scales, "scales", _torch.float32, adapters)
     ws_ptr, ws_bytes = _room(workspace)
+    if X.requires_grad or W.requires_grad or A.requires_grad or B.requires_grad or (
+            scales is not None and scales.requires_grad):
+        _unrecorded("ozaki25_adapter_matmul")
     if Y is None:
         _together(X, ("X", "W", "ids", "A", "B", "scales", "workspace"), W, ids, A, B, scales, workspace)
         Y, ldy = _new(X, (rows, n), stream), n or 1
@@ -700,6 +720,8 @@ def ozaki25_orthogonalise(G, X=None, steps: int = 5, coefficients=(3.4445, -4.77
     size, ldg, g_stride = _pitched(G, "G", dims, (*types, _torch.float32))
     m, n = size[-2:]
     a, b, c = coefficients
+    if G.requires_grad:
+        _unrecorded("ozaki25_orthogonalise")
     if X is None:
         X = _new(G, size, stream, _torch.bfloat16)
     _, ldx, x_stride = _pitched(X, "X", dims, (_torch.bfloat16,), size)
