@@ -432,8 +432,8 @@ ozaki25_status ozaki25_adapter_matmul(int64_t rows, int64_t n, int64_t k, int64_
  *    or NaN.
  * X is carried from step to step in FP32; the products' operands are rounded
  * to half (11 bits) and summed in FP32, whatever G's type; the diagonal of S is
- * kept in FP32, and that of b S + c S^2 in rows of S that are mostly their
- * diagonal, as they are unless G has few directions.  The norm is a 64-bit sum.
+ * kept in FP32, and in the last two steps that of b S + c S^2.  The norm is a
+ * 64-bit sum.
  * A matrix of zeros gives zeros; one with a NaN or infinity gives NaN.
  *  workspace: NULL to allocate stream-ordered, else at least
  *    ozaki25_orthogonalise_workspace_size() bytes, 256-byte aligned (about 8

@@ -223,7 +223,7 @@ ozaki25_status ozaki25_orthogonalise(int64_t count, int64_t m, int64_t n, const 
   o.g = G, o.ldg = ldg, o.g_stride = g_stride;
   o.x = X, o.ldx = ldx, o.x_stride = x_stride;
   o.count = (int)count, o.m = (int)m, o.n = (int)n, o.mp = (int)pad8(m), o.np = (int)pad8(n);
-  o.a = a, o.b = b, o.c = c, o.eps = eps, o.per_c = c != 0.0f ? 1.0f / c : 0.0f;
+  o.a = a, o.b = b, o.c = c, o.eps = eps;
   o.squares = (double*)(room.p + r.squares);
   o.x32 = (float*)(room.p + r.x32);
   o.x16[0] = room.p + r.x16[0], o.x16[1] = room.p + r.x16[1];

@@ -67,15 +67,15 @@ struct Orthogonalise {
   int count, m, n;
   int mp, np;  // m, n padded to multiples of 8
   float a, b, c, eps;
-  float per_c;  // 1 / c, zero for c = 0
+  bool diagonal_in_32_bits;  // P's, in this step (set by the launch)
   // workspace
   double* squares;  // count x orthogonalise_parts
   float* x32;       // count x mp x np
   void* x16[2];     // the same
   void* s16;        // count x s x s, s the shorter padded side; zero diagonal
-  void* p16;        // the same; a share of the diagonal
+  void* p16;        // the same; the diagonal in steps that round it
   float* d32;       // count x s: the diagonal of S
-  float* p32;       // the rest of P's diagonal
+  float* p32;       // P's diagonal, or what its rounding left
 };
 
 // Matrices of at most this side run in one launch that needs no workspace.

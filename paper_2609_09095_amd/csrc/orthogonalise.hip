@@ -21,16 +21,16 @@
 //   (S^2)_ij = (So^2)_ij + (d_i + d_j) So_ij,  (S^2)_ii = (So^2)_ii + d_i^2,
 //   (P X)_ij = (Po X)_ij + p_i X_ij.
 //
-// Po meets X rounded to half, with an error e, and p meets it in 32 bits.  Where S
-// is near a multiple of the identity what is beside P's diagonal is small, and so
-// is its product with e.  Where G has few directions (r of s) P e lies in them, but
-// without the diagonal it does not: -p e is noise in all the others, which every
-// later step multiplies by a.  So Po keeps a share of its diagonal, rounded, and p
-// is the rest of it, by how much of a row of S is its diagonal,
-//   k_i = d_i^2 / (S^2)_ii   (1: the identity; about r / s for r directions):
-// all up to 1/2, none from 7/10 on.  Distance from 64 bits before the result's
-// rounding (1.7e-3), 128 x 40 of rank 16 and 40: none 4.7e-3 and 0.8e-3, all 1.2e-3
-// and 1.5e-3, shares 1.2e-3 and 0.8e-3.
+// Po meets X rounded to half, with an error e, and p meets it in 32 bits.  Near the
+// end S is near a multiple of the identity, and what is beside P's diagonal is
+// small, and so is its product with e.  But without the diagonal that product is
+// full of directions that X may not have (P e is not), and every later step
+// multiplies such noise by a: 128 x 40 of rank 1 was 9e-3 of its norm from 64 bits,
+// and 4 x 12 after eight steps all of it.  So only the last two steps take p in 32
+// bits; in the others Po has a diagonal, rounded, and p is what that rounding left.
+// Distance from 64 bits before the result's rounding (1.7e-3), 128 x 128 of rank 16
+// and 128: p in 32 bits in all steps 2.1e-3 and 0.8e-3, in none 0.8e-3 and 1.4e-3,
+// in the last two 0.8e-3 and 1.0e-3.
 //
 // Matrices are padded with zero rows and columns to multiples of 8 (zeros stay
 // zeros through every step), so all loads are DMA.
@@ -151,18 +151,18 @@ struct WidePlace {
   }
 };
 
-// P_ii in two: what Po has of it, as it is stored, and the rest; c_s2: c (So^2)_ii.
-// per_c: 1 / c, or zero for c = 0, where P says nothing of (So^2)_ii: all in Po.
+// P_ii in two: what Po has of it, as it is stored, and the rest, in 32 bits all of it;
+// c_s2: c (So^2)_ii.
 struct Diagonal {
   float stored, rest;
-  __device__ __forceinline__ Diagonal(float b, float c, float per_c, float d, float c_s2) {
-    const float p = (b + c * d) * d + c_s2, dd = d * d;
-    const float k = per_c != 0.0f ? dd * __builtin_amdgcn_rcpf(dd + c_s2 * per_c) : 0.0f;
-    const float share = fminf(fmaxf((0.7f - k) * 5.0f, 0.0f), 1.0f);
-    stored = (float)(_Float16)(p * share * kScaleP);
+  __device__ __forceinline__ Diagonal(float b, float c, float d, float c_s2, bool in_32_bits) {
+    const float p = (b + c * d) * d + c_s2;
+    stored = in_32_bits ? 0.0f : (float)(_Float16)(p * kScaleP);
     rest = p - stored * (1.0f / kScaleP);
   }
 };
+
+constexpr __host__ __device__ bool diagonal_in_32_bits(int step, int steps) { return step + 2 >= steps; }
 
 // The diagonal element that the lane holds of a WIDE block on the diagonal, set
 // to zero there; false: it holds none.
@@ -318,7 +318,7 @@ __global__ __launch_bounds__(T::THREADS, 1) void gram_kernel(Orthogonalise o, co
       const int at = r0 + (r < rows ? r : rows - 1);
       if constexpr (SQUARE) {
         // c (So^2)_ii 2^8 (So_ii is zero)
-        const Diagonal p(o.b, o.c, o.per_c, d[at], mine * (1.0f / kScaleP));
+        const Diagonal p(o.b, o.c, d[at], mine * (1.0f / kScaleP), o.diagonal_in_32_bits);
         stored[x] = p.stored;
         if (here) diagonal[at] = p.rest;
       } else if (here) {
@@ -618,7 +618,7 @@ __global__ __launch_bounds__(512, 1) void small_kernel(Orthogonalise o, int step
         float mine;
         if (row0 + 32 * x == col0) {
           const bool holds = take_diagonal(acc[x], mine);
-          const Diagonal p(o.b, o.c, o.per_c, d, mine * (1.0f / kScaleP));
+          const Diagonal p(o.b, o.c, d, mine * (1.0f / kScaleP), diagonal_in_32_bits(step, steps));
           if (holds) diag_p[r] = p.rest;
           give_diagonal(acc[x], p.stored);
         }
@@ -718,11 +718,12 @@ void update(const Orthogonalise& o, const char* x, char* next, hipStream_t st) {
 }
 
 template <bool TALL>
-hipError_t steps(const Orthogonalise& o, int count, hipStream_t st) {
+hipError_t steps(Orthogonalise o, int count, hipStream_t st) {
   const int s = TALL ? o.np : o.mp, l = TALL ? o.mp : o.np;
   for (int i = 0; i < count; ++i) {
     const char* x = (const char*)o.x16[i & 1];
     char* next = (char*)o.x16[(i + 1) & 1];
+    o.diagonal_in_32_bits = diagonal_in_32_bits(i, count);
     gram<TALL ? kAcross : kAlong, false>(o, x, s, l, o.np, st);
     gram<kAlong, true>(o, (const char*)o.s16, s, s, s, st);
     if (i + 1 < count)

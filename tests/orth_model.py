@@ -1,8 +1,8 @@
 """The orthogonalisation with the roundings that its header states, in 64-bit
 arithmetic on one matrix: the operands X, S and b S + c S^2 of the products in
-half at the kernels' powers of two, the diagonal of S, what is left of the
-diagonal of b S + c S^2 and X itself in float32.  What is left is all of it
-where a row of S is mostly its diagonal, and a rounding where it is not."""
+half at the kernels' powers of two; X itself, the diagonal of S and, in the
+last two steps, that of b S + c S^2 in float32 (in the others what its
+rounding leaves is)."""
 import torch
 
 
@@ -22,7 +22,7 @@ def model(G, steps=5, coefficients=(3.4445, -4.7750, 2.0315), eps=1e-7, scale_x=
     tall = X.shape[0] > X.shape[1]
     X = X.t() if tall else X
     X = _single(X / (X.square().sum().sqrt() + eps))
-    for _ in range(steps):
+    for step in range(steps):
         x = _half(X, scale_x)
         S = x @ x.t()
         if not diagonals_apart:
@@ -34,8 +34,7 @@ def model(G, steps=5, coefficients=(3.4445, -4.7750, 2.0315), eps=1e-7, scale_x=
         S2 = So @ So
         P = (b + c * (d[:, None] + d)) * So + c * S2
         p = _single((b + c * d) * d + c * torch.diag(S2))
-        share = ((0.7 - d * d / (d * d + torch.diag(S2))) * 5).nan_to_num(1.0).clamp(0, 1) if c else 1 + 0 * d
-        kept = _half(p * share, 256.0)
+        kept = 0 * p if step + 2 >= steps else _half(p, 256.0)
         P = _half(P - torch.diag(torch.diag(P)), 256.0) + torch.diag(kept)
         X = _single((a + p - kept)[:, None] * X + P @ x)
     return X.t() if tall else X

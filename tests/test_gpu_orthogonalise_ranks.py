@@ -24,6 +24,16 @@ def test_few_directions(shape, rank, dtype):
     check((n(*shape[:-1], rank) @ n(*shape[:-2], rank, shape[-1])).to(dtype))
 
 
+@pytest.mark.parametrize("steps", [1, 2, 5, 8])
+@pytest.mark.parametrize("shape", [(3, 2, 9), (2, 102, 2), (7, 4, 12), (3, 8, 8), (3, 7, 1200), (2, 16, 113), (3, 192, 32), (2, 64, 448)])
+def test_few_rows_of_few_directions(shape, steps):
+    gen = torch.Generator(device="cuda").manual_seed(sum(shape))
+    n = lambda *s: torch.randn(s, device="cuda", generator=gen)  # noqa: E731
+    for rank in (1, 2, 3, 5, 12, 24):
+        if rank < min(shape[1:]):
+            check(n(*shape[:-1], rank) @ n(*shape[:-2], rank, shape[-1]), steps=steps)
+
+
 @pytest.mark.parametrize("shape", [(1, 96, 128), (1, 130, 264), (1, 1000, 700)])
 def test_singular_values_over_three_decades(shape):
     gen = torch.Generator(device="cuda").manual_seed(5)
