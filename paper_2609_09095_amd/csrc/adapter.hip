@@ -3,9 +3,9 @@
 //   Y[t, :] = X[t, :] W^T + s_a (X[t, :] A_a^T) B_a^T,   a = ids[t]
 //
 // Many rows: H[t, :] = X[t, :] A_a^T is formed first, in partial sums of a
-// split depth, and s_a H written as two 16-bit numbers, its rounded value and
-// the rest, so that it keeps 16 bits (bfloat16) or 22 (half, at a power of two
-// of each row's own).  Then the projection's tiles
+// split depth, and s_a H written as two 16-bit numbers, a rounded value and the
+// rest, so that it keeps 16 bits (bfloat16) or 22 (half, at a power of two of each
+// row's own).  Then the projection's tiles
 // run and, before a tile is stored, add for each adapter that its rows name
 // the product of those rows of H with that adapter's B_a: the projection's
 // output is written once and never read.
@@ -121,16 +121,38 @@ __global__ __launch_bounds__(T::THREADS, 1) void shrink_tiles_kernel(Adapter p) 
   }
 }
 
-// s_a H from its partial sums, as the rounded values (rank_pad of a row) and
-// the rests (rank_pad more); rows without an adapter are not written.  One 16-bit
-// number would round what the result's own rounding has not asked for; two keep
-// 16 bits (bfloat16) or 22 (half) and cost 64 more ranks of the matrix cores.
+// A number of 16 bits and the rest of x, of x's sign and neither zero unless x is:
+// an infinity that both are multiplied by stays one.  The number is x rounded toward
+// zero, or the one before it where that would leave nothing; the rest is rounded
+// to nearest.  Together they keep 16 bits of x in bfloat16 and 22 in half.
+template <int TYPE>
+__device__ __forceinline__ void split(float x, uint16_t& number, uint16_t& rest) {
+  using O = typename Out<TYPE>::type;
+  const float size = __builtin_fabsf(x);
+  const uint16_t sign = __builtin_bit_cast(uint32_t, x) >> 16 & 0x8000;
+  uint32_t n, r;
+  if constexpr (TYPE == kF16)
+    n = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_pkrtz(size, 0.0f));
+  else
+    n = __builtin_bit_cast(uint32_t, size) >> 16;
+  const auto value = [](uint32_t u) { return (float)__builtin_bit_cast(O, (uint16_t)u); };
+  n -= n > 1 && value(n) == size ? 1 : 0;
+  r = __builtin_bit_cast(uint16_t, (O)(size - value(n)));
+  if (size > 0.0f) n = n > 1 ? n : 1, r = r > 1 ? r : 1;
+  if (!__builtin_isfinite(size)) n = r = __builtin_bit_cast(uint16_t, (O)size);
+  number = n | sign;
+  rest = r | sign;
+}
+
+// s_a H from its partial sums, as two 16-bit numbers (rank_pad of a row and
+// rank_pad more); rows without an adapter are not written.  One would round what the
+// result's own rounding has not asked for; two cost 64 more ranks of the matrix
+// cores.  4096 rows, rank 64: 5.0 us, mostly the launch.
 //
 // Half's range is not that of s_a H: a row's values are divided by a power of
 // two that brings its largest finite one to [2^14, 2^15), and the tiles multiply
-// its sums by that power in 32 bits.  No value overflows, and the rests' least
-// difference, 2^-24, is 2^-38 of the row's largest value or less.  bfloat16 has
-// float32's range; a value past its largest number leaves more to the rest.
+// its sums by that power in 32 bits.  No value overflows, and the least number,
+// 2^-24, is 2^-38 of the row's largest value or less.  bfloat16 has float32's range.
 // `lanes`, a power of two, hold a row, four ranks each.
 template <int TYPE>
 __global__ __launch_bounds__(256) void split_kernel(Adapter p, int lanes) {
@@ -161,55 +183,24 @@ __global__ __launch_bounds__(256) void split_kernel(Adapter p, int lanes) {
       if (r == 0) p.factors[t] = __builtin_ldexpf(1.0f, power);
     }
     if (r >= p.rank_pad) continue;
-    constexpr float kMost = TYPE == kF16 ? 65504.0f : 0x1.fep127f;
-    float hi[4], rest[4];
+    uint16_t numbers[4], rests[4];
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      hi[e] = (float)(O)v[e];
-      const bool finite = __builtin_isfinite(v[e]);
-      if (finite && !__builtin_isfinite(hi[e])) hi[e] = __builtin_copysignf(kMost, v[e]);
-      rest[e] = finite ? v[e] - hi[e] : 0.0f;
-    }
+    for (int e = 0; e < 4; ++e) split<TYPE>(v[e], numbers[e], rests[e]);
     char* const out = (char*)p.h16 + (t * 2 * p.rank_pad + r) * 2;
-    *(uint2*)out = pack4<TYPE>(hi[0], hi[1], hi[2], hi[3]);
-    *(uint2*)(out + p.rank_pad * 2) = pack4<TYPE>(rest[0], rest[1], rest[2], rest[3]);
+    __builtin_memcpy(out, numbers, 8);
+    __builtin_memcpy(out + p.rank_pad * 2, rests, 8);
   }
-}
-
-// Infinities and NaN among 8 elements.
-template <int TYPE>
-__device__ __forceinline__ bool any_special(v4i v) {
-  constexpr uint32_t kExponent = TYPE == kF16 ? 0x7c00 : 0x7f80;
-  bool any = false;
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const uint32_t lo = (uint32_t)v[i] & kExponent, hi = (uint32_t)v[i] >> 16 & kExponent;
-    any |= lo == kExponent || hi == kExponent;
-  }
-  return any;
-}
-
-// They as zeros.
-template <int TYPE>
-__device__ __forceinline__ v4i without_special(v4i v) {
-  constexpr short kExponent = TYPE == kF16 ? 0x7c00 : 0x7f80;
-  v8s e = __builtin_bit_cast(v8s, v);
-#pragma unroll
-  for (int i = 0; i < 8; ++i) e[i] = (e[i] & kExponent) == kExponent ? (short)0 : e[i];
-  return __builtin_bit_cast(v4i, e);
 }
 
 // The adapters' share of a tile, added to its sums: 64 ranks at a time, H's
 // rounded values, its rests and B_a in LDS.  A lane's outputs of a block lie in
 // one row (WIDE): it takes the sums where that row names this adapter.  (Rows
 // of other adapters as zeros would do without that choice, but pass on an
-// infinity of this adapter's B.)  An infinity of the row's own B_a meets the
-// rounded values only: a rest has either sign, or is zero.  `special`, zero at
-// first, is set once any has been seen.
+// infinity of this adapter's B.)  An infinity of the row's own B_a meets two
+// numbers of one sign (split_kernel).
 template <class T>
 __device__ __forceinline__ void expand(const Adapter& p, int r0, int rows, int c0, int cols, const int* ids,
-                                       const float* factors, int* special, char* lds,
-                                       v16f (&acc)[T::MB][T::NB]) {
+                                       const float* factors, char* lds, v16f (&acc)[T::MB][T::NB]) {
   static_assert(T::LA == kAlong && T::LB == kAlong && T::WIDE);
   static_assert(2 * T::A_BYTES + T::B_BYTES <= T::LDS);
   const int lane = threadIdx.x & 63;
@@ -242,12 +233,8 @@ __device__ __forceinline__ void expand(const Adapter& p, int r0, int rows, int c
         lo.put(i, rests, wave, lane);
       }
 #pragma unroll
-      for (int i = 0; i < T::BDMA; ++i) {
-        b.put(i, bs, wave, lane);
-        if (any_special<T::TYPE>(b.reg[i])) *special = 1;
-      }
+      for (int i = 0; i < T::BDMA; ++i) b.put(i, bs, wave, lane);
       __syncthreads();
-      const bool finite = __builtin_amdgcn_readfirstlane(*special) == 0;
       const int ks_end = left / 16;
 #pragma unroll
       for (int x = 0; x < T::MB; ++x) {
@@ -262,7 +249,7 @@ __device__ __forceinline__ void expand(const Adapter& p, int r0, int rows, int c
           for (int y = 0; y < T::NB; ++y) {
             const v4i xb = *(const v4i*)(bs + fb.at(ks) + y * 4096);
             t[y] = mfma<T::TYPE>(xb, xh, t[y]);
-            t[y] = mfma<T::TYPE>(finite ? xb : without_special<T::TYPE>(xb), xl, t[y]);
+            t[y] = mfma<T::TYPE>(xb, xl, t[y]);
           }
         }
 #pragma unroll
@@ -283,17 +270,15 @@ template <class T>
 __global__ __launch_bounds__(T::THREADS, 1) void adapter_kernel(Adapter p) {
   // one array: with two, the compiler would tell them apart by alias scopes of
   // its own and wait for the loads into LDS before every fragment
-  __shared__ __attribute__((aligned(1024))) char lds[T::LDS + T::BM * 8 + 16];
+  __shared__ __attribute__((aligned(1024))) char lds[T::LDS + T::BM * 8];
   int* const ids = (int*)(lds + T::LDS);
   float* const factors = (float*)(ids + T::BM);
-  int* const special = (int*)(factors + T::BM);
   const uint32_t tiles_n = ((uint32_t)p.n + T::BN - 1) / T::BN, tiles_m = ((uint32_t)p.rows + T::BM - 1) / T::BM;
   uint32_t place, tm, tn;
   if (!block_place(blockIdx.x, tiles_m * tiles_n, place)) return;
   place_to_tile(place, tiles_m, tiles_n, tm, tn);
   const int r0 = (int)tm * T::BM, c0 = (int)tn * T::BN;
   const int rows = p.rows - r0 < T::BM ? p.rows - r0 : T::BM, cols = p.n - c0 < T::BN ? p.n - c0 : T::BN;
-  if (threadIdx.x == 0) *special = 0;
   if (p.rank > 0)
     for (int i = threadIdx.x; i < T::BM; i += T::THREADS) {
       ids[i] = i < rows ? p.ids[r0 + i] : -1;
@@ -303,7 +288,7 @@ __global__ __launch_bounds__(T::THREADS, 1) void adapter_kernel(Adapter p) {
   if (!product<T>(Operand{(const char*)p.x + r0 * p.ldx * 2, p.ldx, rows, p.k},
                   Operand{(const char*)p.w + c0 * p.ldw * 2, p.ldw, cols, p.k}, p.k, lds, acc))
     return;
-  if (p.rank > 0) expand<T>(p, r0, rows, c0, cols, ids, factors, special, lds, acc);
+  if (p.rank > 0) expand<T>(p, r0, rows, c0, cols, ids, factors, lds, acc);
   store<T>(acc, lds, (char*)p.y + (r0 * p.ldy + c0) * 2, p.ldy, rows, cols, p.stream);
 }
 
