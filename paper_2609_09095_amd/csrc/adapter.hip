@@ -263,9 +263,9 @@ __device__ __forceinline__ void expand(const Adapter& p, int r0, int rows, int c
 }
 
 // The projection's tiles with their adapters' share.  Bound by the matrix cores:
-// 4096 x 4096 x 4096, rank 64, eight adapters in runs: 146 us (137 + 4.3 GFLOP: 970
-// TFLOP/s), without adapters 124; the tiles are one round of the CUs, whose first
-// loads and last stores overlap nothing.
+// 4096 x 4096 x 4096, rank 64, eight adapters in runs: 125 us in bfloat16 and 128 in
+// half (137 + 4.3 GFLOP: 1130 and 1100 TFLOP/s), without adapters 117; the tiles are one
+// round of the CUs, whose first loads and last stores overlap nothing.
 template <class T>
 __global__ __launch_bounds__(T::THREADS, 1) void adapter_kernel(Adapter p) {
   // one array: with two, the compiler would tell them apart by alias scopes of
@@ -295,8 +295,8 @@ __global__ __launch_bounds__(T::THREADS, 1) void adapter_kernel(Adapter p) {
 // ---- few rows (serving): the weights are read once ------------------------------
 // First launch: the projection's partial sums over parts of the depth, and
 // beside them H[t, :], a block per row, 16 ranks and part.  4096 x 4096, rank 16:
-// one row 9.4 us (33.6 MB of weights: 3.6 TB/s, the launch and first loads among
-// it), 64 rows of 64 adapters 15.8.  (One launch for both, with a counter that
+// one row 8.1 us (33.6 MB of weights: 4.2 TB/s, the launch and first loads among
+// it), 64 rows of 64 adapters 15.7.  (One launch for both, with a counter that
 // tells the last block to join, would order the blocks' writes by fences; two
 // launches need none and give the same sums in every run.)
 constexpr int kServeWaves = 4;
@@ -348,7 +348,7 @@ __global__ __launch_bounds__(kServeWaves * 64) void serve_partials_kernel(Adapte
 
 // Second launch: the partial sums in their order, then the row's adapter: a
 // thread per output, s_a H and the sum over the ranks in FP32.  As long as its
-// chain of loads: 4.1 us for one row, 5.2 for 64 (4096 columns, rank 16).
+// chain of loads: 4.4 us for one row, 5.2 for 64 (4096 columns, rank 16).
 // grid (columns / 256, rows)
 template <int TYPE>
 __global__ __launch_bounds__(256) void serve_join_kernel(Adapter p) {

@@ -49,9 +49,9 @@ __global__ __launch_bounds__(T::THREADS, 1) void grouped_rows_kernel(GroupedRows
 
 // The same for few rows per group (serving): a block reads 16 NB columns of a
 // group's weights once, for at most 16 TB of its rows.  Bound by that read: 256
-// rows of 64 groups, 1024 x 2048: 50 us (5.4 TB/s, a large copy's rate).  With
-// little to read by the launch and the chain of loads: 2 rows, two of 8 groups,
-// 2048 x 1024: 4.0 us.
+// rows of 64 groups, 1024 x 2048: 42 us (6.3 TB/s; a large copy reads and writes at
+// 4.9).  With little to read by the launch and the chain of loads: 2 rows, two of 8
+// groups, 2048 x 1024: 4.5 us.
 template <int TYPE, int NB, int TB, int WAVES, int U>
 __global__ __launch_bounds__(WAVES * 64) void grouped_few_kernel(GroupedRows g) {
   using O = typename Out<TYPE>::type;

@@ -141,13 +141,20 @@ constexpr int clamp_parts(int64_t parts, int64_t most) {
 constexpr int64_t kServeRows = 128, kServeOutputs = 1 << 18;
 
 // Rows whose adapters the tiles would go through one after the other, up to 64 in
-// a tile of 64 rows.  Few-row form / tiles, an adapter of its own choice for each
-// row (rows, n, k, rank, adapters): 256, 4096, 4096, 16, 8 47 / 60; the same of 16
-// 47 / 87; rank 64 of 64 92 / 185; 512, 1024, 1024, 16, 32 19 / 103; 333, 1000, 1111,
-// 16, 16 22 / 89; 512, 2048, 2048, 64, 32 76 / 152, but the same in runs of 16 rows
-// 75 / 45 and 512, 4096, 4096, 16, 16 85 / 95, in runs 85 / 57.
-// Depths that cannot go to LDS by DMA: 256, 4096, 4095, 16, 16 129 / 149, in runs
-// 126 / 57.
+// a tile of 64 rows.  The host knows how many adapters there are, not how many the
+// rows name, and the form that wins where each row chooses its own loses where rows
+// come in runs.  Few-row form / tiles (rows, n, k, rank, adapters), rows of their own
+// choice and in runs of 16 and 64:
+//   256, 4096, 4096, 16, 16   47 / 94    47 / 41   47 / 33
+//   256, 4096, 4096, 64, 64   96 / 222   92 / 46   83 / 35
+//   256, 2048, 2048, 16, 16   23 / 78    23 / 29   23 / 22
+//   192, 4096, 4096, 32, 32   64 / 139   61 / 42   60 / 33
+//   512, 1024, 1024, 16, 32   19 / 114   19 / 24   19 / 17
+//   333, 1000, 1111, 16, 16   23 / 97    23 / 33   23 / 24
+//   512, 2048, 2048, 64, 32   80 / 170   77 / 36   74 / 26
+// so the rule keeps the lesser worst loss; beyond it 512, 4096, 4096, 16, 16 85 / 95, in
+// runs 85 / 57.  Depths that cannot go to LDS by DMA: 256, 4096, 4095, 16, 16 129 / 149,
+// in runs 126 / 57.
 constexpr bool serve_many(int64_t rows, int64_t n, int64_t k, int64_t rank_pad, int64_t adapters) {
   if (rank_pad == 0) return false;
   if (rows <= 2 * kServeRows && k % 8 == 0) return 2 * adapters >= rank_pad;

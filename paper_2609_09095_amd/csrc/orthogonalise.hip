@@ -68,7 +68,7 @@ __device__ __forceinline__ void row8(const void* g, int64_t row, int c, int n, f
 
 // Sums of squares of a matrix, one per block, in 64 bits: no overflow or
 // underflow for any 32-bit input.  Bound by the read: 2 x 4096 x 4096 bfloat16
-// 17.6 us (3.8 TB/s).  grid (parts, count)
+// 18.7 us (3.6 TB/s).  grid (parts, count)
 template <int TYPE>
 __global__ __launch_bounds__(256) void squares_kernel(Orthogonalise o) {
   const uint32_t chunks = (uint32_t)o.np / 8, total = chunks * (uint32_t)o.m;
@@ -102,8 +102,8 @@ struct Scaling {
   __device__ __forceinline__ float operator()(float x) const { return __builtin_ldexpf(x, power) * factor; }
 };
 
-// X_0 in both forms, padding included.  Bound by memory: 2 x 4096 x 4096 51 us
-// (268 MB: 5.3 TB/s).  grid (blocks, count)
+// X_0 in both forms, padding included.  Bound by memory: 2 x 4096 x 4096 53 us
+// (268 MB: 5.1 TB/s).  grid (blocks, count)
 template <int TYPE>
 __global__ __launch_bounds__(256) void start_kernel(Orthogonalise o, int parts) {
   double sum = 0;
@@ -220,8 +220,8 @@ __device__ __forceinline__ void mirror_wide(char* lds, _Float16* out, int64_t ld
 // are meant.
 //
 // Bound by the matrix cores and, as one round of tiles, by what they do not
-// overlap (first loads, mirror image): 2 x 4096 x 4096, 256 of 272 tiles: S 125 us,
-// P 137 (1100 and 1000 TFLOP/s), the 16 left 25 each.  A contiguous range of the
+// overlap (first loads, mirror image): 2 x 4096 x 4096, 256 of 272 tiles: S 127 us,
+// P 136 (1080 and 1010 TFLOP/s), the 16 left 26 and 27.  A contiguous range of the
 // triangle per XCD instead of every eighth tile: 8 x 512 x 2048 262 / 306 us in all.
 template <class T, bool SQUARE>
 __global__ __launch_bounds__(T::THREADS, 1) void gram_kernel(Orthogonalise o, const char* in, int s, int depth,
@@ -393,7 +393,7 @@ struct TileRows {
 // X <- a X + P X (kAlong x kAcross) or, TALL, a X + X P (kAlong x kAlong: P is
 // symmetric).  LAST: the result to the caller's matrix.  grid (tiles, count)
 //
-// 2 x 4096 x 4096: 277 us for 275 GFLOP and 335 MB of X in and out (two rounds of
+// 2 x 4096 x 4096: 280 us for 275 GFLOP and 335 MB of X in and out (two rounds of
 // tiles, 100 us of products each); 3 x 1537 x 515: 15 us.
 template <class T, bool TALL, bool LAST>
 __global__ __launch_bounds__(T::THREADS, 1) void update_kernel(Orthogonalise o, const char* x16, char* next) {
@@ -486,7 +486,7 @@ __global__ __launch_bounds__(T::THREADS, 1) void update_kernel(Orthogonalise o, 
 // rows of 256 bytes have their 16-byte chunks XOR-swizzled by the row and are
 // read both ways, along a row and (transposing loads) across rows.  Tall
 // matrices are transposed as they are read and written.  32 x 128 x 128: a launch
-// of 37 us where the steps' launches took 95.
+// of 35 us where the steps' launches took 95.
 constexpr int kSide = kOneLaunchSide, kRow = kSide * 2;
 constexpr float kBlockX = 32.0f;  // X's scale here, whose square is S's
 static_assert(kBlockX * kBlockX == kScaleS);
@@ -500,7 +500,7 @@ template <bool ACROSS>
 __device__ __forceinline__ void block_product(lds_bytes a, lds_bytes b, int row0, int col0, int depth, v16f (&acc)[2]) {
   const int lane = threadIdx.x & 63;
   acc[0] = acc[1] = v16f{};
-#pragma unroll  // loads of later depths ahead: 32 x 128 x 128 42.4 -> 38.9 us
+#pragma unroll  // offsets known when compiled: 32 x 128 x 128 42.4 -> 38.9 us
   for (int k = 0; k < kSide; k += 16) {
     if (k >= depth) break;
 
