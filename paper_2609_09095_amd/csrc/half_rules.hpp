@@ -152,8 +152,9 @@ constexpr int64_t kServeRows = 128, kServeOutputs = 1 << 18;
 //   512, 1024, 1024, 16, 32   19 / 114   19 / 24   19 / 17
 //   333, 1000, 1111, 16, 16   23 / 97    23 / 33   23 / 24
 //   512, 2048, 2048, 64, 32   80 / 170   77 / 36   74 / 26
-// so the rule keeps the lesser worst loss; beyond it 512, 4096, 4096, 16, 16 85 / 95, in
-// runs 85 / 57.  Depths that cannot go to LDS by DMA: 256, 4096, 4095, 16, 16 129 / 149,
+// The tiles' worst loss (2 to 6 times, rows of their own choice) is the larger one up
+// to rank 32; at rank 64 the few-row form's in runs is as large (2.4 and 2.9).  Beyond
+// the rule 512, 4096, 4096, 16, 16 85 / 95, in runs 85 / 57.  Depths that cannot go to LDS by DMA: 256, 4096, 4095, 16, 16 129 / 149,
 // in runs 126 / 57.
 constexpr bool serve_many(int64_t rows, int64_t n, int64_t k, int64_t rank_pad, int64_t adapters) {
   if (rank_pad == 0) return false;
