@@ -154,8 +154,8 @@ constexpr int64_t kServeRows = 128, kServeOutputs = 1 << 18;
 //   512, 2048, 2048, 64, 32   80 / 170   77 / 36   74 / 26
 // The tiles' worst loss (2 to 6 times, rows of their own choice) is the larger one up
 // to rank 32; at rank 64 the few-row form's in runs is as large (2.4 and 2.9).  Beyond
-// the rule 512, 4096, 4096, 16, 16 85 / 95, in runs 85 / 57.  Depths that cannot go to LDS by DMA: 256, 4096, 4095, 16, 16 129 / 149,
-// in runs 126 / 57.
+// the rule 512, 4096, 4096, 16, 16 85 / 95, in runs 85 / 57.  Depths that cannot go to
+// LDS by DMA: 256, 4096, 4095, 16, 16 129 / 149, in runs 126 / 57.
 constexpr bool serve_many(int64_t rows, int64_t n, int64_t k, int64_t rank_pad, int64_t adapters) {
   if (rank_pad == 0) return false;
   if (rows <= 2 * kServeRows && k % 8 == 0) return 2 * adapters >= rank_pad;
