@@ -448,6 +448,69 @@ ozaki25_status ozaki25_orthogonalise(int64_t count, int64_t m, int64_t n, const 
                                      int64_t x_stride, int steps, float a, float b, float c, float eps,
                                      void* workspace, size_t workspace_bytes, void* stream);
 
+/* ---- The 8-bit path of a transformer block ---------------------------------
+ * Products of 8-bit floating-point operands (OCP e4m3) with a scale per block of
+ * 128 along the depth, what makes the operands, and a layer of experts for few
+ * tokens.  A block's scale and numbers:
+ *   s = max(max |x| / 448, 2^-126),  q = e4m3(x / s)  (to nearest even),
+ * and a block that holds a NaN or infinity has a NaN for its scale and numbers.
+ * Conventions as for the 16-bit operands; e4m3 bytes at any pitch and address
+ * (rows that start on 16 bytes take the faster loads, whatever their length; such
+ * a row's last 16 bytes are read whole and what lies past its end is not used). */
+#define OZAKI25_MAX_NORM_WIDTH 32768
+
+/* Root-mean-square norm of rows with the residual's addition:
+ *   H = X + residual (rounded to the type),
+ *   Y = H rho weight,  rho = 1 / sqrt(mean of H^2 over the row + eps),
+ * and the norm of X itself where residual is NULL (then H has to be NULL too).
+ *  X, residual, H: rows x width of `type` (OZAKI25_BF16, _F16 or _F32), pitches
+ *  ldx, ldr, ldh;  weight: width of `type`, or NULL for 1.
+ *  Y: rows x width (ldy): of `type`, or, with scales, e4m3 with a scale per row
+ *    and 128 columns: scales float32 [ceil(width/128)][rows], pitch lds.
+ * H may be X's or residual's own memory (the same pitch); Y and scales overlap
+ * nothing.  Sums run in FP32 (values beyond 1.8e19 overflow them); with eps == 0 a
+ * row of zeros gives NaN.  rows == 0 or width == 0: no-op.
+ * Errors: INVALID_VALUE, UNSUPPORTED (sizes; width beyond
+ * OZAKI25_MAX_NORM_WIDTH), HIP. */
+ozaki25_status ozaki25_rms_norm(int64_t rows, int64_t width, const void* X, int64_t ldx, const void* residual,
+                                int64_t ldr, const void* weight, ozaki25_dtype type, float eps, void* H, int64_t ldh,
+                                void* Y, int64_t ldy, float* scales, int64_t lds, void* stream);
+
+/* Its gradients, from H (X where there was no residual):
+ *   g = dY weight,  dX = rho (g - H rho^2 mean(g H)) + dH,
+ *   dweight = sum over the rows of dY H rho,
+ * dX being the gradient of X and of the residual.
+ *  dY, H, dX: rows x width of `type`;  dH: the same, the gradient that reaches H
+ *  from the residual stream, or NULL;  dweight: float32 [width], written.
+ *  Of an e4m3 Y, dY is the gradient of the numbers it stands for.
+ *  dX may be dY's or dH's own memory (the same pitch).  dweight's sum runs in an
+ *  order that the sizes fix.  workspace: NULL to allocate stream-ordered, else at least
+ *  ozaki25_rms_norm_backward_workspace_size() bytes, 256-byte aligned.
+ * rows == 0: dweight is zeros.  Errors: as above, and WORKSPACE. */
+size_t ozaki25_rms_norm_backward_workspace_size(int64_t rows, int64_t width);
+ozaki25_status ozaki25_rms_norm_backward(int64_t rows, int64_t width, const void* dY, int64_t lddy, const void* H,
+                                         int64_t ldh, const void* weight, const void* dH, int64_t lddh,
+                                         ozaki25_dtype type, float eps, void* dX, int64_t lddx, float* dweight,
+                                         void* workspace, size_t workspace_bytes, void* stream);
+
+/* A stack of matrices in e4m3, in either or both of two layouts.
+ *  X: count matrices rows x cols (ldx), x_stride elements apart, of `type`
+ *    (OZAKI25_BF16, _F16 or _F32).
+ *  squares == 0: a scale per vector of 128; squares == 1: per 128 x 128 block.
+ *  Q, scales (or both NULL): Q rows x cols (ldq, q_stride); blocks along the rows:
+ *    scales float32 [count][ceil(cols/128)][rows], or, of squares,
+ *    [count][ceil(rows/128)][ceil(cols/128)].
+ *  QT, scalesT (or both NULL): the transposed matrix, cols x rows (ldqt,
+ *    qt_stride); blocks along its rows, which are X's columns: scalesT
+ *    [count][ceil(rows/128)][cols], or [count][ceil(cols/128)][ceil(rows/128)].
+ * No output overlaps anything.  An empty matrix: no-op.  Errors:
+ * INVALID_VALUE (also with neither layout), UNSUPPORTED (sizes, or more tiles than
+ * a launch holds), HIP. */
+ozaki25_status ozaki25_quantise(int64_t count, int64_t rows, int64_t cols, const void* X, int64_t ldx, int64_t x_stride,
+                                ozaki25_dtype type, int squares, uint8_t* Q, int64_t ldq, int64_t q_stride,
+                                float* scales, uint8_t* QT, int64_t ldqt, int64_t qt_stride, float* scalesT,
+                                void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -28,6 +28,7 @@ __all__ = [
     "ozaki25_grouped_matmul", "ozaki25_grouped_matmul_dx", "ozaki25_grouped_matmul_dw",
     "ozaki25_adapter_matmul_workspace_size", "ozaki25_adapter_matmul",
     "ozaki25_orthogonalise_workspace_size", "ozaki25_orthogonalise",
+    "ozaki25_rms_norm", "ozaki25_rms_norm_backward_workspace_size", "ozaki25_rms_norm_backward", "ozaki25_quantise",
 ]
 
 _PKG = os.path.dirname(os.path.abspath(__file__))
@@ -55,6 +56,8 @@ MAX_GROUPS = 65536
 MAX_RANK = 256
 MAX_SIDE = 32768
 MAX_STEPS = 64
+MAX_NORM_WIDTH = 32768      # limits of the 8-bit path
+SCALE_BLOCK = 128           # elements that share a scale
 
 SUCCESS, ERR_INVALID_VALUE, ERR_UNSUPPORTED, ERR_WORKSPACE, ERR_HIP = range(5)
 
@@ -112,6 +115,10 @@ def lib():
             "ozaki25_orthogonalise_workspace_size": ([i64, i64, i64], sz),
             "ozaki25_orthogonalise": ([i64, i64, i64, P, i64, i64, i32, P, i64, i64, i32, f32, f32, f32, f32, P, sz, P],
                                       i32),
+            "ozaki25_rms_norm": ([i64, i64, P, i64, P, i64, P, i32, f32, P, i64, P, i64, P, i64, P], i32),
+            "ozaki25_rms_norm_backward_workspace_size": ([i64, i64], sz),
+            "ozaki25_rms_norm_backward": ([i64, i64, P, i64, P, i64, P, P, i64, i32, f32, P, i64, P, P, sz, P], i32),
+            "ozaki25_quantise": ([i64, i64, i64, P, i64, i64, i32, i32, P, i64, i64, P, P, i64, i64, P, P], i32),
             "ozaki25_grouped_matmul_dw": ([i64, i64, i64, i64, P, i64, P, i64, P, P, i64, i64, i32, i32, P], i32),
         }
         for name, (args, res) in sig.items():
@@ -731,3 +738,159 @@ def ozaki25_orthogonalise(G, X=None, steps: int = 5, coefficients=(3.4445, -4.77
                                        types.get(G.dtype, F32), X.data_ptr(), ldx, x_stride, steps, a, b, c, eps,
                                        ws_ptr, ws_bytes, _stream(stream)), "ozaki25_orthogonalise")
     return X
+
+
+# ----------------------------------------------------------------- the 8-bit path
+# e4m3 matrices are torch.float8_e4m3fn.  The library lays their rows out on 16
+# bytes (a view of a wider tensor where the row is shorter), which its products
+# read fastest; any row-major tensor will do as an input.  As above, the calls are
+# not recorded for gradients and warn where an input asks for one.
+_FLOATS = None    # torch dtype -> ozaki25_dtype, 32 bits included
+
+
+def _float_types():
+    global _FLOATS
+    if _FLOATS is None:
+        _FLOATS = {**_half_types(), _torch.float32: F32}
+    return _FLOATS
+
+
+def _here(t, what):
+    """The tensor's GPU is the current one, whose stream the call takes."""
+    if t.is_cuda and t.get_device() != _torch.cuda.current_device():
+        raise ValueError(f"{what}: the operands are on {t.device}, the current device is cuda:{_torch.cuda.current_device()}")
+
+
+def _new_e4m3(like, shape, stream):
+    """An e4m3 output beside `like`, its rows on 16 bytes."""
+    wide = -(-shape[-1] // 16) * 16
+    q = _new(like, (*shape[:-1], wide), stream, _torch.float8_e4m3fn)
+    return q if wide == shape[-1] else q[..., :shape[-1]]
+
+
+def _blocks(n):
+    return -(-n // SCALE_BLOCK)
+
+
+def _like_vector(t, name, like, count):
+    """None, or a vector of `like`'s dtype."""
+    if t is not None:
+        _vector(t, name, like.dtype, count)
+
+
+def ozaki25_rms_norm(X, weight=None, residual=None, eps: float = 1e-6, quantised: bool = False, Y=None, scales=None,
+                     H=None, stream=None):
+    """H = X + residual, Y = H / sqrt(mean(H^2) + eps) * weight by rows.  X and
+    residual: rows x width, bfloat16, float16 or float32; weight: width, of X's
+    dtype.  Returns Y, of X's dtype, or with `quantised` (Y, scales): Y in e4m3,
+    scales float32 [ceil(width/128)][rows].  With a residual H is returned after
+    them; H may be given as X or residual, to be overwritten."""
+    types = _float_types()
+    size, ldx, _ = _pitched(X, "X", 2, types)
+    rows, width = size
+    kind = (X.dtype,)
+    _like_vector(weight, "weight", X, width)
+    ldr = ldh = 1
+    if residual is not None:
+        _, ldr, _ = _pitched(residual, "residual", 2, kind, size)
+    elif H is not None:
+        raise ValueError("H needs a residual")
+    if scales is not None and not quantised:
+        raise ValueError("scales need quantised=True")
+    if X.requires_grad or (weight is not None and weight.requires_grad) or (residual is not None and residual.requires_grad):
+        _unrecorded("ozaki25_rms_norm")
+    if Y is None:
+        Y = _new_e4m3(X, size, stream) if quantised else _new(X, size, stream)
+    _, ldy, _ = _pitched(Y, "Y", 2, (_torch.float8_e4m3fn,) if quantised else kind, size)
+    lds = 1
+    if quantised:
+        if scales is None:
+            scales = _new(X, (_blocks(width), rows), stream, _torch.float32)
+        _, lds, _ = _pitched(scales, "scales", 2, (_torch.float32,), (_blocks(width), rows))
+    if residual is not None:
+        if H is None:
+            H = _new(X, size, stream)
+        _, ldh, _ = _pitched(H, "H", 2, kind, size)
+    _together(X, ("X", "weight", "residual", "H", "Y", "scales"), weight, residual, H, Y, scales)
+    _here(X, "ozaki25_rms_norm")
+    _check(lib().ozaki25_rms_norm(rows, width, X.data_ptr(), ldx, _ptr(residual), ldr, _ptr(weight), types[X.dtype], eps,
+                                  _ptr(H), ldh, Y.data_ptr(), ldy, _ptr(scales), lds, _stream(stream)),
+           "ozaki25_rms_norm")
+    out = (Y, scales) if quantised else (Y,)
+    if residual is not None:
+        out += (H,)
+    return out if len(out) > 1 else Y
+
+
+def ozaki25_rms_norm_backward_workspace_size(rows: int, width: int) -> int:
+    return lib().ozaki25_rms_norm_backward_workspace_size(rows, width)
+
+
+def ozaki25_rms_norm_backward(dY, H, weight=None, dH=None, eps: float = 1e-6, dX=None, dweight=None, workspace=None,
+                              stream=None):
+    """The gradients of ozaki25_rms_norm from the H it returned (X without a
+    residual): dX, that of X and of the residual, with dH (the gradient that H gets
+    from the residual stream) added, and dweight, float32.  dX may be given as dY
+    or dH, to be overwritten.  Returns (dX, dweight)."""
+    types = _float_types()
+    size, lddy, _ = _pitched(dY, "dY", 2, types)
+    rows, width = size
+    kind = (dY.dtype,)
+    _, ldh, _ = _pitched(H, "H", 2, kind, size)
+    _like_vector(weight, "weight", dY, width)
+    lddh = 1
+    if dH is not None:
+        _, lddh, _ = _pitched(dH, "dH", 2, kind, size)
+    ws_ptr, ws_bytes = _room(workspace)
+    if dY.requires_grad or H.requires_grad or any(t is not None and t.requires_grad for t in (weight, dH)):
+        _unrecorded("ozaki25_rms_norm_backward")
+    if dX is None:
+        dX = _new(dY, size, stream)
+    _, lddx, _ = _pitched(dX, "dX", 2, kind, size)
+    if dweight is None:
+        dweight = _new(dY, (width,), stream, _torch.float32)
+    else:
+        _vector(dweight, "dweight", _torch.float32, width)
+    _together(dY, ("dY", "H", "weight", "dH", "dX", "dweight", "workspace"), H, weight, dH, dX, dweight, workspace)
+    _here(dY, "ozaki25_rms_norm_backward")
+    _check(lib().ozaki25_rms_norm_backward(rows, width, dY.data_ptr(), lddy, H.data_ptr(), ldh, _ptr(weight), _ptr(dH),
+                                           lddh, types[dY.dtype], eps, dX.data_ptr(), lddx, dweight.data_ptr(), ws_ptr,
+                                           ws_bytes, _stream(stream)), "ozaki25_rms_norm_backward")
+    return dX, dweight
+
+
+_LAYOUTS = {"rows": (True, False), "columns": (False, True), "both": (True, True)}
+
+
+def ozaki25_quantise(X, squares: bool = False, layout: str = "rows", stream=None):
+    """X (rows x cols or count x rows x cols; bfloat16, float16 or float32) in
+    e4m3 with float32 scales of blocks of 128, or of 128 x 128 with `squares`.
+    layout "rows": (Q, scales), Q of X's shape with its blocks along the rows,
+    scales [ceil(cols/128)][rows] (squares: [ceil(rows/128)][ceil(cols/128)]);
+    "columns": (QT, scalesT), the same of X's transpose; "both": all four."""
+    types = _float_types()
+    if not (isinstance(X, _torch.Tensor) and X.dim() in (2, 3)):
+        raise ValueError("X must be a 2-D or 3-D tensor")
+    if layout not in _LAYOUTS:
+        raise ValueError(f"layout must be one of {', '.join(_LAYOUTS)}, not {layout!r}")
+    dims = X.dim()
+    size, ldx, x_stride = _pitched(X, "X", dims, types)
+    rows, cols = size[-2:]
+    head = tuple(size[:-2])
+    if X.requires_grad:
+        _unrecorded("ozaki25_quantise")
+    args, out = [], []
+    for wanted, r, c in zip(_LAYOUTS[layout], (rows, cols), (cols, rows)):
+        if not wanted:
+            args += [0, 1, 0, 0]
+            continue
+        Q = _new_e4m3(X, (*head, r, c), stream)
+        s = _new(X, (*head, *((_blocks(r), _blocks(c)) if squares else (_blocks(c), r))), stream, _torch.float32)
+        _, ldq, q_stride = _pitched(Q, "Q", dims, (_torch.float8_e4m3fn,))
+        args += [Q.data_ptr(), ldq, q_stride, s.data_ptr()]
+        out += [Q, s]
+    _on_gpu([("X", X)])
+    _here(X, "ozaki25_quantise")
+    _check(lib().ozaki25_quantise(head[0] if dims == 3 else 1, rows, cols, X.data_ptr(), ldx, x_stride, types[X.dtype],
+                                  1 if squares else 0, *args, _stream(stream)), "ozaki25_quantise")
+    return tuple(out)

@@ -1,0 +1,165 @@
+// Numbers in 8 bits (OCP e4m3) with a scale per block of 128: the scale of a
+// block, its rounding, and loads and stores of 8 elements at any alignment.
+//
+//   s = max(max |x| / 448, 2^-126),  q = e4m3(x / s)
+//
+// 448 is the largest e4m3 number and 2^-126 the least normal FP32 number, so a
+// block of zeros has a scale whose reciprocal is finite.  A NaN or infinity in a
+// block makes its scale and all its bytes NaN.
+#pragma once
+
+#include <hip/hip_runtime.h>
+
+#include <cstdint>
+
+#include "half_tile.hpp"
+
+namespace oz {
+namespace eight {
+
+using half::kBF16;
+using half::kF16;
+using half::kF32;
+using half::Out;
+using half::v4f;
+using half::v4i;
+
+constexpr int kBlock = 128;         // elements that share a scale
+constexpr float kTop = 448.0f;      // the largest e4m3 number
+constexpr float kLeast = 0x1p-126f;
+
+// |x| as bits: their order is that of the numbers, NaN above infinity
+__device__ __forceinline__ uint32_t size_bits(float x) { return __builtin_bit_cast(uint32_t, x) & 0x7fffffffu; }
+
+struct Scale {
+  float s, inverse;
+};
+
+__device__ __forceinline__ Scale scale_of(uint32_t most) {
+  Scale r;
+  r.s = fmaxf(__builtin_bit_cast(float, most) / kTop, kLeast);
+  if (most >= 0x7f800000u) r.s = __builtin_nanf("");
+  r.inverse = 1.0f / r.s;
+  return r;
+}
+
+// x / s, rounded as a division is: the residual of the first quotient is exact
+__device__ __forceinline__ float quotient(float x, Scale s) {
+  const float q = x * s.inverse;
+  return __builtin_fmaf(__builtin_fmaf(-q, s.s, x), s.inverse, q);
+}
+
+// Four numbers of at most 448 (or NaN) in e4m3, the first in the lowest byte.
+__device__ __forceinline__ uint32_t pack_e4m3(float a, float b, float c, float d) {
+  int w = __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false);
+  return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(c, d, w, true);
+}
+
+// 8 elements as they are in memory
+template <int TYPE>
+struct Raw {
+  static constexpr int Q = TYPE == kF32 ? 2 : 1;
+  v4i q[Q];
+};
+
+template <int TYPE>
+constexpr int kBytes = TYPE == kF32 ? 4 : 2;
+
+// Elements p[0 .. n), zeros above them, n at most 8; nothing is read for n < 1.
+template <int TYPE>
+__device__ __forceinline__ Raw<TYPE> load_raw(const char* p, int n) {
+  Raw<TYPE> r{};
+  const auto g = (const __attribute__((address_space(1))) char*)(half::global_bytes)p;
+  if (n >= 8) {
+#pragma unroll
+    for (int i = 0; i < Raw<TYPE>::Q; ++i)
+      __builtin_memcpy(&r.q[i], (const __attribute__((address_space(1))) void*)(g + i * 16), 16);
+  } else if (n > 0) {
+    using E = typename Out<TYPE>::type;
+    E e[8] = {};
+#pragma unroll
+    for (int j = 0; j < 7; ++j)
+      if (j < n) e[j] = ((const __attribute__((address_space(1))) E*)g)[j];
+    __builtin_memcpy(&r, e, sizeof(e));
+  }
+  return r;
+}
+
+template <int TYPE>
+__device__ __forceinline__ void values(const Raw<TYPE>& r, float (&v)[8]) {
+  using E = typename Out<TYPE>::type;
+  E e[8];
+  __builtin_memcpy(e, &r, sizeof(e));
+#pragma unroll
+  for (int j = 0; j < 8; ++j) v[j] = (float)e[j];
+}
+
+// v[0 .. n) rounded to TYPE, n at most 8
+template <int TYPE>
+__device__ __forceinline__ Raw<TYPE> rounded(const float (&v)[8]) {
+  using E = typename Out<TYPE>::type;
+  E e[8];
+#pragma unroll
+  for (int j = 0; j < 8; ++j) e[j] = (E)v[j];
+  Raw<TYPE> r;
+  __builtin_memcpy(&r, e, sizeof(e));
+  return r;
+}
+
+template <int TYPE>
+__device__ __forceinline__ void store_raw(char* p, const Raw<TYPE>& r, int n) {
+  const auto g = (__attribute__((address_space(1))) char*)p;
+  if (n >= 8) {
+#pragma unroll
+    for (int i = 0; i < Raw<TYPE>::Q; ++i)
+      __builtin_memcpy((__attribute__((address_space(1))) void*)(g + i * 16), &r.q[i], 16);
+  } else if (n > 0) {
+    using E = typename Out<TYPE>::type;
+    E e[8];
+    __builtin_memcpy(e, &r, sizeof(e));
+#pragma unroll
+    for (int j = 0; j < 7; ++j)
+      if (j < n) ((__attribute__((address_space(1))) E*)g)[j] = e[j];
+  }
+}
+
+// 8 bytes, of which n exist
+__device__ __forceinline__ void store_bytes(uint8_t* p, uint2 w, int n) {
+  const auto g = (__attribute__((address_space(1))) uint8_t*)p;
+  if (n >= 8) {
+    __builtin_memcpy((__attribute__((address_space(1))) void*)g, &w, 8);
+  } else if (n > 0) {
+    const uint64_t v = (uint64_t)w.y << 32 | w.x;
+#pragma unroll
+    for (int j = 0; j < 7; ++j)
+      if (j < n) g[j] = (uint8_t)(v >> (8 * j));
+  }
+}
+
+// A value from the lane `ror` further round the 16 lanes of its row.
+template <int ROR>
+__device__ __forceinline__ uint32_t turned(uint32_t v) {
+  return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x120 + ROR, 0xf, 0xf, false);
+}
+
+__device__ __forceinline__ uint32_t umax(uint32_t a, uint32_t b) { return a > b ? a : b; }
+
+// The largest of 16 neighbouring lanes, in all of them.
+__device__ __forceinline__ uint32_t max16(uint32_t v) {
+  v = umax(v, turned<8>(v));
+  v = umax(v, turned<4>(v));
+  v = umax(v, turned<2>(v));
+  return umax(v, turned<1>(v));
+}
+
+// The sum of 16 neighbouring lanes, in all of them; the order is the lanes'.
+__device__ __forceinline__ float sum16(float v) {
+  auto add = [](float a, uint32_t b) { return a + __builtin_bit_cast(float, b); };
+  v = add(v, turned<8>(__builtin_bit_cast(uint32_t, v)));
+  v = add(v, turned<4>(__builtin_bit_cast(uint32_t, v)));
+  v = add(v, turned<2>(__builtin_bit_cast(uint32_t, v)));
+  return add(v, turned<1>(__builtin_bit_cast(uint32_t, v)));
+}
+
+}  // namespace eight
+}  // namespace oz

@@ -1,0 +1,64 @@
+// Host interface of the 8-bit path (norm.hip, quantise.hip, scaled.hip,
+// expert_layer.hip).  Arguments were checked by the entry points.
+#pragma once
+
+#include <hip/hip_runtime.h>
+
+#include <cstdint>
+
+#include "eight_rules.hpp"
+
+namespace oz {
+namespace eight {
+
+struct Norm {
+  const void* x;  // rows x width
+  int64_t ldx;
+  const void* residual;  // the same, or null
+  int64_t ldr;
+  const void* weight;  // width, or null: 1
+  float eps;
+  void* h;  // X + residual, where there is one
+  int64_t ldh;
+  void* y;  // rows x width, of the type or e4m3
+  int64_t ldy;
+  float* scales;  // blocks x rows; null: y has the type
+  int64_t lds;
+  int rows, width;
+};
+
+struct NormGradient {
+  const void* dy;  // rows x width
+  int64_t lddy;
+  const void* h;
+  int64_t ldh;
+  const void* weight;  // or null: 1
+  const void* dh;      // the residual stream's gradient, or null
+  int64_t lddh;
+  float eps;
+  void* dx;
+  int64_t lddx;
+  float* dw;     // width
+  float* parts;  // workspace: norm_parts(rows, width) x width
+  int rows, width;
+};
+
+struct Quantise {
+  const void* x;  // count matrices rows x cols
+  int64_t ldx, x_stride;
+  uint8_t* q;  // rows x cols, or null
+  int64_t ldq, q_stride;
+  float* scales;
+  uint8_t* qt;  // cols x rows, or null
+  int64_t ldqt, qt_stride;
+  float* scales_t;
+  int count, rows, cols;
+};
+
+hipError_t launch_norm(const Norm& p, int type, hipStream_t s);
+hipError_t launch_norm_gradient(const NormGradient& p, int type, hipStream_t s);
+hipError_t launch_zeros(float* p, int64_t count, hipStream_t s);
+hipError_t launch_quantise(const Quantise& p, int type, bool squares, hipStream_t s);
+
+}  // namespace eight
+}  // namespace oz

@@ -1,0 +1,52 @@
+// The rules by which the 8-bit path chooses its kernels, from sizes alone.
+// Plain C++, so that they also compile for the host's tests.
+#pragma once
+
+#include <cstddef>
+#include <cstdint>
+
+namespace oz {
+namespace eight {
+
+constexpr int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+
+constexpr int kMaxNormWidth = 32768;
+
+// How a norm's row is spread: `lanes` threads with `chunks` times 8 elements each.
+struct NormForm {
+  int lanes, chunks;
+};
+
+constexpr NormForm norm_form(int64_t width) {
+  const int64_t c = ceil_div(width, 8);
+  if (c <= 16) return {16, 1};
+  if (c <= 32) return {32, 1};
+  if (c <= 64) return {64, 1};
+  if (c <= 128) return {64, 2};
+  if (c <= 256) return {256, 1};
+  if (c <= 512) return {512, 1};
+  if (c <= 1024) return {1024, 1};
+  if (c <= 2048) return {1024, 2};
+  return {1024, 4};
+}
+
+// Threads of a block, and rows that it holds at a time.
+constexpr int norm_threads(NormForm f) { return f.lanes < 256 ? 256 : f.lanes; }
+
+// Blocks of a norm's launch: a row at a time each, at most as many as the card
+// runs at once, so that the weights are loaded and the next row's loads are in
+// flight while a row is worked on.
+constexpr int64_t norm_blocks(int64_t rows, int64_t width, int64_t per_cu) {
+  const NormForm f = norm_form(width);
+  const int64_t threads = norm_threads(f), need = ceil_div(rows, threads / f.lanes);
+  const int64_t most = 256 * (per_cu > threads ? per_cu / threads : 1);
+  return need < most ? need : most;
+}
+
+constexpr int64_t kNormThreads = 2048;          // per CU: the forward pass
+constexpr int64_t kNormGradientThreads = 1024;  // the gradient; its blocks leave a partial sum each
+
+constexpr int64_t norm_parts(int64_t rows, int64_t width) { return norm_blocks(rows, width, kNormGradientThreads); }
+
+}  // namespace eight
+}  // namespace oz

@@ -1,43 +1,16 @@
 // The C entry points of the 16-bit products: argument checks and launches.
 #include <hip/hip_runtime.h>
 
+#include "api_checks.hpp"
 #include "half_products.hpp"
 #include "ozaki25.h"
+
+using namespace oz::api;
 
 namespace {
 
 static_assert(OZAKI25_BF16 == oz::half::kBF16 && OZAKI25_F16 == oz::half::kF16 && OZAKI25_F32 == oz::half::kF32,
               "type numbering");
-
-bool half_type(ozaki25_dtype t) { return t == OZAKI25_BF16 || t == OZAKI25_F16; }
-size_t bytes_of(ozaki25_dtype t) { return t == OZAKI25_F32 ? 4 : 2; }
-
-// Bytes from the first to the last element of a stack of matrices.
-size_t span(int64_t count, int64_t stride, int64_t rows, int64_t ld, int64_t cols, size_t elem) {
-  if (count <= 0 || rows <= 0 || cols <= 0) return 0;
-  return ((size_t)(count - 1) * (size_t)stride + (size_t)(rows - 1) * (size_t)ld + (size_t)cols) * elem;
-}
-
-bool overlaps(const void* p, size_t bytes, const void* q, size_t qbytes) {
-  const uintptr_t a = (uintptr_t)p, b = (uintptr_t)q;
-  return bytes && qbytes && a < b + qbytes && b < a + bytes;
-}
-
-bool aligned(const void* p, size_t elem) { return (uintptr_t)p % elem == 0; }
-
-// sizes of one matrix: rows x cols with pitch ld
-bool bad_matrix(int64_t rows, int64_t cols, int64_t ld) {
-  return rows < 0 || cols < 0 || ld < cols || ld < 1 || ld > OZAKI25_MAX_LD;
-}
-
-bool too_large(int64_t rows, int64_t n, int64_t k, int64_t groups) {
-  return rows > OZAKI25_MAX_ROWS || n > OZAKI25_MAX_WIDTH || k > OZAKI25_MAX_WIDTH || groups > OZAKI25_MAX_GROUPS;
-}
-
-ozaki25_status status_of(hipError_t e) {
-  if (e == hipSuccess) return OZAKI25_SUCCESS;
-  return e == hipErrorInvalidConfiguration ? OZAKI25_ERR_UNSUPPORTED : OZAKI25_ERR_HIP;
-}
 
 // the checks that the two products by rows share; W a stack of n x k
 ozaki25_status check_rows(int64_t rows, int64_t n, int64_t k, int64_t groups, const void* in, int64_t ldin,
@@ -58,9 +31,6 @@ ozaki25_status check_rows(int64_t rows, int64_t n, int64_t k, int64_t groups, co
     return OZAKI25_ERR_INVALID_VALUE;
   return OZAKI25_SUCCESS;
 }
-
-constexpr size_t kAlign = 256;
-size_t align_up(size_t x) { return (x + kAlign - 1) / kAlign * kAlign; }
 
 int64_t pad8(int64_t x) { return (x + 7) / 8 * 8; }
 int64_t pad16(int64_t x) { return (x + 15) / 16 * 16; }
@@ -100,38 +70,6 @@ OrthRoom orth_room(int64_t count, int64_t m, int64_t n) {
 bool orth_fits(int64_t count, int64_t m, int64_t n) {
   return count <= OZAKI25_MAX_GROUPS - 1 && m <= OZAKI25_MAX_SIDE && n <= OZAKI25_MAX_SIDE;
 }
-
-// A workspace of `need` bytes: the caller's, or one allocated on the stream
-// and released there when this goes out of scope.
-struct Room {
-  char* p = nullptr;
-  bool own = false;
-  hipStream_t s;
-  explicit Room(hipStream_t stream) : s(stream) {}
-  ozaki25_status take(void* workspace, size_t bytes, size_t need) {
-    if (workspace) {
-      if ((uintptr_t)workspace % kAlign) return OZAKI25_ERR_INVALID_VALUE;
-      if (bytes < need) return OZAKI25_ERR_WORKSPACE;
-      p = (char*)workspace;
-      return OZAKI25_SUCCESS;
-    }
-    void* q = nullptr;
-    if (hipMallocAsync(&q, need, s) != hipSuccess) {
-      (void)hipGetLastError();
-      return OZAKI25_ERR_WORKSPACE;
-    }
-    p = (char*)q;
-    own = true;
-    return OZAKI25_SUCCESS;
-  }
-  ozaki25_status give(ozaki25_status st) {
-    if (own) {
-      own = false;
-      if (hipFreeAsync(p, s) != hipSuccess && st == OZAKI25_SUCCESS) return OZAKI25_ERR_HIP;
-    }
-    return st;
-  }
-};
 
 }  // namespace
 

@@ -1,0 +1,133 @@
+"""What the operators of the 8-bit path refuse, before anything is launched: the C
+entry points with addresses that are never read, and the binding with CPU
+tensors."""
+import ctypes
+
+import pytest
+import torch
+
+import paper_2609_09095_amd as oz
+
+OK, BAD, UNSUPPORTED, ROOM = oz.SUCCESS, oz.ERR_INVALID_VALUE, oz.ERR_UNSUPPORTED, oz.ERR_WORKSPACE
+BF = oz.BF16
+NAN, INF = float("nan"), float("inf")
+
+
+@pytest.fixture(scope="module", autouse=True)
+def built_library():
+    import os
+    if not os.path.exists(oz.library_path()):
+        from paper_2609_09095_amd import build
+        build.build()
+    oz.lib()
+
+
+def p(i, off=0):
+    """The i-th of addresses far apart."""
+    return ctypes.c_void_p((i << 32) + off)
+
+
+def raises(match, fn, *a, **kw):
+    with pytest.raises(ValueError, match=match):
+        fn(*a, **kw)
+
+
+def test_norm_refusals():
+    f = oz.lib().ozaki25_rms_norm
+
+    def call(rows=8, width=300, X=p(1), ldx=300, R=p(2), ldr=300, w=p(3), type=BF, eps=1e-6, H=p(4), ldh=300, Y=p(5),
+             ldy=300, s=p(6), lds=8):
+        return f(rows, width, X, ldx, R, ldr, w, type, eps, H, ldh, Y, ldy, s, lds, None)
+
+    for kw in (dict(rows=-1), dict(width=-1), dict(ldx=299), dict(ldr=299), dict(ldh=299), dict(ldy=299), dict(lds=7),
+               dict(type=3), dict(type=-1), dict(eps=-1.0), dict(eps=NAN), dict(eps=INF), dict(X=None), dict(Y=None),
+               dict(H=None), dict(R=None), dict(X=p(1, 1)), dict(R=p(2, 1)), dict(w=p(3, 1)), dict(H=p(4, 1)), dict(s=p(6, 2)),
+               dict(Y=p(5, 1), s=None), dict(type=oz.F32, X=p(1, 2)), dict(ldx=oz.MAX_LD + 1),
+               # overlaps: the sum may only take the whole place of a part, the others none
+               dict(H=p(1), ldh=301), dict(H=p(1, 2)), dict(H=p(2, 600)), dict(H=p(3)), dict(Y=p(1)), dict(Y=p(2)), dict(Y=p(3)),
+               dict(Y=p(4)), dict(Y=p(6)), dict(s=p(1)), dict(s=p(4)), dict(X=p(1), R=p(1), H=p(1, 2))):
+        assert call(**kw) == BAD, kw
+    wide = oz.MAX_NORM_WIDTH + 1
+    assert call(width=wide, ldx=wide, ldr=wide, ldh=wide, ldy=wide) == UNSUPPORTED
+    assert call(rows=oz.MAX_ROWS + 1, lds=oz.MAX_ROWS + 1) == UNSUPPORTED
+    assert call(rows=0, X=None, Y=None, H=None) == OK and call(width=0, X=None, Y=None) == OK
+
+
+def test_norm_backward_refusals():
+    f = oz.lib().ozaki25_rms_norm_backward
+    need = oz.ozaki25_rms_norm_backward_workspace_size(8, 300)
+    assert need > 0 and need % 256 == 0
+    assert oz.ozaki25_rms_norm_backward_workspace_size(0, 300) == 0 == oz.ozaki25_rms_norm_backward_workspace_size(8, -1)
+
+    def call(rows=8, width=300, Y=p(1), ldy=300, H=p(2), ldh=300, w=p(3), D=p(4), ldd=300, type=BF, eps=1e-6, X=p(5), ldx=300,
+             g=p(6), room=p(7), size=need):
+        return f(rows, width, Y, ldy, H, ldh, w, D, ldd, type, eps, X, ldx, g, room, size, None)
+
+    for kw in (dict(rows=-1), dict(width=-1), dict(ldy=299), dict(ldh=299), dict(ldd=299), dict(ldx=299), dict(type=5),
+               dict(eps=-1.0), dict(eps=NAN), dict(Y=None), dict(H=None), dict(X=None), dict(g=None), dict(Y=p(1, 1)),
+               dict(H=p(2, 1)), dict(w=p(3, 1)), dict(D=p(4, 1)), dict(X=p(5, 1)), dict(g=p(6, 2)), dict(X=p(1), ldx=301),
+               dict(X=p(1, 2)), dict(X=p(4, 2)), dict(X=p(2)), dict(X=p(3)), dict(g=p(1)), dict(g=p(2)), dict(g=p(5)),
+               dict(room=p(7, 128)), dict(room=p(1)), dict(room=p(5)), dict(room=p(6))):
+        assert call(**kw) == BAD, kw
+    assert call(size=need - 1) == ROOM
+    wide = oz.MAX_NORM_WIDTH + 1
+    assert call(width=wide, ldy=wide, ldh=wide, ldd=wide, ldx=wide) == UNSUPPORTED
+    assert call(width=0, g=None) == OK
+
+
+def test_quantise_refusals():
+    f = oz.lib().ozaki25_quantise
+
+    def call(count=2, rows=8, cols=300, X=p(1), ldx=300, xs=2400, type=BF, squares=0, Q=p(2), ldq=304, qs=2432, s=p(3),
+             T=p(4), ldt=16, ts=4800, st=p(5)):
+        return f(count, rows, cols, X, ldx, xs, type, squares, Q, ldq, qs, s, T, ldt, ts, st, None)
+
+    for kw in (dict(count=-1), dict(rows=-1), dict(cols=-1), dict(ldx=299), dict(ldq=299), dict(ldt=7), dict(type=3),
+               dict(squares=2), dict(xs=-1), dict(qs=2427), dict(ts=4791), dict(X=None), dict(Q=None), dict(s=None), dict(T=None),
+               dict(st=None), dict(Q=None, s=None, T=None, st=None), dict(X=p(1, 1)), dict(s=p(3, 2)), dict(st=p(5, 1)),
+               dict(Q=p(1)), dict(T=p(1)), dict(s=p(1)), dict(st=p(1)), dict(Q=p(4)), dict(s=p(5)), dict(Q=p(3)), dict(T=p(5))):
+        assert call(**kw) == BAD, kw
+    assert call(count=oz.MAX_GROUPS) == UNSUPPORTED and call(rows=oz.MAX_ROWS + 1, ldt=oz.MAX_ROWS + 1) == UNSUPPORTED
+    wide = oz.MAX_WIDTH + 1
+    assert call(cols=wide, ldx=wide, ldq=wide) == UNSUPPORTED
+    # more tiles than a launch holds
+    assert call(count=1, rows=1 << 30, cols=1 << 12, ldx=1 << 12, X=p(1 << 12), Q=p(1 << 14), ldq=1 << 12, s=p(1 << 15), T=None,
+                st=None) == UNSUPPORTED
+    assert call(rows=0, X=None) == OK and call(count=0) == OK and call(cols=0, ldq=1) == OK
+
+
+def test_binding_norm():
+    X, w = torch.zeros(4, 20, dtype=torch.bfloat16), torch.ones(20, dtype=torch.bfloat16)
+    raises("X must be a 2-D", oz.ozaki25_rms_norm, X[0], w)
+    raises("X must be a 2-D", oz.ozaki25_rms_norm, X.double(), w)
+    raises("unit column stride", oz.ozaki25_rms_norm, X.t(), w)
+    raises("weight must be", oz.ozaki25_rms_norm, X, w.float())
+    raises("weight holds 19", oz.ozaki25_rms_norm, X, w[:19])
+    raises("residual has shape", oz.ozaki25_rms_norm, X, w, residual=X[:3])
+    raises("residual must be", oz.ozaki25_rms_norm, X, w, residual=X.float())
+    raises("H needs a residual", oz.ozaki25_rms_norm, X, w, H=X)
+    raises("scales need", oz.ozaki25_rms_norm, X, w, scales=torch.zeros(1, 4))
+    raises("Y must be", oz.ozaki25_rms_norm, X, w, Y=X.float())
+    raises("Y must be", oz.ozaki25_rms_norm, X, w, quantised=True, Y=X)
+    raises("scales has shape", oz.ozaki25_rms_norm, X, w, quantised=True, scales=torch.zeros(4, 1))
+    raises("must be a CUDA tensor", oz.ozaki25_rms_norm, X, w)
+    raises("H has shape", oz.ozaki25_rms_norm_backward, X, X[:2], w)
+    raises("dH must be", oz.ozaki25_rms_norm_backward, X, X, w, dH=X.float())
+    raises("dweight must be", oz.ozaki25_rms_norm_backward, X, X, w, dweight=w)
+    raises("workspace must be", oz.ozaki25_rms_norm_backward, X, X, w, workspace=w)
+    raises("must be a CUDA tensor", oz.ozaki25_rms_norm_backward, X, X, w)
+
+
+def test_binding_quantise():
+    X = torch.zeros(4, 20)
+    raises("2-D or 3-D", oz.ozaki25_quantise, X[0])
+    raises("X must be a 2-D tensor of dtype", oz.ozaki25_quantise, X.double())
+    raises("layout must be", oz.ozaki25_quantise, X, layout="cols")
+    raises("X must be a CUDA tensor", oz.ozaki25_quantise, X)
+
+
+def test_gradients_are_not_recorded():
+    X, w = torch.zeros(4, 20, requires_grad=True), torch.ones(20)
+    for call in (lambda: oz.ozaki25_rms_norm(X, w), lambda: oz.ozaki25_quantise(X), lambda: oz.ozaki25_rms_norm_backward(X, X, w)):
+        with pytest.warns(UserWarning, match="does not record gradients"), pytest.raises(ValueError, match="CUDA"):
+            call()
