@@ -511,6 +511,30 @@ ozaki25_status ozaki25_quantise(int64_t count, int64_t rows, int64_t cols, const
                                 float* scales, uint8_t* QT, int64_t ldqt, int64_t qt_stride, float* scalesT,
                                 void* stream);
 
+/* The product of two e4m3 matrices with a scale per block of 128 depths:
+ *   Y[r, c] = sum over blocks b of a[b, r] s[b, c]
+ *             sum over the depths l of block b of A[r, l] B[c, l].
+ *  A: rows x k (lda);  a_scales: float32 [ceil(k/128)][rows], pitch ldas;
+ *  B: n x k (ldb);  b_scales: with squares == 1 those of 128 x 128 blocks, float32
+ *    [ceil(n/128)][ceil(k/128)], s[b, c] = b_scales[c / 128][b]; with squares == 0
+ *    [ceil(k/128)][n]; pitch ldbs;
+ *  Y: rows x n (ldy) of out_type (OZAKI25_BF16, _F16 or _F32).
+ * A projection Y = X W^T takes W quantised in squares; its input's gradient the
+ * transposed bytes of the same numbers as B; its weights' gradient both operands
+ * transposed.  Sums run in FP32, the two scales of an output are multiplied first
+ * (their product has to be in FP32's range), in an order fixed by the sizes.
+ *  workspace: NULL to allocate stream-ordered, else at least
+ *    ozaki25_scaled_matmul_workspace_size() bytes (0 for most sizes), 256-byte
+ *    aligned.
+ * Y overlaps nothing.  rows == 0 or n == 0: no-op; k == 0: zeros.  Errors:
+ * INVALID_VALUE, UNSUPPORTED (sizes, or more tiles than a launch holds),
+ * WORKSPACE, HIP. */
+size_t ozaki25_scaled_matmul_workspace_size(int64_t rows, int64_t n, int64_t k);
+ozaki25_status ozaki25_scaled_matmul(int64_t rows, int64_t n, int64_t k, const uint8_t* A, int64_t lda,
+                                     const float* a_scales, int64_t ldas, const uint8_t* B, int64_t ldb,
+                                     const float* b_scales, int64_t ldbs, int squares, void* Y, int64_t ldy,
+                                     ozaki25_dtype out_type, void* workspace, size_t workspace_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -29,6 +29,7 @@ __all__ = [
     "ozaki25_adapter_matmul_workspace_size", "ozaki25_adapter_matmul",
     "ozaki25_orthogonalise_workspace_size", "ozaki25_orthogonalise",
     "ozaki25_rms_norm", "ozaki25_rms_norm_backward_workspace_size", "ozaki25_rms_norm_backward", "ozaki25_quantise",
+    "ozaki25_scaled_matmul_workspace_size", "ozaki25_scaled_matmul",
 ]
 
 _PKG = os.path.dirname(os.path.abspath(__file__))
@@ -118,6 +119,8 @@ def lib():
             "ozaki25_rms_norm": ([i64, i64, P, i64, P, i64, P, i32, f32, P, i64, P, i64, P, i64, P], i32),
             "ozaki25_rms_norm_backward_workspace_size": ([i64, i64], sz),
             "ozaki25_rms_norm_backward": ([i64, i64, P, i64, P, i64, P, P, i64, i32, f32, P, i64, P, P, sz, P], i32),
+            "ozaki25_scaled_matmul_workspace_size": ([i64, i64, i64], sz),
+            "ozaki25_scaled_matmul": ([i64, i64, i64, P, i64, P, i64, P, i64, P, i64, i32, P, i64, i32, P, sz, P], i32),
             "ozaki25_quantise": ([i64, i64, i64, P, i64, i64, i32, i32, P, i64, i64, P, P, i64, i64, P, P], i32),
             "ozaki25_grouped_matmul_dw": ([i64, i64, i64, i64, P, i64, P, i64, P, P, i64, i64, i32, i32, P], i32),
         }
@@ -894,3 +897,39 @@ def ozaki25_quantise(X, squares: bool = False, layout: str = "rows", stream=None
     _check(lib().ozaki25_quantise(head[0] if dims == 3 else 1, rows, cols, X.data_ptr(), ldx, x_stride, types[X.dtype],
                                   1 if squares else 0, *args, _stream(stream)), "ozaki25_quantise")
     return tuple(out)
+
+
+def ozaki25_scaled_matmul_workspace_size(rows: int, n: int, k: int) -> int:
+    return lib().ozaki25_scaled_matmul_workspace_size(rows, n, k)
+
+
+def ozaki25_scaled_matmul(A, a_scales, B, b_scales, squares: bool = True, out_dtype=None, Y=None, workspace=None,
+                          stream=None):
+    """Y = A B^T of e4m3 matrices (rows x k and n x k) whose blocks of 128 depths
+    have scales: a_scales float32 [ceil(k/128)][rows]; b_scales
+    [ceil(n/128)][ceil(k/128)] with `squares`, else [ceil(k/128)][n], as
+    ozaki25_quantise gives them.  out_dtype: bfloat16 (the default), float16 or
+    float32.  Returns Y, rows x n."""
+    types = _float_types()
+    eight = (_torch.float8_e4m3fn,)
+    (rows, k), lda, _ = _pitched(A, "A", 2, eight)
+    (n, kb), ldb, _ = _pitched(B, "B", 2, eight)
+    if kb != k:
+        raise ValueError(f"B has {kb} columns, A has {k}")
+    single, blocks = (_torch.float32,), _blocks(k)
+    _, ldas, _ = _pitched(a_scales, "a_scales", 2, single, (blocks, rows))
+    _, ldbs, _ = _pitched(b_scales, "b_scales", 2, single, (_blocks(n), blocks) if squares else (blocks, n))
+    ws_ptr, ws_bytes = _room(workspace)
+    if A.requires_grad or B.requires_grad or a_scales.requires_grad or b_scales.requires_grad:
+        _unrecorded("ozaki25_scaled_matmul")
+    if Y is None:
+        Y = _new(A, (rows, n), stream, out_dtype or _torch.bfloat16)
+    elif out_dtype is not None and Y.dtype != out_dtype:
+        raise ValueError(f"Y has dtype {Y.dtype}, out_dtype is {out_dtype}")
+    _, ldy, _ = _pitched(Y, "Y", 2, types, (rows, n))
+    _together(A, ("A", "a_scales", "B", "b_scales", "Y", "workspace"), a_scales, B, b_scales, Y, workspace)
+    _here(A, "ozaki25_scaled_matmul")
+    _check(lib().ozaki25_scaled_matmul(rows, n, k, A.data_ptr(), lda, a_scales.data_ptr(), ldas, B.data_ptr(), ldb,
+                                       b_scales.data_ptr(), ldbs, 1 if squares else 0, Y.data_ptr(), ldy, types[Y.dtype],
+                                       ws_ptr, ws_bytes, _stream(stream)), "ozaki25_scaled_matmul")
+    return Y

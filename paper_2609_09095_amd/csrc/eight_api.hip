@@ -129,4 +129,39 @@ ozaki25_status ozaki25_quantise(int64_t count, int64_t rows, int64_t cols, const
   return status_of(oz::eight::launch_quantise(p, (int)type, squares != 0, (hipStream_t)stream));
 }
 
+size_t ozaki25_scaled_matmul_workspace_size(int64_t rows, int64_t n, int64_t k) {
+  if (rows <= 0 || n <= 0 || k <= 0 || too_large(rows, n, k, 0)) return 0;
+  return align_up(oz::eight::scaled_room(rows, n, k));
+}
+
+ozaki25_status ozaki25_scaled_matmul(int64_t rows, int64_t n, int64_t k, const uint8_t* A, int64_t lda,
+                                     const float* a_scales, int64_t ldas, const uint8_t* B, int64_t ldb,
+                                     const float* b_scales, int64_t ldbs, int squares, void* Y, int64_t ldy,
+                                     ozaki25_dtype out_type, void* workspace, size_t workspace_bytes, void* stream) {
+  if (!float_type(out_type) || (squares != 0 && squares != 1) || n < 0 || k < 0) return OZAKI25_ERR_INVALID_VALUE;
+  const int64_t kb = ceil_div(k, 128), sr = squares ? ceil_div(n, 128) : kb, sc = squares ? kb : n;
+  if (bad_matrix(rows, k, lda) || bad_matrix(n, k, ldb) || bad_matrix(rows, n, ldy) || bad_matrix(kb, rows, ldas) ||
+      bad_matrix(sr, sc, ldbs))
+    return OZAKI25_ERR_INVALID_VALUE;
+  if (too_large(rows, n, k, 0)) return OZAKI25_ERR_UNSUPPORTED;
+  if (rows == 0 || n == 0) return OZAKI25_SUCCESS;
+  const size_t e = bytes_of(out_type);
+  if (!Y || !aligned(Y, e)) return OZAKI25_ERR_INVALID_VALUE;
+  if (k > 0 && (!A || !B || !a_scales || !b_scales || !aligned(a_scales, 4) || !aligned(b_scales, 4)))
+    return OZAKI25_ERR_INVALID_VALUE;
+  const Piece a{A, span(1, 0, rows, lda, k, 1)}, as{a_scales, span(1, 0, kb, ldas, rows, 4)}, b{B, span(1, 0, n, ldb, k, 1)},
+      bs{b_scales, span(1, 0, sr, ldbs, sc, 4)}, y{Y, span(1, 0, rows, ldy, n, e)};
+  if (meets(y, {a, as, b, bs})) return OZAKI25_ERR_INVALID_VALUE;
+  const size_t need = ozaki25_scaled_matmul_workspace_size(rows, n, k);
+  if (workspace && meets({workspace, need}, {a, as, b, bs, y})) return OZAKI25_ERR_INVALID_VALUE;
+  Room room((hipStream_t)stream);
+  if (need) {
+    const ozaki25_status st = room.take(workspace, workspace_bytes, need);
+    if (st != OZAKI25_SUCCESS) return st;
+  }
+  const oz::eight::Scaled p{A, lda, a_scales,  ldas,   B,      ldb,   b_scales,
+                            ldbs, Y, ldy, (float*)room.p, (int)rows, (int)n, (int)k, false};
+  return room.give(status_of(oz::eight::launch_scaled(p, squares != 0, (int)out_type, (hipStream_t)stream)));
+}
+
 }  // extern "C"

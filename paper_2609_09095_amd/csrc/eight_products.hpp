@@ -55,10 +55,27 @@ struct Quantise {
   int count, rows, cols;
 };
 
+struct Scaled {
+  const uint8_t* a;  // rows x k
+  int64_t lda;
+  const float* as;  // blocks x rows
+  int64_t ldas;
+  const uint8_t* b;  // n x k
+  int64_t ldb;
+  const float* bs;  // blocks x n, or of squares n blocks x blocks
+  int64_t ldbs;
+  void* y;  // rows x n
+  int64_t ldy;
+  float* parts;  // workspace: scaled_parts x rows x n
+  int rows, n, k;
+  bool stream;  // y past the caches (set by the launch)
+};
+
 hipError_t launch_norm(const Norm& p, int type, hipStream_t s);
 hipError_t launch_norm_gradient(const NormGradient& p, int type, hipStream_t s);
 hipError_t launch_zeros(float* p, int64_t count, hipStream_t s);
 hipError_t launch_quantise(const Quantise& p, int type, bool squares, hipStream_t s);
+hipError_t launch_scaled(Scaled p, bool squares, int out, hipStream_t s);
 
 }  // namespace eight
 }  // namespace oz

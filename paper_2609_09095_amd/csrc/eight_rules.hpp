@@ -48,5 +48,20 @@ constexpr int64_t kNormGradientThreads = 1024;  // the gradient; its blocks leav
 
 constexpr int64_t norm_parts(int64_t rows, int64_t width) { return norm_blocks(rows, width, kNormGradientThreads); }
 
+// An 8-bit product's form: few rows, or tiles of 64 x 64, 128 x 128, 256 x 256.
+enum ScaledForm { kScaledFew16, kScaledFew32, kScaledFew64, kScaledSmall, kScaledMiddle, kScaledLarge };
+
+constexpr ScaledForm scaled_form(int64_t rows, int64_t n, int64_t) {
+  if (rows <= 16) return kScaledFew16;
+  if (rows <= 32) return kScaledFew32;
+  if (rows <= 64) return kScaledFew64;
+  const int64_t middle = ceil_div(rows, 128) * ceil_div(n, 128), large = ceil_div(rows, 256) * ceil_div(n, 256);
+  if (middle < 205) return kScaledSmall;
+  return large >= 205 ? kScaledLarge : kScaledMiddle;
+}
+
+// Bytes that the parts of a split depth take.
+constexpr size_t scaled_room(int64_t, int64_t, int64_t) { return 0; }
+
 }  // namespace eight
 }  // namespace oz

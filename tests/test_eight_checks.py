@@ -96,6 +96,43 @@ def test_quantise_refusals():
     assert call(rows=0, X=None) == OK and call(count=0) == OK and call(cols=0, ldq=1) == OK
 
 
+def test_scaled_matmul_refusals():
+    f = oz.lib().ozaki25_scaled_matmul
+
+    def call(rows=300, n=200, k=1000, A=p(1), lda=1000, a=p(2), ldas=300, B=p(3), ldb=1000, b=p(4), ldbs=None, squares=1, Y=p(5),
+             ldy=200, out=BF, room=p(6), size=1 << 40):
+        ldbs = (8 if squares else 200) if ldbs is None else ldbs
+        return f(rows, n, k, A, lda, a, ldas, B, ldb, b, ldbs, squares, Y, ldy, out, room, size, None)
+
+    for kw in (dict(rows=-1), dict(n=-1), dict(k=-1), dict(lda=999), dict(ldb=999), dict(ldas=299), dict(ldbs=7),
+               dict(squares=0, ldbs=199), dict(squares=2), dict(ldy=199), dict(out=3), dict(out=-1), dict(A=None), dict(a=None),
+               dict(B=None), dict(b=None), dict(Y=None), dict(a=p(2, 2)), dict(b=p(4, 1)), dict(Y=p(5, 1)),
+               dict(Y=p(5, 2), out=oz.F32), dict(Y=p(1)), dict(Y=p(2)), dict(Y=p(3)), dict(Y=p(4)), dict(lda=oz.MAX_LD + 1)):
+        assert call(**kw) == BAD, kw
+    wide = oz.MAX_WIDTH + 1
+    assert call(n=wide, ldy=wide, squares=0, ldbs=wide) == UNSUPPORTED and call(k=wide, lda=wide, ldb=wide, ldbs=wide) == UNSUPPORTED
+    assert call(rows=oz.MAX_ROWS + 1, ldas=oz.MAX_ROWS + 1) == UNSUPPORTED
+    assert call(rows=1 << 30, n=1 << 22, k=1, lda=1, ldb=1, ldas=1 << 30, ldbs=1, ldy=1 << 22, a=p(64), B=p(128), b=p(129),
+                Y=p(1 << 25)) == UNSUPPORTED
+    assert call(rows=0, A=None, Y=None) == OK and call(n=0, B=None, Y=None) == OK
+
+
+def test_binding_scaled_matmul():
+    A, B = torch.zeros(4, 300).to(torch.float8_e4m3fn), torch.zeros(200, 300).to(torch.float8_e4m3fn)
+    a, b = torch.ones(3, 4), torch.ones(2, 3)
+    f = oz.ozaki25_scaled_matmul
+    raises("A must be", f, A.float(), a, B, b)
+    raises("B has 299 columns", f, A, a, B[:, :299], b)
+    raises("a_scales has shape", f, A, a[:2], B, b)
+    raises("b_scales has shape", f, A, a, B, torch.ones(3, 200))
+    raises("b_scales has shape", f, A, a, B, b, squares=False)
+    raises("b_scales must be", f, A, a, B, b.double())
+    raises("Y has dtype", f, A, a, B, b, out_dtype=torch.float16, Y=torch.zeros(4, 200))
+    raises("Y must be", f, A, a, B, b, out_dtype=torch.float64)
+    raises("Y has shape", f, A, a, B, b, Y=torch.zeros(4, 201))
+    raises("must be a CUDA tensor", f, A, a, B, b)
+
+
 def test_binding_norm():
     X, w = torch.zeros(4, 20, dtype=torch.bfloat16), torch.ones(20, dtype=torch.bfloat16)
     raises("X must be a 2-D", oz.ozaki25_rms_norm, X[0], w)
