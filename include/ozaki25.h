@@ -535,6 +535,45 @@ ozaki25_status ozaki25_scaled_matmul(int64_t rows, int64_t n, int64_t k, const u
                                      const float* b_scales, int64_t ldbs, int squares, void* Y, int64_t ldy,
                                      ozaki25_dtype out_type, void* workspace, size_t workspace_bytes, void* stream);
 
+#define OZAKI25_MAX_LAYER_TOKENS 256
+#define OZAKI25_MAX_TOP 32
+#define OZAKI25_MAX_LAYER_EXPERTS 4096
+
+/* A stack of experts' weights, experts matrices rows x cols. */
+typedef struct {
+  const void* weights;   /* of the layer's type, or e4m3 bytes where scales are given */
+  int64_t ld, stride;    /* elements from row to row, from expert to expert */
+  const float* scales;   /* of 128 x 128 blocks, [ceil(rows/128)][ceil(cols/128)] each, or NULL */
+  int64_t scales_ld, scales_stride;
+} ozaki25_expert_weights;
+
+/* A layer of experts for few tokens (a decode step), in two launches, or three for
+ * more than 16 tokens; larger batches take the grouped products.
+ *   Y[t] = sum over j of gates[t, j] D_e (silu(G_e X[t]) * (U_e X[t])),  e = which[t, j],
+ * silu(x) = x / (1 + exp(-x)), and silu(U_e X[t]) where gate is NULL.
+ *  X: tokens x width (ldx);  which: int32 [tokens][top], read on the device;
+ *  gates: float32 [tokens][top].  A choice outside [0, experts) adds nothing; one that
+ *  a token makes twice counts with both gates.
+ *  up, gate: experts x inner x width;  down: experts x out x inner;  Y: tokens x out
+ *  (ldy).  Either all stacks have scales or none.
+ *  type: OZAKI25_BF16 or OZAKI25_F16, of X, Y and of weights without scales.
+ *  Sums, the hidden values and the gates are FP32; the second product takes the hidden
+ *  values as two bfloat16 numbers, the rounded value and the rest (16 bits of it).  A
+ *  weight or hidden value that is not finite may make the outputs that it reaches NaN
+ *  where their sum is an infinity; tokens that do not reach it do not see it.
+ *  workspace: NULL to allocate stream-ordered, else at least
+ *    ozaki25_expert_layer_workspace_size() bytes, 256-byte aligned.
+ * Y overlaps nothing.  tokens == 0 or out == 0: no-op; no choice, no expert or an empty
+ * side: zeros.  Errors: INVALID_VALUE, UNSUPPORTED (more than
+ * OZAKI25_MAX_LAYER_TOKENS tokens, OZAKI25_MAX_TOP choices or
+ * OZAKI25_MAX_LAYER_EXPERTS experts; sizes), WORKSPACE, HIP. */
+size_t ozaki25_expert_layer_workspace_size(int64_t tokens, int64_t top, int64_t width, int64_t inner, int64_t out);
+ozaki25_status ozaki25_expert_layer(int64_t tokens, int64_t top, int64_t experts, int64_t width, int64_t inner,
+                                    int64_t out, const void* X, int64_t ldx, const int32_t* which, const float* gates,
+                                    const ozaki25_expert_weights* up, const ozaki25_expert_weights* gate,
+                                    const ozaki25_expert_weights* down, void* Y, int64_t ldy, ozaki25_dtype type,
+                                    void* workspace, size_t workspace_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

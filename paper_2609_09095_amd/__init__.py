@@ -30,6 +30,7 @@ __all__ = [
     "ozaki25_orthogonalise_workspace_size", "ozaki25_orthogonalise",
     "ozaki25_rms_norm", "ozaki25_rms_norm_backward_workspace_size", "ozaki25_rms_norm_backward", "ozaki25_quantise",
     "ozaki25_scaled_matmul_workspace_size", "ozaki25_scaled_matmul",
+    "ozaki25_expert_layer_workspace_size", "ozaki25_expert_layer",
 ]
 
 _PKG = os.path.dirname(os.path.abspath(__file__))
@@ -59,8 +60,17 @@ MAX_SIDE = 32768
 MAX_STEPS = 64
 MAX_NORM_WIDTH = 32768      # limits of the 8-bit path
 SCALE_BLOCK = 128           # elements that share a scale
+MAX_LAYER_TOKENS = 256
+MAX_TOP = 32
+MAX_LAYER_EXPERTS = 4096
 
 SUCCESS, ERR_INVALID_VALUE, ERR_UNSUPPORTED, ERR_WORKSPACE, ERR_HIP = range(5)
+
+
+class ExpertWeights(ctypes.Structure):
+    """ozaki25_expert_weights"""
+    _fields_ = [("weights", ctypes.c_void_p), ("ld", ctypes.c_int64), ("stride", ctypes.c_int64), ("scales", ctypes.c_void_p),
+                ("scales_ld", ctypes.c_int64), ("scales_stride", ctypes.c_int64)]
 
 
 class Ozaki25Error(RuntimeError):
@@ -121,6 +131,8 @@ def lib():
             "ozaki25_rms_norm_backward": ([i64, i64, P, i64, P, i64, P, P, i64, i32, f32, P, i64, P, P, sz, P], i32),
             "ozaki25_scaled_matmul_workspace_size": ([i64, i64, i64], sz),
             "ozaki25_scaled_matmul": ([i64, i64, i64, P, i64, P, i64, P, i64, P, i64, i32, P, i64, i32, P, sz, P], i32),
+            "ozaki25_expert_layer_workspace_size": ([i64] * 5, sz),
+            "ozaki25_expert_layer": ([i64, i64, i64, i64, i64, i64, P, i64, P, P, P, P, P, P, i64, i32, P, sz, P], i32),
             "ozaki25_quantise": ([i64, i64, i64, P, i64, i64, i32, i32, P, i64, i64, P, P, i64, i64, P, P], i32),
             "ozaki25_grouped_matmul_dw": ([i64, i64, i64, i64, P, i64, P, i64, P, P, i64, i64, i32, i32, P], i32),
         }
@@ -932,4 +944,72 @@ def ozaki25_scaled_matmul(A, a_scales, B, b_scales, squares: bool = True, out_dt
     _check(lib().ozaki25_scaled_matmul(rows, n, k, A.data_ptr(), lda, a_scales.data_ptr(), ldas, B.data_ptr(), ldb,
                                        b_scales.data_ptr(), ldbs, 1 if squares else 0, Y.data_ptr(), ldy, types[Y.dtype],
                                        ws_ptr, ws_bytes, _stream(stream)), "ozaki25_scaled_matmul")
+    return Y
+
+
+def ozaki25_expert_layer_workspace_size(tokens: int, top: int, width: int, inner: int, out: int) -> int:
+    return lib().ozaki25_expert_layer_workspace_size(tokens, top, width, inner, out)
+
+
+def _table(t, name, dtype, size):
+    """A contiguous matrix of dtype and size."""
+    if not (isinstance(t, _torch.Tensor) and t.dtype == dtype and t.dim() == 2 and t.is_contiguous()):
+        raise ValueError(f"{name} must be a contiguous 2-D {str(dtype).replace('torch.', '')} tensor")
+    if t.shape != size:
+        raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {tuple(size)}")
+
+
+def _stack(W, name, scales, kind, size):
+    """The argument for a stack of weights with or without scales."""
+    (experts, rows, cols), ld, stride = _pitched(W, name, 3, kind, size)
+    if scales is None:
+        return ExpertWeights(W.data_ptr(), ld, stride, 0, 1, 0)
+    _, lds, s_stride = _pitched(scales, f"{name}_scales", 3, (_torch.float32,), (experts, _blocks(rows), _blocks(cols)))
+    return ExpertWeights(W.data_ptr(), ld, stride, scales.data_ptr(), lds, s_stride)
+
+
+def ozaki25_expert_layer(X, which, gates, up, down, gate=None, up_scales=None, down_scales=None, gate_scales=None, Y=None,
+                         workspace=None, stream=None):
+    """Y[t] = sum over j of gates[t, j] down[e] (silu(gate[e] X[t]) * (up[e] X[t])),
+    e = which[t, j] (silu(up[e] X[t]) without gate), for up to MAX_LAYER_TOKENS tokens.
+    X: tokens x width, bfloat16 or float16; which: int32 tokens x top, read on the
+    device, a choice outside [0, experts) adding nothing; gates: float32, the same.
+    up, gate: experts x inner x width, down: experts x out x inner, of X's dtype, or
+    float8_e4m3fn with scales of 128 x 128 blocks as ozaki25_quantise gives them.
+    Returns Y, tokens x out."""
+    types = _half_types()
+    (tokens, width), ldx, _ = _pitched(X, "X", 2, types)
+    kind = (X.dtype,)
+    top = which.shape[1] if isinstance(which, _torch.Tensor) and which.dim() == 2 else 0
+    _table(which, "which", _torch.int32, (tokens, top))
+    _table(gates, "gates", _torch.float32, (tokens, top))
+    eight = up_scales is not None
+    if (down_scales is not None) != eight or (gate is not None and (gate_scales is not None) != eight):
+        raise ValueError("either all weights have scales or none")
+    if gate is None and gate_scales is not None:
+        raise ValueError("gate_scales need gate")
+    stored = (_torch.float8_e4m3fn,) if eight else kind
+    (experts, inner, wu), _, _ = _pitched(up, "up", 3, stored)
+    if wu != width:
+        raise ValueError(f"up has {wu} columns, X has {width}")
+    (ed, out, wd), _, _ = _pitched(down, "down", 3, stored)
+    if (ed, wd) != (experts, inner):
+        raise ValueError(f"down has shape {tuple(down.shape)}, expected ({experts}, out, {inner})")
+    u = _stack(up, "up", up_scales, stored, up.shape)
+    d = _stack(down, "down", down_scales, stored, down.shape)
+    g = None if gate is None else _stack(gate, "gate", gate_scales, stored, up.shape)
+    ws_ptr, ws_bytes = _room(workspace)
+    others = (which, gates, up, down, gate, up_scales, down_scales, gate_scales)
+    if X.requires_grad or any(t is not None and t.requires_grad for t in others):
+        _unrecorded("ozaki25_expert_layer")
+    if Y is None:
+        Y = _new(X, (tokens, out), stream)
+    _, ldy, _ = _pitched(Y, "Y", 2, kind, (tokens, out))
+    _together(X, ("X", "which", "gates", "up", "down", "gate", "up_scales", "down_scales", "gate_scales", "Y", "workspace"),
+              *others, Y, workspace)
+    _here(X, "ozaki25_expert_layer")
+    _check(lib().ozaki25_expert_layer(tokens, top, experts, width, inner, out, X.data_ptr(), ldx, which.data_ptr(),
+                                      gates.data_ptr(), ctypes.addressof(u), 0 if g is None else ctypes.addressof(g),
+                                      ctypes.addressof(d), Y.data_ptr(), ldy, types[X.dtype], ws_ptr, ws_bytes,
+                                      _stream(stream)), "ozaki25_expert_layer")
     return Y

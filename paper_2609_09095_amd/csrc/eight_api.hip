@@ -12,7 +12,9 @@ namespace {
 
 using oz::eight::ceil_div;
 
-static_assert(OZAKI25_MAX_NORM_WIDTH == oz::eight::kMaxNormWidth, "limits");
+static_assert(OZAKI25_MAX_NORM_WIDTH == oz::eight::kMaxNormWidth && OZAKI25_MAX_LAYER_TOKENS == oz::eight::kMaxLayerTokens &&
+                  OZAKI25_MAX_TOP == oz::eight::kMaxTop && OZAKI25_MAX_LAYER_EXPERTS == oz::eight::kMaxLayerExperts,
+              "limits");
 
 bool float_type(ozaki25_dtype t) { return half_type(t) || t == OZAKI25_F32; }
 
@@ -33,6 +35,24 @@ bool meets(Piece out, const Piece (&in)[N]) {
   for (const Piece& i : in)
     if (i.p && out.p && overlaps(out.p, out.bytes, i.p, i.bytes)) return true;
   return false;
+}
+
+// A stack of rows x cols weights: its sizes.
+bool bad_stack(const ozaki25_expert_weights& w, int64_t experts, int64_t rows, int64_t cols) {
+  if (bad_matrix(rows, cols, w.ld) || (experts > 1 && w.stride < 0)) return true;
+  return w.scales && (bad_matrix(ceil_div(rows, 128), ceil_div(cols, 128), w.scales_ld) || (experts > 1 && w.scales_stride < 0));
+}
+
+bool bad_pointers(const ozaki25_expert_weights& w) {
+  return !w.weights || !aligned(w.weights, w.scales ? 1 : 2) || !aligned(w.scales, 4);
+}
+
+Piece weights_of(const ozaki25_expert_weights& w, int64_t experts, int64_t rows, int64_t cols) {
+  return {w.weights, span(experts, w.stride, rows, w.ld, cols, w.scales ? 1 : 2)};
+}
+
+Piece scales_of(const ozaki25_expert_weights& w, int64_t experts, int64_t rows, int64_t cols) {
+  return {w.scales, span(experts, w.scales_stride, ceil_div(rows, 128), w.scales_ld, ceil_div(cols, 128), 4)};
 }
 
 bool bad_eps(float eps) { return !(eps >= 0.0f) || !__builtin_isfinite(eps); }
@@ -162,6 +182,68 @@ ozaki25_status ozaki25_scaled_matmul(int64_t rows, int64_t n, int64_t k, const u
   const oz::eight::Scaled p{A, lda, a_scales,  ldas,   B,      ldb,   b_scales,
                             ldbs, Y, ldy, (float*)room.p, (int)rows, (int)n, (int)k, false};
   return room.give(status_of(oz::eight::launch_scaled(p, squares != 0, (int)out_type, (hipStream_t)stream)));
+}
+
+size_t ozaki25_expert_layer_workspace_size(int64_t tokens, int64_t top, int64_t width, int64_t inner, int64_t out) {
+  if (tokens <= 0 || top <= 0 || width <= 0 || inner <= 0 || out <= 0 || tokens > OZAKI25_MAX_LAYER_TOKENS ||
+      top > OZAKI25_MAX_TOP || too_large(0, inner, width, 0) || out > OZAKI25_MAX_WIDTH)
+    return 0;
+  return align_up(oz::eight::layer_hidden_bytes(tokens, top, inner)) + align_up(oz::eight::layer_part_bytes(tokens, top, out));
+}
+
+ozaki25_status ozaki25_expert_layer(int64_t tokens, int64_t top, int64_t experts, int64_t width, int64_t inner,
+                                    int64_t out, const void* X, int64_t ldx, const int32_t* which, const float* gates,
+                                    const ozaki25_expert_weights* up, const ozaki25_expert_weights* gate,
+                                    const ozaki25_expert_weights* down, void* Y, int64_t ldy, ozaki25_dtype type,
+                                    void* workspace, size_t workspace_bytes, void* stream) {
+  if (!half_type(type) || !up || !down || top < 0 || experts < 0 || bad_matrix(tokens, width, ldx) ||
+      bad_matrix(tokens, out, ldy))
+    return OZAKI25_ERR_INVALID_VALUE;
+  if (bad_stack(*up, experts, inner, width) || (gate && bad_stack(*gate, experts, inner, width)) ||
+      bad_stack(*down, experts, out, inner))
+    return OZAKI25_ERR_INVALID_VALUE;
+  if (!up->scales != !down->scales || (gate && !gate->scales != !up->scales)) return OZAKI25_ERR_INVALID_VALUE;
+  if (tokens > OZAKI25_MAX_LAYER_TOKENS || top > OZAKI25_MAX_TOP || experts > OZAKI25_MAX_LAYER_EXPERTS ||
+      too_large(0, inner, width, 0) || out > OZAKI25_MAX_WIDTH)
+    return OZAKI25_ERR_UNSUPPORTED;
+  if (tokens == 0 || out == 0) return OZAKI25_SUCCESS;
+  if (!Y || !aligned(Y, 2)) return OZAKI25_ERR_INVALID_VALUE;
+  const bool any = top > 0 && experts > 0 && width > 0 && inner > 0;
+  if (any && (!X || !which || !gates || !aligned(X, 2) || !aligned(which, 4) || !aligned(gates, 4) || bad_pointers(*up) ||
+              bad_pointers(*down) || (gate && bad_pointers(*gate))))
+    return OZAKI25_ERR_INVALID_VALUE;
+  const ozaki25_expert_weights none{}, *g = gate ? gate : &none;
+  const Piece y{Y, span(1, 0, tokens, ldy, out, 2)};
+  const Piece in[9] = {{X, span(1, 0, tokens, ldx, width, 2)},
+                       {which, (size_t)(tokens * top) * 4},
+                       {gates, (size_t)(tokens * top) * 4},
+                       weights_of(*up, experts, inner, width),
+                       scales_of(*up, experts, inner, width),
+                       weights_of(*g, experts, inner, width),
+                       scales_of(*g, experts, inner, width),
+                       weights_of(*down, experts, out, inner),
+                       scales_of(*down, experts, out, inner)};
+  const size_t need = any ? ozaki25_expert_layer_workspace_size(tokens, top, width, inner, out) : 0;
+  if (meets(y, in) || (workspace && (meets({workspace, need}, in) || meets({workspace, need}, {y}))))
+    return OZAKI25_ERR_INVALID_VALUE;
+  Room room((hipStream_t)stream);
+  if (need) {
+    const ozaki25_status st = room.take(workspace, workspace_bytes, need);
+    if (st != OZAKI25_SUCCESS) return st;
+  }
+  auto stack = [](const ozaki25_expert_weights& w) {
+    return oz::eight::ExpertWeights{w.weights, w.ld, w.stride, w.scales, w.scales_ld, w.scales_stride};
+  };
+  oz::eight::Layer p{};
+  p.x = X, p.ldx = ldx, p.which = which, p.gates = gates;
+  p.up = stack(*up), p.gate = stack(*g), p.down = stack(*down);
+  p.y = Y, p.ldy = ldy;
+  p.hidden = (float*)room.p;
+  p.parts = (float*)(room.p + align_up(oz::eight::layer_hidden_bytes(tokens, top, inner)));
+  p.tokens = (int)tokens, p.top = (int)top, p.experts = (int)experts;
+  p.width = (int)width, p.inner = (int)inner, p.out = (int)out;
+  p.inner_pad = (int)oz::eight::pad4(inner), p.out_pad = (int)oz::eight::pad4(out);
+  return room.give(status_of(oz::eight::launch_layer(p, (int)type, up->scales != nullptr, (hipStream_t)stream)));
 }
 
 }  // extern "C"

@@ -71,6 +71,30 @@ struct Scaled {
   bool stream;  // y past the caches (set by the launch)
 };
 
+// A stack of experts' weights: of the layer's type, or e4m3 with the scales of
+// 128 x 128 blocks.
+struct ExpertWeights {
+  const void* w;
+  int64_t ld, stride;
+  const float* scales;  // or null
+  int64_t scales_ld, scales_stride;
+};
+
+struct Layer {
+  const void* x;  // tokens x width
+  int64_t ldx;
+  const int32_t* which;  // tokens x top
+  const float* gates;
+  ExpertWeights up, gate, down;  // experts x inner x width, the same (w null: none), experts x out x inner
+  void* y;                       // tokens x out
+  int64_t ldy;
+  float* hidden;  // workspace: tokens top x inner_pad
+  float* parts;   // workspace of more than kTogether tokens: tokens top x out_pad
+  int tokens, top, experts, width, inner, out;
+  int inner_pad, out_pad;  // multiples of 4
+};
+
+hipError_t launch_layer(const Layer& p, int type, bool eight, hipStream_t s);
 hipError_t launch_norm(const Norm& p, int type, hipStream_t s);
 hipError_t launch_norm_gradient(const NormGradient& p, int type, hipStream_t s);
 hipError_t launch_zeros(float* p, int64_t count, hipStream_t s);

@@ -63,5 +63,17 @@ constexpr ScaledForm scaled_form(int64_t rows, int64_t n, int64_t) {
 // Bytes that the parts of a split depth take.
 constexpr size_t scaled_room(int64_t, int64_t, int64_t) { return 0; }
 
+// A layer of experts for few tokens.
+constexpr int kMaxLayerTokens = 256, kMaxTop = 32, kMaxLayerExperts = 4096;
+constexpr int kTogether = 16;  // tokens whose sums over their experts stay in one block
+
+constexpr int64_t pad4(int64_t n) { return (n + 3) / 4 * 4; }
+constexpr size_t layer_hidden_bytes(int64_t tokens, int64_t top, int64_t inner) {
+  return (size_t)(tokens * top * pad4(inner)) * 4;
+}
+constexpr size_t layer_part_bytes(int64_t tokens, int64_t top, int64_t out) {
+  return tokens > kTogether ? (size_t)(tokens * top * pad4(out)) * 4 : 0;
+}
+
 }  // namespace eight
 }  // namespace oz

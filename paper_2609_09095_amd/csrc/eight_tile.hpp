@@ -94,38 +94,6 @@ struct ByteDma {
   static constexpr int IN_FLIGHT = T::ADMA + T::BDMA;
 };
 
-// 16 bytes of which the upper `have` are moved down, zeros above them.
-__device__ __forceinline__ v4i keep_upper_bytes(v4i v, int have) {
-  const int s = 8 * (16 - have);  // bits to drop; 128: all
-  const uint4 x = __builtin_bit_cast(uint4, v);
-  uint64_t lo = (uint64_t)x.y << 32 | x.x, hi = (uint64_t)x.w << 32 | x.z;
-  const uint64_t up = hi << 1 << (63 - (s & 63));  // hi << (64 - s), also for s = 0
-  lo = s < 64 ? lo >> (s & 63) | up : hi >> (s & 63);
-  hi = s < 64 ? hi >> (s & 63) : 0;
-  if (s == 128) lo = 0;
-  return v4i{(int)lo, (int)(lo >> 32), (int)hi, (int)(hi >> 32)};
-}
-
-// Bytes o .. o + 15 of a row of `size`, zeros past its end, at any alignment.  A
-// chunk that the end cuts is read as the row's last 16 bytes; no branch around the
-// load where rows have 16.
-__device__ __forceinline__ v4i load16(const char* row, int64_t o, int64_t size) {
-  const int64_t n = size - o;
-  const int have = n < 0 ? 0 : n < 16 ? (int)n : 16;
-  if (size >= 16) return keep_upper_bytes(half::load_whole(row + (have > 0 ? o - (16 - have) : 0)), have);
-  uint64_t lo = 0, hi = 0;
-  const auto q = (const __attribute__((address_space(1))) uint8_t*)(half::global_bytes)row;
-#pragma unroll
-  for (int j = 0; j < 15; ++j)
-    if (j < have) {
-      if (j < 8)
-        lo |= (uint64_t)q[o + j] << (8 * j);
-      else
-        hi |= (uint64_t)q[o + j] << (8 * (j - 8));
-    }
-  return v4i{(int)lo, (int)(lo >> 32), (int)hi, (int)(hi >> 32)};
-}
-
 // Any alignment and pitch, through registers.
 template <int V, int N>
 struct ByteSide {
@@ -223,16 +191,6 @@ struct ByteFragments {
   }
 };
 
-// 8 e4m3 numbers (two words) in bfloat16, which holds them exactly.
-__device__ __forceinline__ v4i widened(int lo, int hi) {
-  typedef __bf16 v2b __attribute__((ext_vector_type(2)));
-  const v2b e[4] = {__builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, 1.0f, false), __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, 1.0f, true),
-                    __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, 1.0f, false), __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, 1.0f, true)};
-  v4i r;
-  __builtin_memcpy(&r, e, 16);
-  return r;
-}
-
 // c + a b, 64 depths of 32 x 32 outputs.  The 8-bit products add the eight products
 // of neighbouring depths with 13 bits below the largest of them (measured: 1.4e-5 of
 // a result's norm on normal numbers, whatever the depth), which a 16-bit output's
@@ -243,7 +201,7 @@ __device__ __forceinline__ v16f mfma64(v8i a, v8i b, v16f c) {
   if constexpr (OUT == kF32) {
 #pragma unroll
     for (int j = 0; j < 4; ++j)
-      c = half::mfma<kBF16>(widened(a[2 * j], a[2 * j + 1]), widened(b[2 * j], b[2 * j + 1]), c);
+      c = half::mfma<kBF16>(widened<kBF16>(a[2 * j], a[2 * j + 1]), widened<kBF16>(b[2 * j], b[2 * j + 1]), c);
     return c;
   } else {
     // scale operands of 0 are 2^0
@@ -257,7 +215,7 @@ __device__ __forceinline__ v4f mfma128(v8i a, v8i b, v4f c) {
   if constexpr (OUT == kF32) {
 #pragma unroll
     for (int j = 0; j < 4; ++j)
-      c = half::mfma16<kBF16>(widened(a[2 * j], a[2 * j + 1]), widened(b[2 * j], b[2 * j + 1]), c);
+      c = half::mfma16<kBF16>(widened<kBF16>(a[2 * j], a[2 * j + 1]), widened<kBF16>(b[2 * j], b[2 * j + 1]), c);
     return c;
   } else {
     return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, b, c, 0, 0, 0, 0, 0, 0);

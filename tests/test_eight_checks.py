@@ -133,6 +133,72 @@ def test_binding_scaled_matmul():
     raises("must be a CUDA tensor", f, A, a, B, b)
 
 
+def test_expert_layer_refusals():
+    f = oz.lib().ozaki25_expert_layer
+    size = oz.ozaki25_expert_layer_workspace_size
+    need = size(20, 2, 300, 200, 400)
+    assert need > 0 and need % 256 == 0
+    assert size(0, 2, 300, 200, 400) == 0 == size(20, 0, 300, 200, 400) == size(257, 2, 300, 200, 400) == size(20, 33, 300, 200, 400)
+
+    def stack(w, ld, stride, s=None, lds=1, ss=0):
+        return oz.ExpertWeights(w, ld, stride, s, lds, ss)
+
+    def call(tokens=20, top=2, experts=8, width=300, inner=200, out=400, X=p(1), ldx=300, which=p(2), gates=p(3), up=None, gate=None,
+             down=None, Y=p(7), ldy=400, type=BF, room=p(8), size=need, no=()):
+        up = up or stack(4 << 32, 300, 60000)
+        gate = gate or stack(5 << 32, 300, 60000)
+        down = down or stack(6 << 32, 200, 80000)
+        at = [None if n in no else ctypes.addressof(v) for n, v in (("up", up), ("gate", gate), ("down", down))]
+        return f(tokens, top, experts, width, inner, out, X, ldx, which, gates, *at, Y, ldy, type, room, size, None)
+
+    eight = dict(up=stack(4 << 32, 300, 60000, 9 << 32, 3, 6), gate=stack(5 << 32, 300, 60000, 10 << 32, 3, 6),
+                 down=stack(6 << 32, 200, 80000, 11 << 32, 2, 8))
+    for kw in (dict(tokens=-1), dict(top=-1), dict(experts=-1), dict(width=-1), dict(inner=-1), dict(out=-1), dict(ldx=299),
+               dict(ldy=399), dict(type=oz.F32), dict(type=4), dict(X=None), dict(which=None), dict(gates=None), dict(Y=None),
+               dict(X=p(1, 1)), dict(which=p(2, 2)), dict(gates=p(3, 1)), dict(Y=p(7, 1)), dict(no=("up",)), dict(no=("down",)),
+               dict(up=stack(None, 300, 60000)), dict(up=stack((4 << 32) + 1, 300, 60000)), dict(up=stack(4 << 32, 299, 60000)),
+               dict(down=stack(6 << 32, 199, 80000)), dict(gate=stack(5 << 32, 300, -1)), dict(eight, gate=stack(5 << 32, 300, 60000)),
+               dict(eight, down=stack(6 << 32, 200, 80000)), dict(eight, up=stack(4 << 32, 300, 60000, 9 << 32, 2, 6)),
+               dict(eight, up=stack(4 << 32, 300, 60000, (9 << 32) + 2, 3, 6)), dict(eight, up=stack(4 << 32, 300, 60000, 9 << 32, 3, -1)),
+               dict(Y=p(1)), dict(Y=p(2)), dict(Y=p(3)), dict(Y=p(4)), dict(Y=p(5)), dict(Y=p(6)), dict(Y=p(8)), dict(eight, Y=p(9)),
+               dict(room=p(8, 64)), dict(room=p(1)), dict(room=p(4)), dict(eight, room=p(11))):
+        assert call(**kw) == BAD, kw
+    assert call(size=need - 1) == ROOM
+    assert call(tokens=257) == UNSUPPORTED and call(top=33) == UNSUPPORTED and call(experts=4097) == UNSUPPORTED
+    wide = oz.MAX_WIDTH + 1
+    assert call(width=wide, ldx=wide, up=stack(4 << 32, wide, 0), gate=stack(5 << 32, wide, 0)) == UNSUPPORTED
+    assert call(out=wide, ldy=wide) == UNSUPPORTED and call(inner=wide, down=stack(6 << 32, wide, 0)) == UNSUPPORTED
+    assert call(tokens=0, X=None, Y=None) == OK and call(out=0, Y=None) == OK
+
+
+def test_binding_expert_layer():
+    H = torch.bfloat16
+    X, up, down = torch.zeros(4, 20, dtype=H), torch.zeros(3, 16, 20, dtype=H), torch.zeros(3, 24, 16, dtype=H)
+    which, gates = torch.zeros(4, 2, dtype=torch.int32), torch.zeros(4, 2)
+    f = oz.ozaki25_expert_layer
+    raises("X must be", f, X.float(), which, gates, up, down)
+    raises("which must be", f, X, which.long(), gates, up, down)
+    raises("which must be", f, X, which[:, 0], gates, up, down)
+    raises("which has shape", f, X, which[:3], gates, up, down)
+    raises("gates has shape", f, X, which, gates[:, :1].contiguous(), up, down)
+    raises("gates must be", f, X, which, gates.to(H), up, down)
+    raises("up must be", f, X, which, gates, up.float(), down)
+    raises("up has 19 columns", f, X, which, gates, up[:, :, :19], down)
+    raises("down has shape", f, X, which, gates, up, down[:2])
+    raises("down has shape", f, X, which, gates, up, down[:, :, :15])
+    raises("gate has shape", f, X, which, gates, up, down, gate=up[:, :15])
+    raises("either all", f, X, which, gates, up, down, up_scales=torch.ones(3, 1, 1))
+    raises("gate_scales need", f, X, which, gates, up, down, gate_scales=torch.ones(3, 1, 1))
+    e = dict(up_scales=torch.ones(3, 1, 1), down_scales=torch.ones(3, 1, 1))
+    raises("up must be", f, X, which, gates, up, down, **e)
+    q, d = up.to(torch.float8_e4m3fn), down.to(torch.float8_e4m3fn)
+    raises("up_scales has shape", f, X, which, gates, q, d, **dict(e, up_scales=torch.ones(3, 1, 2)))
+    raises("Y has shape", f, X, which, gates, up, down, Y=X)
+    raises("workspace must be", f, X, which, gates, up, down, workspace=X)
+    raises("must be a CUDA tensor", f, X, which, gates, up, down)
+    raises("must be a CUDA tensor", f, X, which, gates, q, d, **e)
+
+
 def test_binding_norm():
     X, w = torch.zeros(4, 20, dtype=torch.bfloat16), torch.ones(20, dtype=torch.bfloat16)
     raises("X must be a 2-D", oz.ozaki25_rms_norm, X[0], w)
