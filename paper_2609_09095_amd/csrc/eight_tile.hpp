@@ -61,35 +61,75 @@ struct Tile8 {
   static_assert(NB * 32 <= 128 && 128 % (NB * 32) == 0, "a wavefront's columns lie in one square");
 };
 
-// Rows that start on 16 bytes, whatever their length: chunks past the depth are
-// sent outside the descriptor and read as zero; the chunk that the depth's end
-// cuts is read whole (its 16 aligned bytes lie in one page) and cleaned in LDS.
+// Rows that start on 16 bytes, whatever their length.  The last block of depths
+// comes first: chunks past its end are sent outside the descriptor and read as zero,
+// and the chunk that the end cuts is read whole (its 16 aligned bytes lie in one
+// page) and cleaned in LDS, so that all later stages are whole.
+template <int V, int N>
+struct ByteDmaSide {
+  static_assert(N % 2 == 0);
+  const char* p;
+  int64_t extent;  // bytes from p to the end of the last valid row
+  int voff[2];     // of the lane's chunk of even and odd slabs, less the slab's rows
+  int rows8;       // bytes from slab to slab
+  __device__ __forceinline__ void init(const Bytes& op, int depth, int wave, int lane) {
+    p = half::uniform(op.p);
+    extent = op.vecs > 0 ? (op.vecs - 1) * op.ld + (depth + 15) / 16 * 16 : 0;
+    rows8 = __builtin_amdgcn_readfirstlane((int)op.ld * 8);
+    const int r = wave * N * 8 + (lane >> 3), c = (lane & 7) ^ (lane >> 3);  // the swizzle of row r, bar its bit 3
+    voff[0] = (int)(r * op.ld) + c * 16;
+    voff[1] = (int)(r * op.ld) + (c ^ 1) * 16;
+  }
+  // `depth`: of the stage, at most 128; all: bytes before the stage's first depth
+  __device__ __forceinline__ __amdgpu_buffer_rsrc_t rsrc(int64_t all, bool any) const {
+    const int64_t e = any ? extent - all : 0;
+    const int n = (int)(e < 0x7ffffff0 ? e : 0x7ffffff0);
+    return __builtin_amdgcn_make_buffer_rsrc((void*)(p + all), (short)0, __builtin_amdgcn_readfirstlane(n), 0x00020000);
+  }
+  __device__ __forceinline__ void load(int i, __amdgpu_buffer_rsrc_t r, char* lds, int wave) const {
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (half::lds_ptr)(lds + (wave * N + i) * 1024), 16, voff[i & 1] + i * rows8, 0, 0, 0);
+  }
+  __device__ __forceinline__ void load_cut(int i, __amdgpu_buffer_rsrc_t r, char* lds, int wave, int lane, int depth) const {
+    const int c = (lane & 7) ^ (lane >> 3) ^ (i & 1);
+    const int off = c * 16 < depth ? voff[i & 1] + i * rows8 : 0x7ffffff8;
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (half::lds_ptr)(lds + (wave * N + i) * 1024), 16, off, 0, 0, 0);
+  }
+};
+
 template <class T>
 struct ByteDma {
-  half::DmaSide<kAlong, T::BM, T::ADMA> a;
-  half::DmaSide<kAlong, T::BN, T::BDMA> b;
+  ByteDmaSide<T::BM, T::ADMA> a;
+  ByteDmaSide<T::BN, T::BDMA> b;
   __amdgpu_buffer_rsrc_t ra, rb;
-  int left;  // depths that remain, in pairs of bytes
+  int stage, stages;
+  int64_t at;
   __device__ __forceinline__ void init(const Bytes& oa, const Bytes& ob, int depth, int wave, int lane) {
-    left = (depth + 15) / 16 * 8;
-    a.init(half::Operand{oa.p, oa.ld / 2, oa.vecs, left}, left, wave, lane);
-    b.init(half::Operand{ob.p, ob.ld / 2, ob.vecs, left}, left, wave, lane);
+    a.init(oa, depth, wave, lane);
+    b.init(ob, depth, wave, lane);
+    stages = (depth + kStage - 1) / kStage;
+    stage = 1, at = 0;
+  }
+  __device__ __forceinline__ void first(char* buf, int depth, int wave, int lane) {
+    const int64_t before = (int64_t)(stages - 1) * kStage;
+    const __amdgpu_buffer_rsrc_t x = a.rsrc(before, true), y = b.rsrc(before, true);
+#pragma unroll
+    for (int i = 0; i < T::ADMA; ++i) a.load_cut(i, x, buf, wave, lane, depth - (int)before);
+#pragma unroll
+    for (int i = 0; i < T::BDMA; ++i) b.load_cut(i, y, buf + T::A_BYTES, wave, lane, depth - (int)before);
   }
   __device__ __forceinline__ void early(int, int) {}
   __device__ __forceinline__ void begin() {
-    ra = a.rsrc(left);
-    rb = b.rsrc(left);
+    const bool any = stage < stages;
+    ra = a.rsrc(at, any);
+    rb = b.rsrc(at, any);
+    ++stage;
+    at += kStage;
   }
   __device__ __forceinline__ void late(int j, char* buf, int wave, int) {
     if (j < T::ADMA)
-      a.load(j, ra, buf, wave, left);
+      a.load(j, ra, buf, wave);
     else
-      b.load(j - T::ADMA, rb, buf + T::A_BYTES, wave, left);
-  }
-  __device__ __forceinline__ void end() {
-    left -= half::kDepth;
-    a.advance();
-    b.advance();
+      b.load(j - T::ADMA, rb, buf + T::A_BYTES, wave);
   }
   static constexpr int IN_FLIGHT = T::ADMA + T::BDMA;
 };
@@ -126,6 +166,13 @@ struct ByteMasked {
     b.p = half::uniform(ob.p), b.ld = ob.ld, b.vecs = ob.vecs;
     at = 0, depth = d;
   }
+  __device__ __forceinline__ void first(char* buf, int d, int wave, int lane) {
+    at = (int64_t)((d - 1) / kStage) * kStage;
+    early(wave, lane);
+#pragma unroll
+    for (int j = 0; j < T::ADMA + T::BDMA; ++j) late(j, buf, wave, lane);
+    at = 0;
+  }
   __device__ __forceinline__ void early(int wave, int lane) {
     a.load(wave, lane, at, depth);
     b.load(wave, lane, at, depth);
@@ -138,7 +185,6 @@ struct ByteMasked {
     else
       b.put(j - T::ADMA, buf + T::A_BYTES, wave, lane);
   }
-  __device__ __forceinline__ void end() {}
   static constexpr int IN_FLIGHT = 0;
 };
 
@@ -146,28 +192,35 @@ struct ByteMasked {
 // each.  Vectors past the edge take the last one's (their sums are not stored).
 template <class T>
 struct ScaleLoads {
-  const float* p;
+  const float* p;  // of the wavefront (uniform), at the block that is loaded next
   int64_t step;
+  int off;  // the lane's vector
   int stage, stages;
   float next;
+  static_assert(T::BM % 64 == 0 && T::BN % 64 == 0, "a wavefront carries one operand's scales");
   __device__ __forceinline__ void init(const Scales& sa, const Scales& sb, int rows, int cols, int n) {
-    const int t = threadIdx.x;
-    if (t < T::BM) {
-      p = sa.p + (t < rows ? t : rows - 1);
+    const int t = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(t >> 6);
+    if (wave * 64 < T::BM) {
+      off = t < rows ? t : rows - 1;
+      p = sa.p;
       step = sa.step;
     } else {
       const int c = t - T::BM < cols ? t - T::BM : cols - 1;
-      p = T::SQUARES ? sb.p + (int64_t)(c / kBlock) * sb.step : sb.p + c;
+      off = T::SQUARES ? 0 : c;
+      p = T::SQUARES ? sb.p + (int64_t)(__builtin_amdgcn_readfirstlane(c) / kBlock) * sb.step : sb.p;
       step = T::SQUARES ? 1 : sb.step;
     }
+    p = (const float*)half::uniform(p);
     stage = 0, stages = n;
   }
+  // the last block first, like the bytes
   __device__ __forceinline__ void load() {
-    next = stage < stages && threadIdx.x < T::BM + T::BN ? p[stage * step] : 0.0f;
+    const int64_t b = stage == 0 ? stages - 1 : stage < stages ? stage - 1 : stages - 1;
+    next = p[b * step + off];
     ++stage;
   }
   __device__ __forceinline__ void put(float* slot) const {
-    if (threadIdx.x < T::BM + T::BN) slot[threadIdx.x] = next;
+    if (T::THREADS == T::BM + T::BN || threadIdx.x < T::BM + T::BN) slot[threadIdx.x] = next;
   }
 };
 
@@ -179,15 +232,17 @@ __device__ __forceinline__ v8i two(v4i lo, v4i hi) {
 // and the next, as they lie in LDS.
 template <int N>
 struct ByteFragments {
-  int base[4];  // (half, chunk of the two)
+  int base[2][2];
   __device__ __forceinline__ void init(int w0, int lane) {
     const int v = w0 * 32 + (lane & 31);
 #pragma unroll
-    for (int j = 0; j < 4; ++j) base[j] = v * kStage + (((j >> 1) * 4 + 2 * (lane >> 5) + (j & 1)) ^ half::swz_along(v)) * 16;
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+      for (int j = 0; j < 2; ++j) base[h][j] = v * kStage + ((h * 4 + 2 * (lane >> 5) + j) ^ half::swz_along(v)) * 16;
   }
   __device__ __forceinline__ v8i read(half::lds_bytes lds, int h, int x) const {
     using q = const __attribute__((address_space(3))) v4i*;
-    return two(*(q)(lds + base[2 * h] + x * 4096), *(q)(lds + base[2 * h + 1] + x * 4096));
+    return two(*(q)(lds + base[h][0] + x * 4096), *(q)(lds + base[h][1] + x * 4096));
   }
 };
 
@@ -239,16 +294,106 @@ __device__ __forceinline__ void clean_tail(char* lds, int left) {
   }
 }
 
+__device__ __forceinline__ void wait_lds_and_barrier() {
+  half::wait_lds();
+  half::block_barrier();
+}
+
 template <class T>
 __device__ __forceinline__ int next_stage(int cur) {
   return cur + T::STAGE < T::SET ? cur + T::STAGE : 0;
 }
 
+// A block's products, scaled, into its sums.  fs: the lane's row's scale (times the
+// squares'); cs: the columns' scales.
+template <class T>
+__device__ __forceinline__ void add_scaled(v16f& acc, const v16f& t, float fs, const float* cs) {
+  v4f c[4];
+  if constexpr (!T::SQUARES) {
+#pragma unroll
+    for (int q = 0; q < 4; ++q) c[q] = *(const v4f*)(cs + 8 * q);
+  }
+#pragma unroll
+  for (int i = 0; i < 16; ++i) acc[i] = __builtin_fmaf(t[i], T::SQUARES ? fs : fs * c[i / 4][i % 4], acc[i]);
+  // here and not later: the compiler would carry the products over the barrier
+  asm volatile("" : "+v"(acc));
+}
+
+// One stage's products, a block at a time: a block's two products are issued, then the
+// block before it, whose products have ended by then, is added up.  On entry the
+// fragments of the first row of blocks are in af[0], of all columns in bf.  cur, next:
+// this stage's and the next one's buffer; freed: cur, as the target of the loads (the
+// three are declared not to alias, or the compiler would wait for all loads in flight
+// before every read of LDS: what keeps them apart is the barrier).  here, there: this
+// stage's and the next one's scales.
+template <class T, class Loader>
+__device__ __forceinline__ void stage_products8(Loader& ld, ScaleLoads<T>& sl, const ByteFragments<T::MB>& fa,
+                                                const ByteFragments<T::NB>& fb, half::lds_bytes __restrict__ cur,
+                                                half::lds_bytes __restrict__ next, char* __restrict__ freed,
+                                                const float* here, float* there, int wave, int lane, v8i (&af)[2][2],
+                                                v8i (&bf)[T::NB][2], v16f (&acc)[T::MB][T::NB]) {
+  constexpr int ND = T::ADMA + T::BDMA, MB = T::MB, NB = T::NB, M = MB * NB;
+  ld.early(wave, lane);
+  float fs[MB];
+  const int wr = wave / T::WC, wc = wave % T::WC;
+  const float* const cs = here + T::BM + wc * NB * 32 + (T::SQUARES ? 0 : 4 * (lane >> 5));
+  const float* const rs = here + wr * MB * 32 + (lane & 31);
+#pragma unroll
+  for (int x = 0; x < MB; ++x) fs[x] = rs[x * 32];
+  if constexpr (T::SQUARES) {
+    const float c = cs[0];
+#pragma unroll
+    for (int x = 0; x < MB; ++x) fs[x] *= c;
+  }
+  v16f t[2];
+#pragma unroll
+  for (int x = 0; x < MB; ++x) {
+    const bool last = x + 1 == MB;
+    if (last) {
+      // the next stage's scales, and (older than the loads that may be in flight) its bytes
+      sl.put(there);
+      half::wait_loads_and_lds<(T::BUFS - 2) * T::Loads::IN_FLIGHT>();
+      half::block_barrier();
+      sl.load();
+      ld.begin();
+    }
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int y = 0; y < NB; ++y) {
+      const int i = x * NB + y;
+      t[i & 1] = mfma64<T::OUT>(bf[y][0], af[x & 1][0], v16f{});
+      t[i & 1] = mfma64<T::OUT>(bf[y][1], af[x & 1][1], t[i & 1]);
+      if (y == 0) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) af[(x + 1) & 1][h] = fa.read(last ? next : cur, h, last ? 0 : x + 1);
+      }
+      if (last) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) bf[y][h] = fb.read(next + T::A_BYTES, h, y);
+#pragma unroll
+        for (int j = y * ND / NB; j < (y + 1) * ND / NB; ++j) ld.late(j, freed, wave, lane);
+      }
+      __builtin_amdgcn_sched_barrier(0);
+      if (i > 0) {
+        add_scaled<T>(acc[(i - 1) / NB][(i - 1) % NB], t[(i - 1) & 1], fs[(i - 1) / NB], cs + (i - 1) % NB * 32);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+    }
+  }
+  add_scaled<T>(acc[MB - 1][NB - 1], t[(M - 1) & 1], fs[MB - 1], cs + (NB - 1) * 32);
+  if constexpr (MB % 2) {
+    af[0][0] = af[1][0];
+    af[0][1] = af[1][1];
+  }
+  __builtin_amdgcn_sched_barrier(0);
+}
+
 // acc += A B over `depth` (at least 1), scaled.  lds: T::LDS bytes, 1024-aligned.
 //
-// As in the 16-bit tiles the last column of products of a stage runs behind the
-// barrier that hands over to the next stage, whose first fragments are read
-// meanwhile, and the buffer just freed takes the loads of the stage BUFS later.
+// As in the 16-bit tiles the last row of a stage's products runs behind the barrier
+// that hands over to the next stage, whose first fragments are read meanwhile, and the
+// buffer just freed takes the loads of the stage BUFS later.  Wavefronts whose outputs
+// all lie past the tile's edge load and wait like the others.
 template <class T>
 __device__ __forceinline__ void product8(const Bytes& oa, const Bytes& ob, const Scales& sa, const Scales& sb, int cols,
                                          int depth, char* lds, v16f (&acc)[T::MB][T::NB]) {
@@ -257,127 +402,63 @@ __device__ __forceinline__ void product8(const Bytes& oa, const Bytes& ob, const
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int wr = wave / T::WC, wc = wave % T::WC;
   const int nst = (depth + kStage - 1) / kStage;
-  const int tail = T::DMA && depth % 16 ? depth % kStage : 0;  // depths of a last stage whose end cuts a chunk
   typename T::Loads ld;
   ScaleLoads<T> sl;
   ld.init(oa, ob, depth, wave, lane);
   sl.init(sa, sb, oa.vecs, cols, nst);
   float* const slots = (float*)(lds + T::SET);
+  constexpr int SLOT = T::SLOT / 4;
   sl.load();
   sl.put(slots);
   sl.load();
+  ld.first(lds, depth, wave, lane);
 #pragma unroll
-  for (int s = 0; s < T::BUFS; ++s) {
+  for (int s = 1; s < T::BUFS; ++s) {
     ld.early(wave, lane);
     ld.begin();
 #pragma unroll
     for (int j = 0; j < ND; ++j) ld.late(j, lds + s * T::STAGE, wave, lane);
-    ld.end();
   }
   half::wait_loads_and_lds<(T::BUFS - 1) * T::Loads::IN_FLIGHT>();
   half::block_barrier();
-  if (tail && nst == 1) {
-    clean_tail<T>(lds, tail);
-    __syncthreads();
+  if (T::DMA && depth % 16) {
+    clean_tail<T>(lds, depth % kStage);
+    wait_lds_and_barrier();
   }
-  const bool active = wr * MB * 32 < oa.vecs && wc * NB * 32 < cols;
-  ByteFragments<MB> fa;
-  ByteFragments<NB> fb;
-  fa.init(wr * MB, lane);
-  fb.init(wc * NB, lane);
-  const auto l3 = (half::lds_bytes)lds;
-  v8i af[2][2], bf[NB][2];
-  if (active) {
+  int cur = 0, slot = 0;
+  if (wr * MB * 32 >= oa.vecs || wc * NB * 32 >= cols) {
+    for (int s = 0; s < nst; ++s) {
+      slot = slot == 2 * SLOT ? 0 : slot + SLOT;
+      ld.early(wave, lane);
+      sl.put(slots + slot);
+      half::wait_loads_and_lds<(T::BUFS - 2) * T::Loads::IN_FLIGHT>();
+      half::block_barrier();
+      sl.load();
+      ld.begin();
+#pragma unroll
+      for (int j = 0; j < ND; ++j) ld.late(j, lds + cur, wave, lane);
+      cur = next_stage<T>(cur);
+    }
+  } else {
+    ByteFragments<MB> fa;
+    ByteFragments<NB> fb;
+    fa.init(wr * MB, lane);
+    fb.init(wc * NB, lane);
+    const auto l3 = (half::lds_bytes)lds;
+    v8i af[2][2], bf[NB][2];
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
       af[0][h] = fa.read(l3, h, 0);
 #pragma unroll
       for (int y = 0; y < NB; ++y) bf[y][h] = fb.read(l3 + T::A_BYTES, h, y);
     }
-  }
-  int cur = 0, slot = 0;
-  for (int s = 0; s < nst; ++s) {
-    const int next = next_stage<T>(cur), next_slot = slot == 2 ? 0 : slot + 1;
-    ld.early(wave, lane);
-    float fs[MB], cs[NB][T::SQUARES ? 1 : 16];
-    if (active) {
-      const float* const here = slots + slot * (T::SLOT / 4);
-#pragma unroll
-      for (int x = 0; x < MB; ++x) fs[x] = here[(wr * MB + x) * 32 + (lane & 31)];
-      const float* const there = here + T::BM + wc * NB * 32;
-      if constexpr (T::SQUARES) {
-#pragma unroll
-        for (int x = 0; x < MB; ++x) fs[x] *= there[0];
-      } else {
-#pragma unroll
-        for (int y = 0; y < NB; ++y)
-#pragma unroll
-          for (int q = 0; q < 4; ++q) {
-            const v4f v = *(const v4f*)(there + y * 32 + 8 * q + 4 * (lane >> 5));
-#pragma unroll
-            for (int e = 0; e < 4; ++e) cs[y][4 * q + e] = v[e];
-          }
-      }
+    for (int s = 0; s < nst; ++s) {
+      const int next = next_stage<T>(cur), next_slot = slot == 2 * SLOT ? 0 : slot + SLOT;
+      stage_products8<T>(ld, sl, fa, fb, l3 + cur, l3 + next, lds + cur, slots + slot, slots + next_slot, wave, lane, af, bf,
+                         acc);
+      cur = next;
+      slot = next_slot;
     }
-    auto hand_over = [&] {
-      // the next stage's scales, and (older than the loads that may be in flight) its bytes
-      sl.put(slots + next_slot * (T::SLOT / 4));
-      half::wait_loads_and_lds<(T::BUFS - 2) * T::Loads::IN_FLIGHT>();
-      half::block_barrier();
-      if (tail && s + 2 == nst) {
-        clean_tail<T>(lds + next, tail);
-        __syncthreads();
-      }
-      sl.load();
-      ld.begin();
-    };
-    if (active) {
-#pragma unroll
-      for (int x = 0; x < MB; ++x) {
-        const bool last = x + 1 == MB;
-        if (last) hand_over();
-        __builtin_amdgcn_sched_barrier(0);
-        if (!last) {
-#pragma unroll
-          for (int h = 0; h < 2; ++h) af[(x + 1) & 1][h] = fa.read(l3 + cur, h, x + 1);
-        }
-        v16f t[NB];
-#pragma unroll
-        for (int y = 0; y < NB; ++y) {
-          t[y] = mfma64<T::OUT>(bf[y][0], af[x & 1][0], v16f{});
-          t[y] = mfma64<T::OUT>(bf[y][1], af[x & 1][1], t[y]);
-        }
-        if (last) {
-#pragma unroll
-          for (int j = 0; j < ND; ++j) ld.late(j, lds + cur, wave, lane);
-#pragma unroll
-          for (int h = 0; h < 2; ++h) {
-            af[(x + 1) & 1][h] = fa.read(l3 + next, h, 0);
-#pragma unroll
-            for (int y = 0; y < NB; ++y) bf[y][h] = fb.read(l3 + next + T::A_BYTES, h, y);
-          }
-        }
-#pragma unroll
-        for (int y = 0; y < NB; ++y)
-#pragma unroll
-          for (int i = 0; i < 16; ++i) {
-            const float f = T::SQUARES ? fs[x] : fs[x] * cs[y][T::SQUARES ? 0 : i];
-            acc[x][y][i] = __builtin_fmaf(t[y][i], f, acc[x][y][i]);
-          }
-        __builtin_amdgcn_sched_barrier(0);
-      }
-      if constexpr (MB % 2) {
-        af[0][0] = af[1][0];
-        af[0][1] = af[1][1];
-      }
-    } else {
-      hand_over();
-#pragma unroll
-      for (int j = 0; j < ND; ++j) ld.late(j, lds + cur, wave, lane);
-    }
-    ld.end();
-    cur = next;
-    slot = next_slot;
   }
   __builtin_amdgcn_s_waitcnt(0);  // the look-ahead past the end lands before LDS is used again
   __syncthreads();

@@ -190,7 +190,7 @@ hipError_t of_type(const Scaled& g, hipStream_t s) {
     case kScaledSmall: return run_tiles<Tile8<2, 2, 1, 1, true, OUT, SQUARES, 3>>(g, s);
     case kScaledMiddle: return run_tiles<Tile8<2, 2, 2, 2, true, OUT, SQUARES>>(g, s);
     default:
-      if constexpr (OUT == kF32) return run_tiles<Tile8<2, 2, 2, 2, true, OUT, SQUARES>>(g, s);
+      if constexpr (OUT == kF32 || !SQUARES) return run_tiles<Tile8<2, 2, 2, 2, true, OUT, SQUARES>>(g, s);
       return run_tiles<Tile8<2, 4, 4, 2, true, OUT, SQUARES>>(g, s);
   }
 }
