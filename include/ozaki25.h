@@ -548,7 +548,7 @@ typedef struct {
 } ozaki25_expert_weights;
 
 /* A layer of experts for few tokens (a decode step), in two launches, or three for
- * more than 16 tokens; larger batches take the grouped products.
+ * more than 16 choices; larger batches take the grouped products.
  *   Y[t] = sum over j of gates[t, j] D_e (silu(G_e X[t]) * (U_e X[t])),  e = which[t, j],
  * silu(x) = x / (1 + exp(-x)), and silu(U_e X[t]) where gate is NULL.
  *  X: tokens x width (ldx);  which: int32 [tokens][top], read on the device;

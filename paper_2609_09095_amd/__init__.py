@@ -14,6 +14,7 @@ from __future__ import annotations
 import ctypes
 import os
 import re
+import struct
 import warnings
 
 __all__ = [
@@ -65,12 +66,6 @@ MAX_TOP = 32
 MAX_LAYER_EXPERTS = 4096
 
 SUCCESS, ERR_INVALID_VALUE, ERR_UNSUPPORTED, ERR_WORKSPACE, ERR_HIP = range(5)
-
-
-class ExpertWeights(ctypes.Structure):
-    """ozaki25_expert_weights"""
-    _fields_ = [("weights", ctypes.c_void_p), ("ld", ctypes.c_int64), ("stride", ctypes.c_int64), ("scales", ctypes.c_void_p),
-                ("scales_ld", ctypes.c_int64), ("scales_stride", ctypes.c_int64)]
 
 
 class Ozaki25Error(RuntimeError):
@@ -160,18 +155,20 @@ def _check(status: int, what: str):
 
 _torch = None     # torch, imported by the first call that handles tensors
 _raw_stream = None  # () -> the current stream's handle
+_raw_device = _raw_stream_of = None  # () -> the current device; device -> its current stream's handle
 
 
 def _tensors():
     """torch; also picks the cheapest way to the current stream's handle (a
     Stream object costs a few microseconds, as much as a small product)."""
-    global _torch, _raw_stream
+    global _torch, _raw_stream, _raw_device, _raw_stream_of
     if _torch is None:
         import torch
         raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
         dev = getattr(torch._C, "_cuda_getDevice", None)
         if raw is not None and dev is not None:
             _raw_stream = lambda: raw(dev())  # noqa: E731
+            _raw_device, _raw_stream_of = dev, raw
         else:
             _raw_stream = lambda: torch.cuda.current_stream().cuda_stream  # noqa: E731
         _torch = torch
@@ -770,10 +767,24 @@ def _float_types():
     return _FLOATS
 
 
-def _here(t, what):
-    """The tensor's GPU is the current one, whose stream the call takes."""
-    if t.is_cuda and t.get_device() != _torch.cuda.current_device():
-        raise ValueError(f"{what}: the operands are on {t.device}, the current device is cuda:{_torch.cuda.current_device()}")
+def _here(t, stream):
+    """The handle of the stream that a call takes; the tensor's GPU has to be the
+    current one."""
+    if _raw_device is None:
+        if t.is_cuda and t.get_device() != _torch.cuda.current_device():
+            raise ValueError(f"the operands are on {t.device}, the current device is cuda:{_torch.cuda.current_device()}")
+        return _stream(stream)
+    dev = _raw_device()
+    if t.get_device() != dev:
+        raise ValueError(f"the operands are on {t.device}, the current device is cuda:{dev}")
+    return _raw_stream_of(dev) if stream is None else _stream(stream)
+
+
+def _new_like(t, stream, dtype=None):
+    """A contiguous output of a matrix's shape, of its dtype if none is given."""
+    if stream is None or not t.is_cuda:
+        return _torch.empty_like(t, dtype=dtype)
+    return _new(t, t.shape, stream, dtype)
 
 
 def _new_e4m3(like, shape, stream):
@@ -814,27 +825,29 @@ def ozaki25_rms_norm(X, weight=None, residual=None, eps: float = 1e-6, quantised
         raise ValueError("scales need quantised=True")
     if X.requires_grad or (weight is not None and weight.requires_grad) or (residual is not None and residual.requires_grad):
         _unrecorded("ozaki25_rms_norm")
-    if Y is None:
-        Y = _new_e4m3(X, size, stream) if quantised else _new(X, size, stream)
-    _, ldy, _ = _pitched(Y, "Y", 2, (_torch.float8_e4m3fn,) if quantised else kind, size)
-    lds = 1
-    if quantised:
-        if scales is None:
-            scales = _new(X, (_blocks(width), rows), stream, _torch.float32)
+    lds, ldy = rows or 1, width or 1
+    if Y is not None:
+        _, ldy, _ = _pitched(Y, "Y", 2, (_torch.float8_e4m3fn,) if quantised else kind, size)
+    elif not quantised:
+        Y = _new_like(X, stream)
+    elif width % 16 == 0:
+        Y = _new_like(X, stream, _torch.float8_e4m3fn)
+    else:
+        Y, ldy = _new_e4m3(X, size, stream), -(-width // 16) * 16
+    if scales is not None:
         _, lds, _ = _pitched(scales, "scales", 2, (_torch.float32,), (_blocks(width), rows))
-    if residual is not None:
-        if H is None:
-            H = _new(X, size, stream)
+    elif quantised:
+        scales = _new(X, (_blocks(width), rows), stream, _torch.float32)
+    if H is not None:
         _, ldh, _ = _pitched(H, "H", 2, kind, size)
+    elif residual is not None:
+        H, ldh = _new_like(X, stream), width or 1
     _together(X, ("X", "weight", "residual", "H", "Y", "scales"), weight, residual, H, Y, scales)
-    _here(X, "ozaki25_rms_norm")
     _check(lib().ozaki25_rms_norm(rows, width, X.data_ptr(), ldx, _ptr(residual), ldr, _ptr(weight), types[X.dtype], eps,
-                                  _ptr(H), ldh, Y.data_ptr(), ldy, _ptr(scales), lds, _stream(stream)),
-           "ozaki25_rms_norm")
-    out = (Y, scales) if quantised else (Y,)
-    if residual is not None:
-        out += (H,)
-    return out if len(out) > 1 else Y
+                                  _ptr(H), ldh, Y.data_ptr(), ldy, _ptr(scales), lds, _here(X, stream)), "ozaki25_rms_norm")
+    if quantised:
+        return (Y, scales) if residual is None else (Y, scales, H)
+    return Y if residual is None else (Y, H)
 
 
 def ozaki25_rms_norm_backward_workspace_size(rows: int, width: int) -> int:
@@ -857,20 +870,21 @@ def ozaki25_rms_norm_backward(dY, H, weight=None, dH=None, eps: float = 1e-6, dX
     if dH is not None:
         _, lddh, _ = _pitched(dH, "dH", 2, kind, size)
     ws_ptr, ws_bytes = _room(workspace)
-    if dY.requires_grad or H.requires_grad or any(t is not None and t.requires_grad for t in (weight, dH)):
+    if dY.requires_grad or H.requires_grad or (weight is not None and weight.requires_grad) or (
+            dH is not None and dH.requires_grad):
         _unrecorded("ozaki25_rms_norm_backward")
     if dX is None:
-        dX = _new(dY, size, stream)
-    _, lddx, _ = _pitched(dX, "dX", 2, kind, size)
+        dX, lddx = _new_like(dY, stream), width or 1
+    else:
+        _, lddx, _ = _pitched(dX, "dX", 2, kind, size)
     if dweight is None:
         dweight = _new(dY, (width,), stream, _torch.float32)
     else:
         _vector(dweight, "dweight", _torch.float32, width)
     _together(dY, ("dY", "H", "weight", "dH", "dX", "dweight", "workspace"), H, weight, dH, dX, dweight, workspace)
-    _here(dY, "ozaki25_rms_norm_backward")
     _check(lib().ozaki25_rms_norm_backward(rows, width, dY.data_ptr(), lddy, H.data_ptr(), ldh, _ptr(weight), _ptr(dH),
                                            lddh, types[dY.dtype], eps, dX.data_ptr(), lddx, dweight.data_ptr(), ws_ptr,
-                                           ws_bytes, _stream(stream)), "ozaki25_rms_norm_backward")
+                                           ws_bytes, _here(dY, stream)), "ozaki25_rms_norm_backward")
     return dX, dweight
 
 
@@ -899,15 +913,15 @@ def ozaki25_quantise(X, squares: bool = False, layout: str = "rows", stream=None
         if not wanted:
             args += [0, 1, 0, 0]
             continue
-        Q = _new_e4m3(X, (*head, r, c), stream)
+        q = _new_e4m3(X, (*head, r, c), stream)
         s = _new(X, (*head, *((_blocks(r), _blocks(c)) if squares else (_blocks(c), r))), stream, _torch.float32)
-        _, ldq, q_stride = _pitched(Q, "Q", dims, (_torch.float8_e4m3fn,))
-        args += [Q.data_ptr(), ldq, q_stride, s.data_ptr()]
-        out += [Q, s]
-    _on_gpu([("X", X)])
-    _here(X, "ozaki25_quantise")
+        ld = -(-c // 16) * 16 or 1
+        args += [q.data_ptr(), ld, r * ld, s.data_ptr()]
+        out += [q, s]
+    if not X.is_cuda:
+        _on_gpu([("X", X)])
     _check(lib().ozaki25_quantise(head[0] if dims == 3 else 1, rows, cols, X.data_ptr(), ldx, x_stride, types[X.dtype],
-                                  1 if squares else 0, *args, _stream(stream)), "ozaki25_quantise")
+                                  1 if squares else 0, *args, _here(X, stream)), "ozaki25_quantise")
     return tuple(out)
 
 
@@ -935,15 +949,17 @@ def ozaki25_scaled_matmul(A, a_scales, B, b_scales, squares: bool = True, out_dt
     if A.requires_grad or B.requires_grad or a_scales.requires_grad or b_scales.requires_grad:
         _unrecorded("ozaki25_scaled_matmul")
     if Y is None:
-        Y = _new(A, (rows, n), stream, out_dtype or _torch.bfloat16)
-    elif out_dtype is not None and Y.dtype != out_dtype:
-        raise ValueError(f"Y has dtype {Y.dtype}, out_dtype is {out_dtype}")
-    _, ldy, _ = _pitched(Y, "Y", 2, types, (rows, n))
+        if out_dtype is not None and out_dtype not in types:
+            raise ValueError(f"out_dtype must be {' or '.join(str(d) for d in types)}")
+        Y, ldy = _new(A, (rows, n), stream, out_dtype or _torch.bfloat16), n or 1
+    else:
+        _, ldy, _ = _pitched(Y, "Y", 2, types, (rows, n))
+        if out_dtype is not None and Y.dtype != out_dtype:
+            raise ValueError(f"Y has dtype {Y.dtype}, out_dtype is {out_dtype}")
     _together(A, ("A", "a_scales", "B", "b_scales", "Y", "workspace"), a_scales, B, b_scales, Y, workspace)
-    _here(A, "ozaki25_scaled_matmul")
     _check(lib().ozaki25_scaled_matmul(rows, n, k, A.data_ptr(), lda, a_scales.data_ptr(), ldas, B.data_ptr(), ldb,
                                        b_scales.data_ptr(), ldbs, 1 if squares else 0, Y.data_ptr(), ldy, types[Y.dtype],
-                                       ws_ptr, ws_bytes, _stream(stream)), "ozaki25_scaled_matmul")
+                                       ws_ptr, ws_bytes, _here(A, stream)), "ozaki25_scaled_matmul")
     return Y
 
 
@@ -959,13 +975,14 @@ def _table(t, name, dtype, size):
         raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {tuple(size)}")
 
 
-def _stack(W, name, scales, kind, size):
-    """The argument for a stack of weights with or without scales."""
-    (experts, rows, cols), ld, stride = _pitched(W, name, 3, kind, size)
+def _stack(W, name, scales, kind, size=None):
+    """The size of a stack of weights, and ozaki25_expert_weights for it."""
+    size, ld, stride = _pitched(W, name, 3, kind, size)
     if scales is None:
-        return ExpertWeights(W.data_ptr(), ld, stride, 0, 1, 0)
+        return size, struct.pack("6q", W.data_ptr(), ld, stride, 0, 1, 0)
+    experts, rows, cols = size
     _, lds, s_stride = _pitched(scales, f"{name}_scales", 3, (_torch.float32,), (experts, _blocks(rows), _blocks(cols)))
-    return ExpertWeights(W.data_ptr(), ld, stride, scales.data_ptr(), lds, s_stride)
+    return size, struct.pack("6q", W.data_ptr(), ld, stride, scales.data_ptr(), lds, s_stride)
 
 
 def ozaki25_expert_layer(X, which, gates, up, down, gate=None, up_scales=None, down_scales=None, gate_scales=None, Y=None,
@@ -989,27 +1006,26 @@ def ozaki25_expert_layer(X, which, gates, up, down, gate=None, up_scales=None, d
     if gate is None and gate_scales is not None:
         raise ValueError("gate_scales need gate")
     stored = (_torch.float8_e4m3fn,) if eight else kind
-    (experts, inner, wu), _, _ = _pitched(up, "up", 3, stored)
+    up_size, u = _stack(up, "up", up_scales, stored)
+    experts, inner, wu = up_size
     if wu != width:
         raise ValueError(f"up has {wu} columns, X has {width}")
-    (ed, out, wd), _, _ = _pitched(down, "down", 3, stored)
-    if (ed, wd) != (experts, inner):
+    (ed, out, wd), d = _stack(down, "down", down_scales, stored)
+    if ed != experts or wd != inner:
         raise ValueError(f"down has shape {tuple(down.shape)}, expected ({experts}, out, {inner})")
-    u = _stack(up, "up", up_scales, stored, up.shape)
-    d = _stack(down, "down", down_scales, stored, down.shape)
-    g = None if gate is None else _stack(gate, "gate", gate_scales, stored, up.shape)
+    g = None if gate is None else _stack(gate, "gate", gate_scales, stored, up_size)[1]
     ws_ptr, ws_bytes = _room(workspace)
-    others = (which, gates, up, down, gate, up_scales, down_scales, gate_scales)
-    if X.requires_grad or any(t is not None and t.requires_grad for t in others):
+    if X.requires_grad or gates.requires_grad or up.requires_grad or down.requires_grad or (
+            gate is not None and gate.requires_grad) or (eight and (up_scales.requires_grad or down_scales.requires_grad or (
+                gate is not None and gate_scales.requires_grad))):
         _unrecorded("ozaki25_expert_layer")
     if Y is None:
-        Y = _new(X, (tokens, out), stream)
-    _, ldy, _ = _pitched(Y, "Y", 2, kind, (tokens, out))
+        Y, ldy = _new(X, (tokens, out), stream) if out != width else _new_like(X, stream), out or 1
+    else:
+        _, ldy, _ = _pitched(Y, "Y", 2, kind, (tokens, out))
     _together(X, ("X", "which", "gates", "up", "down", "gate", "up_scales", "down_scales", "gate_scales", "Y", "workspace"),
-              *others, Y, workspace)
-    _here(X, "ozaki25_expert_layer")
+              which, gates, up, down, gate, up_scales, down_scales, gate_scales, Y, workspace)
     _check(lib().ozaki25_expert_layer(tokens, top, experts, width, inner, out, X.data_ptr(), ldx, which.data_ptr(),
-                                      gates.data_ptr(), ctypes.addressof(u), 0 if g is None else ctypes.addressof(g),
-                                      ctypes.addressof(d), Y.data_ptr(), ldy, types[X.dtype], ws_ptr, ws_bytes,
-                                      _stream(stream)), "ozaki25_expert_layer")
+                                      gates.data_ptr(), u, g, d, Y.data_ptr(), ldy, types[X.dtype], ws_ptr, ws_bytes,
+                                      _here(X, stream)), "ozaki25_expert_layer")
     return Y

@@ -89,7 +89,7 @@ struct Layer {
   void* y;                       // tokens x out
   int64_t ldy;
   float* hidden;  // workspace: tokens top x inner_pad
-  float* parts;   // workspace of more than kTogether tokens: tokens top x out_pad
+  float* parts;   // workspace of more than kTogether choices: tokens top x out_pad
   int tokens, top, experts, width, inner, out;
   int inner_pad, out_pad;  // multiples of 4
 };

@@ -63,16 +63,40 @@ constexpr ScaledForm scaled_form(int64_t rows, int64_t n, int64_t) {
 // Bytes that the parts of a split depth take.
 constexpr size_t scaled_room(int64_t, int64_t, int64_t) { return 0; }
 
-// A layer of experts for few tokens.
+// A layer of experts for few tokens.  Times in us, of the kernel alone: tokens, top,
+// experts, width, inner; "e" weights in e4m3.
 constexpr int kMaxLayerTokens = 256, kMaxTop = 32, kMaxLayerExperts = 4096;
-constexpr int kTogether = 16;  // tokens whose sums over their experts stay in one block
+
+// Choices whose outputs are summed in one launch (a block goes through every expert),
+// others in two (a block per expert, then the sum).  One / two launches: 1, 2, 8, 2048,
+// 1024 5.6 / 4.7 + 2.6; 4, 2, 8, 4096, 2048 20.6 / 20.5 + 4.7; 16, 4, 64, 2048, 1024 e 46
+// / 26 + 4.7.
+constexpr int kTogether = 16;
+constexpr bool layer_together(int64_t tokens, int64_t top) { return tokens * top <= kTogether; }
+// Its blocks: 16 output columns, or 8 where that would leave CUs without one.  16 / 8:
+// 4, 2, 8, 4096, 2048 20.6 / 35; 1, 2, 8, 2048, 1024 6.1 / 5.6.
+constexpr bool together_wide(int64_t out) { return out >= 4096; }
+
+// Hidden values: blocks of 16 or 32 rows of weights (8 or 16 columns of both
+// projections), 16 or 32 tokens, four or eight wavefronts.
+enum HiddenForm { kHiddenOne, kHiddenSmall, kHiddenWide, kHiddenRows };
+// 16 / 32 rows: 4, 2, 8, 4096, 2048 33 / 36; 32, 2, 8, 4096, 1024 e 24 / 20; 64, 4, 64, 2048,
+// 1024 e 61 / 49.  32 tokens where an expert has 12 on average: 64, 2, 8, 4096, 1024 44 /
+// 52, but 32, 2, 8, 4096, 1024 e 26 / 20.  Eight wavefronts where CUs have one block:
+// 1, 2, 8, 2048, 1024 7.2 / 7.5.
+constexpr HiddenForm hidden_form(int64_t choices, int64_t experts, int64_t inner, bool gated, bool eight) {
+  const int64_t wide = experts * ceil_div(inner, gated ? 16 : 32);
+  if (wide < 256) return kHiddenOne;
+  if (choices >= 12 * experts) return kHiddenRows;
+  return wide < (eight ? 512 : 1536) ? kHiddenSmall : kHiddenWide;
+}
 
 constexpr int64_t pad4(int64_t n) { return (n + 3) / 4 * 4; }
 constexpr size_t layer_hidden_bytes(int64_t tokens, int64_t top, int64_t inner) {
   return (size_t)(tokens * top * pad4(inner)) * 4;
 }
 constexpr size_t layer_part_bytes(int64_t tokens, int64_t top, int64_t out) {
-  return tokens > kTogether ? (size_t)(tokens * top * pad4(out)) * 4 : 0;
+  return layer_together(tokens, top) ? 0 : (size_t)(tokens * top * pad4(out)) * 4;
 }
 
 }  // namespace eight

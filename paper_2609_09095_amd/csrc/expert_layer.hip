@@ -4,7 +4,7 @@
 //   act[t, e] = silu(G_e X[t]) * (U_e X[t]),  or silu(U_e X[t]) without G
 //
 // Two launches, the hidden values and the outputs (a third, which adds the experts'
-// shares, for more than kTogether tokens).  Bound by the read of the weights that
+// shares, for more than kTogether choices).  Bound by the read of the weights that
 // tokens reach, each once: a block reads 16 rows of an expert's weights straight
 // into the matrix cores' fragments, for all tokens of that expert, and its
 // wavefronts split the depth.  Every block reads `which` by itself, so the host
@@ -12,86 +12,124 @@
 //
 // The hidden values stay in FP32.  As operands they are two bfloat16 numbers, the
 // rounded value and the rest (16 bits of it); half's weights then too (all 11 bits).
-#include "eight_products.hpp"
 #include "eight_bits.hpp"
+#include "eight_products.hpp"
 
 namespace oz {
 namespace eight {
 namespace {
 
-constexpr int kStep = 128;  // depths of a step; lane l has 32 (l / 16) .. + 31 of vector l % 16
+
+constexpr int kStep = 128;  // depths of a step; lane l has four chunks of 8 of vector l % 16
 constexpr int kMaxPairs = kMaxLayerTokens * kMaxTop;
 
 // ---- which experts, and whose tokens -------------------------------------------
-struct Reached {
-  uint32_t bits[kMaxLayerExperts / 32];
-  int before[kMaxLayerExperts / 32];  // experts reached in the words before
-  int count;
+// Up to 64 choices are one lane's each, and a wavefront finds its way by itself: the
+// experts in the order of their first choice, an expert's choices as a mask.
+struct FewChoices {
+  int mine;       // the lane's choice, -1 for none
+  uint64_t left;  // choices of experts that were not taken yet
+  __device__ __forceinline__ void init(const Layer& p, int lane) {
+    const int e = lane < p.tokens * p.top ? p.which[lane] : -1;
+    mine = e >= 0 && e < p.experts ? e : -1;
+    left = __builtin_amdgcn_ballot_w64(mine >= 0);
+  }
+  // the next expert and its choices; 0 choices past the last
+  __device__ __forceinline__ int take(uint64_t& choices) {
+    choices = 0;
+    if (!left) return 0;
+    const int e = __builtin_amdgcn_readlane(mine, __builtin_ctzll(left));
+    choices = __builtin_amdgcn_ballot_w64(mine == e);
+    left &= ~choices;
+    return e;
+  }
 };
 
-// The experts that tokens reach.
+// More choices: the experts reached as bits in LDS, in ascending order.
+constexpr int kWords = kMaxLayerExperts / 32;
+
+struct Reached {
+  uint32_t bits[kWords];
+  int counts[16];
+};
+
+// Sets the bits; `first`: the thread's choice number threadIdx.x, for P up to THREADS
+// the only one.
 template <int THREADS>
-__device__ __forceinline__ void find_reached(const Layer& p, Reached& s) {
-  constexpr int WORDS = kMaxLayerExperts / 32;
-  for (int i = threadIdx.x; i < WORDS; i += THREADS) s.bits[i] = 0;
-  __syncthreads();
+__device__ __forceinline__ void find_reached(const Layer& p, Reached& s, int first) {
   const int pairs = p.tokens * p.top;
+  for (int i = threadIdx.x; i < kWords; i += THREADS) s.bits[i] = 0;
+  __syncthreads();
   for (int i = threadIdx.x; i < pairs; i += THREADS) {
-    const int e = p.which[i];
+    const int e = i < THREADS ? first : p.which[i];
     if (e >= 0 && e < p.experts) atomicOr(&s.bits[e >> 5], 1u << (e & 31));
   }
   __syncthreads();
-  if (threadIdx.x < 64) {
-    int total = 0;
-#pragma unroll
-    for (int w0 = 0; w0 < WORDS; w0 += 64) {
-      const int mine = __builtin_popcount(s.bits[w0 + threadIdx.x]);
-      const int incl = half::scan64(mine, [](int a, int b) { return a + b; });
-      s.before[w0 + threadIdx.x] = total + incl - mine;
-      total += __builtin_amdgcn_readlane(incl, 63);
-    }
-    if (threadIdx.x == 0) s.count = total;
-  }
-  __syncthreads();
 }
 
-__device__ __forceinline__ int rank_of(const Reached& s, int e) {
-  return s.before[e >> 5] + __builtin_popcount(s.bits[e >> 5] & ((1u << (e & 31)) - 1));
+// The lane's words, and how many experts the words before them hold; returns all.
+__device__ __forceinline__ int count_reached(const Reached& s, int lane, uint64_t& mine, int& before) {
+  static_assert(kWords == 128);
+  mine = (uint64_t)s.bits[2 * lane + 1] << 32 | s.bits[2 * lane];
+  const int own = __builtin_popcountll(mine), incl = half::scan64(own, [](int a, int b) { return a + b; });
+  before = incl - own;
+  return __builtin_amdgcn_readlane(incl, 63);
 }
 
-// One expert's tokens, in order.
+// One expert's choices, in order (t top + j).
 struct Tokens {
-  int expert, count;
-  uint16_t list[kMaxPairs];  // t top + j
+  Reached reached;
+  uint16_t list[kMaxPairs];
 };
 
-// The reached expert number `rank` and its tokens; false past the last.
+// The expert number `rank` of a block and its choices in s.list; `count` of them, 0
+// past the last expert.
 template <int THREADS>
-__device__ __forceinline__ bool find_tokens(const Layer& p, const Reached& s, int rank, Tokens& t) {
-  if (rank >= s.count) return false;
-  for (int w = threadIdx.x; w < kMaxLayerExperts / 32; w += THREADS) {
-    int nth = rank - s.before[w];
-    uint32_t b = s.bits[w];
-    if (nth >= 0 && nth < __builtin_popcount(b)) {
-      for (; nth > 0; --nth) b &= b - 1;
-      t.expert = w * 32 + __builtin_ctz(b);
-    }
+__device__ __forceinline__ int find_tokens(const Layer& p, int rank, Tokens& s, int& count) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, pairs = p.tokens * p.top;
+  count = 0;
+  if (pairs <= 64) {
+    FewChoices c;
+    c.init(p, lane);
+    uint64_t m;
+    int e = c.take(m);
+    for (int i = 0; i < rank && m; ++i) e = c.take(m);
+    if (!m) return 0;
+    // every wavefront writes the same
+    if (c.mine == e) s.list[__builtin_popcountll(m & (((uint64_t)1 << lane) - 1))] = (uint16_t)lane;
+    count = __builtin_popcountll(m);
+    __syncthreads();
+    return e;
   }
-  __syncthreads();
-  if (threadIdx.x < 64) {
-    const int pairs = p.tokens * p.top, e = t.expert;
-    int n = 0;
-    for (int i0 = 0; i0 < pairs; i0 += 64) {
-      const int i = i0 + threadIdx.x;
-      const bool is = i < pairs && p.which[i] == e;
-      const uint64_t m = __builtin_amdgcn_ballot_w64(is);
-      if (is) t.list[n + __builtin_popcountll(m & (((uint64_t)1 << threadIdx.x) - 1))] = (uint16_t)i;
-      n += __builtin_popcountll(m);
+  const int first = (int)threadIdx.x < pairs ? p.which[threadIdx.x] : -1;
+  find_reached<THREADS>(p, s.reached, first);
+  uint64_t mine;
+  int before;
+  if (rank >= count_reached(s.reached, lane, mine, before)) return 0;
+  // the word that holds it is one lane's
+  const uint64_t holds = __builtin_amdgcn_ballot_w64(rank >= before && rank < before + __builtin_popcountll(mine));
+  const int at = __builtin_ctzll(holds);
+  uint64_t b = (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(mine >> 32), at) << 32 |
+               (uint32_t)__builtin_amdgcn_readlane((int)mine, at);
+  for (int nth = rank - __builtin_amdgcn_readlane(before, at); nth > 0; --nth) b &= b - 1;
+  const int e = at * 64 + __builtin_ctzll(b);
+  for (int i0 = 0; i0 < pairs; i0 += THREADS) {
+    const int i = i0 + threadIdx.x;
+    const bool is = i < pairs && (i0 == 0 ? first : p.which[i]) == e;
+    const uint64_t m = __builtin_amdgcn_ballot_w64(is);
+    if (lane == 0) s.reached.counts[wave] = __builtin_popcountll(m);
+    __syncthreads();
+    int n = count;
+#pragma unroll
+    for (int w = 0; w < THREADS / 64; ++w) {
+      const int c = s.reached.counts[w];
+      n += w < wave ? c : 0;
+      count += c;
     }
-    if (threadIdx.x == 0) t.count = n;
+    if (is) s.list[n + __builtin_popcountll(m & (((uint64_t)1 << lane) - 1))] = (uint16_t)i;
+    __syncthreads();
   }
-  __syncthreads();
-  return true;
+  return e;
 }
 
 // ---- operands --------------------------------------------------------------------
@@ -101,16 +139,41 @@ struct Weights {
   v4i q[EIGHT ? 2 : 4];
 };
 
-// row: the vector's first element; o: the lane's first depth
+// Where chunk j (8 elements) of a step lies for the lanes of part `part`: a load's lanes
+// of one vector read 64 bytes in a row of its weights.
 template <bool EIGHT>
-__device__ __forceinline__ Weights<EIGHT> load_weights(const char* row, int64_t o, int depth, bool whole) {
+__device__ __forceinline__ int depth_of(int part, int j) {
+  return EIGHT ? 64 * (j >> 1) + 16 * part + 8 * (j & 1) : 32 * j + 8 * part;
+}
+
+// row: the vector's first element; o: the step's first depth
+template <bool EIGHT>
+__device__ __forceinline__ Weights<EIGHT> load_weights(const char* row, int64_t o, int part, int depth, bool whole) {
   Weights<EIGHT> r;
   if constexpr (EIGHT) {
 #pragma unroll
-    for (int j = 0; j < 2; ++j) r.q[j] = whole ? half::load_whole(row + o + 16 * j) : load16(row, o + 16 * j, depth);
+    for (int j = 0; j < 2; ++j) {
+      const int64_t at = o + depth_of<true>(part, 2 * j);
+      r.q[j] = whole ? half::load_whole(row + at) : load16(row, at, depth);
+    }
   } else {
 #pragma unroll
-    for (int j = 0; j < 4; ++j) r.q[j] = whole ? half::load_whole(row + (o + 8 * j) * 2) : half::load8(row, (int)o + 8 * j, depth);
+    for (int j = 0; j < 4; ++j) {
+      const int64_t at = o + depth_of<false>(part, j);
+      r.q[j] = whole ? half::load_whole(row + at * 2) : half::load8(row, (int)at, depth);
+    }
+  }
+  return r;
+}
+
+// The same depths of a vector of 16-bit numbers beside weights of either kind.
+template <bool EIGHT>
+__device__ __forceinline__ Weights<false> load_beside(const char* row, int64_t o, int part, int depth, bool whole) {
+  Weights<false> r;
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    const int64_t at = o + depth_of<EIGHT>(part, j);
+    r.q[j] = whole ? half::load_whole(row + at * 2) : half::load8(row, (int)at, depth);
   }
   return r;
 }
@@ -160,12 +223,20 @@ __device__ __forceinline__ v4f down_product(const Weights<EIGHT>& w, int j, v4i 
 
 __device__ __forceinline__ float silu(float x) { return x / (1.0f + expf(-x)); }
 
-// Hidden values h[o .. o + 8), zeros past `inner`, times g.
-__device__ __forceinline__ void load_hidden(const float* h, int64_t o, int inner, float g, float (&v)[8]) {
-  const Raw<kF32> r = load_raw<kF32>((const char*)(h + o), (int)(inner - o));
+// Hidden values h[o .. o + 8), zeros past `inner`.
+__device__ __forceinline__ void load_hidden(const float* h, int64_t o, int inner, bool whole, float (&v)[8]) {
+  const Raw<kF32> r = load_raw<kF32>((const char*)(h + o), whole ? 8 : (int)(inner - o));
   values<kF32>(r, v);
-#pragma unroll
-  for (int j = 0; j < 8; ++j) v[j] *= g;
+}
+
+// Steps s0 .. s1 - 1, those below `whole` without an end inside.
+template <class F>
+__device__ __forceinline__ void each_step(int s0, int s1, int whole, F step) {
+  const int most = whole < s1 ? whole : s1;
+  int s = s0;
+#pragma unroll 2
+  for (; s < most; ++s) step(s, true);
+  if (s < s1) step(s, false);
 }
 
 // ---- hidden values ---------------------------------------------------------------
@@ -173,16 +244,15 @@ __device__ __forceinline__ void load_hidden(const float* h, int64_t o, int inner
 // the others U's, of the same 8 NB hidden columns (of one product's 16 rows where
 // NB is 1).
 template <int TYPE, bool EIGHT, bool GATED, int NB, int TB, int WAVES>
-__global__ __launch_bounds__(WAVES * 64) void hidden_kernel(Layer p) {
+__global__ __launch_bounds__(WAVES * 64, 4) void hidden_kernel(Layer p) {
   constexpr int COLS = GATED ? 8 * NB : 16 * NB, E = EIGHT ? 1 : 2, Q = NB * 4, ROWS = TB * 16;
-  __shared__ Reached reached;
   __shared__ Tokens tokens;
   __shared__ v4f lds[WAVES * ROWS * Q];
   const int tiles = (p.inner + COLS - 1) / COLS;
   const int rank = blockIdx.x / tiles, c0 = (blockIdx.x - rank * tiles) * COLS;
-  find_reached<WAVES * 64>(p, reached);
-  if (!find_tokens<WAVES * 64>(p, reached, rank, tokens)) return;
-  const int64_t e = tokens.expert;
+  int count;
+  const int64_t e = find_tokens<WAVES * 64>(p, rank, tokens, count);
+  if (count == 0) return;
   const int lane = threadIdx.x & 63, at = lane & 15, part = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int steps = (p.width + kStep - 1) / kStep, s0 = steps * wave / WAVES, s1 = steps * (wave + 1) / WAVES;
@@ -205,8 +275,8 @@ __global__ __launch_bounds__(WAVES * 64) void hidden_kernel(Layer p) {
     const ExpertWeights& n = g ? p.gate : p.up;
     sw[i] = EIGHT ? n.scales + e * n.scales_stride + c / kBlock * n.scales_ld : nullptr;
   }
-  for (int r0 = 0; r0 < tokens.count; r0 += ROWS) {
-    const int rows = tokens.count - r0 < ROWS ? tokens.count - r0 : ROWS;
+  for (int r0 = 0; r0 < count; r0 += ROWS) {
+    const int rows = count - r0 < ROWS ? count - r0 : ROWS;
     const char* px[TB];
 #pragma unroll
     for (int j = 0; j < TB; ++j) {
@@ -214,14 +284,14 @@ __global__ __launch_bounds__(WAVES * 64) void hidden_kernel(Layer p) {
       px[j] = (const char*)p.x + tokens.list[r0 + r] / p.top * p.ldx * 2;
     }
     v4f acc[NB][TB] = {};
-    auto run = [&](int s, bool whole) {
-      const int64_t o = (int64_t)s * kStep + part * 32;
+    each_step(s0, s1, p.width / kStep, [&](int s, bool whole) {
+      const int64_t o = (int64_t)s * kStep;
       Weights<EIGHT> w[NB];
       Weights<false> x[TB];
 #pragma unroll
-      for (int i = 0; i < NB; ++i) w[i] = load_weights<EIGHT>(pw[i], o, p.width, whole);
+      for (int i = 0; i < NB; ++i) w[i] = load_weights<EIGHT>(pw[i], o, part, p.width, whole);
 #pragma unroll
-      for (int j = 0; j < TB; ++j) x[j] = load_weights<false>(px[j], o, p.width, whole);
+      for (int j = 0; j < TB; ++j) x[j] = load_beside<EIGHT>(px[j], o, part, p.width, whole);
 #pragma unroll
       for (int i = 0; i < NB; ++i) {
         v4f t[TB];
@@ -241,12 +311,7 @@ __global__ __launch_bounds__(WAVES * 64) void hidden_kernel(Layer p) {
             acc[i][j] = t[j];
         }
       }
-    };
-    const int most = p.width / kStep < s1 ? p.width / kStep : s1;
-    int s = s0;
-#pragma unroll 2
-    for (; s < most; ++s) run(s, true);
-    if (s < s1) run(s, false);
+    });
     // the wavefronts' sums in their order
 #pragma unroll
     for (int i = 0; i < NB; ++i)
@@ -278,72 +343,74 @@ __global__ __launch_bounds__(WAVES * 64) void hidden_kernel(Layer p) {
   }
 }
 
-// ---- outputs of at most kTogether tokens -----------------------------------------
+// ---- outputs of at most kTogether choices ----------------------------------------
 // A block: COLS output columns of every reached expert, whose sums stay in one set of
 // registers: product column t is token t, left out where it does not reach the expert.
-struct Table {
-  int expert[kTogether * kMaxTop];
-  float gate[kTogether * kMaxTop][kTogether];
-  int16_t pair[kTogether * kMaxTop][kTogether];  // -1: not reached
-};
-
 template <int TYPE, bool EIGHT, int COLS, int WAVES>
 __global__ __launch_bounds__(WAVES * 64) void together_kernel(Layer p) {
   constexpr int E = EIGHT ? 1 : 2;
   using O = typename Out<TYPE>::type;
-  __shared__ Reached reached;
-  __shared__ Table table;
   __shared__ v4f lds[WAVES * 16 * 4];
-  find_reached<WAVES * 64>(p, reached);
-  const int count = reached.count;
-  for (int i = threadIdx.x; i < count * kTogether; i += WAVES * 64) {
-    table.gate[i / kTogether][i % kTogether] = 0.0f;
-    table.pair[i / kTogether][i % kTogether] = -1;
-  }
-  __syncthreads();
-  if ((int)threadIdx.x < p.tokens) {
-    // a token that names an expert twice has it with the sum of the gates
-    for (int j = 0; j < p.top; ++j) {
-      const int i = threadIdx.x * p.top + j, e = p.which[i];
-      if (e < 0 || e >= p.experts) continue;
-      const int r = rank_of(reached, e);
-      table.expert[r] = e;
-      table.gate[r][threadIdx.x] += p.gates[i];
-      if (table.pair[r][threadIdx.x] < 0) table.pair[r][threadIdx.x] = (int16_t)i;
-    }
-  }
-  __syncthreads();
   const int lane = threadIdx.x & 63, at = lane & 15, part = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const float gates = lane < p.tokens * p.top ? p.gates[lane] : 0.0f;
+  FewChoices choices;
+  choices.init(p, lane);
+  const uint64_t valid = choices.left;
+  int count = 0;
+  for (uint64_t m; choices.take(m), m;) ++count;
+  choices.left = valid;
+  int taken = 0;
+  // expert number r (of ascending calls), and the lane's token's choice of it (-1: none)
+  // with its gate; a token that names it twice has the sum of the gates
+  auto look_up = [&](int r, int64_t& e, int& pair, float& gate) {
+    uint64_t all = 0;
+    for (; taken <= r; ++taken) e = choices.take(all);
+    uint64_t m = at < p.tokens ? all >> (at * p.top) & (((uint64_t)1 << p.top) - 1) : 0;
+    pair = m ? at * p.top + __builtin_ctzll(m) : -1;
+    gate = 0.0f;
+    while (__builtin_amdgcn_ballot_w64(m != 0)) {
+      const float g = __shfl(gates, m ? at * p.top + __builtin_ctzll(m) : 0);
+      gate += m ? g : 0.0f;
+      m &= m - 1;
+    }
+  };
   const int c0 = blockIdx.x * COLS, c = c0 + (at < COLS ? at : COLS - 1) < p.out ? c0 + (at < COLS ? at : COLS - 1) : p.out - 1;
   const int each = (p.inner + kStep - 1) / kStep, whole = p.inner / kStep;  // steps of an expert
   const int64_t all = (int64_t)count * each;
   const int s0 = (int)(all * wave / WAVES), s1 = (int)(all * (wave + 1) / WAVES);
   v4f acc{};
-  int r = s0 / each, s = s0 - r * each;
-#pragma unroll 2
-  for (int i = s0; i < s1; ++i) {
-    const int64_t e = table.expert[r];
-    const int64_t o = (int64_t)s * kStep + part * 32;
-    const Weights<EIGHT> w =
-        load_weights<EIGHT>((const char*)p.down.w + (e * p.down.stride + c * p.down.ld) * E, o, p.inner, s < whole);
-    const int pair = table.pair[r][at];
-    const float g = table.gate[r][at];
+  for (int i = s0; i < s1;) {
+    const int r = i / each, first = i - r * each, end = s1 - r * each < each ? s1 - r * each : each;
+    int64_t e;
+    int pair;
+    float gate;
+    look_up(r, e, pair, gate);
+    const char* const w = (const char*)p.down.w + (e * p.down.stride + c * p.down.ld) * E;
     const float* const h = p.hidden + (int64_t)(pair < 0 ? 0 : pair) * p.inner_pad;
-    v4f t{};
+    const float* const scales = EIGHT ? p.down.scales + e * p.down.scales_stride + c0 / kBlock * p.down.scales_ld : nullptr;
+    each_step(first, end, whole, [&](int s, bool is_whole) {
+      const int64_t o = (int64_t)s * kStep;
+      const Weights<EIGHT> q = load_weights<EIGHT>(w, o, part, p.inner, is_whole);
+      float values[4][8];
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      float v[8];
-      load_hidden(h, o + 8 * j, p.inner, g, v);
-      v4i hi, lo;
-      split(v, hi, lo);
-      t = down_product<TYPE>(w, j, hi, lo, t);
-    }
-    if constexpr (EIGHT) t *= p.down.scales[e * p.down.scales_stride + c0 / kBlock * p.down.scales_ld + s];
-    // a token that does not reach the expert sees nothing of it, not even a NaN
+      for (int j = 0; j < 4; ++j) load_hidden(h, o + depth_of<EIGHT>(part, j), p.inner, is_whole, values[j]);
+      v4f t{};
 #pragma unroll
-    for (int k = 0; k < 4; ++k) acc[k] = pair < 0 ? acc[k] : acc[k] + t[k];
-    if (++s == each) s = 0, ++r;
+      for (int j = 0; j < 4; ++j) {
+        float v[8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) v[k] = values[j][k] * gate;
+        v4i hi, lo;
+        split(v, hi, lo);
+        t = down_product<TYPE>(q, j, hi, lo, t);
+      }
+      if constexpr (EIGHT) t *= scales[s];
+      // a token that does not reach the expert sees nothing of it, not even a NaN
+#pragma unroll
+      for (int k = 0; k < 4; ++k) acc[k] = pair < 0 ? acc[k] : acc[k] + t[k];
+    });
+    i += end - first;
   }
   lds[(wave * 16 + at) * 4 + ((part + at) & 3)] = acc;
   __syncthreads();
@@ -361,20 +428,19 @@ __global__ __launch_bounds__(WAVES * 64) void together_kernel(Layer p) {
   }
 }
 
-// ---- outputs of more tokens --------------------------------------------------------
+// ---- outputs of more choices --------------------------------------------------------
 // A block: 16 NB output columns of one expert, for its tokens; combine_kernel adds a
 // token's shares in the order of its choices.
 template <int TYPE, bool EIGHT, int NB, int TB, int WAVES>
-__global__ __launch_bounds__(WAVES * 64) void share_kernel(Layer p) {
+__global__ __launch_bounds__(WAVES * 64, 4) void share_kernel(Layer p) {
   constexpr int COLS = 16 * NB, E = EIGHT ? 1 : 2, Q = NB * 4, ROWS = TB * 16;
-  __shared__ Reached reached;
   __shared__ Tokens tokens;
   __shared__ v4f lds[WAVES * ROWS * Q];
   const int tiles = (p.out + COLS - 1) / COLS;
   const int rank = blockIdx.x / tiles, c0 = (blockIdx.x - rank * tiles) * COLS;
-  find_reached<WAVES * 64>(p, reached);
-  if (!find_tokens<WAVES * 64>(p, reached, rank, tokens)) return;
-  const int64_t e = tokens.expert;
+  int count;
+  const int64_t e = find_tokens<WAVES * 64>(p, rank, tokens, count);
+  if (count == 0) return;
   const int lane = threadIdx.x & 63, at = lane & 15, part = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int steps = (p.inner + kStep - 1) / kStep, s0 = steps * wave / WAVES, s1 = steps * (wave + 1) / WAVES;
@@ -384,24 +450,28 @@ __global__ __launch_bounds__(WAVES * 64) void share_kernel(Layer p) {
   for (int i = 0; i < NB; ++i) {
     const int c = c0 + i * 16 + at < p.out ? c0 + i * 16 + at : p.out - 1;
     pw[i] = (const char*)p.down.w + (e * p.down.stride + c * p.down.ld) * E;
-    const int first = c0 + i * 16 < p.out ? c0 + i * 16 : c0;
-    sw[i] = EIGHT ? p.down.scales + e * p.down.scales_stride + first / kBlock * p.down.scales_ld : nullptr;
+    const int square = c0 + i * 16 < p.out ? c0 + i * 16 : c0;
+    sw[i] = EIGHT ? p.down.scales + e * p.down.scales_stride + square / kBlock * p.down.scales_ld : nullptr;
   }
-  for (int r0 = 0; r0 < tokens.count; r0 += ROWS) {
-    const int rows = tokens.count - r0 < ROWS ? tokens.count - r0 : ROWS;
-    const float *ph[TB], one = 1.0f;
+  for (int r0 = 0; r0 < count; r0 += ROWS) {
+    const int rows = count - r0 < ROWS ? count - r0 : ROWS;
+    const float* ph[TB];
 #pragma unroll
     for (int j = 0; j < TB; ++j) {
       const int r = j * 16 + at < rows ? j * 16 + at : rows - 1;
       ph[j] = p.hidden + (int64_t)tokens.list[r0 + r] * p.inner_pad;
     }
     v4f acc[NB][TB] = {};
-    for (int s = s0; s < s1; ++s) {
-      const int64_t o = (int64_t)s * kStep + part * 32;
-      const bool whole = s < p.inner / kStep;
+    each_step(s0, s1, p.inner / kStep, [&](int s, bool whole) {
+      const int64_t o = (int64_t)s * kStep;
       Weights<EIGHT> w[NB];
+      float h[TB][4][8];
 #pragma unroll
-      for (int i = 0; i < NB; ++i) w[i] = load_weights<EIGHT>(pw[i], o, p.inner, whole);
+      for (int i = 0; i < NB; ++i) w[i] = load_weights<EIGHT>(pw[i], o, part, p.inner, whole);
+#pragma unroll
+      for (int j = 0; j < TB; ++j)
+#pragma unroll
+        for (int k = 0; k < 4; ++k) load_hidden(ph[j], o + depth_of<EIGHT>(part, k), p.inner, whole, h[j][k]);
       v4f t[NB][TB];
 #pragma unroll
       for (int i = 0; i < NB; ++i)
@@ -411,10 +481,8 @@ __global__ __launch_bounds__(WAVES * 64) void share_kernel(Layer p) {
       for (int k = 0; k < 4; ++k)
 #pragma unroll
         for (int j = 0; j < TB; ++j) {
-          float v[8];
-          load_hidden(ph[j], o + 8 * k, p.inner, one, v);
           v4i hi, lo;
-          split(v, hi, lo);
+          split(h[j][k], hi, lo);
 #pragma unroll
           for (int i = 0; i < NB; ++i) t[i][j] = down_product<TYPE>(w[i], k, hi, lo, t[i][j]);
         }
@@ -427,7 +495,7 @@ __global__ __launch_bounds__(WAVES * 64) void share_kernel(Layer p) {
           else
             acc[i][j] = t[i][j];
         }
-    }
+    });
 #pragma unroll
     for (int i = 0; i < NB; ++i)
 #pragma unroll
@@ -457,9 +525,13 @@ __global__ __launch_bounds__(256) void combine_kernel(Layer p) {
   const int t = (int)(i / groups), c = (int)(i % groups) * 4;
   if (t >= p.tokens) return;
   v4f v{};
+#pragma unroll 4
   for (int j = 0; j < p.top; ++j) {
+    // what a choice of no expert left in the workspace is read and not used
     const int pair = t * p.top + j, e = p.which[pair];
-    if (e >= 0 && e < p.experts) v += *(const v4f*)(p.parts + (int64_t)pair * p.out_pad + c);
+    const v4f w = *(const v4f*)(p.parts + (int64_t)pair * p.out_pad + c);
+#pragma unroll
+    for (int k = 0; k < 4; ++k) v[k] += e >= 0 && e < p.experts ? w[k] : 0.0f;
   }
   O* const y = (O*)p.y + t * p.ldy + c;
 #pragma unroll
@@ -467,35 +539,42 @@ __global__ __launch_bounds__(256) void combine_kernel(Layer p) {
     if (c + k < p.out) y[k] = (O)v[k];
 }
 
-template <int TYPE, bool EIGHT, bool GATED, int NB, int TB>
-hipError_t run_hidden(const Layer& p, hipStream_t s) {
-  constexpr int COLS = GATED ? 8 * NB : 16 * NB, WAVES = 8;
-  const int64_t pairs = (int64_t)p.tokens * p.top, most = p.experts < pairs ? p.experts : pairs;
-  const int64_t blocks = most * ceil_div(p.inner, COLS);
+template <int TYPE, bool EIGHT, bool GATED, int NB, int TB, int WAVES>
+hipError_t run_hidden(const Layer& p, int64_t experts, hipStream_t s) {
+  const int64_t blocks = experts * ceil_div(p.inner, GATED ? 8 * NB : 16 * NB);
   if (blocks * WAVES * 64 >= ((int64_t)1 << 32)) return hipErrorInvalidConfiguration;
   hidden_kernel<TYPE, EIGHT, GATED, NB, TB, WAVES><<<dim3((uint32_t)blocks), dim3(WAVES * 64), 0, s>>>(p);
   return hipGetLastError();
 }
 
+template <int TYPE, bool EIGHT, bool GATED>
+hipError_t run_hidden(const Layer& p, int64_t experts, hipStream_t s) {
+  switch (hidden_form(p.tokens * p.top, experts, p.inner, GATED, EIGHT)) {
+    case kHiddenOne: return run_hidden<TYPE, EIGHT, GATED, 1, 1, 8>(p, experts, s);
+    case kHiddenSmall: return run_hidden<TYPE, EIGHT, GATED, 1, 1, 4>(p, experts, s);
+    case kHiddenWide: return run_hidden<TYPE, EIGHT, GATED, 2, 1, 4>(p, experts, s);
+    default: return run_hidden<TYPE, EIGHT, GATED, 2, 2, 4>(p, experts, s);
+  }
+}
+
+template <int TYPE, bool EIGHT, int COLS>
+hipError_t run_together(const Layer& p, hipStream_t s) {
+  constexpr int WAVES = 8;
+  together_kernel<TYPE, EIGHT, COLS, WAVES><<<dim3((uint32_t)ceil_div(p.out, COLS)), dim3(WAVES * 64), 0, s>>>(p);
+  return hipGetLastError();
+}
+
 template <int TYPE, bool EIGHT>
 hipError_t run_layer(const Layer& p, hipStream_t s) {
-  hipError_t e;
-  const bool many = p.tokens > kTogether;
-  if (p.gate.w)
-    e = many ? run_hidden<TYPE, EIGHT, true, 2, 2>(p, s) : run_hidden<TYPE, EIGHT, true, 1, 1>(p, s);
-  else
-    e = many ? run_hidden<TYPE, EIGHT, false, 1, 2>(p, s) : run_hidden<TYPE, EIGHT, false, 1, 1>(p, s);
-  if (e != hipSuccess) return e;
-  if (!many) {
-    constexpr int WAVES = 8, COLS = 8;
-    together_kernel<TYPE, EIGHT, COLS, WAVES><<<dim3((uint32_t)ceil_div(p.out, COLS)), dim3(WAVES * 64), 0, s>>>(p);
-    return hipGetLastError();
-  }
-  constexpr int WAVES = 8, NB = 1, TB = 2;
   const int64_t pairs = (int64_t)p.tokens * p.top, most = p.experts < pairs ? p.experts : pairs;
+  hipError_t e = p.gate.w ? run_hidden<TYPE, EIGHT, true>(p, most, s) : run_hidden<TYPE, EIGHT, false>(p, most, s);
+  if (e != hipSuccess) return e;
+  if (layer_together(p.tokens, p.top))
+    return together_wide(p.out) ? run_together<TYPE, EIGHT, 16>(p, s) : run_together<TYPE, EIGHT, 8>(p, s);
+  constexpr int WAVES = 4, NB = 2;
   const int64_t blocks = most * ceil_div(p.out, 16 * NB);
   if (blocks * WAVES * 64 >= ((int64_t)1 << 32)) return hipErrorInvalidConfiguration;
-  share_kernel<TYPE, EIGHT, NB, TB, WAVES><<<dim3((uint32_t)blocks), dim3(WAVES * 64), 0, s>>>(p);
+  share_kernel<TYPE, EIGHT, NB, 1, WAVES><<<dim3((uint32_t)blocks), dim3(WAVES * 64), 0, s>>>(p);
   if ((e = hipGetLastError()) != hipSuccess) return e;
   combine_kernel<TYPE><<<dim3((uint32_t)ceil_div((int64_t)p.tokens * (p.out_pad / 4), 256)), dim3(256), 0, s>>>(p);
   return hipGetLastError();

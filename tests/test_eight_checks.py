@@ -2,6 +2,7 @@
 entry points with addresses that are never read, and the binding with CPU
 tensors."""
 import ctypes
+import struct
 
 import pytest
 import torch
@@ -128,7 +129,7 @@ def test_binding_scaled_matmul():
     raises("b_scales has shape", f, A, a, B, b, squares=False)
     raises("b_scales must be", f, A, a, B, b.double())
     raises("Y has dtype", f, A, a, B, b, out_dtype=torch.float16, Y=torch.zeros(4, 200))
-    raises("Y must be", f, A, a, B, b, out_dtype=torch.float64)
+    raises("out_dtype must be", f, A, a, B, b, out_dtype=torch.float64)
     raises("Y has shape", f, A, a, B, b, Y=torch.zeros(4, 201))
     raises("must be a CUDA tensor", f, A, a, B, b)
 
@@ -140,15 +141,15 @@ def test_expert_layer_refusals():
     assert need > 0 and need % 256 == 0
     assert size(0, 2, 300, 200, 400) == 0 == size(20, 0, 300, 200, 400) == size(257, 2, 300, 200, 400) == size(20, 33, 300, 200, 400)
 
-    def stack(w, ld, stride, s=None, lds=1, ss=0):
-        return oz.ExpertWeights(w, ld, stride, s, lds, ss)
+    def stack(w, ld, stride, s=0, lds=1, ss=0):
+        return struct.pack("6q", w or 0, ld, stride, s, lds, ss)
 
     def call(tokens=20, top=2, experts=8, width=300, inner=200, out=400, X=p(1), ldx=300, which=p(2), gates=p(3), up=None, gate=None,
              down=None, Y=p(7), ldy=400, type=BF, room=p(8), size=need, no=()):
         up = up or stack(4 << 32, 300, 60000)
         gate = gate or stack(5 << 32, 300, 60000)
         down = down or stack(6 << 32, 200, 80000)
-        at = [None if n in no else ctypes.addressof(v) for n, v in (("up", up), ("gate", gate), ("down", down))]
+        at = [None if n in no else v for n, v in (("up", up), ("gate", gate), ("down", down))]
         return f(tokens, top, experts, width, inner, out, X, ldx, which, gates, *at, Y, ldy, type, room, size, None)
 
     eight = dict(up=stack(4 << 32, 300, 60000, 9 << 32, 3, 6), gate=stack(5 << 32, 300, 60000, 10 << 32, 3, 6),
