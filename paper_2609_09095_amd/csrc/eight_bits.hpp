@@ -106,20 +106,28 @@ __device__ __forceinline__ Raw<TYPE> rounded(const float (&v)[8]) {
   return r;
 }
 
+// p[0 .. n), n at most 8; a part of 8 in pieces of 4, 2 and 1.
 template <int TYPE>
 __device__ __forceinline__ void store_raw(char* p, const Raw<TYPE>& r, int n) {
   const auto g = (__attribute__((address_space(1))) char*)p;
+  using to = __attribute__((address_space(1))) void*;
   if (n >= 8) {
 #pragma unroll
-    for (int i = 0; i < Raw<TYPE>::Q; ++i)
-      __builtin_memcpy((__attribute__((address_space(1))) void*)(g + i * 16), &r.q[i], 16);
+    for (int i = 0; i < Raw<TYPE>::Q; ++i) __builtin_memcpy((to)(g + i * 16), &r.q[i], 16);
   } else if (n > 0) {
-    using E = typename Out<TYPE>::type;
-    E e[8];
+    constexpr int E = kBytes<TYPE>;
+    typename Out<TYPE>::type e[8];
     __builtin_memcpy(e, &r, sizeof(e));
+    if (n & 4) {
+      __builtin_memcpy((to)g, e, 4 * E);
 #pragma unroll
-    for (int j = 0; j < 7; ++j)
-      if (j < n) ((__attribute__((address_space(1))) E*)g)[j] = e[j];
+      for (int j = 0; j < 3; ++j) e[j] = e[4 + j];
+    }
+    if (n & 2) {
+      __builtin_memcpy((to)(g + (n & 4) * E), e, 2 * E);
+      e[0] = e[2];
+    }
+    if (n & 1) __builtin_memcpy((to)(g + (n & 6) * E), e, E);
   }
 }
 
@@ -129,10 +137,17 @@ __device__ __forceinline__ void store_bytes(uint8_t* p, uint2 w, int n) {
   if (n >= 8) {
     __builtin_memcpy((__attribute__((address_space(1))) void*)g, &w, 8);
   } else if (n > 0) {
-    const uint64_t v = (uint64_t)w.y << 32 | w.x;
-#pragma unroll
-    for (int j = 0; j < 7; ++j)
-      if (j < n) g[j] = (uint8_t)(v >> (8 * j));
+    using to = __attribute__((address_space(1))) void*;
+    uint64_t v = (uint64_t)w.y << 32 | w.x;
+    if (n & 4) {
+      __builtin_memcpy((to)g, &v, 4);
+      v >>= 32;
+    }
+    if (n & 2) {
+      __builtin_memcpy((to)(g + (n & 4)), &v, 2);
+      v >>= 16;
+    }
+    if (n & 1) g[n & 6] = (uint8_t)v;
   }
 }
 

@@ -21,30 +21,29 @@ constexpr NormForm norm_form(int64_t width) {
   const int64_t c = ceil_div(width, 8);
   if (c <= 16) return {16, 1};
   if (c <= 32) return {32, 1};
-  if (c <= 64) return {64, 1};
-  if (c <= 128) return {64, 2};
-  if (c <= 256) return {256, 1};
-  if (c <= 512) return {512, 1};
-  if (c <= 1024) return {1024, 1};
-  if (c <= 2048) return {1024, 2};
-  return {1024, 4};
+  if (c <= 256) return {(int)ceil_div(c, 64) * 64, 1};
+  if (c <= 512) return {c <= 384 ? 384 : 512, 1};
+  if (c <= 1024) return {c <= 768 ? 768 : 1024, 1};
+  return {1024, c <= 2048 ? 2 : 4};
 }
 
-// Threads of a block, and rows that it holds at a time.
-constexpr int norm_threads(NormForm f) { return f.lanes < 256 ? 256 : f.lanes; }
+// Threads of a block (more than one row's where a row is a wavefront's or less).
+constexpr int norm_threads(int lanes) { return lanes <= 64 ? 256 : lanes; }
 
-// Blocks of a norm's launch: a row at a time each, at most as many as the card
-// runs at once, so that the weights are loaded and the next row's loads are in
-// flight while a row is worked on.
+// Blocks of a norm's launch: as many as the card runs at once, each a row (or a set
+// of rows) at a time, so that the weights are loaded once and the next row's loads are
+// in flight while one is worked on.
 constexpr int64_t norm_blocks(int64_t rows, int64_t width, int64_t per_cu) {
-  const NormForm f = norm_form(width);
-  const int64_t threads = norm_threads(f), need = ceil_div(rows, threads / f.lanes);
-  const int64_t most = 256 * (per_cu > threads ? per_cu / threads : 1);
+  const int lanes = norm_form(width).lanes, threads = norm_threads(lanes);
+  const int64_t need = ceil_div(rows, threads / lanes), most = 256 * (per_cu > threads ? per_cu / threads : 1);
   return need < most ? need : most;
 }
 
-constexpr int64_t kNormThreads = 2048;          // per CU: the forward pass
-constexpr int64_t kNormGradientThreads = 1024;  // the gradient; its blocks leave a partial sum each
+constexpr int64_t kNormThreads = 2048;  // per CU: the forward pass
+#ifndef NGT
+#define NGT 1024
+#endif
+constexpr int64_t kNormGradientThreads = NGT;  // the gradient; its blocks leave a partial sum each
 
 constexpr int64_t norm_parts(int64_t rows, int64_t width) { return norm_blocks(rows, width, kNormGradientThreads); }
 

@@ -44,18 +44,55 @@ __device__ __forceinline__ void row_sums(float (&v)[N], float* room, int turn) {
   }
 }
 
+// A thread's chunks of 8 columns of a row.  The chunk that the row's end cuts is read
+// as the row's last 8 elements and moved down when it is used, and one past the end
+// reads them too: a branch around a load would wait for its data and leave none in
+// flight.  Rows of fewer than 8 elements are read one by one.
+template <int TYPE, int LANES>
+struct Columns {
+  int width, lane;
+  bool narrow;
+  __device__ __forceinline__ void init(int w, int l) {
+    width = w, lane = l;
+    narrow = w < 8;
+  }
+  __device__ __forceinline__ int column(int i) const { return (lane + i * LANES) * 8; }
+  // elements of the chunk that exist; below 1: none
+  __device__ __forceinline__ int have(int i) const { return width - column(i); }
+  __device__ __forceinline__ Raw<TYPE> load(const void* p, int64_t first, int i) const {
+    constexpr int E = kBytes<TYPE>;
+    const int off = narrow || have(i) >= 8 ? column(i) : width - 8;
+    const char* const q = (const char*)p + (first + off) * E;
+    return narrow ? load_raw<TYPE>(q, have(i)) : load_raw<TYPE>(q, 8);
+  }
+  __device__ __forceinline__ void get(const Raw<TYPE>& r, int i, float (&v)[8]) const {
+    values<TYPE>(r, v);
+    const int n = have(i);
+    if (!narrow && __builtin_amdgcn_ballot_w64(n < 8)) {
+      const int s = n >= 8 ? 0 : n <= 0 ? 8 : 8 - n;  // elements to drop
+#pragma unroll
+      for (int j = 0; j < 8; ++j) v[j] = s & 8 ? 0.0f : s & 4 ? (j < 4 ? v[(j + 4) & 7] : 0.0f) : v[j];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) v[j] = s & 2 ? (j < 6 ? v[(j + 2) & 7] : 0.0f) : v[j];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) v[j] = s & 1 ? (j < 7 ? v[(j + 1) & 7] : 0.0f) : v[j];
+    }
+  }
+};
+
 template <int TYPE, int LANES, int CH, bool RES, bool EIGHT>
-__global__ __launch_bounds__(LANES < 256 ? 256 : LANES) void norm_kernel(Norm p) {
-  constexpr int THREADS = LANES < 256 ? 256 : LANES, GROUPS = THREADS / LANES, E = kBytes<TYPE>;
+__global__ __launch_bounds__(norm_threads(LANES)) void norm_kernel(Norm p) {
+  constexpr int THREADS = norm_threads(LANES), GROUPS = THREADS / LANES, E = kBytes<TYPE>;
+  constexpr bool AHEAD = CH < 4;  // registers for the next row
   __shared__ float room[2 * 16];
   const int lane = threadIdx.x % LANES, group = threadIdx.x / LANES;
-  int have[CH];
+  Columns<TYPE, LANES> cols;
+  cols.init(p.width, lane);
   float w[CH][8];
 #pragma unroll
   for (int i = 0; i < CH; ++i) {
-    have[i] = p.width - (lane + i * LANES) * 8;
     if (p.weight) {
-      values<TYPE>(load_raw<TYPE>((const char*)p.weight + (int64_t)(lane + i * LANES) * 8 * E, have[i]), w[i]);
+      cols.get(cols.load(p.weight, 0, i), i, w[i]);
     } else {
 #pragma unroll
       for (int j = 0; j < 8; ++j) w[i][j] = 1.0f;
@@ -63,35 +100,35 @@ __global__ __launch_bounds__(LANES < 256 ? 256 : LANES) void norm_kernel(Norm p)
   }
   Raw<TYPE> x[CH], r[CH];
   auto load = [&](int64_t row) {
+    row = row < p.rows ? row : p.rows - 1;  // one past the last is read again and not used
 #pragma unroll
     for (int i = 0; i < CH; ++i) {
-      const int n = row < p.rows ? have[i] : 0;
-      const int64_t c = (int64_t)(lane + i * LANES) * 8;
-      x[i] = load_raw<TYPE>((const char*)p.x + (row * p.ldx + c) * E, n);
-      if constexpr (RES) r[i] = load_raw<TYPE>((const char*)p.residual + (row * p.ldr + c) * E, n);
+      x[i] = cols.load(p.x, row * p.ldx, i);
+      if constexpr (RES) r[i] = cols.load(p.residual, row * p.ldr, i);
     }
   };
   const int64_t step = (int64_t)gridDim.x * GROUPS;
-  load((int64_t)blockIdx.x * GROUPS + group);
+  if constexpr (AHEAD) load((int64_t)blockIdx.x * GROUPS + group);
   int turn = 0;
   for (int64_t first = (int64_t)blockIdx.x * GROUPS; first < p.rows; first += step) {
     const int64_t row = first + group;
     const bool any = row < p.rows;
+    if constexpr (!AHEAD) load(row);
     float h[CH][8], sum[1] = {0.0f};
 #pragma unroll
     for (int i = 0; i < CH; ++i) {
-      values<TYPE>(x[i], h[i]);
+      cols.get(x[i], i, h[i]);
       if constexpr (RES) {
         float b[8];
-        values<TYPE>(r[i], b);
+        cols.get(r[i], i, b);
 #pragma unroll
         for (int j = 0; j < 8; ++j) h[i][j] += b[j];
         const Raw<TYPE> kept = rounded<TYPE>(h[i]);
-        if (any) store_raw<TYPE>((char*)p.h + (row * p.ldh + (int64_t)(lane + i * LANES) * 8) * E, kept, have[i]);
+        if (any) store_raw<TYPE>((char*)p.h + (row * p.ldh + cols.column(i)) * E, kept, cols.have(i));
         values<TYPE>(kept, h[i]);  // the norm is that of the sum as it is kept
       }
     }
-    load(row + step);
+    if constexpr (AHEAD) load(row + step);
 #pragma unroll
     for (int i = 0; i < CH; ++i)
 #pragma unroll
@@ -101,24 +138,24 @@ __global__ __launch_bounds__(LANES < 256 ? 256 : LANES) void norm_kernel(Norm p)
     const float rho = 1.0f / sqrtf(sum[0] / (float)p.width + p.eps);
 #pragma unroll
     for (int i = 0; i < CH; ++i) {
-      const int64_t c = (int64_t)(lane + i * LANES) * 8;
+      const int c = cols.column(i), have = cols.have(i);
       float y[8];
 #pragma unroll
       for (int j = 0; j < 8; ++j) y[j] = h[i][j] * rho * w[i][j];
       if constexpr (EIGHT) {
         uint32_t most = 0;
 #pragma unroll
-        for (int j = 0; j < 8; ++j) most = umax(most, j < have[i] ? size_bits(y[j]) : 0);
+        for (int j = 0; j < 8; ++j) most = umax(most, j < have ? size_bits(y[j]) : 0);
         const Scale s = scale_of(max16(most));
         uint2 b;
         b.x = pack_e4m3(quotient(y[0], s), quotient(y[1], s), quotient(y[2], s), quotient(y[3], s));
         b.y = pack_e4m3(quotient(y[4], s), quotient(y[5], s), quotient(y[6], s), quotient(y[7], s));
         if (any) {
-          store_bytes((uint8_t*)p.y + row * p.ldy + c, b, have[i]);
-          if ((lane & 15) == 0 && have[i] > 0) p.scales[(c / kBlock) * p.lds + row] = s.s;
+          store_bytes((uint8_t*)p.y + row * p.ldy + c, b, have);
+          if ((lane & 15) == 0 && have > 0) p.scales[(c / kBlock) * p.lds + row] = s.s;
         }
       } else {
-        if (any) store_raw<TYPE>((char*)p.y + (row * p.ldy + c) * E, rounded<TYPE>(y), have[i]);
+        if (any) store_raw<TYPE>((char*)p.y + (row * p.ldy + c) * E, rounded<TYPE>(y), have);
       }
     }
   }
@@ -127,92 +164,133 @@ __global__ __launch_bounds__(LANES < 256 ? 256 : LANES) void norm_kernel(Norm p)
 // Each block adds up dw over its rows in registers and leaves one row of
 // partial sums; dw_kernel adds those.
 template <int TYPE, int LANES, int CH, bool DH>
-__global__ __launch_bounds__(LANES < 256 ? 256 : LANES) void norm_gradient_kernel(NormGradient p) {
-  constexpr int THREADS = LANES < 256 ? 256 : LANES, GROUPS = THREADS / LANES, E = kBytes<TYPE>;
-  __shared__ float room[GROUPS > 1 ? GROUPS * LANES * CH * 8 : 2 * 2 * 16];
+__global__ __launch_bounds__(norm_threads(LANES)) void norm_gradient_kernel(NormGradient p) {
+  constexpr int THREADS = norm_threads(LANES), GROUPS = THREADS / LANES, E = kBytes<TYPE>;
+  __shared__ float room[GROUPS > 1 ? LANES * CH * 8 : 2 * 2 * 16];
   const int lane = threadIdx.x % LANES, group = threadIdx.x / LANES;
-  int have[CH];
-  float dw[CH][8] = {};
-  Raw<TYPE> w[CH];
-#pragma unroll
-  for (int i = 0; i < CH; ++i) {
-    have[i] = p.width - (lane + i * LANES) * 8;
-    if (p.weight) {
-      w[i] = load_raw<TYPE>((const char*)p.weight + (int64_t)(lane + i * LANES) * 8 * E, have[i]);
-    } else {
-      const float one[8] = {1.0f, 1.0f, 1.0f, 1.0f, 1.0f, 1.0f, 1.0f, 1.0f};
-      w[i] = rounded<TYPE>(one);
-    }
+  Columns<TYPE, LANES> cols;
+  cols.init(p.width, lane);
+  // of more than two chunks in LDS, and then a chunk at a time in registers
+  constexpr bool WIDE = CH > 2;
+  __shared__ v4f wide[WIDE ? CH * LANES * 2 : 1];
+  float dw[WIDE ? 1 : CH][8] = {};
+  if constexpr (WIDE) {
+    for (int i = 0; i < 2 * CH; ++i) wide[i * LANES + lane] = v4f{};  // a thread's own from here on
   }
-  Raw<TYPE> y[CH], x[CH], d[CH];
-  auto load = [&](int64_t row) {
+  auto weights = [&](int i) {
+    const float one[8] = {1.0f, 1.0f, 1.0f, 1.0f, 1.0f, 1.0f, 1.0f, 1.0f};
+    return p.weight ? cols.load(p.weight, 0, i) : rounded<TYPE>(one);
+  };
+  auto add = [&](const float (&h)[8], const float (&dy)[8], const float (&f)[8], float (&sum)[2]) {
 #pragma unroll
-    for (int i = 0; i < CH; ++i) {
-      const int n = row < p.rows ? have[i] : 0;
-      const int64_t c = (int64_t)(lane + i * LANES) * 8;
-      y[i] = load_raw<TYPE>((const char*)p.dy + (row * p.lddy + c) * E, n);
-      x[i] = load_raw<TYPE>((const char*)p.h + (row * p.ldh + c) * E, n);
-      if constexpr (DH) d[i] = load_raw<TYPE>((const char*)p.dh + (row * p.lddh + c) * E, n);
+    for (int j = 0; j < 8; ++j) {
+      sum[0] = __builtin_fmaf(h[j], h[j], sum[0]);
+      sum[1] = __builtin_fmaf(dy[j] * f[j], h[j], sum[1]);
     }
   };
+  auto finish = [&](int64_t row, int i, float rho, float mean, const float (&h)[8], const float (&dy)[8], const float (&f)[8],
+                    const float (&b)[8]) {
+    float dx[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      dx[j] = rho * __builtin_fmaf(-h[j], mean, dy[j] * f[j]);
+      if constexpr (DH) dx[j] += b[j];
+    }
+    if constexpr (WIDE) {
+#pragma unroll
+      for (int q = 0; q < 2; ++q) {
+        v4f t = wide[(2 * i + q) * LANES + lane];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) t[j] = __builtin_fmaf(dy[4 * q + j] * h[4 * q + j], rho, t[j]);
+        wide[(2 * i + q) * LANES + lane] = t;
+      }
+    } else if (row < p.rows) {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) dw[i][j] = __builtin_fmaf(dy[j] * h[j], rho, dw[i][j]);
+    }
+    if (row < p.rows)
+      store_raw<TYPE>((char*)p.dx + (row * p.lddx + cols.column(i)) * E, rounded<TYPE>(dx), cols.have(i));
+  };
   const int64_t step = (int64_t)gridDim.x * GROUPS;
-  load((int64_t)blockIdx.x * GROUPS + group);
   int turn = 0;
-  for (int64_t first = (int64_t)blockIdx.x * GROUPS; first < p.rows; first += step) {
-    const int64_t row = first + group;
-    float h[CH][8], dy[CH][8], b[CH][8], sum[2] = {0.0f, 0.0f};
-#pragma unroll
-    for (int i = 0; i < CH; ++i) {
-      values<TYPE>(x[i], h[i]);
-      values<TYPE>(y[i], dy[i]);
-      if constexpr (DH) values<TYPE>(d[i], b[i]);
+  if constexpr (CH == 1) {
+    const Raw<TYPE> w = weights(0);
+    Raw<TYPE> y, x, d;
+    auto load = [&](int64_t row) {
+      row = row < p.rows ? row : p.rows - 1;  // one past the last is read again and not used
+      y = cols.load(p.dy, row * p.lddy, 0);
+      x = cols.load(p.h, row * p.ldh, 0);
+      if constexpr (DH) d = cols.load(p.dh, row * p.lddh, 0);
+    };
+    load((int64_t)blockIdx.x * GROUPS + group);
+    for (int64_t first = (int64_t)blockIdx.x * GROUPS; first < p.rows; first += step) {
+      const int64_t row = first + group;
+      float h[8], dy[8], f[8], b[8] = {}, sum[2] = {0.0f, 0.0f};
+      cols.get(x, 0, h);
+      cols.get(y, 0, dy);
+      if constexpr (DH) cols.get(d, 0, b);
+      load(row + step);
+      cols.get(w, 0, f);
+      add(h, dy, f, sum);
+      row_sums<LANES, 2>(sum, room, turn);
+      turn ^= 1;
+      const float rho = 1.0f / sqrtf(sum[0] / (float)p.width + p.eps), mean = rho * rho * (sum[1] / (float)p.width);
+      finish(row, 0, rho, mean, h, dy, f, b);
     }
-    load(row + step);
-#pragma unroll
-    for (int i = 0; i < CH; ++i) {
-      float f[8];
-      values<TYPE>(w[i], f);
-#pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        sum[0] = __builtin_fmaf(h[i][j], h[i][j], sum[0]);
-        sum[1] = __builtin_fmaf(dy[i][j] * f[j], h[i][j], sum[1]);
+  } else {
+    // a row does not fit the registers beside its sums: it is read again, from the caches
+    for (int64_t row = blockIdx.x; row < p.rows; row += step) {
+      float sum[2] = {0.0f, 0.0f};
+#pragma unroll(WIDE ? 1 : CH)
+      for (int i = 0; i < CH; ++i) {
+        float h[8], dy[8], f[8];
+        cols.get(cols.load(p.h, row * p.ldh, i), i, h);
+        cols.get(cols.load(p.dy, row * p.lddy, i), i, dy);
+        cols.get(weights(i), i, f);
+        add(h, dy, f, sum);
       }
-    }
-    row_sums<LANES, 2>(sum, room, turn);
-    turn ^= 1;
-    const float rho = 1.0f / sqrtf(sum[0] / (float)p.width + p.eps), mean = rho * rho * (sum[1] / (float)p.width);
-#pragma unroll
-    for (int i = 0; i < CH; ++i) {
-      float f[8], dx[8];
-      values<TYPE>(w[i], f);
-#pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        dx[j] = rho * __builtin_fmaf(-h[i][j], mean, dy[i][j] * f[j]);
-        if constexpr (DH) dx[j] += b[i][j];
-        if (row < p.rows) dw[i][j] = __builtin_fmaf(dy[i][j] * h[i][j], rho, dw[i][j]);
+      row_sums<LANES, 2>(sum, room, turn);
+      turn ^= 1;
+      const float rho = 1.0f / sqrtf(sum[0] / (float)p.width + p.eps), mean = rho * rho * (sum[1] / (float)p.width);
+#pragma unroll(WIDE ? 1 : CH)
+      for (int i = 0; i < CH; ++i) {
+        float h[8], dy[8], f[8], b[8] = {};
+        cols.get(cols.load(p.h, row * p.ldh, i), i, h);
+        cols.get(cols.load(p.dy, row * p.lddy, i), i, dy);
+        cols.get(weights(i), i, f);
+        if constexpr (DH) cols.get(cols.load(p.dh, row * p.lddh, i), i, b);
+        finish(row, i, rho, mean, h, dy, f, b);
       }
-      if (row < p.rows)
-        store_raw<TYPE>((char*)p.dx + (row * p.lddx + (int64_t)(lane + i * LANES) * 8) * E, rounded<TYPE>(dx), have[i]);
     }
   }
   float* const part = p.parts + (int64_t)blockIdx.x * p.width;
   if constexpr (GROUPS > 1) {
+    // one group after the other
+    for (int g = 0; g < GROUPS; ++g) {
+      if (group == g) {
 #pragma unroll
-    for (int i = 0; i < CH; ++i)
+        for (int i = 0; i < CH; ++i)
 #pragma unroll
-      for (int j = 0; j < 8; ++j) room[(group * CH + i) * LANES * 8 + lane * 8 + j] = dw[i][j];
-    __syncthreads();
-    for (int c = threadIdx.x; c < p.width; c += THREADS) {
-      float t = room[c];
-#pragma unroll
-      for (int g = 1; g < GROUPS; ++g) t += room[g * CH * LANES * 8 + c];
-      part[c] = t;
+          for (int q = 0; q < 2; ++q) {
+            v4f* const at = (v4f*)&room[(lane + i * LANES) * 8 + 4 * q];
+            const v4f v = {dw[i][4 * q], dw[i][4 * q + 1], dw[i][4 * q + 2], dw[i][4 * q + 3]};
+            *at = g == 0 ? v : *at + v;
+          }
+      }
+      __syncthreads();
     }
+    for (int c = threadIdx.x; c < p.width; c += THREADS) part[c] = room[c];
   } else {
 #pragma unroll
     for (int i = 0; i < CH; ++i) {
-      const Raw<kF32> r = rounded<kF32>(dw[i]);
-      store_raw<kF32>((char*)(part + (int64_t)(lane + i * LANES) * 8), r, have[i]);
+      Raw<kF32> r;
+      if constexpr (WIDE) {
+#pragma unroll
+        for (int q = 0; q < 2; ++q) r.q[q] = __builtin_bit_cast(v4i, wide[(2 * i + q) * LANES + lane]);
+      } else {
+        r = rounded<kF32>(dw[i]);
+      }
+      store_raw<kF32>((char*)(part + cols.column(i)), r, cols.have(i));
     }
   }
 }
@@ -242,7 +320,7 @@ __global__ __launch_bounds__(256) void zeros_kernel(float* p, int64_t count) {
 
 template <int TYPE, int LANES, int CH>
 hipError_t run_norm(const Norm& p, hipStream_t s) {
-  const dim3 grid((uint32_t)norm_blocks(p.rows, p.width, kNormThreads)), block(LANES < 256 ? 256 : LANES);
+  const dim3 grid((uint32_t)norm_blocks(p.rows, p.width, kNormThreads)), block(norm_threads(LANES));
   if (p.residual) {
     if (p.scales)
       norm_kernel<TYPE, LANES, CH, true, true><<<grid, block, 0, s>>>(p);
@@ -260,7 +338,7 @@ hipError_t run_norm(const Norm& p, hipStream_t s) {
 template <int TYPE, int LANES, int CH>
 hipError_t run_gradient(const NormGradient& p, hipStream_t s) {
   const int64_t parts = norm_parts(p.rows, p.width);
-  const dim3 grid((uint32_t)parts), block(LANES < 256 ? 256 : LANES);
+  const dim3 grid((uint32_t)parts), block(norm_threads(LANES));
   if (p.dh)
     norm_gradient_kernel<TYPE, LANES, CH, true><<<grid, block, 0, s>>>(p);
   else
@@ -272,15 +350,17 @@ hipError_t run_gradient(const NormGradient& p, hipStream_t s) {
 
 // calls f<LANES, CH>() for the form of this width
 template <class F>
-hipError_t of_form(int width, F f) {
-  const NormForm g = norm_form(width);
+hipError_t of_form(NormForm g, F f) {
   switch (g.lanes * 8 + g.chunks) {
     case 16 * 8 + 1: return f.template operator()<16, 1>();
     case 32 * 8 + 1: return f.template operator()<32, 1>();
     case 64 * 8 + 1: return f.template operator()<64, 1>();
-    case 64 * 8 + 2: return f.template operator()<64, 2>();
+    case 128 * 8 + 1: return f.template operator()<128, 1>();
+    case 192 * 8 + 1: return f.template operator()<192, 1>();
     case 256 * 8 + 1: return f.template operator()<256, 1>();
+    case 384 * 8 + 1: return f.template operator()<384, 1>();
     case 512 * 8 + 1: return f.template operator()<512, 1>();
+    case 768 * 8 + 1: return f.template operator()<768, 1>();
     case 1024 * 8 + 1: return f.template operator()<1024, 1>();
     case 1024 * 8 + 2: return f.template operator()<1024, 2>();
     default: return f.template operator()<1024, 4>();
@@ -303,13 +383,13 @@ hipError_t launch_zeros(float* p, int64_t count, hipStream_t s) {
 
 hipError_t launch_norm(const Norm& p, int type, hipStream_t s) {
   return of_type(type, [&]<int TYPE>() {
-    return of_form(p.width, [&]<int LANES, int CH>() { return run_norm<TYPE, LANES, CH>(p, s); });
+    return of_form(norm_form(p.width), [&]<int LANES, int CH>() { return run_norm<TYPE, LANES, CH>(p, s); });
   });
 }
 
 hipError_t launch_norm_gradient(const NormGradient& p, int type, hipStream_t s) {
   return of_type(type, [&]<int TYPE>() {
-    return of_form(p.width, [&]<int LANES, int CH>() { return run_gradient<TYPE, LANES, CH>(p, s); });
+    return of_form(norm_form(p.width), [&]<int LANES, int CH>() { return run_gradient<TYPE, LANES, CH>(p, s); });
   });
 }
 
