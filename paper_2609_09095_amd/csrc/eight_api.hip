@@ -180,7 +180,7 @@ ozaki25_status ozaki25_scaled_matmul(int64_t rows, int64_t n, int64_t k, const u
     if (st != OZAKI25_SUCCESS) return st;
   }
   const oz::eight::Scaled p{A, lda, a_scales,  ldas,   B,      ldb,   b_scales,
-                            ldbs, Y, ldy, (float*)room.p, (int)rows, (int)n, (int)k, false};
+                            ldbs, Y, ldy, (float*)room.p, (int)rows, (int)n, (int)k, 1, false};
   return room.give(status_of(oz::eight::launch_scaled(p, squares != 0, (int)out_type, (hipStream_t)stream)));
 }
 

@@ -66,9 +66,10 @@ struct Scaled {
   int64_t ldbs;
   void* y;  // rows x n
   int64_t ldy;
-  float* parts;  // workspace: scaled_parts x rows x n
+  float* parts;  // workspace: split x rows x n padded to 4
   int rows, n, k;
-  bool stream;  // y past the caches (set by the launch)
+  int split;    // parts of the depth (set by the launch, like the next)
+  bool stream;  // y past the caches
 };
 
 // A stack of experts' weights: of the layer's type, or e4m3 with the scales of

@@ -47,20 +47,50 @@ constexpr int64_t kNormGradientThreads = NGT;  // the gradient; its blocks leave
 
 constexpr int64_t norm_parts(int64_t rows, int64_t width) { return norm_blocks(rows, width, kNormGradientThreads); }
 
-// An 8-bit product's form: few rows, or tiles of 64 x 64, 128 x 128, 256 x 256.
-enum ScaledForm { kScaledFew16, kScaledFew32, kScaledFew64, kScaledSmall, kScaledMiddle, kScaledLarge };
+constexpr int64_t pad4(int64_t n) { return (n + 3) / 4 * 4; }
 
-constexpr ScaledForm scaled_form(int64_t rows, int64_t n, int64_t) {
-  if (rows <= 16) return kScaledFew16;
-  if (rows <= 32) return kScaledFew32;
-  if (rows <= 64) return kScaledFew64;
-  const int64_t middle = ceil_div(rows, 128) * ceil_div(n, 128), large = ceil_div(rows, 256) * ceil_div(n, 256);
-  if (middle < 205) return kScaledSmall;
-  return large >= 205 ? kScaledLarge : kScaledMiddle;
+// An 8-bit product's form: few rows, or tiles of 64 x 64, 128 x 128, 256 x 256; and the
+// parts of the depth that its tiles are split into.  Times in us, bfloat16 outputs,
+// squares.
+enum ScaledForm { kScaledFew16, kScaledFew32, kScaledFew64, kScaledSmall, kScaledMiddle, kScaledLarge };
+struct ScaledPlan {
+  ScaledForm form;
+  int split;
+};
+
+// A tile's stage takes its time however few tiles there are, so a long depth is split
+// where that leaves CUs without one, into parts of at least 8 blocks of 128 depths; the
+// second launch, which adds the parts, pays from 24 blocks on where most CUs are idle and
+// from 48 on else.  Whole / split: 512, 512, 8192 27 / 17; 285, 128, 7355 24 / 12; 65,
+// 4096, 4096 15.5 / 13.6; 1024, 1024, 16384 67 / 38; but 300, 4096, 4096 22.4 / 23.1, 512,
+// 4096, 4096 23.6 / 26.5.
+constexpr int scaled_parts(int64_t tiles, int64_t blocks) {
+  if (blocks < 24) return 1;
+  int64_t p = (blocks < 48 ? 256 : 768) / tiles;
+  p = p < blocks / 8 ? p : blocks / 8;
+  return (int)(p < 1 ? 1 : p > 8 ? 8 : p);
+}
+
+// Up to 16 rows, or 64 with a depth of up to 4096: the few-row form, which reads B once
+// and the rows once per 16 columns.  Few-row form / tiles: 17, 4096, 4096 9.2 / 11.8; 33,
+// 4096, 4096 10.7 / 11.8; 32, 8192, 8192 28 / 20; 64, 8192, 8192 43 / 23; 64, 1024, 8192
+// 22 / 12.  Tiles of 256 x 256 for 205 of them and more (80 of 100 CUs), as for 16-bit
+// operands; FP32 outputs and scales per vector take 128 x 128 (registers).
+constexpr ScaledPlan scaled_plan(int64_t rows, int64_t n, int64_t k) {
+  if (rows <= 16) return {kScaledFew16, 1};
+  if (rows <= 64 && k <= 4096) return {rows <= 32 ? kScaledFew32 : kScaledFew64, 1};
+  const int64_t small = ceil_div(rows, 64) * ceil_div(n, 64), middle = ceil_div(rows, 128) * ceil_div(n, 128),
+                large = ceil_div(rows, 256) * ceil_div(n, 256), blocks = ceil_div(k, 128);
+  if (middle >= 205) return {large >= 205 ? kScaledLarge : kScaledMiddle, 1};
+  if (middle >= 64 && blocks >= 64) return {kScaledMiddle, scaled_parts(middle, blocks)};
+  return {kScaledSmall, scaled_parts(small, blocks)};
 }
 
 // Bytes that the parts of a split depth take.
-constexpr size_t scaled_room(int64_t, int64_t, int64_t) { return 0; }
+constexpr size_t scaled_room(int64_t rows, int64_t n, int64_t k) {
+  const int split = scaled_plan(rows, n, k).split;
+  return split > 1 ? (size_t)split * rows * pad4(n) * 4 : 0;
+}
 
 // A layer of experts for few tokens.  Times in us, of the kernel alone: tokens, top,
 // experts, width, inner; "e" weights in e4m3.
@@ -90,7 +120,6 @@ constexpr HiddenForm hidden_form(int64_t choices, int64_t experts, int64_t inner
   return wide < (eight ? 512 : 1536) ? kHiddenSmall : kHiddenWide;
 }
 
-constexpr int64_t pad4(int64_t n) { return (n + 3) / 4 * 4; }
 constexpr size_t layer_hidden_bytes(int64_t tokens, int64_t top, int64_t inner) {
   return (size_t)(tokens * top * pad4(inner)) * 4;
 }

@@ -464,35 +464,30 @@ __device__ __forceinline__ void product8(const Bytes& oa, const Bytes& ob, const
   __syncthreads();
 }
 
-// The tile to a row-major matrix of type T::OUT, rounded once.
+// The tile's sums to a row-major FP32 matrix.
 template <class T>
-__device__ __forceinline__ void store8(const v16f (&acc)[T::MB][T::NB], char* lds, void* out, int64_t ld, int rows, int cols,
-                                       bool stream) {
-  if constexpr (T::OUT != kF32) {
-    half::store_wide<T>(acc, lds, out, ld, rows, cols, stream, [](int, int, float*) {});
-  } else {
-    const int lane = threadIdx.x & 63;
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int row = wave / T::WC * T::MB * 32 + (lane & 31), col = wave % T::WC * T::NB * 32 + 4 * (lane >> 5);
+__device__ __forceinline__ void store_sums(const v16f (&acc)[T::MB][T::NB], float* out, int64_t ld, int rows, int cols) {
+  const int lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int row = wave / T::WC * T::MB * 32 + (lane & 31), col = wave % T::WC * T::NB * 32 + 4 * (lane >> 5);
 #pragma unroll
-    for (int a = 0; a < T::MB; ++a) {
-      float* const p = (float*)out + (int64_t)(row + a * 32) * ld + col;
-      if (row + a * 32 >= rows) continue;
+  for (int a = 0; a < T::MB; ++a) {
+    float* const p = out + (int64_t)(row + a * 32) * ld + col;
+    if (row + a * 32 >= rows) continue;
 #pragma unroll
-      for (int b = 0; b < T::NB; ++b)
+    for (int b = 0; b < T::NB; ++b)
 #pragma unroll
-        for (int q = 0; q < 4; ++q) {
-          const int c = col + b * 32 + 8 * q;
-          const v4f v = {acc[a][b][4 * q], acc[a][b][4 * q + 1], acc[a][b][4 * q + 2], acc[a][b][4 * q + 3]};
-          if (c + 4 <= cols) {
-            __builtin_memcpy(p + b * 32 + 8 * q, &v, 16);
-          } else {
+      for (int q = 0; q < 4; ++q) {
+        const int c = col + b * 32 + 8 * q;
+        const v4f v = {acc[a][b][4 * q], acc[a][b][4 * q + 1], acc[a][b][4 * q + 2], acc[a][b][4 * q + 3]};
+        if (c + 4 <= cols) {
+          __builtin_memcpy(p + b * 32 + 8 * q, &v, 16);
+        } else {
 #pragma unroll
-            for (int e = 0; e < 3; ++e)
-              if (c + e < cols) p[b * 32 + 8 * q + e] = v[e];
-          }
+          for (int e = 0; e < 3; ++e)
+            if (c + e < cols) p[b * 32 + 8 * q + e] = v[e];
         }
-    }
+      }
   }
 }
 

@@ -12,22 +12,69 @@ namespace oz {
 namespace eight {
 namespace {
 
-template <class T>
-__global__ __launch_bounds__(T::THREADS, 1) void scaled_kernel(Scaled g) {
+// A tile, or (SPLIT) one of g.split parts of its depth, which leaves FP32 sums.
+template <class T, bool SPLIT>
+__global__ __launch_bounds__(T::THREADS, 2) void scaled_kernel(Scaled g) {
   __shared__ __attribute__((aligned(1024))) char lds[T::LDS];
   const uint32_t tiles_n = ((uint32_t)g.n + T::BN - 1) / T::BN, tiles_m = ((uint32_t)g.rows + T::BM - 1) / T::BM;
+  const uint32_t tiles = tiles_m * tiles_n;
   uint32_t place, tm, tn;
-  if (!half::block_place(blockIdx.x, tiles_m * tiles_n, place)) return;
+  if (!half::block_place(blockIdx.x, SPLIT ? tiles * g.split : tiles, place)) return;
+  uint32_t part = 0;
+  int64_t b0 = 0;  // blocks of depths before the part
+  int depth = g.k;
+  if constexpr (SPLIT) {
+    part = place / tiles;
+    place -= part * tiles;
+    const int64_t blocks = (g.k + kBlock - 1) / kBlock;
+    b0 = blocks * part / g.split;
+    const int64_t b1 = blocks * (part + 1) / g.split;
+    depth = (int)((b1 * kBlock < g.k ? b1 * kBlock : g.k) - b0 * kBlock);
+  }
   half::place_to_tile(place, tiles_m, tiles_n, tm, tn);
   const int r0 = (int)tm * T::BM, c0 = (int)tn * T::BN;
   const int rows = g.rows - r0 < T::BM ? g.rows - r0 : T::BM, cols = g.n - c0 < T::BN ? g.n - c0 : T::BN;
-  const Bytes a{(const char*)g.a + r0 * g.lda, g.lda, rows}, b{(const char*)g.b + c0 * g.ldb, g.ldb, cols};
-  const Scales sa{g.as + r0, g.ldas};
-  const Scales sb{T::SQUARES ? g.bs + c0 / kBlock * g.ldbs : g.bs + c0, g.ldbs};
+  const Bytes a{(const char*)g.a + r0 * g.lda + b0 * kBlock, g.lda, rows};
+  const Bytes b{(const char*)g.b + c0 * g.ldb + b0 * kBlock, g.ldb, cols};
+  const Scales sa{g.as + b0 * g.ldas + r0, g.ldas};
+  const Scales sb{T::SQUARES ? g.bs + c0 / kBlock * g.ldbs + b0 : g.bs + b0 * g.ldbs + c0, g.ldbs};
   v16f acc[T::MB][T::NB] = {};
-  product8<T>(a, b, sa, sb, cols, g.k, lds, acc);
-  constexpr int E = sizeof(typename Out<T::OUT>::type);
-  store8<T>(acc, lds, (char*)g.y + (r0 * g.ldy + c0) * E, g.ldy, rows, cols, g.stream);
+  product8<T>(a, b, sa, sb, cols, depth, lds, acc);
+  if constexpr (SPLIT) {
+    const int64_t ld = pad4(g.n);
+    store_sums<T>(acc, g.parts + ((int64_t)part * g.rows + r0) * ld + c0, ld, rows, cols);
+  } else if constexpr (T::OUT == kF32) {
+    store_sums<T>(acc, (float*)g.y + r0 * g.ldy + c0, g.ldy, rows, cols);
+  } else {
+    half::store_wide<T>(acc, lds, (uint16_t*)g.y + r0 * g.ldy + c0, g.ldy, rows, cols, g.stream, [](int, int, float*) {});
+  }
+}
+
+// The parts' sums in their order.
+template <int OUT>
+__global__ __launch_bounds__(256) void scaled_join_kernel(Scaled g) {
+  using O = typename Out<OUT>::type;
+  const int64_t ld = pad4(g.n), groups = ld / 4, i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  const int64_t r = i / groups, c = i % groups * 4;
+  if (r >= g.rows) return;
+  const float* p = g.parts + r * ld + c;
+  v4f v = *(const v4f*)p;
+#pragma unroll 8
+  for (int q = 1; q < g.split; ++q) v += *(const v4f*)(p + q * g.rows * ld);
+  O* const y = (O*)g.y + r * g.ldy + c;
+  const int left = (int)(g.n - c);
+  if (left >= 4) {
+    if constexpr (OUT == kF32) {
+      __builtin_memcpy(y, &v, 16);
+    } else {
+      const uint2 w = half::pack4<OUT>(v[0], v[1], v[2], v[3]);
+      __builtin_memcpy(y, &w, 8);  // any alignment
+    }
+  } else {
+#pragma unroll
+    for (int e = 0; e < 3; ++e)
+      if (e < left) y[e] = (O)v[e];
+  }
 }
 
 // Few rows: a block reads 16 NB columns of B once, straight into fragments, for at
@@ -152,9 +199,16 @@ __global__ __launch_bounds__(256) void scaled_zero_kernel(Scaled g) {
 
 template <class T>
 hipError_t run_tiles(const Scaled& g, hipStream_t s) {
-  const int64_t tiles = ceil_div(g.rows, T::BM) * ceil_div(g.n, T::BN);
+  const int64_t tiles = ceil_div(g.rows, T::BM) * ceil_div(g.n, T::BN) * g.split;
   if ((tiles + 8) * T::THREADS >= ((int64_t)1 << 32)) return hipErrorInvalidConfiguration;
-  scaled_kernel<T><<<dim3((uint32_t)((tiles + 7) & ~(int64_t)7)), dim3(T::THREADS), 0, s>>>(g);
+  const dim3 grid((uint32_t)((tiles + 7) & ~(int64_t)7)), block(T::THREADS);
+  if (g.split == 1) {
+    scaled_kernel<T, false><<<grid, block, 0, s>>>(g);
+    return hipGetLastError();
+  }
+  scaled_kernel<T, true><<<grid, block, 0, s>>>(g);
+  if (const hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+  scaled_join_kernel<T::OUT><<<dim3((uint32_t)ceil_div(g.rows * (pad4(g.n) / 4), 256)), dim3(256), 0, s>>>(g);
   return hipGetLastError();
 }
 
@@ -173,7 +227,8 @@ hipError_t of_type(const Scaled& g, hipStream_t s) {
     scaled_zero_kernel<OUT><<<dim3(2048), dim3(256), 0, s>>>(g);
     return hipGetLastError();
   }
-  switch (scaled_form(g.rows, g.n, g.k)) {
+  const ScaledForm form = scaled_plan(g.rows, g.n, g.k).form;
+  switch (form) {
     case kScaledFew16: return run_few<OUT, SQUARES, 1, 1, 8, 4>(g, s);
     case kScaledFew32: return run_few<OUT, SQUARES, 1, 2, 8, 4>(g, s);
     case kScaledFew64: return run_few<OUT, SQUARES, 1, 4, 8, 2>(g, s);
@@ -182,17 +237,13 @@ hipError_t of_type(const Scaled& g, hipStream_t s) {
   const bool dma = (uintptr_t)g.a % 16 == 0 && (uintptr_t)g.b % 16 == 0 && g.lda % 16 == 0 && g.ldb % 16 == 0 &&
                    g.lda < (1 << 22) && g.ldb < (1 << 22);
   if (!dma) {
-    if (scaled_form(g.rows, g.n, g.k) == kScaledSmall)
-      return run_tiles<Tile8<2, 2, 1, 1, false, OUT, SQUARES>>(g, s);
+    if (form == kScaledSmall) return run_tiles<Tile8<2, 2, 1, 1, false, OUT, SQUARES>>(g, s);
     return run_tiles<Tile8<2, 4, 2, 1, false, OUT, SQUARES>>(g, s);
   }
-  switch (scaled_form(g.rows, g.n, g.k)) {
-    case kScaledSmall: return run_tiles<Tile8<2, 2, 1, 1, true, OUT, SQUARES, 3>>(g, s);
-    case kScaledMiddle: return run_tiles<Tile8<2, 2, 2, 2, true, OUT, SQUARES>>(g, s);
-    default:
-      if constexpr (OUT == kF32 || !SQUARES) return run_tiles<Tile8<2, 2, 2, 2, true, OUT, SQUARES>>(g, s);
-      return run_tiles<Tile8<2, 4, 4, 2, true, OUT, SQUARES>>(g, s);
-  }
+  if (form == kScaledSmall) return run_tiles<Tile8<2, 2, 1, 1, true, OUT, SQUARES, 3>>(g, s);
+  if constexpr (OUT != kF32 && SQUARES)
+    if (form == kScaledLarge) return run_tiles<Tile8<2, 4, 4, 2, true, OUT, SQUARES>>(g, s);
+  return run_tiles<Tile8<2, 2, 2, 2, true, OUT, SQUARES>>(g, s);
 }
 
 template <int OUT>
@@ -206,6 +257,7 @@ hipError_t launch_scaled(Scaled g, bool squares, int out, hipStream_t s) {
   // a single row starts where its matrix does, whatever the pitch says
   if (g.rows == 1) g.lda = (g.k + 15) / 16 * 16;
   if (g.n == 1) g.ldb = (g.k + 15) / 16 * 16;
+  g.split = scaled_plan(g.rows, g.n, g.k).split;
   g.stream = (int64_t)g.rows * g.n * (out == kF32 ? 4 : 2) > ((int64_t)32 << 20);
   if (out == kBF16) return of_scales<kBF16>(g, squares, s);
   if (out == kF16) return of_scales<kF16>(g, squares, s);
