@@ -73,7 +73,7 @@ constexpr int scaled_parts(int64_t tiles, int64_t blocks) {
 
 // Up to 16 rows, or 64 with a depth of up to 4096: the few-row form, which reads B once
 // and the rows once per 16 columns.  Few-row form / tiles: 17, 4096, 4096 9.2 / 11.8; 33,
-// 4096, 4096 10.7 / 11.8; 32, 8192, 8192 28 / 20; 64, 8192, 8192 43 / 23; 64, 1024, 8192
+// 4096, 4096 10.7 / 11.8; 32, 8192, 8192 28 / 19; 64, 8192, 8192 43 / 21; 64, 1024, 8192
 // 22 / 12.  Tiles of 256 x 256 for 205 of them and more (80 of 100 CUs), as for 16-bit
 // operands; FP32 outputs and scales per vector take 128 x 128 (registers).
 constexpr ScaledPlan scaled_plan(int64_t rows, int64_t n, int64_t k) {
@@ -82,7 +82,7 @@ constexpr ScaledPlan scaled_plan(int64_t rows, int64_t n, int64_t k) {
   const int64_t small = ceil_div(rows, 64) * ceil_div(n, 64), middle = ceil_div(rows, 128) * ceil_div(n, 128),
                 large = ceil_div(rows, 256) * ceil_div(n, 256), blocks = ceil_div(k, 128);
   if (middle >= 205) return {large >= 205 ? kScaledLarge : kScaledMiddle, 1};
-  if (middle >= 64 && blocks >= 64) return {kScaledMiddle, scaled_parts(middle, blocks)};
+  if (middle >= 64 && rows > 64 && blocks >= 64) return {kScaledMiddle, scaled_parts(middle, blocks)};
   return {kScaledSmall, scaled_parts(small, blocks)};
 }
 

@@ -100,6 +100,20 @@ def test_layer(tokens, top, experts, width, inner, out, dtype, eight, gated):
     run(tokens, top, experts, width, inner, out, dtype, eight, gated, seed=tokens + width, layout=(0, 3, 16)[(width + tokens) % 3])
 
 
+@pytest.mark.parametrize("gated", [True, False])
+@pytest.mark.parametrize("eight", [False, True])
+@pytest.mark.parametrize("tokens,experts,inner", [(20, 20, 500), (64, 64, 900), (130, 20, 500), (200, 16, 520)])
+def test_forms(tokens, experts, inner, eight, gated):
+    """Enough blocks for the narrower, the wider and the many-row form of the hidden
+    values."""
+    run(tokens, 2, experts, 70, inner, 40, "bf16" if inner == 500 else "f16", eight, gated, seed=inner, layout=(0, 16)[eight])
+
+
+def test_wide_outputs_of_few_choices():
+    for eight in (False, True):
+        run(2, 3, 5, 130, 70, 4100, "bf16", eight, True)
+
+
 @pytest.mark.parametrize("eight", [False, True])
 def test_larger(eight):
     run(1, 2, 4, 2048, 1024, 2048, "bf16", eight, True)

@@ -49,12 +49,21 @@ def operands(rows, n, k, squares, seed, layout="padded", spread=2.0):
 
 
 def check(rows, n, k, squares, dtype, seed=0, layout="padded", **kw):
+    import torch
     import eight_util as u
     (A, a, VA), (B, b, VB) = operands(rows, n, k, squares, seed, layout)
     Y = oz.ozaki25_scaled_matmul(A, a, B, b, squares=squares, out_dtype=u.TYPES[dtype], **kw)
     want, size = VA @ VB.t(), VA.abs() @ VB.t().abs()
     tiny = 2.0 ** -25 if dtype == "f16" else 0.0
-    off = (Y.double() - want).abs() - want.abs() * u.half_step(Y.dtype) - size * ((128 + 12 + -(-k // 128)) * u.U if dtype == "f32" else 2.0 ** -10) - tiny
+    allowed = size * ((128 + 12 + -(-k // 128)) * u.U if dtype == "f32" else 2.0 ** -10)
+    off = (Y.double() - want).abs() - want.abs() * u.half_step(Y.dtype) - allowed - tiny
+    if dtype == "f16":
+        # half rounds from 65520 on (65504 and half a step, 16) to an infinity of the sign:
+        # it has to where all of the sum's range lies beyond, and may where some does
+        most = 65520.0
+        beyond = torch.isinf(Y) & (torch.sign(Y.double()) == torch.sign(want)) & (want.abs() + allowed >= most)
+        assert bool(beyond[want.abs() - allowed >= most].all())
+        off = torch.where(beyond, 0.0, off)
     assert Y.shape == (rows, n) and bool((off <= 0).all()), (float(off.max()), int((off > 0).sum()))
     return Y
 
@@ -80,6 +89,19 @@ def test_many_tiles(rows, n, k, squares):
     for dtype in ("bf16", "f32"):
         check(rows, n, k, squares, dtype, 3, "padded")
     check(rows, n, k, squares, "f16", 4, "odd")
+
+
+@pytest.mark.parametrize("squares", [True, False])
+@pytest.mark.parametrize("rows,n,k", [(100, 70, 3075), (65, 130, 3200), (285, 128, 7355), (1100, 1030, 8200), (40, 33, 6145)])
+def test_depths_in_parts(rows, n, k, squares):
+    """Few tiles of a long depth: its parts' sums, in a workspace given or not."""
+    import torch
+    room = oz.ozaki25_scaled_matmul_workspace_size(rows, n, k)
+    assert room > 0
+    for dtype, layout in (("bf16", "padded"), ("f32", "tight"), ("f16", "odd")):
+        Y = check(rows, n, k, squares, dtype, k, layout)
+        again = check(rows, n, k, squares, dtype, k, layout, workspace=torch.full((room,), 0xff, dtype=torch.uint8, device="cuda"))
+        assert torch.equal(Y, again)
 
 
 def test_large_tiles_of_every_depth():
