@@ -295,20 +295,27 @@ __global__ __launch_bounds__(norm_threads(LANES)) void norm_gradient_kernel(Norm
   }
 }
 
-// 16 columns a block, the parts over 16 sets of lanes
-__global__ __launch_bounds__(256) void dw_kernel(const float* parts, int count, int width, float* dw) {
-  __shared__ float room[16][17];
-  const int c = blockIdx.x * 16 + (threadIdx.x & 15), set = threadIdx.x >> 4;
+// 16 columns a block, the parts over 64 sets of lanes: a few loads one after the other.
+__global__ __launch_bounds__(1024) void dw_kernel(const float* parts, int count, int width, float* dw) {
+  __shared__ float room[64][17];
+  const int c = blockIdx.x * 16 + (threadIdx.x & 15), at = threadIdx.x & 15, set = threadIdx.x >> 4;
   float t = 0.0f;
   if (c < width) {
 #pragma unroll 8
-    for (int i = set; i < count; i += 16) t += parts[(int64_t)i * width + c];
+    for (int i = set; i < count; i += 64) t += parts[(int64_t)i * width + c];
   }
-  room[set][threadIdx.x & 15] = t;
+  room[set][at] = t;
+  __syncthreads();
+  if (set < 8) {
+#pragma unroll
+    for (int i = 1; i < 8; ++i) t += room[set + 8 * i][at];
+  }
+  __syncthreads();
+  if (set < 8) room[set][at] = t;
   __syncthreads();
   if (set == 0 && c < width) {
 #pragma unroll
-    for (int i = 1; i < 16; ++i) t += room[i][threadIdx.x];
+    for (int i = 1; i < 8; ++i) t += room[i][at];
     dw[c] = t;
   }
 }
@@ -344,7 +351,7 @@ hipError_t run_gradient(const NormGradient& p, hipStream_t s) {
   else
     norm_gradient_kernel<TYPE, LANES, CH, false><<<grid, block, 0, s>>>(p);
   if (const hipError_t e = hipGetLastError(); e != hipSuccess) return e;
-  dw_kernel<<<dim3((uint32_t)ceil_div(p.width, 16)), dim3(256), 0, s>>>(p.parts, (int)parts, p.width, p.dw);
+  dw_kernel<<<dim3((uint32_t)ceil_div(p.width, 16)), dim3(1024), 0, s>>>(p.parts, (int)parts, p.width, p.dw);
   return hipGetLastError();
 }
 
