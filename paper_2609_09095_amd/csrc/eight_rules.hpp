@@ -86,6 +86,11 @@ constexpr ScaledPlan scaled_plan(int64_t rows, int64_t n, int64_t k) {
   return {kScaledSmall, scaled_parts(small, blocks)};
 }
 
+// Of rows that do not start on 16 bytes the few-row form's pieces straddle cache lines,
+// and more than 16 rows go to tiles.  Few-row form / tiles: 64, 4096, 4095 39 / 28; 16,
+// 4096, 4095 18 / 23.
+constexpr bool few_as_tiles(int64_t rows) { return rows > 16; }
+
 // Bytes that the parts of a split depth take.
 constexpr size_t scaled_room(int64_t rows, int64_t n, int64_t k) {
   const int split = scaled_plan(rows, n, k).split;

@@ -134,21 +134,35 @@ struct ByteDma {
   static constexpr int IN_FLIGHT = T::ADMA + T::BDMA;
 };
 
-// Any alignment and pitch, through registers.
+// Any alignment and pitch, through registers.  A vector past the edge is read as the
+// last one.
 template <int V, int N>
 struct ByteSide {
   v4i reg[N];
   const char* p;
-  int64_t ld;
+  int64_t at[N];  // of the lane's chunks in a stage
   int vecs;
-  __device__ __forceinline__ void load(int wave, int lane, int64_t at, int64_t depth) {
+  __device__ __forceinline__ void init(const Bytes& op, int wave, int lane) {
+    p = half::uniform(op.p);
+    vecs = op.vecs;
 #pragma unroll
     for (int i = 0; i < N; ++i) {
       int r, c;
       half::chunk_at<kAlong, V>((wave * N + i) * 1024 + lane * 16, r, c);
-      // a vector past the edge is read as the last one
-      const bool is = r < vecs;
-      reg[i] = load16(p + (int64_t)(is ? r : vecs - 1) * ld, at + c * 16, depth);
+      at[i] = (r < vecs ? r : vecs - 1) * op.ld + c * 16;
+    }
+  }
+  __device__ __forceinline__ void load(const char* stage) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) reg[i] = half::load_whole(stage + at[i]);
+  }
+  // the stage from depth o on, which the depth's end may cut
+  __device__ __forceinline__ void load_cut(int wave, int lane, int64_t o, int64_t depth) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      int r, c;
+      half::chunk_at<kAlong, V>((wave * N + i) * 1024 + lane * 16, r, c);
+      reg[i] = load16(p + at[i] - c * 16, o + c * 16, depth);
     }
   }
   __device__ __forceinline__ void put(int i, char* lds, int wave, int lane) const {
@@ -160,23 +174,30 @@ template <class T>
 struct ByteMasked {
   ByteSide<T::BM, T::ADMA> a;
   ByteSide<T::BN, T::BDMA> b;
-  int64_t at, depth;
-  __device__ __forceinline__ void init(const Bytes& oa, const Bytes& ob, int d, int, int) {
-    a.p = half::uniform(oa.p), a.ld = oa.ld, a.vecs = oa.vecs;
-    b.p = half::uniform(ob.p), b.ld = ob.ld, b.vecs = ob.vecs;
-    at = 0, depth = d;
+  const char *pa, *pb;
+  int stage, stages;
+  __device__ __forceinline__ void init(const Bytes& oa, const Bytes& ob, int depth, int wave, int lane) {
+    a.init(oa, wave, lane);
+    b.init(ob, wave, lane);
+    pa = a.p, pb = b.p;
+    stages = (depth + kStage - 1) / kStage;
+    stage = 1;
   }
-  __device__ __forceinline__ void first(char* buf, int d, int wave, int lane) {
-    at = (int64_t)((d - 1) / kStage) * kStage;
-    early(wave, lane);
+  __device__ __forceinline__ void first(char* buf, int depth, int wave, int lane) {
+    const int64_t o = (int64_t)(stages - 1) * kStage;
+    a.load_cut(wave, lane, o, depth);
+    b.load_cut(wave, lane, o, depth);
 #pragma unroll
     for (int j = 0; j < T::ADMA + T::BDMA; ++j) late(j, buf, wave, lane);
-    at = 0;
   }
-  __device__ __forceinline__ void early(int wave, int lane) {
-    a.load(wave, lane, at, depth);
-    b.load(wave, lane, at, depth);
-    at += kStage;
+  __device__ __forceinline__ void early(int, int) {
+    // later stages are whole; past the last the registers' old bytes are put and not used
+    if (stage < stages) {
+      a.load(pa);
+      b.load(pb);
+    }
+    ++stage;
+    pa += kStage, pb += kStage;
   }
   __device__ __forceinline__ void begin() {}
   __device__ __forceinline__ void late(int j, char* buf, int wave, int lane) {

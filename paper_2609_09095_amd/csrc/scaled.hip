@@ -227,15 +227,16 @@ hipError_t of_type(const Scaled& g, hipStream_t s) {
     scaled_zero_kernel<OUT><<<dim3(2048), dim3(256), 0, s>>>(g);
     return hipGetLastError();
   }
-  const ScaledForm form = scaled_plan(g.rows, g.n, g.k).form;
+  ScaledForm form = scaled_plan(g.rows, g.n, g.k).form;
+  const bool dma = (uintptr_t)g.a % 16 == 0 && (uintptr_t)g.b % 16 == 0 && g.lda % 16 == 0 && g.ldb % 16 == 0 &&
+                   g.lda < (1 << 22) && g.ldb < (1 << 22);
+  if (!dma && few_as_tiles(g.rows)) form = form < kScaledSmall ? kScaledSmall : form;
   switch (form) {
     case kScaledFew16: return run_few<OUT, SQUARES, 1, 1, 8, 4>(g, s);
     case kScaledFew32: return run_few<OUT, SQUARES, 1, 2, 8, 4>(g, s);
     case kScaledFew64: return run_few<OUT, SQUARES, 1, 4, 8, 2>(g, s);
     default: break;
   }
-  const bool dma = (uintptr_t)g.a % 16 == 0 && (uintptr_t)g.b % 16 == 0 && g.lda % 16 == 0 && g.ldb % 16 == 0 &&
-                   g.lda < (1 << 22) && g.ldb < (1 << 22);
   if (!dma) {
     if (form == kScaledSmall) return run_tiles<Tile8<2, 2, 1, 1, false, OUT, SQUARES>>(g, s);
     return run_tiles<Tile8<2, 4, 2, 1, false, OUT, SQUARES>>(g, s);

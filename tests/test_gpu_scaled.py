@@ -198,6 +198,21 @@ def test_a_projection_and_its_gradients():
         assert float((got.double() - want).norm() / want.norm()) < 2 * 2.0 ** -4
 
 
+@pytest.mark.parametrize("rows", [3, 20, 80])
+def test_pitches_beyond_the_tiles_offsets(rows):
+    """Rows 2^22 bytes and more apart."""
+    import torch
+    import eight_util as u
+    (A, a, VA), (B, b, VB) = operands(rows, 90, 300, True, rows)
+    for pitch in (1 << 22, (1 << 22) + 3):
+        wide = torch.empty(((rows - 1) * pitch + 300,), dtype=torch.uint8, device="cuda")
+        far = wide.as_strided((rows, 300), (pitch, 1))
+        far.copy_(A.view(torch.uint8))
+        Y = oz.ozaki25_scaled_matmul(far.view(u.E4M3), a, B, b)
+        want, size = VA @ VB.t(), VA.abs() @ VB.t().abs()
+        assert bool(((Y.double() - want).abs() <= want.abs() * 2.0 ** -8 + size * 2.0 ** -10).all())
+
+
 def test_large_offsets():
     """Rows of A and Y beyond 2^32 bytes."""
     import torch
