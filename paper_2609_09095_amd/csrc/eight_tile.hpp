@@ -55,6 +55,10 @@ struct Tile8 {
   static constexpr int STAGE = A_BYTES + B_BYTES, SET = BUFS * STAGE;
   static constexpr int SLOT = (BM + BN) * 4, LDS = SET + 3 * SLOT;  // scales: three stages'
   static constexpr int ADMA = A_BYTES / 1024 / WAVES, BDMA = B_BYTES / 1024 / WAVES;
+  // Loads issued right behind the barrier that frees their buffer; the others follow
+  // beside the next stage's first products (all at once they keep the wavefront from
+  // issuing products: 8192 x 8192 x 8192 484 / 470 us).
+  static constexpr int SOON = DMA && BUFS == 2 && MB == 4 ? (ADMA + BDMA) / 2 : ADMA + BDMA;
   using Loads = std::conditional_t<DMA, ByteDma<Tile8>, ByteMasked<Tile8>>;
   static_assert(ADMA * WAVES * 1024 == A_BYTES && BDMA * WAVES * 1024 == B_BYTES, "whole slabs per wavefront");
   static_assert(BM + BN <= THREADS, "a thread carries one scale");
@@ -343,15 +347,16 @@ __device__ __forceinline__ void add_scaled(v16f& acc, const v16f& t, float fs, c
 // One stage's products, a block at a time: a block's two products are issued, then the
 // block before it, whose products have ended by then, is added up.  On entry the
 // fragments of the first row of blocks are in af[0], of all columns in bf.  cur, next:
-// this stage's and the next one's buffer; freed: cur, as the target of the loads (the
-// three are declared not to alias, or the compiler would wait for all loads in flight
-// before every read of LDS: what keeps them apart is the barrier).  here, there: this
+// this stage's and the next one's buffer; freed: cur, as the target of the loads;
+// freed_before: next, as that of the loads which the stage before left (they are declared
+// not to alias, or the compiler would wait for all loads in flight before every read of
+// LDS: what keeps them apart is the barrier).  here, there: this
 // stage's and the next one's scales.
 template <class T, class Loader>
 __device__ __forceinline__ void stage_products8(Loader& ld, ScaleLoads<T>& sl, const ByteFragments<T::MB>& fa,
                                                 const ByteFragments<T::NB>& fb, half::lds_bytes __restrict__ cur,
                                                 half::lds_bytes __restrict__ next, char* __restrict__ freed,
-                                                const float* here, float* there, int wave, int lane, v8i (&af)[2][2],
+                                                char* __restrict__ freed_before, const float* here, float* there, int wave, int lane, v8i (&af)[2][2],
                                                 v8i (&bf)[T::NB][2], v16f (&acc)[T::MB][T::NB]) {
   constexpr int ND = T::ADMA + T::BDMA, MB = T::MB, NB = T::NB, M = MB * NB;
   ld.early(wave, lane);
@@ -392,7 +397,12 @@ __device__ __forceinline__ void stage_products8(Loader& ld, ScaleLoads<T>& sl, c
 #pragma unroll
         for (int h = 0; h < 2; ++h) bf[y][h] = fb.read(next + T::A_BYTES, h, y);
 #pragma unroll
-        for (int j = y * ND / NB; j < (y + 1) * ND / NB; ++j) ld.late(j, freed, wave, lane);
+        for (int j = y * T::SOON / NB; j < (y + 1) * T::SOON / NB; ++j) ld.late(j, freed, wave, lane);
+      }
+      if (x == 0) {
+#pragma unroll
+        for (int j = T::SOON + y * (ND - T::SOON) / NB; j < T::SOON + (y + 1) * (ND - T::SOON) / NB; ++j)
+          ld.late(j, freed_before, wave, lane);
       }
       __builtin_amdgcn_sched_barrier(0);
       if (i > 0) {
@@ -438,9 +448,9 @@ __device__ __forceinline__ void product8(const Bytes& oa, const Bytes& ob, const
     ld.early(wave, lane);
     ld.begin();
 #pragma unroll
-    for (int j = 0; j < ND; ++j) ld.late(j, lds + s * T::STAGE, wave, lane);
+    for (int j = 0; j < (s + 1 == T::BUFS ? T::SOON : ND); ++j) ld.late(j, lds + s * T::STAGE, wave, lane);
   }
-  half::wait_loads_and_lds<(T::BUFS - 1) * T::Loads::IN_FLIGHT>();
+  half::wait_loads_and_lds<(T::DMA ? (T::BUFS - 2) * ND + T::SOON : 0)>();
   half::block_barrier();
   if (T::DMA && depth % 16) {
     clean_tail<T>(lds, depth % kStage);
@@ -451,13 +461,15 @@ __device__ __forceinline__ void product8(const Bytes& oa, const Bytes& ob, const
     for (int s = 0; s < nst; ++s) {
       slot = slot == 2 * SLOT ? 0 : slot + SLOT;
       ld.early(wave, lane);
+#pragma unroll
+      for (int j = T::SOON; j < ND; ++j) ld.late(j, lds + next_stage<T>(cur), wave, lane);
       sl.put(slots + slot);
       half::wait_loads_and_lds<(T::BUFS - 2) * T::Loads::IN_FLIGHT>();
       half::block_barrier();
       sl.load();
       ld.begin();
 #pragma unroll
-      for (int j = 0; j < ND; ++j) ld.late(j, lds + cur, wave, lane);
+      for (int j = 0; j < T::SOON; ++j) ld.late(j, lds + cur, wave, lane);
       cur = next_stage<T>(cur);
     }
   } else {
@@ -475,8 +487,8 @@ __device__ __forceinline__ void product8(const Bytes& oa, const Bytes& ob, const
     }
     for (int s = 0; s < nst; ++s) {
       const int next = next_stage<T>(cur), next_slot = slot == 2 * SLOT ? 0 : slot + SLOT;
-      stage_products8<T>(ld, sl, fa, fb, l3 + cur, l3 + next, lds + cur, slots + slot, slots + next_slot, wave, lane, af, bf,
-                         acc);
+      stage_products8<T>(ld, sl, fa, fb, l3 + cur, l3 + next, lds + cur, lds + next, slots + slot, slots + next_slot,
+                         wave, lane, af, bf, acc);
       cur = next;
       slot = next_slot;
     }
