@@ -469,7 +469,8 @@ ozaki25_status ozaki25_orthogonalise(int64_t count, int64_t m, int64_t n, const 
  *    and 128 columns: scales float32 [ceil(width/128)][rows], pitch lds.
  * H may be X's or residual's own memory (the same pitch); Y and scales overlap
  * nothing.  Sums run in FP32 (values beyond 1.8e19 overflow them); with eps == 0 a
- * row of zeros gives NaN.  rows == 0 or width == 0: no-op.
+ * row of zeros, or of numbers whose squares underflow, gives NaN or infinities.
+ * rows == 0 or width == 0: no-op.
  * Errors: INVALID_VALUE, UNSUPPORTED (sizes; width beyond
  * OZAKI25_MAX_NORM_WIDTH), HIP. */
 ozaki25_status ozaki25_rms_norm(int64_t rows, int64_t width, const void* X, int64_t ldx, const void* residual,

@@ -12,7 +12,13 @@ constexpr int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
 constexpr int kMaxNormWidth = 32768;
 
-// How a norm's row is spread: `lanes` threads with `chunks` times 8 elements each.
+// How a norm's row is spread: `lanes` threads with `chunks` times 8 elements each: one
+// chunk a lane where a block has the lanes, in steps of 64 lanes up to 256 and as fine
+// as the kernels' instances go beyond.  us, steps of 64 / powers of two: gradients of
+// 4999 x 1031 halves 21.7 / 23.0, the norm of 8192 x 1031 18.6 / 20.8.  One chunk a lane
+// / two on half the lanes: gradients of 16384 x 4096 bfloat16 103 / 158 (a second read
+// of the row), of 4999 x 1031 22 / 31, the norms of 8192 x 4096 46 / 45, 8192 x 1031
+// 18.6 / 22.
 struct NormForm {
   int lanes, chunks;
 };
@@ -39,11 +45,13 @@ constexpr int64_t norm_blocks(int64_t rows, int64_t width, int64_t per_cu) {
   return need < most ? need : most;
 }
 
-constexpr int64_t kNormThreads = 2048;  // per CU: the forward pass
-#ifndef NGT
-#define NGT 1024
-#endif
-constexpr int64_t kNormGradientThreads = NGT;  // the gradient; its blocks leave a partial sum each
+// Threads per CU: fewer keep too few loads in flight, more leave a block too few rows to
+// load ahead (and in the gradient more partial sums).  us of 1024 / 1536 / 2048 / 4096:
+// norms of 8192 x 4096 46 / 44 / 46 / 44, 2000 x 16384 43.1 / 42.9 / 46 / 52, 8192 x 1031
+// 19.1 / 17.4 / 18.6 / 18.0.  Of 512 / 768 / 1024 / 2048: gradients of 16384 x 4096 97.4 /
+// 97.3 / 103 / 107, 4999 x 1031 22.8 / 20.4 / 21.7 / 25.5, 16384 x 2048 49.7 / 51 / 54 / 58.
+constexpr int64_t kNormThreads = 1536;         // the forward pass
+constexpr int64_t kNormGradientThreads = 768;  // the gradient; its blocks leave a partial sum each
 
 constexpr int64_t norm_parts(int64_t rows, int64_t width) { return norm_blocks(rows, width, kNormGradientThreads); }
 

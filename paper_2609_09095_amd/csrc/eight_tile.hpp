@@ -57,7 +57,8 @@ struct Tile8 {
   static constexpr int ADMA = A_BYTES / 1024 / WAVES, BDMA = B_BYTES / 1024 / WAVES;
   // Loads issued right behind the barrier that frees their buffer; the others follow
   // beside the next stage's first products (all at once they keep the wavefront from
-  // issuing products: 8192 x 8192 x 8192 484 / 470 us).
+  // issuing products: 8192 x 8192 x 8192 484 / 458 us; but 128 x 128 tiles 2048 x 2048
+  // x 2048 17.0 / 18.7).
   static constexpr int SOON = DMA && BUFS == 2 && MB == 4 ? (ADMA + BDMA) / 2 : ADMA + BDMA;
   using Loads = std::conditional_t<DMA, ByteDma<Tile8>, ByteMasked<Tile8>>;
   static_assert(ADMA * WAVES * 1024 == A_BYTES && BDMA * WAVES * 1024 == B_BYTES, "whole slabs per wavefront");

@@ -804,13 +804,12 @@ __device__ __forceinline__ void skinny_join(const v4f (&acc)[NB][TB], v4f* lds, 
 // 4096, 2048 279 / 277 / 272 / 280, its input gradient 298 / 304 / 320 / 298, 8192^3
 // 844 / 820 / 820 / 820.
 constexpr uint32_t kSet = 2;
-template <uint32_t SET = kSet>
 __device__ __forceinline__ void place_to_tile(uint32_t place, uint32_t tiles_m, uint32_t tiles_n, uint32_t& tm,
                                               uint32_t& tn) {
-  const uint32_t per = SET * tiles_n;
+  const uint32_t per = kSet * tiles_n;
   const uint32_t s = place / per, in = place - s * per;
-  const uint32_t first = s * SET;
-  const uint32_t size = tiles_m - first < SET ? tiles_m - first : SET;
+  const uint32_t first = s * kSet;
+  const uint32_t size = tiles_m - first < kSet ? tiles_m - first : kSet;
   tn = in / size;
   tm = first + in - tn * size;
 }

@@ -4,7 +4,8 @@
 //
 // Bound by its read and writes.  A block of threads holds a tile of 128 x 128 in
 // registers, 8 x 8 elements a thread; the transposed bytes go through LDS once,
-// 8 rows of a column in one 64-bit word.
+// 8 rows of a column in one 64-bit word.  16384 x 4096 bfloat16 to both layouts, scales
+// per vector: 58 us, 4.7 TB/s (a large copy: 5.1).
 #include "eight_bits.hpp"
 #include "eight_products.hpp"
 
