@@ -83,7 +83,7 @@ constexpr int scaled_parts(int64_t tiles, int64_t blocks) {
 // and the rows once per 16 columns.  Few-row form / tiles: 17, 4096, 4096 9.2 / 11.8; 33,
 // 4096, 4096 10.7 / 11.8; 32, 8192, 8192 28 / 19; 64, 8192, 8192 43 / 21; 64, 1024, 8192
 // 22 / 12.  Tiles of 256 x 256 for 205 of them and more (80 of 100 CUs), as for 16-bit
-// operands; FP32 outputs and scales per vector take 128 x 128 (registers).
+// operands.
 constexpr ScaledPlan scaled_plan(int64_t rows, int64_t n, int64_t k) {
   if (rows <= 16) return {kScaledFew16, 1};
   if (rows <= 64 && k <= 4096) return {rows <= 32 ? kScaledFew32 : kScaledFew64, 1};
@@ -93,6 +93,12 @@ constexpr ScaledPlan scaled_plan(int64_t rows, int64_t n, int64_t k) {
   if (middle >= 64 && rows > 64 && blocks >= 64) return {kScaledMiddle, scaled_parts(middle, blocks)};
   return {kScaledSmall, scaled_parts(small, blocks)};
 }
+
+// FP32 outputs and scales per vector leave no registers for 256 x 256; 256 x 128 where
+// there are as many of them.  128 x 128 / 256 x 128, scales per vector: 2048, 4096, 8192
+// FP32 142 / 132, bfloat16 92 / 82; 16384, 4096, 4096 566 / 543, 362 / 331; 6500, 1031, 300
+// 18.4 / 18.8, 12.3 / 12.0; with half as many tiles 2048, 2048, 2048 17.3 / 19.3.
+constexpr bool scaled_tall(int64_t rows, int64_t n) { return ceil_div(rows, 256) * ceil_div(n, 128) >= 205; }
 
 // Of rows that do not start on 16 bytes the few-row form's pieces straddle cache lines,
 // and more than 16 rows go to tiles.  Few-row form / tiles: 64, 4096, 4095 39 / 28; 16,

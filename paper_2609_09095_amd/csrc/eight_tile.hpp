@@ -58,8 +58,15 @@ struct Tile8 {
   // Loads issued right behind the barrier that frees their buffer; the others follow
   // beside the next stage's first products (all at once they keep the wavefront from
   // issuing products: 8192 x 8192 x 8192 484 / 458 us; but 128 x 128 tiles 2048 x 2048
-  // x 2048 17.0 / 18.7).
+  // x 2048 17.0 / 18.7, 256 x 128 tiles 2048 x 4096 x 8192 in FP32 139 / 148).
   static constexpr int SOON = DMA && BUFS == 2 && MB == 4 ? (ADMA + BDMA) / 2 : ADMA + BDMA;
+  // Steps of a block's products, each followed by its part of the block before's additions.
+  // With a scale per column an output takes a multiplication and a multiply-add, an FP32
+  // one's operands their widening too: about the products' time, and whole blocks of either
+  // leave the other's unit idle: 2048 x 4096 x 8192
+  // with scales per vector, 256 x 128 tiles, FP32 in 1 / 4 / 8 steps 139.5 / 136.8 / 138.9 us,
+  // bfloat16 in 1 / 2 85 / 82; but 128 x 128 tiles 2048 x 2048 x 2048 17.2 / 18.3.
+  static constexpr int STEPS = WR < 4 ? 1 : OUT == kF32 ? 4 : 2;
   using Loads = std::conditional_t<DMA, ByteDma<Tile8>, ByteMasked<Tile8>>;
   static_assert(ADMA * WAVES * 1024 == A_BYTES && BDMA * WAVES * 1024 == B_BYTES, "whole slabs per wavefront");
   static_assert(BM + BN <= THREADS, "a thread carries one scale");
@@ -272,25 +279,29 @@ struct ByteFragments {
   }
 };
 
-// c + a b, 64 depths of 32 x 32 outputs.  The 8-bit products add the eight products
-// of neighbouring depths with 13 bits below the largest of them (measured: 1.4e-5 of
-// a result's norm on normal numbers, whatever the depth), which a 16-bit output's
+// Step q of T::STEPS of the products of a 32 x 32 block over a stage's 128 depths; t is
+// their sum after the last step.  The 8-bit products add the eight products of
+// neighbouring depths with 13 bits below the largest of them (measured: 1.4e-5 of a
+// result's norm on normal numbers, whatever the depth), which a 16-bit output's
 // rounding hides.  An FP32 output takes bfloat16 products of the same numbers, exact
 // in FP32, at half the rate.
-template <int OUT>
-__device__ __forceinline__ v16f mfma64(v8i a, v8i b, v16f c) {
-  if constexpr (OUT == kF32) {
+template <class T>
+__device__ __forceinline__ void products(int q, v16f& t, const v8i (&b)[2], const v8i (&a)[2]) {
+  constexpr int EACH = (T::OUT == kF32 ? 8 : 2) / T::STEPS;
 #pragma unroll
-    for (int j = 0; j < 4; ++j)
-      c = half::mfma<kBF16>(widened<kBF16>(a[2 * j], a[2 * j + 1]), widened<kBF16>(b[2 * j], b[2 * j + 1]), c);
-    return c;
-  } else {
-    // scale operands of 0 are 2^0
-    return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(a, b, c, 0, 0, 0, 0, 0, 0);
+  for (int i = q * EACH; i < (q + 1) * EACH; ++i) {
+    const v16f c = i == 0 ? v16f{} : t;
+    if constexpr (T::OUT == kF32) {
+      const int h = i / 4, j = i % 4 * 2;
+      t = half::mfma<kBF16>(widened<kBF16>(b[h][j], b[h][j + 1]), widened<kBF16>(a[h][j], a[h][j + 1]), c);
+    } else {
+      // scale operands of 0 are 2^0
+      t = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(b[i], a[i], c, 0, 0, 0, 0, 0, 0);
+    }
   }
 }
 
-// The same, 128 depths of 16 x 16 outputs.
+// c + a b, 128 depths of 16 x 16 outputs, by the same products.
 template <int OUT>
 __device__ __forceinline__ v4f mfma128(v8i a, v8i b, v4f c) {
   if constexpr (OUT == kF32) {
@@ -330,35 +341,40 @@ __device__ __forceinline__ int next_stage(int cur) {
   return cur + T::STAGE < T::SET ? cur + T::STAGE : 0;
 }
 
-// A block's products, scaled, into its sums.  fs: the lane's row's scale (times the
-// squares'); cs: the columns' scales.
+// The scales of a lane's 16 columns of a block.
 template <class T>
-__device__ __forceinline__ void add_scaled(v16f& acc, const v16f& t, float fs, const float* cs) {
-  v4f c[4];
+__device__ __forceinline__ void column_scales(const float* cs, v4f (&c)[4]) {
   if constexpr (!T::SQUARES) {
 #pragma unroll
     for (int q = 0; q < 4; ++q) c[q] = *(const v4f*)(cs + 8 * q);
   }
-#pragma unroll
-  for (int i = 0; i < 16; ++i) acc[i] = __builtin_fmaf(t[i], T::SQUARES ? fs : fs * c[i / 4][i % 4], acc[i]);
-  // here and not later: the compiler would carry the products over the barrier
-  asm volatile("" : "+v"(acc));
 }
 
-// One stage's products, a block at a time: a block's two products are issued, then the
-// block before it, whose products have ended by then, is added up.  On entry the
-// fragments of the first row of blocks are in af[0], of all columns in bf.  cur, next:
-// this stage's and the next one's buffer; freed: cur, as the target of the loads;
-// freed_before: next, as that of the loads which the stage before left (they are declared
-// not to alias, or the compiler would wait for all loads in flight before every read of
-// LDS: what keeps them apart is the barrier).  here, there: this
-// stage's and the next one's scales.
+// Outputs e0 .. e0 + N - 1 of a lane's 16: a block's products, scaled, into its sums.
+// fs: the lane's row's scale (times the squares').
+template <class T, int N>
+__device__ __forceinline__ void add_scaled(v16f& acc, const v16f& t, float fs, const v4f (&c)[4], int e0) {
+#pragma unroll
+  for (int e = e0; e < e0 + N; ++e) acc[e] = __builtin_fmaf(t[e], T::SQUARES ? fs : fs * c[e / 4][e % 4], acc[e]);
+  // here and not later: the compiler would carry the products over the barrier
+  if (e0 + N == 16) asm volatile("" : "+v"(acc));
+}
+
+// One stage's products, a block at a time, in T::STEPS steps: a step's products are
+// issued, then its part of the block before, whose products have ended by then, is added
+// up.  On entry the fragments of the first row of blocks are in af[0], of all columns in
+// bf.  cur, next: this stage's and the next one's buffer; freed: cur, as the target of the
+// loads; freed_before: next, as that of the loads which the stage before left (they are
+// declared not to alias, or the compiler would wait for all loads in flight before every
+// read of LDS: what keeps them apart is the barrier).  here, there: this stage's and the
+// next one's scales.
 template <class T, class Loader>
 __device__ __forceinline__ void stage_products8(Loader& ld, ScaleLoads<T>& sl, const ByteFragments<T::MB>& fa,
                                                 const ByteFragments<T::NB>& fb, half::lds_bytes __restrict__ cur,
                                                 half::lds_bytes __restrict__ next, char* __restrict__ freed,
-                                                char* __restrict__ freed_before, const float* here, float* there, int wave, int lane, v8i (&af)[2][2],
-                                                v8i (&bf)[T::NB][2], v16f (&acc)[T::MB][T::NB]) {
+                                                char* __restrict__ freed_before, const float* here, float* there,
+                                                int wave, int lane, v8i (&af)[2][2], v8i (&bf)[T::NB][2],
+                                                v16f (&acc)[T::MB][T::NB]) {
   constexpr int ND = T::ADMA + T::BDMA, MB = T::MB, NB = T::NB, M = MB * NB;
   ld.early(wave, lane);
   float fs[MB];
@@ -388,31 +404,40 @@ __device__ __forceinline__ void stage_products8(Loader& ld, ScaleLoads<T>& sl, c
 #pragma unroll
     for (int y = 0; y < NB; ++y) {
       const int i = x * NB + y;
-      t[i & 1] = mfma64<T::OUT>(bf[y][0], af[x & 1][0], v16f{});
-      t[i & 1] = mfma64<T::OUT>(bf[y][1], af[x & 1][1], t[i & 1]);
-      if (y == 0) {
+      const int o = i - 1, ox = o / NB, oy = o % NB;  // the block before
+      v4f c[4];
+      if (i > 0) column_scales<T>(cs + oy * 32, c);
 #pragma unroll
-        for (int h = 0; h < 2; ++h) af[(x + 1) & 1][h] = fa.read(last ? next : cur, h, last ? 0 : x + 1);
-      }
-      if (last) {
+      for (int q = 0; q < T::STEPS; ++q) {
+        products<T>(q, t[i & 1], bf[y], af[x & 1]);
+        if (q + 1 == T::STEPS) {
+          if (y == 0) {
 #pragma unroll
-        for (int h = 0; h < 2; ++h) bf[y][h] = fb.read(next + T::A_BYTES, h, y);
+            for (int h = 0; h < 2; ++h) af[(x + 1) & 1][h] = fa.read(last ? next : cur, h, last ? 0 : x + 1);
+          }
+          if (last) {
 #pragma unroll
-        for (int j = y * T::SOON / NB; j < (y + 1) * T::SOON / NB; ++j) ld.late(j, freed, wave, lane);
-      }
-      if (x == 0) {
+            for (int h = 0; h < 2; ++h) bf[y][h] = fb.read(next + T::A_BYTES, h, y);
 #pragma unroll
-        for (int j = T::SOON + y * (ND - T::SOON) / NB; j < T::SOON + (y + 1) * (ND - T::SOON) / NB; ++j)
-          ld.late(j, freed_before, wave, lane);
-      }
-      __builtin_amdgcn_sched_barrier(0);
-      if (i > 0) {
-        add_scaled<T>(acc[(i - 1) / NB][(i - 1) % NB], t[(i - 1) & 1], fs[(i - 1) / NB], cs + (i - 1) % NB * 32);
+            for (int j = y * T::SOON / NB; j < (y + 1) * T::SOON / NB; ++j) ld.late(j, freed, wave, lane);
+          }
+          if (x == 0) {
+#pragma unroll
+            for (int j = T::SOON + y * (ND - T::SOON) / NB; j < T::SOON + (y + 1) * (ND - T::SOON) / NB; ++j)
+              ld.late(j, freed_before, wave, lane);
+          }
+        }
         __builtin_amdgcn_sched_barrier(0);
+        if (i > 0) {
+          add_scaled<T, 16 / T::STEPS>(acc[ox][oy], t[o & 1], fs[ox], c, q * (16 / T::STEPS));
+          __builtin_amdgcn_sched_barrier(0);
+        }
       }
     }
   }
-  add_scaled<T>(acc[MB - 1][NB - 1], t[(M - 1) & 1], fs[MB - 1], cs + (NB - 1) * 32);
+  v4f c[4];
+  column_scales<T>(cs + (NB - 1) * 32, c);
+  add_scaled<T, 16>(acc[MB - 1][NB - 1], t[(M - 1) & 1], fs[MB - 1], c, 0);
   if constexpr (MB % 2) {
     af[0][0] = af[1][0];
     af[0][1] = af[1][1];

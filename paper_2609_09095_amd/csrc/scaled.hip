@@ -9,7 +9,7 @@
 // Large products are bound by the matrix cores and the operands' way into LDS: 8192 x
 // 8192 x 8192 2.3 to 2.4 PFLOP/s, 16384 x 4096 x 4096 235 us (with the loads left out
 // 188, with the scaling left out 232 where whole 257); with FP32 outputs and scales per
-// vector, 2048 x 4096 x 8192, 141 us.  Small tiles take 0.45 us a stage, a chain of
+// vector, 2048 x 4096 x 8192, 137 us.  Small tiles take 0.45 us a stage, a chain of
 // barrier, LDS reads, products and scaling.  A few rows are a chain of loads: 1 x 4096 x
 // 4096 6 us, 16 MB of weights.
 #include "eight_products.hpp"
@@ -204,18 +204,21 @@ __global__ __launch_bounds__(256) void scaled_zero_kernel(Scaled g) {
     ((O*)g.y)[i / g.n * g.ldy + i % g.n] = (O)0.0f;
 }
 
-template <class T>
+// PARTS: of forms whose depth may be split
+template <class T, bool PARTS = true>
 hipError_t run_tiles(const Scaled& g, hipStream_t s) {
   const int64_t tiles = ceil_div(g.rows, T::BM) * ceil_div(g.n, T::BN) * g.split;
   if ((tiles + 8) * T::THREADS >= ((int64_t)1 << 32)) return hipErrorInvalidConfiguration;
   const dim3 grid((uint32_t)((tiles + 7) & ~(int64_t)7)), block(T::THREADS);
-  if (g.split == 1) {
-    scaled_kernel<T, false><<<grid, block, 0, s>>>(g);
-    return hipGetLastError();
+  if constexpr (PARTS) {
+    if (g.split > 1) {
+      scaled_kernel<T, true><<<grid, block, 0, s>>>(g);
+      if (const hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+      scaled_join_kernel<T::OUT><<<dim3((uint32_t)ceil_div(g.rows * (pad4(g.n) / 4), 256)), dim3(256), 0, s>>>(g);
+      return hipGetLastError();
+    }
   }
-  scaled_kernel<T, true><<<grid, block, 0, s>>>(g);
-  if (const hipError_t e = hipGetLastError(); e != hipSuccess) return e;
-  scaled_join_kernel<T::OUT><<<dim3((uint32_t)ceil_div(g.rows * (pad4(g.n) / 4), 256)), dim3(256), 0, s>>>(g);
+  scaled_kernel<T, false><<<grid, block, 0, s>>>(g);
   return hipGetLastError();
 }
 
@@ -249,8 +252,11 @@ hipError_t of_type(const Scaled& g, hipStream_t s) {
     return run_tiles<Tile8<2, 4, 2, 1, false, OUT, SQUARES>>(g, s);
   }
   if (form == kScaledSmall) return run_tiles<Tile8<2, 2, 1, 1, true, OUT, SQUARES, 3>>(g, s);
-  if constexpr (OUT != kF32 && SQUARES)
-    if (form == kScaledLarge) return run_tiles<Tile8<2, 4, 4, 2, true, OUT, SQUARES>>(g, s);
+  if constexpr (OUT != kF32 && SQUARES) {
+    if (form == kScaledLarge) return run_tiles<Tile8<2, 4, 4, 2, true, OUT, SQUARES>, false>(g, s);
+  } else {
+    if (g.split == 1 && scaled_tall(g.rows, g.n)) return run_tiles<Tile8<4, 2, 2, 2, true, OUT, SQUARES>, false>(g, s);
+  }
   return run_tiles<Tile8<2, 2, 2, 2, true, OUT, SQUARES>>(g, s);
 }
 

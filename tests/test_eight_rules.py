@@ -21,7 +21,7 @@ def L(tmp_path_factory):
     i64, i32 = ctypes.c_int64, ctypes.c_int
     for name, args, res in (("norm_lanes", [i64], i32), ("norm_chunks", [i64], i32), ("norm_threads", [i64], i32),
                             ("norm_blocks", [i64] * 2, i64), ("norm_parts", [i64] * 2, i64), ("scaled_form", [i64] * 3, i32),
-                            ("scaled_split", [i64] * 3, i32), ("scaled_room", [i64] * 3, i64), ("together", [i64] * 2, i32),
+                            ("scaled_split", [i64] * 3, i32), ("scaled_tall", [i64] * 2, i32), ("scaled_room", [i64] * 3, i64), ("together", [i64] * 2, i32),
                             ("hidden", [i64, i64, i64, i32, i32], i32)):
         f = getattr(lib, "rule_" + name)
         f.argtypes, f.restype = args, res
@@ -62,6 +62,15 @@ def test_parts_have_depths_and_room(L):
                 assert 1 <= split <= 8 and (split == 1 or (form in (SMALL, MIDDLE) and -(-k // 128) >= 8 * split))
                 assert L.rule_scaled_room(rows, n, k) == (0 if split == 1 else split * rows * (-(-n // 4) * 4) * 4)
                 assert L.rule_scaled_room(rows, n, k) < 1 << 30
+
+
+def test_tall_tiles_on_the_measured_side(L):
+    """256 x 128 where the card is full of them; such a product's depth is whole."""
+    for c, want in (((2048, 4096), 1), ((4096, 4096), 1), ((3300, 2050), 1), ((2048, 2048), 0), ((1024, 4096), 0),
+                    ((2049, 2050), 0)):
+        assert L.rule_scaled_tall(*c) == want, c
+        for k in (1, 4096, 1 << 22):
+            assert not want or (L.rule_scaled_form(*c, k) in (MIDDLE, LARGE) and L.rule_scaled_split(*c, k) == 1)
 
 
 def test_layers_on_the_measured_side(L):

@@ -72,7 +72,7 @@ FEW = [(1, 1, 1), (1, 16, 128), (1, 17, 129), (2, 1000, 1111), (16, 48, 4096), (
        (64, 256, 1500), (1, 4096, 4096)]
 TILES = [(65, 64, 128), (65, 1, 1), (100, 70, 15), (128, 128, 129), (200, 129, 1000), (333, 1000, 1111), (500, 300, 2048),
          (256, 256, 16), (97, 333, 640)]
-MANY = [(2000, 2048, 300), (2049, 2050, 257), (4096, 4096, 128), (4100, 4000, 1000)]
+MANY = [(2000, 2048, 300), (2049, 2050, 257), (4096, 4096, 128), (4100, 4000, 1000), (3300, 2050, 1300)]
 
 
 @pytest.mark.parametrize("squares", [True, False])
