@@ -789,9 +789,13 @@ def _new_like(t, stream, dtype=None):
 
 def _new_e4m3(like, shape, stream):
     """An e4m3 output beside `like`, its rows on 16 bytes."""
-    wide = -(-shape[-1] // 16) * 16
-    q = _new(like, (*shape[:-1], wide), stream, _torch.float8_e4m3fn)
-    return q if wide == shape[-1] else q[..., :shape[-1]]
+    rows, cols = shape[-2:]
+    ld = -(-cols // 16) * 16 or 1
+    if ld == cols or stream is not None or not like.is_cuda:
+        q = _new(like, (*shape[:-1], ld), stream, _torch.float8_e4m3fn)
+        return q if ld == cols else q[..., :cols]
+    # in one step: a slice costs as much as the allocation
+    return like.new_empty_strided(shape, (ld, 1) if len(shape) == 2 else (rows * ld, ld, 1), dtype=_torch.float8_e4m3fn)
 
 
 def _blocks(n):
