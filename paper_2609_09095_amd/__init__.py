@@ -543,9 +543,9 @@ def _pitched(t, name, dims, types, shape=None):
     contiguous; returns (shape, row pitch, matrix pitch)."""
     if not (isinstance(t, _torch.Tensor) and t.dtype in types and t.dim() == dims):
         raise ValueError(f"{name} must be a {dims}-D tensor of dtype {' or '.join(str(d) for d in types)}")
-    size = t.shape
+    size = tuple(t.shape)  # a torch.Size takes ten times as long to compare
     if shape is not None and size != shape:
-        raise ValueError(f"{name} has shape {tuple(size)}, expected {tuple(shape)}")
+        raise ValueError(f"{name} has shape {size}, expected {tuple(shape)}")
     if dims == 3:
         count, rows, cols = size
     else:
@@ -975,17 +975,17 @@ def _table(t, name, dtype, size):
     """A contiguous matrix of dtype and size."""
     if not (isinstance(t, _torch.Tensor) and t.dtype == dtype and t.dim() == 2 and t.is_contiguous()):
         raise ValueError(f"{name} must be a contiguous 2-D {str(dtype).replace('torch.', '')} tensor")
-    if t.shape != size:
-        raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {tuple(size)}")
+    if tuple(t.shape) != size:
+        raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {size}")
 
 
-def _stack(W, name, scales, kind, size=None):
+def _stack(W, name, scales, scales_name, kind, size=None):
     """The size of a stack of weights, and ozaki25_expert_weights for it."""
     size, ld, stride = _pitched(W, name, 3, kind, size)
     if scales is None:
         return size, struct.pack("6q", W.data_ptr(), ld, stride, 0, 1, 0)
     experts, rows, cols = size
-    _, lds, s_stride = _pitched(scales, f"{name}_scales", 3, (_torch.float32,), (experts, _blocks(rows), _blocks(cols)))
+    _, lds, s_stride = _pitched(scales, scales_name, 3, (_torch.float32,), (experts, _blocks(rows), _blocks(cols)))
     return size, struct.pack("6q", W.data_ptr(), ld, stride, scales.data_ptr(), lds, s_stride)
 
 
@@ -1010,14 +1010,14 @@ def ozaki25_expert_layer(X, which, gates, up, down, gate=None, up_scales=None, d
     if gate is None and gate_scales is not None:
         raise ValueError("gate_scales need gate")
     stored = (_torch.float8_e4m3fn,) if eight else kind
-    up_size, u = _stack(up, "up", up_scales, stored)
+    up_size, u = _stack(up, "up", up_scales, "up_scales", stored)
     experts, inner, wu = up_size
     if wu != width:
         raise ValueError(f"up has {wu} columns, X has {width}")
-    (ed, out, wd), d = _stack(down, "down", down_scales, stored)
+    (ed, out, wd), d = _stack(down, "down", down_scales, "down_scales", stored)
     if ed != experts or wd != inner:
         raise ValueError(f"down has shape {tuple(down.shape)}, expected ({experts}, out, {inner})")
-    g = None if gate is None else _stack(gate, "gate", gate_scales, stored, up_size)[1]
+    g = None if gate is None else _stack(gate, "gate", gate_scales, "gate_scales", stored, up_size)[1]
     ws_ptr, ws_bytes = _room(workspace)
     if X.requires_grad or gates.requires_grad or up.requires_grad or down.requires_grad or (
             gate is not None and gate.requires_grad) or (eight and (up_scales.requires_grad or down_scales.requires_grad or (
