@@ -18,7 +18,8 @@ constexpr int kMaxNormWidth = 32768;
 // 4999 x 1031 halves 21.7 / 23.0, the norm of 8192 x 1031 18.6 / 20.8.  One chunk a lane
 // / two on half the lanes: gradients of 16384 x 4096 bfloat16 103 / 158 (a second read
 // of the row), of 4999 x 1031 22 / 31, the norms of 8192 x 4096 46 / 45, 8192 x 1031
-// 18.6 / 22.
+// 18.6 / 22.  768 / 1024 lanes with two chunks: 4096 x 12288 bfloat16 71 / 73, gradients 94
+// / 103, of 5852 x 9152 118 / 131.
 struct NormForm {
   int lanes, chunks;
 };
@@ -30,6 +31,7 @@ constexpr NormForm norm_form(int64_t width) {
   if (c <= 256) return {(int)ceil_div(c, 64) * 64, 1};
   if (c <= 512) return {c <= 384 ? 384 : 512, 1};
   if (c <= 1024) return {c <= 768 ? 768 : 1024, 1};
+  if (c <= 1536) return {768, 2};
   return {1024, c <= 2048 ? 2 : 4};
 }
 

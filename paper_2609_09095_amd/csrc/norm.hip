@@ -9,9 +9,9 @@
 // registers of LANES threads (8 CH each) from the load to the store, so each is
 // read and written once; the next row's loads are in flight meanwhile.  8192 x 4096
 // bfloat16 with residual to e4m3: 44 us, 5.4 TB/s; the gradients of 16384 x 4096: 97
-// us, 5.5 TB/s (a large copy: 5.1).  Rows of more than 8192 elements are read twice by
-// the gradient, their registers being taken by dweight's sums: 4096 x 11687 156 us, 2.4
-// TB/s of what has to be moved.
+// us, 5.5 TB/s (a large copy: 5.1).  4096 x 16384: 121 us, 4.4 TB/s (with the row read
+// twice 154).  Rows of more than 16384 elements are read twice by the gradient: 2048 x
+// 20000 151 us, 2.2 TB/s of what has to be moved.
 #include "eight_bits.hpp"
 #include "eight_products.hpp"
 
@@ -174,16 +174,17 @@ __global__ __launch_bounds__(norm_threads(LANES)) void norm_gradient_kernel(Norm
   const int lane = threadIdx.x % LANES, group = threadIdx.x / LANES;
   Columns<TYPE, LANES> cols;
   cols.init(p.width, lane);
-  // of more than two chunks in LDS, and then a chunk at a time in registers
-  constexpr bool WIDE = CH > 2;
+  // of more than a chunk in LDS, so that the row stays in registers
+  constexpr bool WIDE = CH > 1;
   __shared__ v4f wide[WIDE ? CH * LANES * 2 : 1];
   float dw[WIDE ? 1 : CH][8] = {};
   if constexpr (WIDE) {
     for (int i = 0; i < 2 * CH; ++i) wide[i * LANES + lane] = v4f{};  // a thread's own from here on
   }
+  const void* weight = p.weight;
   auto weights = [&](int i) {
     const float one[8] = {1.0f, 1.0f, 1.0f, 1.0f, 1.0f, 1.0f, 1.0f, 1.0f};
-    return p.weight ? cols.load(p.weight, 0, i) : rounded<TYPE>(one);
+    return weight ? cols.load(weight, 0, i) : rounded<TYPE>(one);
   };
   auto add = [&](const float (&h)[8], const float (&dy)[8], const float (&f)[8], float (&sum)[2]) {
 #pragma unroll
@@ -241,11 +242,63 @@ __global__ __launch_bounds__(norm_threads(LANES)) void norm_gradient_kernel(Norm
       const float rho = 1.0f / sqrtf(sum[0] / (float)p.width + p.eps), mean = rho * rho * (sum[1] / (float)p.width);
       finish(row, 0, rho, mean, h, dy, f, b);
     }
+  } else if constexpr (CH == 2) {
+    // registers: a row as it is in memory, and of 16-bit types the next one's H and dY
+    constexpr bool AHEAD = TYPE != kF32;
+    Raw<TYPE> y[CH], x[CH];
+    auto load = [&](int64_t row) {
+      row = row < p.rows ? row : p.rows - 1;
+#pragma unroll
+      for (int i = 0; i < CH; ++i) {
+        y[i] = cols.load(p.dy, row * p.lddy, i);
+        x[i] = cols.load(p.h, row * p.ldh, i);
+      }
+    };
+    if constexpr (AHEAD) load(blockIdx.x);
+    for (int64_t row = blockIdx.x; row < p.rows; row += step) {
+      if constexpr (!AHEAD) {
+        load(row);
+        asm volatile("" : "+s"(weight));  // read again for every row: no registers for it
+      }
+      Raw<TYPE> hr[CH], yr[CH], dr[CH];
+#pragma unroll
+      for (int i = 0; i < CH; ++i) {
+        hr[i] = x[i], yr[i] = y[i];
+        if constexpr (DH) dr[i] = cols.load(p.dh, row * p.lddh, i);
+      }
+      if constexpr (AHEAD) load(row + step);
+      float sum[2] = {0.0f, 0.0f};
+#pragma unroll
+      for (int i = 0; i < CH; ++i) {
+        float h[8], dy[8], f[8];
+        cols.get(hr[i], i, h);
+        cols.get(yr[i], i, dy);
+        cols.get(weights(i), i, f);
+        add(h, dy, f, sum);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      row_sums<LANES, 2>(sum, room, turn);
+      turn ^= 1;
+      const float rho = 1.0f / sqrtf(sum[0] / (float)p.width + p.eps), mean = rho * rho * (sum[1] / (float)p.width);
+#pragma unroll
+      for (int i = 0; i < CH; ++i) {
+        // as they are in memory: the compiler would keep the first pass's conversions
+#pragma unroll
+        for (int q = 0; q < Raw<TYPE>::Q; ++q) asm volatile("" : "+v"(hr[i].q[q]), "+v"(yr[i].q[q]));
+        float h[8], dy[8], f[8], b[8] = {};
+        cols.get(hr[i], i, h);
+        cols.get(yr[i], i, dy);
+        cols.get(weights(i), i, f);
+        if constexpr (DH) cols.get(dr[i], i, b);
+        finish(row, i, rho, mean, h, dy, f, b);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+    }
   } else {
-    // a row does not fit the registers beside its sums: it is read again, from the caches
+    // a row does not fit the registers: it is read again, from the caches
     for (int64_t row = blockIdx.x; row < p.rows; row += step) {
       float sum[2] = {0.0f, 0.0f};
-#pragma unroll(WIDE ? 1 : CH)
+#pragma unroll 1
       for (int i = 0; i < CH; ++i) {
         float h[8], dy[8], f[8];
         cols.get(cols.load(p.h, row * p.ldh, i), i, h);
@@ -256,7 +309,7 @@ __global__ __launch_bounds__(norm_threads(LANES)) void norm_gradient_kernel(Norm
       row_sums<LANES, 2>(sum, room, turn);
       turn ^= 1;
       const float rho = 1.0f / sqrtf(sum[0] / (float)p.width + p.eps), mean = rho * rho * (sum[1] / (float)p.width);
-#pragma unroll(WIDE ? 1 : CH)
+#pragma unroll 1
       for (int i = 0; i < CH; ++i) {
         float h[8], dy[8], f[8], b[8] = {};
         cols.get(cols.load(p.h, row * p.ldh, i), i, h);
@@ -374,6 +427,7 @@ hipError_t of_form(NormForm g, F f) {
     case 512 * 8 + 1: return f.template operator()<512, 1>();
     case 768 * 8 + 1: return f.template operator()<768, 1>();
     case 1024 * 8 + 1: return f.template operator()<1024, 1>();
+    case 768 * 8 + 2: return f.template operator()<768, 2>();
     case 1024 * 8 + 2: return f.template operator()<1024, 2>();
     default: return f.template operator()<1024, 4>();
   }

@@ -164,6 +164,29 @@ def test_gradients(width, dtype):
         assert got.dtype == torch.float32 and bool(((got.double() - dw).abs() <= terms * (rows + 37 + 32) * u.U).all())
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
+@pytest.mark.parametrize("width", [2100, 8192, 8200, 12288, 12296, 16384, 16400])
+def test_gradients_of_wide_rows(width, dtype):
+    """More rows than the card holds blocks, so that each goes through several: the sums
+    that stay from row to row, the loads ahead, dX in dH's place.  Tolerances as above."""
+    import torch
+    import eight_util as u
+    rows = 700
+    H, D, w = case(rows, width, dtype, True, width + 1)
+    dY = u.normal((rows, width), H.dtype, width + 2)
+    want, dw, g, rho = gradients(dY, H, w, D)
+    kept = D.clone()
+    dX, got = oz.ozaki25_rms_norm_backward(dY, H, w, dH=kept, dX=kept, eps=EPS)
+    assert dX is kept
+    size = rho * (g.abs() + H.double().abs() * rho ** 2 * (g * H.double()).abs().mean(1, keepdim=True)) + D.double().abs()
+    tiny = 2.0 ** -25 if H.dtype == torch.float16 else 0.0
+    off = (dX.double() - want).abs() - want.abs() * u.half_step(H.dtype) - size * (3 * 35 + 64) * u.U - tiny
+    assert bool((off <= 0).all()), float(off.max())
+    terms = (dY.double() * H.double() * rho).abs().sum(0)
+    assert bool(((got.double() - dw).abs() <= terms * (rows + 37 + 32) * u.U).all())
+    assert torch.equal(oz.ozaki25_rms_norm_backward(dY, H, w, eps=EPS)[1], got)
+
+
 @pytest.mark.parametrize("rows", [0, 1, 300, 20000])
 def test_gradient_rows(rows):
     """None, one, more than a block and more than the card holds; the same bits twice."""
