@@ -127,18 +127,28 @@ constexpr bool layer_together(int64_t tokens, int64_t top) { return tokens * top
 // 4, 2, 8, 4096, 2048 20.6 / 35; 1, 2, 8, 2048, 1024 6.1 / 5.6.
 constexpr bool together_wide(int64_t out) { return out >= 4096; }
 
-// Hidden values: blocks of 16 or 32 rows of weights (8 or 16 columns of both
+// Hidden values: blocks of 16, 32 or 64 rows of weights (8 to 32 columns of both
 // projections), 16 or 32 tokens, four or eight wavefronts.
-enum HiddenForm { kHiddenOne, kHiddenSmall, kHiddenWide, kHiddenRows };
+enum HiddenForm { kHiddenOne, kHiddenSmall, kHiddenWide, kHiddenRows, kHiddenLarge };
 // 16 / 32 rows: 4, 2, 8, 4096, 2048 33 / 36; 32, 2, 8, 4096, 1024 e 24 / 20; 64, 4, 64, 2048,
 // 1024 e 61 / 49.  32 tokens where an expert has 12 on average: 64, 2, 8, 4096, 1024 44 /
-// 52, but 32, 2, 8, 4096, 1024 e 26 / 20.  Eight wavefronts where CUs have one block:
+// 52, but 32, 2, 8, 4096, 1024 e 26 / 20; then 32 / 64 rows, of the whole layer: 64, 8, 16,
+// 2048, 1024 91 / 87, 32, 8, 8, 2048, 2048 e 48 / 42, but 64, 2, 8, 4096, 1024 76 / 88
+// (256 blocks).  Eight wavefronts where CUs have one block:
 // 1, 2, 8, 2048, 1024 7.2 / 7.5.
 constexpr HiddenForm hidden_form(int64_t choices, int64_t experts, int64_t inner, bool gated, bool eight) {
   const int64_t wide = experts * ceil_div(inner, gated ? 16 : 32);
   if (wide < 256) return kHiddenOne;
-  if (choices >= 12 * experts) return kHiddenRows;
+  if (choices >= 12 * experts) return experts * ceil_div(inner, gated ? 32 : 64) >= 512 ? kHiddenLarge : kHiddenRows;
   return wide < (eight ? 512 : 1536) ? kHiddenSmall : kHiddenWide;
+}
+
+// Outputs of more choices: blocks of 32 columns and 16 choices of an expert, or 64 and 32
+// where experts have 12 on average.  Of the whole layer: 64, 8, 16, 2048, 1024 102 / 92, 32,
+// 8, 8, 2048, 2048 e 58 / 48, 256, 8, 64, 2048, 1024 e 272 / 243; but with few blocks 64, 1,
+// 2, 2048, 2048 e 43 / 48.
+constexpr bool share_rows(int64_t choices, int64_t experts, int64_t out) {
+  return choices >= 12 * experts && experts * ceil_div(out, 64) >= 256;
 }
 
 constexpr size_t layer_hidden_bytes(int64_t tokens, int64_t top, int64_t inner) {

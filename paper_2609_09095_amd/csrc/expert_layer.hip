@@ -5,7 +5,7 @@
 //
 // Two launches, the hidden values and the outputs (a third, which adds the experts'
 // shares, for more than kTogether choices).  Bound by the read of the weights that
-// tokens reach, each once: a block reads 16 rows of an expert's weights straight
+// tokens reach, each once: a block reads 16 to 64 rows of an expert's weights straight
 // into the matrix cores' fragments, for all tokens of that expert, and its
 // wavefronts split the depth.  Every block reads `which` by itself, so the host
 // needs no expert's tokens.  64 tokens with 4 of 64 experts, 2048 x 1024 in e4m3: 46 +
@@ -49,21 +49,52 @@ struct FewChoices {
 // More choices: the experts reached as bits in LDS, in ascending order.
 constexpr int kWords = kMaxLayerExperts / 32;
 
+constexpr int kAtOnce = 8;  // choices that a thread holds
+
 struct Reached {
   uint32_t bits[kWords];
-  int counts[16];
+  int counts[kAtOnce][16];
 };
 
-// Sets the bits; `first`: the thread's choice number threadIdx.x, for P up to THREADS
-// the only one.
+// Choices i0 + k THREADS + threadIdx.x, -1 past the last: their loads are in flight
+// together.
 template <int THREADS>
-__device__ __forceinline__ void find_reached(const Layer& p, Reached& s, int first) {
+__device__ __forceinline__ void load_choices(const Layer& p, int i0, int (&mine)[kAtOnce]) {
   const int pairs = p.tokens * p.top;
+#pragma unroll
+  for (int k = 0; k < kAtOnce; ++k) {
+    mine[k] = -1;
+    const int i = i0 + k * THREADS + threadIdx.x;
+    if (i < pairs) mine[k] = p.which[i];
+  }
+}
+
+// How many of a thread's choices there may be.
+template <int THREADS>
+__device__ __forceinline__ int sets_of_choices(const Layer& p, int i0) {
+  const int n = (p.tokens * p.top - i0 + THREADS - 1) / THREADS;
+  return n < kAtOnce ? n : kAtOnce;
+}
+
+// Sets the bits; leaves the first choices in `mine`.
+template <int THREADS>
+__device__ __forceinline__ void find_reached(const Layer& p, Reached& s, int (&mine)[kAtOnce]) {
+  const int pairs = p.tokens * p.top;
+  auto set = [&](const int (&c)[kAtOnce], int sets) {
+#pragma unroll
+    for (int k = 0; k < kAtOnce; ++k) {
+      if (k >= sets) break;
+      if (c[k] >= 0 && c[k] < p.experts) atomicOr(&s.bits[c[k] >> 5], 1u << (c[k] & 31));
+    }
+  };
+  load_choices<THREADS>(p, 0, mine);
   for (int i = threadIdx.x; i < kWords; i += THREADS) s.bits[i] = 0;
   __syncthreads();
-  for (int i = threadIdx.x; i < pairs; i += THREADS) {
-    const int e = i < THREADS ? first : p.which[i];
-    if (e >= 0 && e < p.experts) atomicOr(&s.bits[e >> 5], 1u << (e & 31));
+  set(mine, sets_of_choices<THREADS>(p, 0));
+  for (int i0 = kAtOnce * THREADS; i0 < pairs; i0 += kAtOnce * THREADS) {
+    int more[kAtOnce];
+    load_choices<THREADS>(p, i0, more);
+    set(more, sets_of_choices<THREADS>(p, i0));
   }
   __syncthreads();
 }
@@ -102,8 +133,8 @@ __device__ __forceinline__ int find_tokens(const Layer& p, int rank, Tokens& s, 
     __syncthreads();
     return e;
   }
-  const int first = (int)threadIdx.x < pairs ? p.which[threadIdx.x] : -1;
-  find_reached<THREADS>(p, s.reached, first);
+  int mine_of[kAtOnce];
+  find_reached<THREADS>(p, s.reached, mine_of);
   uint64_t mine;
   int before;
   if (rank >= count_reached(s.reached, lane, mine, before)) return 0;
@@ -114,20 +145,32 @@ __device__ __forceinline__ int find_tokens(const Layer& p, int rank, Tokens& s, 
                (uint32_t)__builtin_amdgcn_readlane((int)mine, at);
   for (int nth = rank - __builtin_amdgcn_readlane(before, at); nth > 0; --nth) b &= b - 1;
   const int e = at * 64 + __builtin_ctzll(b);
-  for (int i0 = 0; i0 < pairs; i0 += THREADS) {
-    const int i = i0 + threadIdx.x;
-    const bool is = i < pairs && (i0 == 0 ? first : p.which[i]) == e;
-    const uint64_t m = __builtin_amdgcn_ballot_w64(is);
-    if (lane == 0) s.reached.counts[wave] = __builtin_popcountll(m);
-    __syncthreads();
-    int n = count;
+  for (int i0 = 0; i0 < pairs; i0 += kAtOnce * THREADS) {
+    if (i0) load_choices<THREADS>(p, i0, mine_of);
+    const int sets = sets_of_choices<THREADS>(p, i0);
+    // all the ballots, then one exchange of their counts
 #pragma unroll
-    for (int w = 0; w < THREADS / 64; ++w) {
-      const int c = s.reached.counts[w];
-      n += w < wave ? c : 0;
-      count += c;
+    for (int k = 0; k < kAtOnce; ++k) {
+      if (k >= sets) break;
+      const uint64_t m = __builtin_amdgcn_ballot_w64(mine_of[k] == e);
+      if (lane == 0) s.reached.counts[k][wave] = __builtin_popcountll(m);
     }
-    if (is) s.list[n + __builtin_popcountll(m & (((uint64_t)1 << lane) - 1))] = (uint16_t)i;
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < kAtOnce; ++k) {
+      if (k >= sets) break;
+      const bool is = mine_of[k] == e;
+      const uint64_t m = __builtin_amdgcn_ballot_w64(is);
+      int n = count;
+#pragma unroll
+      for (int w = 0; w < THREADS / 64; ++w) {
+        const int c = s.reached.counts[k][w];
+        n += w < wave ? c : 0;
+        count += c;
+      }
+      if (is)
+        s.list[n + __builtin_popcountll(m & (((uint64_t)1 << lane) - 1))] = (uint16_t)(i0 + k * THREADS + threadIdx.x);
+    }
     __syncthreads();
   }
   return e;
@@ -245,7 +288,7 @@ __device__ __forceinline__ void each_step(int s0, int s1, int whole, F step) {
 // the others U's, of the same 8 NB hidden columns (of one product's 16 rows where
 // NB is 1).
 template <int TYPE, bool EIGHT, bool GATED, int NB, int TB, int WAVES>
-__global__ __launch_bounds__(WAVES * 64, 4) void hidden_kernel(Layer p) {
+__global__ __launch_bounds__(WAVES * 64, NB * TB > 4 ? 2 : 4) void hidden_kernel(Layer p) {
   constexpr int COLS = GATED ? 8 * NB : 16 * NB, E = EIGHT ? 1 : 2, Q = NB * 4, ROWS = TB * 16;
   __shared__ Tokens tokens;
   __shared__ v4f lds[WAVES * ROWS * Q];
@@ -433,7 +476,7 @@ __global__ __launch_bounds__(WAVES * 64) void together_kernel(Layer p) {
 // A block: 16 NB output columns of one expert, for its tokens; combine_kernel adds a
 // token's shares in the order of its choices.
 template <int TYPE, bool EIGHT, int NB, int TB, int WAVES>
-__global__ __launch_bounds__(WAVES * 64, 4) void share_kernel(Layer p) {
+__global__ __launch_bounds__(WAVES * 64, NB * TB > 2 ? 2 : 4) void share_kernel(Layer p) {
   constexpr int COLS = 16 * NB, E = EIGHT ? 1 : 2, Q = NB * 4, ROWS = TB * 16;
   __shared__ Tokens tokens;
   __shared__ v4f lds[WAVES * ROWS * Q];
@@ -554,7 +597,8 @@ hipError_t run_hidden(const Layer& p, int64_t experts, hipStream_t s) {
     case kHiddenOne: return run_hidden<TYPE, EIGHT, GATED, 1, 1, 8>(p, experts, s);
     case kHiddenSmall: return run_hidden<TYPE, EIGHT, GATED, 1, 1, 4>(p, experts, s);
     case kHiddenWide: return run_hidden<TYPE, EIGHT, GATED, 2, 1, 4>(p, experts, s);
-    default: return run_hidden<TYPE, EIGHT, GATED, 2, 2, 4>(p, experts, s);
+    case kHiddenRows: return run_hidden<TYPE, EIGHT, GATED, 2, 2, 4>(p, experts, s);
+    default: return run_hidden<TYPE, EIGHT, GATED, 4, 2, 4>(p, experts, s);
   }
 }
 
@@ -565,6 +609,15 @@ hipError_t run_together(const Layer& p, hipStream_t s) {
   return hipGetLastError();
 }
 
+template <int TYPE, bool EIGHT, int NB, int TB>
+hipError_t run_share(const Layer& p, int64_t experts, hipStream_t s) {
+  constexpr int WAVES = 4;
+  const int64_t blocks = experts * ceil_div(p.out, 16 * NB);
+  if (blocks * WAVES * 64 >= ((int64_t)1 << 32)) return hipErrorInvalidConfiguration;
+  share_kernel<TYPE, EIGHT, NB, TB, WAVES><<<dim3((uint32_t)blocks), dim3(WAVES * 64), 0, s>>>(p);
+  return hipGetLastError();
+}
+
 template <int TYPE, bool EIGHT>
 hipError_t run_layer(const Layer& p, hipStream_t s) {
   const int64_t pairs = (int64_t)p.tokens * p.top, most = p.experts < pairs ? p.experts : pairs;
@@ -572,11 +625,8 @@ hipError_t run_layer(const Layer& p, hipStream_t s) {
   if (e != hipSuccess) return e;
   if (layer_together(p.tokens, p.top))
     return together_wide(p.out) ? run_together<TYPE, EIGHT, 16>(p, s) : run_together<TYPE, EIGHT, 8>(p, s);
-  constexpr int WAVES = 4, NB = 2;
-  const int64_t blocks = most * ceil_div(p.out, 16 * NB);
-  if (blocks * WAVES * 64 >= ((int64_t)1 << 32)) return hipErrorInvalidConfiguration;
-  share_kernel<TYPE, EIGHT, NB, 1, WAVES><<<dim3((uint32_t)blocks), dim3(WAVES * 64), 0, s>>>(p);
-  if ((e = hipGetLastError()) != hipSuccess) return e;
+  e = share_rows(pairs, p.experts, p.out) ? run_share<TYPE, EIGHT, 4, 2>(p, most, s) : run_share<TYPE, EIGHT, 2, 1>(p, most, s);
+  if (e != hipSuccess) return e;
   combine_kernel<TYPE><<<dim3((uint32_t)ceil_div((int64_t)p.tokens * (p.out_pad / 4), 256)), dim3(256), 0, s>>>(p);
   return hipGetLastError();
 }

@@ -15,6 +15,7 @@ int rule_scaled_split(int64_t rows, int64_t n, int64_t k) { return scaled_plan(r
 int rule_scaled_tall(int64_t rows, int64_t n) { return scaled_tall(rows, n); }
 int64_t rule_scaled_room(int64_t rows, int64_t n, int64_t k) { return (int64_t)scaled_room(rows, n, k); }
 int rule_together(int64_t tokens, int64_t top) { return layer_together(tokens, top); }
+int rule_share_rows(int64_t choices, int64_t experts, int64_t out) { return share_rows(choices, experts, out); }
 int rule_hidden(int64_t choices, int64_t experts, int64_t inner, int gated, int eight) {
   return hidden_form(choices, experts, inner, gated != 0, eight != 0);
 }

@@ -8,7 +8,7 @@ import pytest
 
 ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 FEW16, FEW32, FEW64, SMALL, MIDDLE, LARGE = range(6)
-ONE, NARROW, WIDE, ROWS = range(4)
+ONE, NARROW, WIDE, ROWS, MANY = range(5)
 
 
 @pytest.fixture(scope="module")
@@ -21,7 +21,7 @@ def L(tmp_path_factory):
     i64, i32 = ctypes.c_int64, ctypes.c_int
     for name, args, res in (("norm_lanes", [i64], i32), ("norm_chunks", [i64], i32), ("norm_threads", [i64], i32),
                             ("norm_blocks", [i64] * 2, i64), ("norm_parts", [i64] * 2, i64), ("scaled_form", [i64] * 3, i32),
-                            ("scaled_split", [i64] * 3, i32), ("scaled_tall", [i64] * 2, i32), ("scaled_room", [i64] * 3, i64), ("together", [i64] * 2, i32),
+                            ("scaled_split", [i64] * 3, i32), ("scaled_tall", [i64] * 2, i32), ("scaled_room", [i64] * 3, i64), ("together", [i64] * 2, i32), ("share_rows", [i64] * 3, i32),
                             ("hidden", [i64, i64, i64, i32, i32], i32)):
         f = getattr(lib, "rule_" + name)
         f.argtypes, f.restype = args, res
@@ -79,5 +79,9 @@ def test_layers_on_the_measured_side(L):
     for c, want in (((2, 2, 1024, 1, 0), ONE), ((8, 8, 2048, 1, 0), NARROW), ((64, 8, 1024, 1, 1), WIDE),
                     ((256, 64, 1024, 1, 1), WIDE), ((256, 64, 1024, 1, 0), WIDE), ((128, 8, 1024, 1, 0), ROWS),
                     ((1, 1, 1, 0, 0), ONE), ((40, 20, 500, 1, 0), NARROW), ((128, 64, 900, 0, 0), WIDE),
-                    ((260, 20, 500, 0, 1), ROWS)):
+                    ((260, 20, 500, 0, 1), ROWS), ((512, 16, 1024, 1, 0), MANY), ((256, 8, 2048, 1, 1), MANY),
+                    ((800, 64, 270, 1, 0), MANY), ((400, 16, 2050, 0, 1), MANY), ((480, 16, 1030, 0, 1), ROWS)):
         assert L.rule_hidden(*c) == want, c
+    for c, want in (((512, 16, 2048), 1), ((256, 8, 2048), 1), ((128, 8, 4096), 1), ((800, 64, 250), 1), ((64, 2, 2048), 0),
+                    ((256, 64, 2048), 0)):
+        assert L.rule_share_rows(*c) == want, c

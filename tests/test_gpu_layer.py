@@ -109,6 +109,15 @@ def test_forms(tokens, experts, inner, eight, gated):
     run(tokens, 2, experts, 70, inner, 40, "bf16" if inner == 500 else "f16", eight, gated, seed=inner, layout=(0, 16)[eight])
 
 
+@pytest.mark.parametrize("gated", [True, False])
+@pytest.mark.parametrize("eight", [False, True])
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("tokens,experts,width,inner,out", [(100, 64, 130, 270, 250), (60, 16, 72, 1030, 1030), (50, 16, 40, 2050, 1030)])
+def test_many_choices_of_an_expert(tokens, experts, width, inner, out, dtype, eight, gated):
+    """The blocks of 64 rows of weights and 32 choices, some of them in part."""
+    run(tokens, 8, experts, width, inner, out, dtype, eight, gated, seed=inner, layout=(3, 16)[eight])
+
+
 def test_wide_outputs_of_few_choices():
     for eight in (False, True):
         run(2, 3, 5, 130, 70, 4100, "bf16", eight, True)
