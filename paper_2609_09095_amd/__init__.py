@@ -754,7 +754,7 @@ def ozaki25_orthogonalise(G, X=None, steps: int = 5, coefficients=(3.4445, -4.77
 
 # ----------------------------------------------------------------- the 8-bit path
 # e4m3 matrices are torch.float8_e4m3fn.  The library lays their rows out on 16
-# bytes (a view of a wider tensor where the row is shorter), which its products
+# bytes (strided where the row is shorter), which its products
 # read fastest; any row-major tensor will do as an input.  As above, the calls are
 # not recorded for gradients and warn where an input asks for one.
 _FLOATS = None    # torch dtype -> ozaki25_dtype, 32 bits included
