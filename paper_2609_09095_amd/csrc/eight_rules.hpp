@@ -62,7 +62,7 @@ constexpr int64_t pad4(int64_t n) { return (n + 3) / 4 * 4; }
 // An 8-bit product's form: few rows, or tiles of 64 x 64, 128 x 128, 256 x 256; and the
 // parts of the depth that its tiles are split into.  Times in us, bfloat16 outputs,
 // squares.
-enum ScaledForm { kScaledFew16, kScaledFew32, kScaledFew64, kScaledSmall, kScaledMiddle, kScaledLarge };
+enum ScaledForm { kScaledFew16, kScaledFew32, kScaledFew48, kScaledSmall, kScaledMiddle, kScaledLarge };
 struct ScaledPlan {
   ScaledForm form;
   int split;
@@ -71,9 +71,9 @@ struct ScaledPlan {
 // A tile's stage takes its time however few tiles there are, so a long depth is split
 // where that leaves CUs without one, into parts of at least 8 blocks of 128 depths; the
 // second launch, which adds the parts, pays from 24 blocks on where most CUs are idle and
-// from 48 on else.  Whole / split: 512, 512, 8192 27 / 17; 285, 128, 7355 24 / 12; 65,
-// 4096, 4096 15.5 / 13.6; 1024, 1024, 16384 67 / 38; but 300, 4096, 4096 22.4 / 23.1, 512,
-// 4096, 4096 23.6 / 26.5.
+// from 48 on else.  Whole / split: 512, 512, 8192 26 / 16; 285, 128, 7355 24 / 12; 65,
+// 4096, 4096 14.9 / 12.7; 1024, 1024, 16384 77 / 34; but 640, 128, 2048 9.0 / 11.3; 192, 1618,
+// 4544 in parts for half the CUs 12.9, for all 14.1.
 constexpr int scaled_parts(int64_t tiles, int64_t blocks) {
   if (blocks < 24) return 1;
   int64_t p = (blocks < 48 ? 256 : 768) / tiles;
@@ -81,14 +81,14 @@ constexpr int scaled_parts(int64_t tiles, int64_t blocks) {
   return (int)(p < 1 ? 1 : p > 8 ? 8 : p);
 }
 
-// Up to 16 rows, or 64 with a depth of up to 4096: the few-row form, which reads B once
-// and the rows once per 16 columns.  Few-row form / tiles: 17, 4096, 4096 9.2 / 11.8; 33,
-// 4096, 4096 10.7 / 11.8; 32, 8192, 8192 28 / 19; 64, 8192, 8192 43 / 21; 64, 1024, 8192
-// 22 / 12.  Tiles of 256 x 256 for 205 of them and more (80 of 100 CUs), as for 16-bit
+// Up to 16 rows, or 48 with a depth of up to 4096: the few-row form, which reads B once
+// and the rows once per 16 columns.  Few-row form / tiles: 17, 4096, 4096 9.0 / 11.3; 33,
+// 4096, 4096 10.0 / 10.8; 64, 4096, 4096 12.6 / 11.5; 32, 8192, 8192 28 / 17.5; 64, 1024, 8192
+// 22 / 11.3.  Tiles of 256 x 256 for 205 of them and more (80 of 100 CUs), as for 16-bit
 // operands.
 constexpr ScaledPlan scaled_plan(int64_t rows, int64_t n, int64_t k) {
   if (rows <= 16) return {kScaledFew16, 1};
-  if (rows <= 64 && k <= 4096) return {rows <= 32 ? kScaledFew32 : kScaledFew64, 1};
+  if (rows <= 48 && k <= 4096) return {rows <= 32 ? kScaledFew32 : kScaledFew48, 1};
   const int64_t small = ceil_div(rows, 64) * ceil_div(n, 64), middle = ceil_div(rows, 128) * ceil_div(n, 128),
                 large = ceil_div(rows, 256) * ceil_div(n, 256), blocks = ceil_div(k, 128);
   if (middle >= 205) return {large >= 205 ? kScaledLarge : kScaledMiddle, 1};

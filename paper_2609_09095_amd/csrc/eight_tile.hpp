@@ -53,7 +53,9 @@ struct Tile8 {
   static constexpr int WAVES = WR * WC, THREADS = WAVES * 64;
   static constexpr int A_BYTES = BM * kStage, B_BYTES = BN * kStage;
   static constexpr int STAGE = A_BYTES + B_BYTES, SET = BUFS * STAGE;
-  static constexpr int SLOT = (BM + BN) * 4, LDS = SET + 3 * SLOT;  // scales: three stages'
+  // a stage's scales, a dword of every lane; a stage more than of bytes, since the last of
+  // its products are added up behind the barrier that frees its bytes
+  static constexpr int SLOT = THREADS * 4, SLOTS = (BUFS + 1) * SLOT, LDS = SET + SLOTS;
   static constexpr int ADMA = A_BYTES / 1024 / WAVES, BDMA = B_BYTES / 1024 / WAVES;
   // Loads issued right behind the barrier that frees their buffer; the others follow
   // beside the next stage's first products (all at once they keep the wavefront from
@@ -69,7 +71,7 @@ struct Tile8 {
   static constexpr int STEPS = WR < 4 ? 1 : OUT == kF32 ? 4 : 2;
   using Loads = std::conditional_t<DMA, ByteDma<Tile8>, ByteMasked<Tile8>>;
   static_assert(ADMA * WAVES * 1024 == A_BYTES && BDMA * WAVES * 1024 == B_BYTES, "whole slabs per wavefront");
-  static_assert(BM + BN <= THREADS, "a thread carries one scale");
+  static_assert(BM + BN <= THREADS, "a lane brings one scale");
   static_assert(NB * 32 <= 128 && 128 % (NB * 32) == 0, "a wavefront's columns lie in one square");
 };
 
@@ -143,7 +145,7 @@ struct ByteDma {
     else
       b.load(j - T::ADMA, rb, buf + T::A_BYTES, wave);
   }
-  static constexpr int IN_FLIGHT = T::ADMA + T::BDMA;
+  static constexpr int IN_FLIGHT = T::ADMA + T::BDMA + 1;  // and the scales
 };
 
 // Any alignment and pitch, through registers.  A vector past the edge is read as the
@@ -221,39 +223,38 @@ struct ByteMasked {
   static constexpr int IN_FLIGHT = 0;
 };
 
-// A stage's scales: thread v < BM carries row v's, the next BN threads a column's
-// each.  Vectors past the edge take the last one's (their sums are not stored).
+// A stage's scales, straight into LDS beside its bytes: lane v < BM brings row v's, the
+// next BN lanes a column's each.  Vectors past the edge take the last one's (their sums
+// are not stored).  As early as the bytes: through a register they came a stage ahead, and
+// small tiles waited for them (256 x 3648 x 5143 26 / 19.5 us, 1024 x 1024 x 4096 20 / 16).
 template <class T>
 struct ScaleLoads {
-  const float* p;  // of the wavefront (uniform), at the block that is loaded next
+  const float* p;  // of the wavefront (uniform)
   int64_t step;
-  int off;  // the lane's vector
+  int off;  // of the lane's vector, in bytes
   int stage, stages;
-  float next;
-  static_assert(T::BM % 64 == 0 && T::BN % 64 == 0, "a wavefront carries one operand's scales");
+  static_assert(T::BM % 64 == 0 && T::BN % 64 == 0, "a wavefront brings one operand's scales");
   __device__ __forceinline__ void init(const Scales& sa, const Scales& sb, int rows, int cols, int n) {
     const int t = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(t >> 6);
     if (wave * 64 < T::BM) {
-      off = t < rows ? t : rows - 1;
+      off = (t < rows ? t : rows - 1) * 4;
       p = sa.p;
       step = sa.step;
     } else {
       const int c = t - T::BM < cols ? t - T::BM : cols - 1;
-      off = T::SQUARES ? 0 : c;
+      off = T::SQUARES ? 0 : c * 4;
       p = T::SQUARES ? sb.p + (int64_t)(__builtin_amdgcn_readfirstlane(c) / kBlock) * sb.step : sb.p;
       step = T::SQUARES ? 1 : sb.step;
     }
-    p = (const float*)half::uniform(p);
     stage = 0, stages = n;
   }
   // the last block first, like the bytes
-  __device__ __forceinline__ void load() {
+  __device__ __forceinline__ void load(char* slot, int wave) {
     const int64_t b = stage == 0 ? stages - 1 : stage < stages ? stage - 1 : stages - 1;
-    next = p[b * step + off];
+    const __amdgpu_buffer_rsrc_t r =
+        __builtin_amdgcn_make_buffer_rsrc((void*)half::uniform((const char*)(p + b * step)), (short)0, 0x7ffffff0, 0x00020000);
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (half::lds_ptr)(slot + wave * 256), 4, off, 0, 0, 0);
     ++stage;
-  }
-  __device__ __forceinline__ void put(float* slot) const {
-    if (T::THREADS == T::BM + T::BN || threadIdx.x < T::BM + T::BN) slot[threadIdx.x] = next;
   }
 };
 
@@ -366,14 +367,14 @@ __device__ __forceinline__ void add_scaled(v16f& acc, const v16f& t, float fs, c
 // bf.  cur, next: this stage's and the next one's buffer; freed: cur, as the target of the
 // loads; freed_before: next, as that of the loads which the stage before left (they are
 // declared not to alias, or the compiler would wait for all loads in flight before every
-// read of LDS: what keeps them apart is the barrier).  here, there: this stage's and the
-// next one's scales.
+// read of LDS: what keeps them apart is the barrier).  here: this stage's scales;
+// scales_freed: those of the stage before, as the target of the loads.
 template <class T, class Loader>
 __device__ __forceinline__ void stage_products8(Loader& ld, ScaleLoads<T>& sl, const ByteFragments<T::MB>& fa,
                                                 const ByteFragments<T::NB>& fb, half::lds_bytes __restrict__ cur,
                                                 half::lds_bytes __restrict__ next, char* __restrict__ freed,
-                                                char* __restrict__ freed_before, const float* here, float* there,
-                                                int wave, int lane, v8i (&af)[2][2], v8i (&bf)[T::NB][2],
+                                                char* __restrict__ freed_before, const float* __restrict__ here,
+                                                char* __restrict__ scales_freed, int wave, int lane, v8i (&af)[2][2], v8i (&bf)[T::NB][2],
                                                 v16f (&acc)[T::MB][T::NB]) {
   constexpr int ND = T::ADMA + T::BDMA, MB = T::MB, NB = T::NB, M = MB * NB;
   ld.early(wave, lane);
@@ -393,11 +394,10 @@ __device__ __forceinline__ void stage_products8(Loader& ld, ScaleLoads<T>& sl, c
   for (int x = 0; x < MB; ++x) {
     const bool last = x + 1 == MB;
     if (last) {
-      // the next stage's scales, and (older than the loads that may be in flight) its bytes
-      sl.put(there);
+      // the next stage's bytes and scales, older than the loads that may stay in flight
       half::wait_loads_and_lds<(T::BUFS - 2) * T::Loads::IN_FLIGHT>();
       half::block_barrier();
-      sl.load();
+      sl.load(scales_freed, wave);
       ld.begin();
     }
     __builtin_amdgcn_sched_barrier(0);
@@ -463,20 +463,18 @@ __device__ __forceinline__ void product8(const Bytes& oa, const Bytes& ob, const
   ScaleLoads<T> sl;
   ld.init(oa, ob, depth, wave, lane);
   sl.init(sa, sb, oa.vecs, cols, nst);
-  float* const slots = (float*)(lds + T::SET);
-  constexpr int SLOT = T::SLOT / 4;
-  sl.load();
-  sl.put(slots);
-  sl.load();
+  char* const slots = lds + T::SET;
+  sl.load(slots, wave);
   ld.first(lds, depth, wave, lane);
 #pragma unroll
   for (int s = 1; s < T::BUFS; ++s) {
     ld.early(wave, lane);
+    sl.load(slots + s * T::SLOT, wave);
     ld.begin();
 #pragma unroll
     for (int j = 0; j < (s + 1 == T::BUFS ? T::SOON : ND); ++j) ld.late(j, lds + s * T::STAGE, wave, lane);
   }
-  half::wait_loads_and_lds<(T::DMA ? (T::BUFS - 2) * ND + T::SOON : 0)>();
+  half::wait_loads_and_lds<(T::DMA ? (T::BUFS - 2) * T::Loads::IN_FLIGHT + T::SOON + 1 : 0)>();
   half::block_barrier();
   if (T::DMA && depth % 16) {
     clean_tail<T>(lds, depth % kStage);
@@ -485,14 +483,14 @@ __device__ __forceinline__ void product8(const Bytes& oa, const Bytes& ob, const
   int cur = 0, slot = 0;
   if (wr * MB * 32 >= oa.vecs || wc * NB * 32 >= cols) {
     for (int s = 0; s < nst; ++s) {
-      slot = slot == 2 * SLOT ? 0 : slot + SLOT;
+      const int before = slot == 0 ? T::BUFS * T::SLOT : slot - T::SLOT;
+      slot = slot == T::BUFS * T::SLOT ? 0 : slot + T::SLOT;
       ld.early(wave, lane);
 #pragma unroll
       for (int j = T::SOON; j < ND; ++j) ld.late(j, lds + next_stage<T>(cur), wave, lane);
-      sl.put(slots + slot);
       half::wait_loads_and_lds<(T::BUFS - 2) * T::Loads::IN_FLIGHT>();
       half::block_barrier();
-      sl.load();
+      sl.load(slots + before, wave);
       ld.begin();
 #pragma unroll
       for (int j = 0; j < T::SOON; ++j) ld.late(j, lds + cur, wave, lane);
@@ -512,11 +510,11 @@ __device__ __forceinline__ void product8(const Bytes& oa, const Bytes& ob, const
       for (int y = 0; y < NB; ++y) bf[y][h] = fb.read(l3 + T::A_BYTES, h, y);
     }
     for (int s = 0; s < nst; ++s) {
-      const int next = next_stage<T>(cur), next_slot = slot == 2 * SLOT ? 0 : slot + SLOT;
-      stage_products8<T>(ld, sl, fa, fb, l3 + cur, l3 + next, lds + cur, lds + next, slots + slot, slots + next_slot,
+      const int next = next_stage<T>(cur), before = slot == 0 ? T::BUFS * T::SLOT : slot - T::SLOT;
+      stage_products8<T>(ld, sl, fa, fb, l3 + cur, l3 + next, lds + cur, lds + next, (const float*)(slots + slot), slots + before,
                          wave, lane, af, bf, acc);
       cur = next;
-      slot = next_slot;
+      slot = slot == T::BUFS * T::SLOT ? 0 : slot + T::SLOT;
     }
   }
   __builtin_amdgcn_s_waitcnt(0);  // the look-ahead past the end lands before LDS is used again

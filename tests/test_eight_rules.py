@@ -7,7 +7,7 @@ import subprocess
 import pytest
 
 ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
-FEW16, FEW32, FEW64, SMALL, MIDDLE, LARGE = range(6)
+FEW16, FEW32, FEW48, SMALL, MIDDLE, LARGE = range(6)
 ONE, NARROW, WIDE, ROWS, MANY = range(5)
 
 
@@ -43,7 +43,7 @@ def test_norms_hold_every_row(L):
 
 def test_scaled_forms_on_the_measured_side(L):
     for c, want in (((1, 4096, 4096), (FEW16, 1)), ((16, 8192, 8192), (FEW16, 1)), ((17, 4096, 4096), (FEW32, 1)),
-                    ((33, 4096, 4096), (FEW64, 1)), ((32, 8192, 8192), (SMALL, 6)), ((64, 1024, 8192), (SMALL, 8)),
+                    ((33, 4096, 4096), (FEW48, 1)), ((32, 8192, 8192), (SMALL, 6)), ((64, 1024, 8192), (SMALL, 8)),
                     ((64, 64, 8192), (SMALL, 8)), ((65, 4096, 4096), (SMALL, 2)), ((300, 4096, 4096), (SMALL, 1)),
                     ((512, 4096, 4096), (SMALL, 1)), ((333, 1000, 1111), (SMALL, 1)), ((512, 512, 8192), (SMALL, 8)),
                     ((285, 128, 7355), (SMALL, 7)), ((1024, 1024, 16384), (MIDDLE, 8)), ((2048, 2048, 2048), (MIDDLE, 1)),

@@ -69,7 +69,7 @@ def check(rows, n, k, squares, dtype, seed=0, layout="padded", **kw):
 
 
 FEW = [(1, 1, 1), (1, 16, 128), (1, 17, 129), (2, 1000, 1111), (16, 48, 4096), (17, 40, 300), (32, 130, 256), (33, 100, 77),
-       (64, 256, 1500), (1, 4096, 4096)]
+       (48, 256, 1500), (41, 1000, 1111), (49, 130, 300), (64, 256, 1500), (1, 4096, 4096)]
 TILES = [(65, 64, 128), (65, 1, 1), (100, 70, 15), (128, 128, 129), (200, 129, 1000), (333, 1000, 1111), (500, 300, 2048),
          (256, 256, 16), (97, 333, 640)]
 MANY = [(2000, 2048, 300), (2049, 2050, 257), (4096, 4096, 128), (4100, 4000, 1000), (3300, 2050, 1300)]
