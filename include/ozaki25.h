@@ -556,7 +556,8 @@ typedef struct {
  *  gates: float32 [tokens][top].  A choice outside [0, experts) adds nothing; one that
  *  a token makes twice counts with both gates.
  *  up, gate: experts x inner x width;  down: experts x out x inner;  Y: tokens x out
- *  (ldy).  Either all stacks have scales or none.
+ *  (ldy).  Either all stacks have scales or none (of those that are not empty: an empty
+ *  matrix of scales may have no address).
  *  type: OZAKI25_BF16 or OZAKI25_F16, of X, Y and of weights without scales.
  *  Sums, the hidden values and the gates are FP32; the second product takes the hidden
  *  values as two bfloat16 numbers, the rounded value and the rest (16 bits of it).  A

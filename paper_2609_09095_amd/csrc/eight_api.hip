@@ -202,7 +202,10 @@ ozaki25_status ozaki25_expert_layer(int64_t tokens, int64_t top, int64_t experts
   if (bad_stack(*up, experts, inner, width) || (gate && bad_stack(*gate, experts, inner, width)) ||
       bad_stack(*down, experts, out, inner))
     return OZAKI25_ERR_INVALID_VALUE;
-  if (!up->scales != !down->scales || (gate && !gate->scales != !up->scales)) return OZAKI25_ERR_INVALID_VALUE;
+  // which kind the weights are, their scales say; an empty stack's may have no address
+  if (experts > 0 && inner > 0 && width > 0 &&
+      ((gate && !gate->scales != !up->scales) || (out > 0 && !down->scales != !up->scales)))
+    return OZAKI25_ERR_INVALID_VALUE;
   if (tokens > OZAKI25_MAX_LAYER_TOKENS || top > OZAKI25_MAX_TOP || experts > OZAKI25_MAX_LAYER_EXPERTS ||
       too_large(0, inner, width, 0) || out > OZAKI25_MAX_WIDTH)
     return OZAKI25_ERR_UNSUPPORTED;
