@@ -151,7 +151,9 @@ ozaki25_status ozaki25_quantise(int64_t count, int64_t rows, int64_t cols, const
 
 size_t ozaki25_scaled_matmul_workspace_size(int64_t rows, int64_t n, int64_t k) {
   if (rows <= 0 || n <= 0 || k <= 0 || too_large(rows, n, k, 0)) return 0;
-  return align_up(oz::eight::scaled_room(rows, n, k));
+  // the more of the two: where operands lie is not known here
+  const size_t words = oz::eight::scaled_room(rows, n, k, true), other = oz::eight::scaled_room(rows, n, k, false);
+  return align_up(words > other ? words : other);
 }
 
 ozaki25_status ozaki25_scaled_matmul(int64_t rows, int64_t n, int64_t k, const uint8_t* A, int64_t lda,
@@ -172,15 +174,19 @@ ozaki25_status ozaki25_scaled_matmul(int64_t rows, int64_t n, int64_t k, const u
   const Piece a{A, span(1, 0, rows, lda, k, 1)}, as{a_scales, span(1, 0, kb, ldas, rows, 4)}, b{B, span(1, 0, n, ldb, k, 1)},
       bs{b_scales, span(1, 0, sr, ldbs, sc, 4)}, y{Y, span(1, 0, rows, ldy, n, e)};
   if (meets(y, {a, as, b, bs})) return OZAKI25_ERR_INVALID_VALUE;
-  const size_t need = ozaki25_scaled_matmul_workspace_size(rows, n, k);
+  oz::eight::Scaled p{};
+  p.a = A, p.lda = lda, p.as = a_scales, p.ldas = ldas;
+  p.b = B, p.ldb = ldb, p.bs = b_scales, p.ldbs = ldbs;
+  p.y = Y, p.ldy = ldy;
+  p.rows = (int)rows, p.n = (int)n, p.k = (int)k;
+  const size_t need = align_up(oz::eight::plan_scaled(p, (int)out_type));
   if (workspace && meets({workspace, need}, {a, as, b, bs, y})) return OZAKI25_ERR_INVALID_VALUE;
   Room room((hipStream_t)stream);
   if (need) {
     const ozaki25_status st = room.take(workspace, workspace_bytes, need);
     if (st != OZAKI25_SUCCESS) return st;
   }
-  const oz::eight::Scaled p{A, lda, a_scales,  ldas,   B,      ldb,   b_scales,
-                            ldbs, Y, ldy, (float*)room.p, (int)rows, (int)n, (int)k, 1, false};
+  p.parts = (float*)room.p;
   return room.give(status_of(oz::eight::launch_scaled(p, squares != 0, (int)out_type, (hipStream_t)stream)));
 }
 

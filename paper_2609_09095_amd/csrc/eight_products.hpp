@@ -68,7 +68,10 @@ struct Scaled {
   int64_t ldy;
   float* parts;  // workspace: split x rows x n padded to 4
   int rows, n, k;
-  int split;    // parts of the depth (set by the launch, like the next)
+  // set by plan_scaled:
+  ScaledForm form;
+  int split;    // parts of the depth
+  bool dma;     // tiles take A and B by DMA
   bool stream;  // y past the caches
 };
 
@@ -100,7 +103,9 @@ hipError_t launch_norm(const Norm& p, int type, hipStream_t s);
 hipError_t launch_norm_gradient(const NormGradient& p, int type, hipStream_t s);
 hipError_t launch_zeros(float* p, int64_t count, hipStream_t s);
 hipError_t launch_quantise(const Quantise& p, int type, bool squares, hipStream_t s);
-hipError_t launch_scaled(Scaled p, bool squares, int out, hipStream_t s);
+// Chooses the form; returns the bytes of workspace that it takes.
+size_t plan_scaled(Scaled& p, int out);
+hipError_t launch_scaled(const Scaled& p, bool squares, int out, hipStream_t s);
 
 }  // namespace eight
 }  // namespace oz

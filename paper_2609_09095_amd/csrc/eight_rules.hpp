@@ -86,11 +86,19 @@ constexpr int scaled_parts(int64_t tiles, int64_t blocks) {
 // 4096, 4096 10.0 / 10.8; 64, 4096, 4096 12.6 / 11.5; 32, 8192, 8192 28 / 17.5; 64, 1024, 8192
 // 22 / 11.3.  Tiles of 256 x 256 for 205 of them and more (80 of 100 CUs), as for 16-bit
 // operands.
-constexpr ScaledPlan scaled_plan(int64_t rows, int64_t n, int64_t k) {
-  if (rows <= 16) return {kScaledFew16, 1};
-  if (rows <= 48 && k <= 4096) return {rows <= 32 ? kScaledFew32 : kScaledFew48, 1};
+//
+// words: the operands' rows start on 4 bytes (scaled_words).  Of others a piece of 16 bytes
+// takes the few-row form several loads.  Few-row form / tiles: 17, 64, 2000 4.3 / 10.3; 32,
+// 4096, 4092 8.7 / 10.8; 48, 4096, 3001 7.5 / 11.6; 48, 64, 4092 10.7 / 10.1; but off 4 bytes 17,
+// 64, 4095 17.3 / 10.0; 32, 256, 4095 23.8 / 10.6; 48, 4096, 2047 17.4 / 15.4; 16, 4096, 4095
+// 16.8 / 11.0; 16, 4096, 3001 9.6 / 10.5; 1, 4096, 2047 6.1 / 10.9 (at the other side of the rule
+// 17, 64, 1111 5.4 / 7.9 and 1, 8192, 4094 16.3 / 17.2).
+constexpr ScaledPlan scaled_plan(int64_t rows, int64_t n, int64_t k, bool words = true) {
+  if (rows <= 16 && (words || k <= 3072)) return {kScaledFew16, 1};
+  if (rows <= 48 && k <= 4096 && words) return {rows <= 32 ? kScaledFew32 : kScaledFew48, 1};
   const int64_t small = ceil_div(rows, 64) * ceil_div(n, 64), middle = ceil_div(rows, 128) * ceil_div(n, 128),
                 large = ceil_div(rows, 256) * ceil_div(n, 256), blocks = ceil_div(k, 128);
+  if (rows <= 16 || (rows <= 48 && k <= 4096)) return {kScaledSmall, scaled_parts(small, blocks)};
   if (middle >= 205) return {large >= 205 ? kScaledLarge : kScaledMiddle, 1};
   if (middle >= 64 && rows > 64 && blocks >= 64) return {kScaledMiddle, scaled_parts(middle, blocks)};
   return {kScaledSmall, scaled_parts(small, blocks)};
@@ -102,14 +110,19 @@ constexpr ScaledPlan scaled_plan(int64_t rows, int64_t n, int64_t k) {
 // 18.4 / 18.8, 12.3 / 12.0; with half as many tiles 2048, 2048, 2048 17.3 / 19.3.
 constexpr bool scaled_tall(int64_t rows, int64_t n) { return ceil_div(rows, 256) * ceil_div(n, 128) >= 205; }
 
-// Of rows that do not start on 16 bytes the few-row form's pieces straddle cache lines,
-// and more than 16 rows go to tiles.  Few-row form / tiles: 64, 4096, 4095 39 / 28; 16,
-// 4096, 4095 18 / 23.
-constexpr bool few_as_tiles(int64_t rows) { return rows > 16; }
+constexpr bool scaled_words(uintptr_t a, int64_t lda, uintptr_t b, int64_t ldb) {
+  return ((a | b | (uintptr_t)lda | (uintptr_t)ldb) & 3) == 0;
+}
+
+// Whether tiles take their operands by DMA: rows that start on 16 bytes and are less than
+// 2^22 bytes apart.
+constexpr bool scaled_dma(uintptr_t a, int64_t lda, uintptr_t b, int64_t ldb) {
+  return ((a | b | (uintptr_t)lda | (uintptr_t)ldb) & 15) == 0 && lda < (1 << 22) && ldb < (1 << 22);
+}
 
 // Bytes that the parts of a split depth take.
-constexpr size_t scaled_room(int64_t rows, int64_t n, int64_t k) {
-  const int split = scaled_plan(rows, n, k).split;
+constexpr size_t scaled_room(int64_t rows, int64_t n, int64_t k, bool words = true) {
+  const int split = scaled_plan(rows, n, k, words).split;
   return split > 1 ? (size_t)split * rows * pad4(n) * 4 : 0;
 }
 

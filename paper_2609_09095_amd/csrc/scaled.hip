@@ -237,23 +237,19 @@ hipError_t of_type(const Scaled& g, hipStream_t s) {
     scaled_zero_kernel<OUT><<<dim3(2048), dim3(256), 0, s>>>(g);
     return hipGetLastError();
   }
-  ScaledForm form = scaled_plan(g.rows, g.n, g.k).form;
-  const bool dma = (uintptr_t)g.a % 16 == 0 && (uintptr_t)g.b % 16 == 0 && g.lda % 16 == 0 && g.ldb % 16 == 0 &&
-                   g.lda < (1 << 22) && g.ldb < (1 << 22);
-  if (!dma && few_as_tiles(g.rows)) form = form < kScaledSmall ? kScaledSmall : form;
-  switch (form) {
+  switch (g.form) {
     case kScaledFew16: return run_few<OUT, SQUARES, 1, 1, 8, 4>(g, s);
     case kScaledFew32: return run_few<OUT, SQUARES, 1, 2, 8, 4>(g, s);
     case kScaledFew48: return run_few<OUT, SQUARES, 1, 3, 8, 2>(g, s);
     default: break;
   }
-  if (!dma) {
-    if (form == kScaledSmall) return run_tiles<Tile8<2, 2, 1, 1, false, OUT, SQUARES>>(g, s);
+  if (!g.dma) {
+    if (g.form == kScaledSmall) return run_tiles<Tile8<2, 2, 1, 1, false, OUT, SQUARES>>(g, s);
     return run_tiles<Tile8<2, 4, 2, 1, false, OUT, SQUARES>>(g, s);
   }
-  if (form == kScaledSmall) return run_tiles<Tile8<2, 2, 1, 1, true, OUT, SQUARES, 3>>(g, s);
+  if (g.form == kScaledSmall) return run_tiles<Tile8<2, 2, 1, 1, true, OUT, SQUARES, 3>>(g, s);
   if constexpr (OUT != kF32 && SQUARES) {
-    if (form == kScaledLarge) return run_tiles<Tile8<2, 4, 4, 2, true, OUT, SQUARES>, false>(g, s);
+    if (g.form == kScaledLarge) return run_tiles<Tile8<2, 4, 4, 2, true, OUT, SQUARES>, false>(g, s);
   } else {
     if (g.split == 1 && scaled_tall(g.rows, g.n)) return run_tiles<Tile8<4, 2, 2, 2, true, OUT, SQUARES>, false>(g, s);
   }
@@ -267,12 +263,20 @@ hipError_t of_scales(const Scaled& g, bool squares, hipStream_t s) {
 
 }  // namespace
 
-hipError_t launch_scaled(Scaled g, bool squares, int out, hipStream_t s) {
+size_t plan_scaled(Scaled& g, int out) {
   // a single row starts where its matrix does, whatever the pitch says
   if (g.rows == 1) g.lda = (g.k + 15) / 16 * 16;
   if (g.n == 1) g.ldb = (g.k + 15) / 16 * 16;
-  g.split = scaled_plan(g.rows, g.n, g.k).split;
+  g.dma = scaled_dma((uintptr_t)g.a, g.lda, (uintptr_t)g.b, g.ldb);
+  const bool words = scaled_words((uintptr_t)g.a, g.lda, (uintptr_t)g.b, g.ldb);
+  const ScaledPlan plan = scaled_plan(g.rows, g.n, g.k, words);
+  g.form = plan.form;
+  g.split = plan.split;
   g.stream = (int64_t)g.rows * g.n * (out == kF32 ? 4 : 2) > ((int64_t)32 << 20);
+  return scaled_room(g.rows, g.n, g.k, words);
+}
+
+hipError_t launch_scaled(const Scaled& g, bool squares, int out, hipStream_t s) {
   if (out == kBF16) return of_scales<kBF16>(g, squares, s);
   if (out == kF16) return of_scales<kF16>(g, squares, s);
   return of_scales<kF32>(g, squares, s);

@@ -28,23 +28,26 @@ def plans():
             os.replace(tmp, _LIB)
         L = ctypes.CDLL(_LIB)
         i64, i32 = ctypes.c_int64, ctypes.c_int
-        for name, args in (("plan_form", [i64, i64, i64, i32]), ("plan_split", [i64, i64, i64, i32]), ("plan_tall", [i64, i64])):
+        for name, args, res in (("plan_form", [i64, i64, i64, i32], i32), ("plan_split", [i64, i64, i64, i32], i32),
+                                ("plan_tall", [i64, i64], i32), ("plan_room", [i64, i64, i64, i32], i64),
+                                ("plan_words", [i64] * 4, i32), ("plan_dma", [i64] * 4, i32)):
             f = getattr(L, name)
-            f.argtypes, f.restype = args, i32
+            f.argtypes, f.restype = args, res
         _lib = L
     return _lib
 
 
-def scaled_route(rows, n, k, squares, dtype, aligned):
+def scaled_route(rows, n, k, squares, dtype, A, B):
     """The form's name, with its loads ("dma" or "masked") where it has tiles, and its
-    parts: e.g. ("small", "masked", 4)."""
+    parts, e.g. ("small", "masked", 4), for operands that lie as A and B do."""
     L = plans()
-    form, split = FORMS[L.plan_form(rows, n, k, aligned)], L.plan_split(rows, n, k, aligned)
+    at = (A.data_ptr(), A.stride(0), B.data_ptr(), B.stride(0))
+    words, dma = L.plan_words(*at), L.plan_dma(*at)
+    form, split = FORMS[L.plan_form(rows, n, k, words)], L.plan_split(rows, n, k, words)
     if form.startswith("few"):
         return form, "", split
-    if not aligned:
+    if not dma:
         return ("small" if form == "small" else "middle"), "masked", split
-    if form != "small":
-        if dtype == "f32" or not squares:
-            form = "tall" if split == 1 and L.plan_tall(rows, n) else "middle"
+    if form != "small" and (dtype == "f32" or not squares):
+        form = "tall" if split == 1 and L.plan_tall(rows, n) else "middle"
     return form, "dma", split

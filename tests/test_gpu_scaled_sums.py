@@ -25,13 +25,15 @@ def gpu():
 
 
 def laid(Q, layout):
+    """Rows on 16 bytes ("padded"), on 4 but not on 16 ("words"), or at odd places."""
     import torch
     import eight_util as u
-    if layout == "padded":
-        return u.e4m3_rows(Q, -Q.shape[1] % 16)
     v, k = Q.shape
-    flat = torch.full(((k + 5) * v + 3,), 0x7f, dtype=torch.uint8, device="cuda")
-    at = flat[3:].as_strided((v, k), (k + 5, 1))
+    if layout == "padded":
+        return u.e4m3_rows(Q, -k % 16)
+    first, pitch = (4, -(-k // 16) * 16 + 4) if layout == "words" else (3, (k + 4) // 2 * 2 + 1)
+    flat = torch.full((pitch * v + first,), 0x7f, dtype=torch.uint8, device="cuda")
+    at = flat[first:].as_strided((v, k), (pitch, 1))
     at.copy_(Q.view(torch.uint8))
     return at.view(u.E4M3)
 
@@ -60,7 +62,12 @@ def values(Q, s, squares):
 
 EXACT = [
     # rows, n, k, layout, the form of a 16-bit output with squares, of another
-    (3, 500, 5000, "padded", ("few16", "", 1), ("few16", "", 1)), (3, 500, 5000, "odd", ("few16", "", 1), ("few16", "", 1)),
+    (3, 500, 5000, "padded", ("few16", "", 1), ("few16", "", 1)), (3, 500, 3000, "odd", ("few16", "", 1), ("few16", "", 1)),
+    (3, 500, 5000, "words", ("few16", "", 1), ("few16", "", 1)), (3, 500, 5000, "odd", ("small", "masked", 5), ("small", "masked", 5)),
+    (16, 70, 3073, "odd", ("small", "masked", 3), ("small", "masked", 3)), (30, 300, 4000, "odd", ("small", "masked", 4), ("small", "masked", 4)),
+    (48, 130, 4095, "odd", ("small", "masked", 4), ("small", "masked", 4)), (33, 200, 2000, "odd", ("small", "masked", 1), ("small", "masked", 1)),
+    (30, 300, 4000, "words", ("few32", "", 1), ("few32", "", 1)), (48, 130, 4095, "words", ("few48", "", 1), ("few48", "", 1)),
+    (49, 130, 4095, "words", ("small", "masked", 4), ("small", "masked", 4)),
     (30, 300, 4000, "padded", ("few32", "", 1), ("few32", "", 1)), (45, 300, 4000, "padded", ("few48", "", 1), ("few48", "", 1)),
     (45, 70, 5000, "padded", ("small", "dma", 5), ("small", "dma", 5)), (45, 70, 5000, "odd", ("small", "masked", 5), ("small", "masked", 5)),
     (300, 200, 2000, "padded", ("small", "dma", 1), ("small", "dma", 1)),
@@ -84,9 +91,12 @@ def test_whole_numbers_are_exact(rows, n, k, layout, form, other, squares):
     assert float(want.abs().max()) < 32768.0  # in half's range
     A, B = laid(A, layout), laid(B, layout)
     for dtype in ("bf16", "f16", "f32"):
-        assert eight_routes.scaled_route(rows, n, k, squares, dtype, layout == "padded") == (form if squares and dtype != "f32" else other)
+        assert eight_routes.scaled_route(rows, n, k, squares, dtype, A, B) == (form if squares and dtype != "f32" else other)
         Y = oz.ozaki25_scaled_matmul(A, a, B, b, squares=squares, out_dtype=u.TYPES[dtype])
         assert torch.equal(Y, want.to(u.TYPES[dtype])), (dtype, int((Y != want.to(u.TYPES[dtype])).sum()))
+        # in a workspace of the stated size, which holds anything
+        room = torch.full((oz.ozaki25_scaled_matmul_workspace_size(rows, n, k),), 0xff, dtype=torch.uint8, device="cuda")
+        assert torch.equal(oz.ozaki25_scaled_matmul(A, a, B, b, squares=squares, out_dtype=u.TYPES[dtype], workspace=room), Y)
 
 
 def cancelling(rows, n, k, seed):
