@@ -429,7 +429,8 @@ hipError_t of_form(NormForm g, F f) {
     case 1024 * 8 + 1: return f.template operator()<1024, 1>();
     case 768 * 8 + 2: return f.template operator()<768, 2>();
     case 1024 * 8 + 2: return f.template operator()<1024, 2>();
-    default: return f.template operator()<1024, 4>();
+    case 1024 * 8 + 4: return f.template operator()<1024, 4>();
+    default: return hipErrorInvalidValue;  // no such form: a grid of other blocks would miss rows
   }
 }
 
