@@ -2,8 +2,10 @@
 two of them share.
 
 Behind a delay on another stream the inputs are renewed, then the call follows: one that
-ran anywhere else would read the old inputs (and the delay has to be still running when
-the call returns, or the test shows nothing).  Results are compared on that stream."""
+ran on the default stream would read the old inputs (the delay has to be still running
+when the call returns, or the test shows nothing).  Results are compared on that stream,
+one whose hardware queue is not the default stream's: streams share a few of those, and
+in one queue the order of the launches would hold by itself."""
 import pytest
 
 import gpu_util
@@ -17,6 +19,26 @@ NAMES = ["norm", "norm_8bit", "norm_backward", "norm_backward_one", "quantise", 
 @pytest.fixture(scope="module", autouse=True)
 def gpu():
     gpu_util.require_gpu()
+
+
+@pytest.fixture(scope="module")
+def side():
+    """A stream that does not hold up the default one."""
+    import torch
+    one = torch.zeros(1, device="cuda")
+    for _ in range(16):
+        stream, done = torch.cuda.Stream(), torch.cuda.Event()
+        torch.cuda.synchronize()
+        with torch.cuda.stream(stream):
+            torch.cuda._sleep(100_000_000)
+        done.record(stream)
+        one.add_(1)
+        torch.cuda.current_stream().synchronize()
+        apart = not done.query()
+        torch.cuda.synchronize()
+        if apart:
+            return stream
+    pytest.skip("every stream shares the default one's queue")
 
 
 def make(name, seed, room):
@@ -77,13 +99,13 @@ def equal(a, b):
 @pytest.mark.parametrize("room", [True, False])
 @pytest.mark.parametrize("way", ["current", "argument", "handle"])
 @pytest.mark.parametrize("name", NAMES)
-def test_the_call_is_behind_what_its_stream_holds(name, way, room):
+def test_the_call_is_behind_what_its_stream_holds(name, way, room, side):
     import torch
     inputs, call = make(name, 10, room)
     renewed, call_renewed = make(name, 20, room)
     old, want = bits(call()), bits(call_renewed())
     assert not equal(old, want)
-    side, done = torch.cuda.Stream(), torch.cuda.Event()
+    done = torch.cuda.Event()
     call(**({} if way == "current" else {"stream": side}))  # whatever a first call loads
     torch.cuda.synchronize()
     with torch.cuda.stream(side):
@@ -102,13 +124,13 @@ def test_the_call_is_behind_what_its_stream_holds(name, way, room):
 
 
 @pytest.mark.parametrize("name", ["norm_8bit", "quantise", "tiles", "layer_40"])
-def test_elsewhere_it_would_read_what_was_there(name):
+def test_elsewhere_it_would_read_what_was_there(name, side):
     """The same with the call on the default stream: the old inputs' result, so that the
     test above would see one that ran there."""
     import torch
     inputs, call = make(name, 10, True)
     renewed, _ = make(name, 20, True)
-    old, side, done = bits(call()), torch.cuda.Stream(), torch.cuda.Event()
+    old, done = bits(call()), torch.cuda.Event()
     torch.cuda.synchronize()
     with torch.cuda.stream(side):
         torch.cuda._sleep(100_000_000)
