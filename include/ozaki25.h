@@ -457,7 +457,9 @@ ozaki25_status ozaki25_orthogonalise(int64_t count, int64_t m, int64_t n, const 
  * Conventions as for the 16-bit operands, bar the sums of ozaki25_scaled_matmul for
  * 16-bit outputs (see there); e4m3 bytes at any pitch and address
  * (rows that start on 16 bytes take the faster loads, whatever their length; such
- * a row's last 16 bytes are read whole and what lies past its end is not used). */
+ * a row's last 16 bytes are read whole and what lies past its end is not used; rows
+ * off 4 bytes take the slowest).  Where an output may not overlap, a matrix counts as
+ * all from its first to its last element: slices of the same rows overlap. */
 #define OZAKI25_MAX_NORM_WIDTH 32768
 
 /* Root-mean-square norm of rows with the residual's addition:
@@ -557,7 +559,8 @@ typedef struct {
 } ozaki25_expert_weights;
 
 /* A layer of experts for few tokens (a decode step), in two launches, or three for
- * more than 16 choices; larger batches take the grouped products.
+ * more than 16 choices; larger batches take the grouped products, whose weights are of
+ * 16 bits (e4m3 weights have no form for more tokens).
  *   Y[t] = sum over j of gates[t, j] D_e (silu(G_e X[t]) * (U_e X[t])),  e = which[t, j],
  * silu(x) = x / (1 + exp(-x)), and silu(U_e X[t]) where gate is NULL.
  *  X: tokens x width (ldx);  which: int32 [tokens][top], read on the device;
@@ -568,9 +571,11 @@ typedef struct {
  *  matrix of scales may have no address).
  *  type: OZAKI25_BF16 or OZAKI25_F16, of X, Y and of weights without scales.
  *  Sums, the hidden values and the gates are FP32; the second product takes the hidden
- *  values as two bfloat16 numbers, the rounded value and the rest (16 bits of it).  A
- *  weight or hidden value that is not finite may make the outputs that it reaches NaN
- *  where their sum is an infinity; tokens that do not reach it do not see it.
+ *  values as two bfloat16 numbers, the rounded value and the rest (16 bits of it), and
+ *  half's weights likewise (all 11 bits; the product of the two rests, 2^-16 of a
+ *  product, is left out).  A weight or hidden value that is not finite may make the
+ *  outputs that it reaches NaN where their sum is an infinity; tokens that do not reach
+ *  it do not see it.
  *  workspace: NULL to allocate stream-ordered, else at least
  *    ozaki25_expert_layer_workspace_size() bytes, 256-byte aligned.
  * Y overlaps nothing.  tokens == 0 or out == 0: no-op; no choice, no expert or an empty

@@ -7,11 +7,12 @@
 // weights' transposed bytes.  dW: A and B the transposed gradient and activations.
 //
 // Large products are bound by the matrix cores and the operands' way into LDS: 8192 x
-// 8192 x 8192 2.3 to 2.4 PFLOP/s, 16384 x 4096 x 4096 235 us (with the loads left out
-// 188, with the scaling left out 232 where whole 257); with FP32 outputs and scales per
-// vector, 2048 x 4096 x 8192, 137 us.  Tiles of 64 x 64 take 0.37 us a stage, a chain
-// of barrier, LDS reads, products and scaling.  A few rows are a chain of loads: 1 x 4096 x
-// 4096 6 us, 16 MB of weights.
+// 8192 x 8192 2.3 to 2.4 PFLOP/s, 16384 x 4096 x 4096 233 to 250 us, as the card's clock is
+// (with the loads left out 188, with the scaling left out 232 where whole 257); with FP32
+// outputs and scales per vector, 2048 x 4096 x 8192, 126 to 138 us; rows that do not start on
+// 16 bytes go through registers, 4096 x 4096 x 4095 181 us.  Tiles of 64 x 64 take 0.37 us a
+// stage, a chain of barrier, LDS reads, products and scaling.  A few rows are a chain of
+// loads: 1 x 4096 x 4096 6 us, 16 MB of weights.
 #include "eight_products.hpp"
 #include "eight_tile.hpp"
 
