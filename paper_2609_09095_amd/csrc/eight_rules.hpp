@@ -92,10 +92,11 @@ constexpr int scaled_parts(int64_t tiles, int64_t blocks) {
 // takes the few-row form several loads.  Few-row form / tiles: 17, 64, 2000 4.3 / 10.3; 32,
 // 4096, 4092 8.7 / 10.8; 48, 4096, 3001 7.5 / 11.6; 48, 64, 4092 10.7 / 10.1; but off 4 bytes 17,
 // 64, 4095 17.3 / 10.0; 32, 256, 4095 23.8 / 10.6; 48, 4096, 2047 17.4 / 15.4; 16, 4096, 4095
-// 16.8 / 11.0; 16, 4096, 3001 9.6 / 10.5; 1, 4096, 2047 6.1 / 10.9 (at the other side of the rule
-// 17, 64, 1111 5.4 / 7.9 and 1, 8192, 4094 16.3 / 17.2).
+// 16.8 / 11.0; 16, 4096, 3001 9.6 / 10.5; 8, 4096, 3843 11.3 / 13.2; 8, 4096, 4225 15.3 / 12.5; 1,
+// 4096, 5001 9.7 / 12.6; 1, 4096, 8191 18.5 / 14.8 (against the rule 17, 64, 1111 5.4 / 7.9; 8, 4096,
+// 4095 14.3 / 10.9; 4, 256, 5001 12.0 / 10.6).
 constexpr ScaledPlan scaled_plan(int64_t rows, int64_t n, int64_t k, bool words = true) {
-  if (rows <= 16 && (words || k <= 3072)) return {kScaledFew16, 1};
+  if (rows <= 16 && (words || k <= (rows <= 4 ? 5120 : rows <= 8 ? 4096 : 3072))) return {kScaledFew16, 1};
   if (rows <= 48 && k <= 4096 && words) return {rows <= 32 ? kScaledFew32 : kScaledFew48, 1};
   const int64_t small = ceil_div(rows, 64) * ceil_div(n, 64), middle = ceil_div(rows, 128) * ceil_div(n, 128),
                 large = ceil_div(rows, 256) * ceil_div(n, 256), blocks = ceil_div(k, 128);

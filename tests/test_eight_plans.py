@@ -8,7 +8,7 @@ import eight_routes
 import paper_2609_09095_amd as oz
 
 FEW16, FEW32, FEW48, SMALL, MIDDLE, LARGE = range(6)
-SIZES = [1, 15, 16, 17, 32, 48, 49, 64, 65, 128, 300, 1000, 2944, 2945, 3072, 3073, 4095, 4096, 4097, 8191, 70000, 1 << 22]
+SIZES = [1, 4, 5, 8, 9, 15, 16, 17, 32, 48, 49, 64, 65, 128, 300, 1000, 2944, 2945, 3072, 3073, 4095, 4096, 4097, 5120, 5121, 8191, 70000, 1 << 22]
 
 
 @pytest.fixture(scope="module")
@@ -36,7 +36,8 @@ def test_forms_on_the_measured_side(L):
     for c, want in (((17, 64, 2000, 1), (FEW32, 1)), ((32, 4096, 4092, 1), (FEW32, 1)), ((48, 4096, 3001, 1), (FEW48, 1)),
                     ((17, 64, 4095, 0), (SMALL, 4)), ((32, 256, 4095, 0), (SMALL, 4)), ((48, 4096, 2047, 0), (SMALL, 1)),
                     ((16, 4096, 4095, 0), (SMALL, 4)), ((16, 4096, 3001, 0), (FEW16, 1)), ((1, 4096, 2047, 0), (FEW16, 1)),
-                    ((16, 8192, 8192, 1), (FEW16, 1)), ((49, 4096, 4095, 0), (SMALL, 4)), ((49, 4096, 4095, 1), (SMALL, 4))):
+                    ((8, 4096, 3843, 0), (FEW16, 1)), ((8, 4096, 4225, 0), (SMALL, 4)), ((1, 4096, 5001, 0), (FEW16, 1)),
+                    ((1, 4096, 8191, 0), (SMALL, 8)), ((16, 8192, 8192, 1), (FEW16, 1)), ((49, 4096, 4095, 0), (SMALL, 4)), ((49, 4096, 4095, 1), (SMALL, 4))):
         assert (L.plan_form(*c), L.plan_split(*c)) == want, c
 
 
