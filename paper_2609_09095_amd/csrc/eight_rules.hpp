@@ -96,7 +96,7 @@ constexpr int scaled_parts(int64_t tiles, int64_t blocks) {
 // 4096, 5001 9.7 / 12.6; 1, 4096, 8191 18.5 / 14.8 (against the rule 17, 64, 1111 5.4 / 7.9; 8, 4096,
 // 4095 14.3 / 10.9; 4, 256, 5001 12.0 / 10.6).
 constexpr ScaledPlan scaled_plan(int64_t rows, int64_t n, int64_t k, bool words = true) {
-  if (rows <= 16 && (words || k <= (rows <= 4 ? 5120 : rows <= 8 ? 4096 : 3072))) return {kScaledFew16, 1};
+  if (rows <= 16 && (words || k <= (rows <= 4 ? 5120 : rows <= 8 ? 4096 : 3200))) return {kScaledFew16, 1};
   if (rows <= 48 && k <= 4096 && words) return {rows <= 32 ? kScaledFew32 : kScaledFew48, 1};
   const int64_t small = ceil_div(rows, 64) * ceil_div(n, 64), middle = ceil_div(rows, 128) * ceil_div(n, 128),
                 large = ceil_div(rows, 256) * ceil_div(n, 256), blocks = ceil_div(k, 128);

@@ -8,7 +8,7 @@ import eight_routes
 import paper_2609_09095_amd as oz
 
 FEW16, FEW32, FEW48, SMALL, MIDDLE, LARGE = range(6)
-SIZES = [1, 4, 5, 8, 9, 15, 16, 17, 32, 48, 49, 64, 65, 128, 300, 1000, 2944, 2945, 3072, 3073, 4095, 4096, 4097, 5120, 5121, 8191, 70000, 1 << 22]
+SIZES = [1, 4, 5, 8, 9, 15, 16, 17, 32, 48, 49, 64, 65, 128, 300, 1000, 2944, 2945, 3200, 3201, 4095, 4096, 4097, 5120, 5121, 8191, 70000, 1 << 22]
 
 
 @pytest.fixture(scope="module")

@@ -65,7 +65,7 @@ EXACT = [
     (3, 500, 5000, "padded", ("few16", "", 1), ("few16", "", 1)), (3, 500, 3000, "odd", ("few16", "", 1), ("few16", "", 1)),
     (3, 500, 5000, "words", ("few16", "", 1), ("few16", "", 1)), (3, 500, 5300, "odd", ("small", "masked", 5), ("small", "masked", 5)),
     (8, 500, 4097, "odd", ("small", "masked", 4), ("small", "masked", 4)), (8, 70, 4095, "odd", ("few16", "", 1), ("few16", "", 1)),
-    (16, 70, 3073, "odd", ("small", "masked", 3), ("small", "masked", 3)), (30, 300, 4000, "odd", ("small", "masked", 4), ("small", "masked", 4)),
+    (16, 70, 3201, "odd", ("small", "masked", 3), ("small", "masked", 3)), (30, 300, 4000, "odd", ("small", "masked", 4), ("small", "masked", 4)),
     (48, 130, 4095, "odd", ("small", "masked", 4), ("small", "masked", 4)), (33, 200, 2000, "odd", ("small", "masked", 1), ("small", "masked", 1)),
     (30, 300, 4000, "words", ("few32", "", 1), ("few32", "", 1)), (48, 130, 4095, "words", ("few48", "", 1), ("few48", "", 1)),
     (49, 130, 4095, "words", ("small", "masked", 4), ("small", "masked", 4)),
